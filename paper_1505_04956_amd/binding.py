@@ -19,6 +19,12 @@ MODE_DETERMINISTIC, MODE_FREE_RUNNING = 0, 1
 LR_CONST, LR_INV_COUNT = 0, 1
 KERNEL_AUTO, KERNEL_GENERIC, KERNEL_SMALL, KERNEL_MFMA = 0, 1, 2, 3
 FORM_NONE, FORM_FP32, FORM_SPLIT_LAUNCH, FORM_SPLIT_PHASES = range(4)
+TYPE_F32, TYPE_BF16, TYPE_F16 = range(3)
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+GROUP_BEST, GROUP_BEST_TWO = 0, 1
+BLOCKS_ROWS, BLOCKS_SQUARES, BLOCKS_RAW = range(3)
+PRODUCT_ALL, PRODUCT_GATHER, PRODUCT_PLACES, PRODUCT_OVER = range(4)
+PRODUCT_RAW_ROWS = 16
 
 # every symbol include/asgd.h declares
 SYMBOLS = (
@@ -27,6 +33,8 @@ SYMBOLS = (
     "asgd_get_mean_state", "asgd_quant_error", "asgd_last_run_ms", "asgd_get_stats", "asgd_get_worker_counters",
     "asgd_schedule_peer", "asgd_schedule_peer_n", "asgd_last_hip_error", "asgd_destroy", "asgd_strerror",
     "asgd_quant_error_noalloc", "asgd_get_exchange", "asgd_set_exchange", "asgd_last_run_form",
+    "asgd_route", "asgd_route_backward", "asgd_route_plan_bytes", "asgd_route_plan", "asgd_route_max_blocks",
+    "asgd_block_quantize", "asgd_block_product", "asgd_experts_sum", "asgd_experts_sum_backward",
 )
 
 
@@ -35,6 +43,21 @@ class asgd_stats(C.Structure):
                 ("received", C.c_int64), ("accepted", C.c_int64), ("parzen_near_ties", C.c_int64),
                 ("exact_rechecks", C.c_int64), ("last_run_ms", C.c_double),
                 ("kernel", C.c_int32), ("launches", C.c_int32)]
+
+
+class asgd_route_rule(C.Structure):
+    _fields_ = [("k", C.c_int32), ("score", C.c_int32), ("groups", C.c_int32), ("kept", C.c_int32),
+                ("group_by", C.c_int32), ("renormalize", C.c_int32), ("scale", C.c_float)]
+
+
+class asgd_route_order(C.Structure):
+    _fields_ = [("T", C.c_int64), ("k", C.c_int32), ("E", C.c_int32), ("offsets", C.c_void_p), ("blocks", C.c_void_p),
+                ("slots", C.c_void_p), ("places", C.c_void_p)]
+
+
+class asgd_blocks(C.Structure):
+    _fields_ = [("values", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("form", C.c_int32), ("count", C.c_int32), ("type", C.c_int32), ("stride", C.c_int64)]
 
 
 class AsgdError(RuntimeError):
@@ -89,6 +112,15 @@ def lib():
             "asgd_destroy": (None, [vp]),
             "asgd_strerror": (C.c_char_p, [C.c_int]),
             "asgd_quant_error_noalloc": (C.c_int, [vp, i64, C.c_int, C.c_int, vp, vp, vp]),
+            "asgd_route": (C.c_int, [vp, C.c_int, i64, C.c_int, i64, vp, vp, vp, vp, vp]),
+            "asgd_route_backward": (C.c_int, [vp, C.c_int, i64, C.c_int, i64, vp, vp, vp, vp, vp, i64, vp]),
+            "asgd_route_plan_bytes": (C.c_size_t, [i64, C.c_int, C.c_int]),
+            "asgd_route_plan": (C.c_int, [vp, vp, vp, C.c_size_t, vp]),
+            "asgd_route_max_blocks": (i64, [i64, C.c_int, C.c_int]),
+            "asgd_block_quantize": (C.c_int, [vp, C.c_int, i64, i64, i64, C.c_int, vp, vp, vp, vp]),
+            "asgd_block_product": (C.c_int, [vp, vp, C.c_int, C.c_int, vp, vp, C.c_int, i64, vp]),
+            "asgd_experts_sum": (C.c_int, [vp, C.c_int, i64, i64, vp, vp, vp, C.c_int, i64, vp]),
+            "asgd_experts_sum_backward": (C.c_int, [vp, C.c_int, i64, vp, C.c_int, i64, i64, vp, vp, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -210,6 +242,48 @@ def asgd_schedule_peer_n(seed, r, i, W, n) -> int:
 
 def asgd_destroy(h):
     lib().asgd_destroy(h)
+
+
+# routed experts: rule, order and blocks are the structures above (host memory); the tensor-level calls are in experts.py
+def asgd_route(logits_ptr, type, T, E, stride, bias_ptr, rule, ids_ptr, weights_ptr, stream=0):
+    _check(lib().asgd_route(logits_ptr, type, T, E, stride, bias_ptr, C.addressof(rule), ids_ptr, weights_ptr, stream), "asgd_route")
+
+
+def asgd_route_backward(logits_ptr, type, T, E, stride, bias_ptr, rule, ids_ptr, d_weights_ptr, d_logits_ptr, d_stride, stream=0):
+    _check(lib().asgd_route_backward(logits_ptr, type, T, E, stride, bias_ptr, C.addressof(rule), ids_ptr, d_weights_ptr, d_logits_ptr,
+                                     d_stride, stream), "asgd_route_backward")
+
+
+def asgd_route_plan_bytes(T, k, E) -> int:
+    return int(lib().asgd_route_plan_bytes(T, k, E))
+
+
+def asgd_route_plan(ids_ptr, order, work_ptr, work_bytes, stream=0):
+    _check(lib().asgd_route_plan(ids_ptr, C.addressof(order), work_ptr, work_bytes, stream), "asgd_route_plan")
+
+
+def asgd_route_max_blocks(T, k, E) -> int:
+    return int(lib().asgd_route_max_blocks(T, k, E))
+
+
+def asgd_block_quantize(x_ptr, type, rows, cols, stride, turned, order, weights_ptr, out, stream=0):
+    _check(lib().asgd_block_quantize(x_ptr, type, rows, cols, stride, turned, None if order is None else C.addressof(order), weights_ptr,
+                                     C.addressof(out), stream), "asgd_block_quantize")
+
+
+def asgd_block_product(a, b, mode, exact, order, out_ptr, type, stride, stream=0):
+    _check(lib().asgd_block_product(C.addressof(a), C.addressof(b), mode, exact, None if order is None else C.addressof(order), out_ptr, type,
+                                    stride, stream), "asgd_block_product")
+
+
+def asgd_experts_sum(y_ptr, y_type, n, y_stride, order, weights_ptr, out_ptr, type, stride, stream=0):
+    _check(lib().asgd_experts_sum(y_ptr, y_type, n, y_stride, C.addressof(order), weights_ptr, out_ptr, type, stride, stream),
+           "asgd_experts_sum")
+
+
+def asgd_experts_sum_backward(d_out_ptr, type, stride, y_ptr, y_type, n, y_stride, order, d_weights_ptr, stream=0):
+    _check(lib().asgd_experts_sum_backward(d_out_ptr, type, stride, y_ptr, y_type, n, y_stride, C.addressof(order), d_weights_ptr, stream),
+           "asgd_experts_sum_backward")
 
 
 # ---- convenience wrapper: owns a handle, keeps the borrowed tensors alive -----------------

@@ -1,0 +1,197 @@
+// To 8 bits in blocks of 128: rows, the transpose's rows, squares.  All three read x once and write a byte an element, so memory
+// bounds them; the largest magnitude of a block is found among the lanes that hold it.
+#include "experts_internal.h"
+
+namespace asgd {
+
+namespace {
+
+// eight consecutive elements of a row; `left` of them exist, `wide`: all rows begin at a multiple of 16 bytes
+template <class Ty> __device__ __forceinline__ void load8(const typename Ty::T *p, int64_t left, bool wide, float (&v)[8])
+{
+    typedef typename Ty::T T;
+    if (wide && left >= 8) {
+        T u[8];
+        *(uint4 *)u = *(const uint4 *)p;
+        if constexpr (sizeof(T) == 4) *((uint4 *)u + 1) = *((const uint4 *)p + 1);
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = (float)u[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = i < left ? (float)p[i] : 0.0f;
+    }
+}
+
+// Sixteen lanes take a block, eight elements each; the lanes of a wave take four blocks of one row next to each other.
+template <class Ty> __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs q, int64_t groups, bool wide)
+{
+    typedef typename Ty::T T;
+    const int64_t kb = q.out_blocks;
+    const int part = threadIdx.x & 15;
+    for (int64_t g = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); g < groups; g += (int64_t)gridDim.x * 16) {
+        const int64_t r = g / kb, b = g - r * kb;
+        int64_t src = r;
+        float w = 1.0f;
+        bool there = true;
+        if (q.order.slots) {
+            const int slot = q.order.slots[r];
+            there = slot >= 0;
+            src = there ? slot / q.order.k : 0;
+            if (q.weights && there) w = q.weights[slot];
+        }
+        if (!there) continue;                                      // (the sixteen lanes of a block go the same way)
+        const int64_t c = b * BLOCK8 + part * 8;
+        float v[8];
+        load8<Ty>((const T *)q.x + src * q.stride + c, q.cols - c, wide, v);
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            if (q.weights) v[i] *= w;
+            top = max(top, magnitude_bits(v[i]));
+        }
+#pragma unroll
+        for (int m = 8; m; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+        float scale, inverse;
+        block_scale(top, scale, inverse);
+        uint2 o;
+        o.x = eight_bits(v[0], v[1], v[2], v[3], inverse);
+        o.y = eight_bits(v[4], v[5], v[6], v[7], inverse);
+        *(uint2 *)(q.values + (r * kb + b) * BLOCK8 + part * 8) = o;
+        if (part == 0) q.scales[b * q.out_rows + r] = scale;
+    }
+}
+
+// The transpose: a workgroup takes 128 rows of x (a block of the result) and 64 columns (rows of the result).  A thread has one column
+// and 32 of the rows in registers, four threads a block; it writes 32 bytes in a row, the four of them a whole line.
+template <class Ty> __global__ __launch_bounds__(256) void quantize_turned_kernel(QuantArgs q)
+{
+    typedef typename Ty::T T;
+    __shared__ uint32_t tops[4][64];
+    __shared__ int64_t source[BLOCK8];
+    __shared__ float factor[BLOCK8];
+    const int64_t rb = blockIdx.x;
+    const int c0 = threadIdx.x & 63, quarter = threadIdx.x >> 6;
+    if (q.order.offsets) {
+        const int E = q.order.E;
+        if (rb >= q.order.blocks[E]) return;
+        // the expert whose blocks hold rb: the last one that begins at or before it and is not empty
+        int lo = 0, hi = E;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (q.order.blocks[mid] <= rb) lo = mid; else hi = mid;
+        }
+        if (threadIdx.x < BLOCK8) {
+            const int64_t p = q.order.offsets[lo] + (rb - q.order.blocks[lo]) * BLOCK8 + threadIdx.x;
+            const bool there = p < q.order.offsets[lo + 1];
+            const int slot = there ? q.order.slots[p] : -1;
+            source[threadIdx.x] = there ? slot / q.order.k : -1;
+            factor[threadIdx.x] = there && q.weights ? q.weights[slot] : 1.0f;
+        }
+    } else if (threadIdx.x < BLOCK8) {
+        const int64_t r = rb * BLOCK8 + threadIdx.x;
+        source[threadIdx.x] = r < q.rows ? r : -1;
+        factor[threadIdx.x] = 1.0f;
+    }
+    __syncthreads();
+    for (int64_t cb = blockIdx.y; cb * 64 < q.cols; cb += gridDim.y) {
+        const int64_t c = cb * 64 + c0;
+        const bool inside = c < q.cols;
+        float v[32];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 32; i++) {
+            const int64_t r = source[quarter * 32 + i];
+            v[i] = inside && r >= 0 ? (float)((const T *)q.x)[r * q.stride + c] : 0.0f;
+            if (q.weights) v[i] *= r >= 0 ? factor[quarter * 32 + i] : 0.0f;
+            top = max(top, magnitude_bits(v[i]));
+        }
+        tops[quarter][c0] = top;
+        __syncthreads();
+        top = max(max(tops[0][c0], tops[1][c0]), max(tops[2][c0], tops[3][c0]));
+        __syncthreads();
+        float scale, inverse;
+        block_scale(top, scale, inverse);
+        if (inside) {
+            uint32_t o[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) o[i] = eight_bits(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inverse);
+            uint4 *to = (uint4 *)(q.values + (c * q.out_blocks + rb) * BLOCK8 + quarter * 32);
+            to[0] = make_uint4(o[0], o[1], o[2], o[3]);
+            to[1] = make_uint4(o[4], o[5], o[6], o[7]);
+            if (quarter == 0) q.scales[rb * q.out_rows + c] = scale;
+        }
+    }
+}
+
+// Squares: a workgroup of 256 takes one, in two passes over its 128 x 128 elements (the second from the caches).  Rows of the
+// result beyond out_rows do not exist; columns beyond the data are zeros.
+template <class Ty> __global__ __launch_bounds__(256) void quantize_squares_kernel(QuantArgs q, bool turned)
+{
+    typedef typename Ty::T T;
+    __shared__ uint32_t tops[4];
+    const int64_t nb = blocks8(q.out_rows), kb = q.out_blocks, square = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
+    if (square >= nb * kb * q.count) return;
+    const int64_t m = square / (nb * kb), ib = square / kb % nb, jb = square % kb;
+    const T *x = (const T *)q.x + m * q.rows * q.stride;
+    const auto at = [&](int i, int j) {
+        const int64_t r = ib * BLOCK8 + i, c = jb * BLOCK8 + j, xr = turned ? c : r, xc = turned ? r : c;
+        return xr < q.rows && xc < q.cols ? (float)x[xr * q.stride + xc] : 0.0f;
+    };
+    uint32_t top = 0;
+    for (int n = threadIdx.x; n < BLOCK8 * BLOCK8; n += 256) {
+        const int u = n >> 7, v = n & 127;                       // v: along x's rows, so that neighbours read neighbours
+        top = max(top, magnitude_bits(turned ? at(v, u) : at(u, v)));
+    }
+#pragma unroll
+    for (int s = 32; s; s >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, s));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+    float scale, inverse;
+    block_scale(top, scale, inverse);
+    for (int n = threadIdx.x; n < BLOCK8 * BLOCK8 / 4; n += 256) {
+        const int i = turned ? n & 127 : n >> 5, j = (turned ? n >> 7 : n & 31) * 4;
+        if (ib * BLOCK8 + i < q.out_rows)
+            *(uint32_t *)(q.values + ((m * q.out_rows + ib * BLOCK8 + i) * kb + jb) * BLOCK8 + j) =
+                eight_bits(at(i, j), at(i, j + 1), at(i, j + 2), at(i, j + 3), inverse);
+    }
+    if (threadIdx.x == 0) q.scales[square] = scale;
+}
+
+bool rows_are_wide(const QuantArgs &q, int type)
+{
+    return ((uintptr_t)q.x & 15) == 0 && q.stride * (int64_t)type_size(type) % 16 == 0;
+}
+
+}  // namespace
+
+hipError_t launch_quantize_rows(const QuantArgs &q, int type, hipStream_t s)
+{
+    const int64_t groups = q.out_rows * q.out_blocks, grid = (groups + 15) / 16;
+    return with_type(type, [&](auto ty) {
+        quantize_rows_kernel<decltype(ty)><<<(unsigned)(grid < (1 << 20) ? grid : (1 << 20)), 256, 0, s>>>(q, groups, rows_are_wide(q, type));
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_quantize_turned(const QuantArgs &q, int type, hipStream_t s)
+{
+    const int64_t strips = (q.cols + 63) / 64;
+    const dim3 grid((unsigned)q.out_blocks, (unsigned)(strips < 1024 ? strips : 1024));
+    return with_type(type, [&](auto ty) {
+        quantize_turned_kernel<decltype(ty)><<<grid, 256, 0, s>>>(q);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_quantize_squares(const QuantArgs &q, int type, bool turned, hipStream_t s)
+{
+    const int64_t squares = blocks8(q.out_rows) * q.out_blocks * q.count, across = squares < (1 << 16) ? squares : (1 << 16);
+    const dim3 grid((unsigned)across, (unsigned)((squares + across - 1) / across));
+    return with_type(type, [&](auto ty) {
+        quantize_squares_kernel<decltype(ty)><<<grid, 256, 0, s>>>(q, turned);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace asgd

@@ -1,0 +1,431 @@
+// Routing of rows to experts: scores, the best k by key, their weights; the gradient of the logits; the order by expert.
+//
+// One wave takes one row.  Lane i holds the V consecutive experts i * V .. i * V + V - 1, so that among equal keys the
+// lowest lane, and in it the lowest register, is the lowest index.
+#include "experts_internal.h"
+
+namespace asgd {
+
+namespace {
+
+constexpr float OUT = -INFINITY;          // key of an expert that cannot be chosen
+
+// l of the lane's experts (out: -infinity), and whether an expert that is in has something that is not a number
+template <class Ty, int V>
+__device__ __forceinline__ bool load_logits(const typename Ty::T *row, const float *bias, int E, int lane, float (&l)[V], float (&b)[V])
+{
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+        const int e = lane * V + i;
+        l[i] = e < E ? (float)row[e] : OUT;
+        b[i] = bias && e < E ? bias[e] : 0.0f;
+        if (b[i] == OUT) l[i] = OUT;
+        if (l[i] != OUT && (l[i] != l[i] || b[i] != b[i])) bad = true;
+    }
+    return __any(bad);
+}
+
+// 1 / (1 + exp(-l)), in the operations of the definition
+__device__ __forceinline__ float sigmoid(float l) { return 1.0f / (1.0f + expf(-l)); }
+
+// an order among numbers: what is not one comes last of those that are in
+__device__ __forceinline__ float as_key(float v) { return v == v ? v : -3.402823466e38f; }
+
+template <int V> __device__ __forceinline__ float lane_best(const float (&v)[V])
+{
+    float m = v[0];
+#pragma unroll
+    for (int i = 1; i < V; i++) m = fmaxf(m, v[i]);
+    return m;
+}
+
+template <class Ty, int V> __device__ __forceinline__ void route_row(const RouteArgs &a, int64_t t, int lane)
+{
+    const typename Ty::T *row = (const typename Ty::T *)a.logits + t * a.stride;
+    const int E = a.E, k = a.rule.k;
+    const bool soft = a.rule.score == ASGD_SCORE_SOFTMAX;
+    float l[V], key[V];
+    const bool bad = load_logits<Ty, V>(row, a.bias, E, lane, l, key);       // key: the bias for now
+    float top = 0.0f, total = 1.0f;
+    if (soft && (!a.rule.renormalize || a.bias || (a.rule.groups > 1 && a.rule.group_by == ASGD_GROUP_BEST_TWO))) {
+        top = wave_max(lane_best(l));
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; i++) sum += l[i] == OUT ? 0.0f : expf(l[i] - top);
+        total = wave_sum(sum);
+    }
+    const auto score = [&](float v) { return v == OUT ? 0.0f : soft ? expf(v - top) / total : sigmoid(v); };
+    if (a.bias) {
+#pragma unroll
+        for (int i = 0; i < V; i++) key[i] = l[i] == OUT ? OUT : as_key(score(l[i]) + key[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i++) key[i] = as_key(l[i]);
+    }
+    if (a.rule.groups > 1) {
+        const int G = a.rule.groups, width = E / G;
+        const bool two = a.rule.group_by == ASGD_GROUP_BEST_TWO;
+        float mine = OUT;                                                     // lane g: how group g is judged
+        for (int g = 0; g < G; g++) {
+            float m1 = OUT, m2 = OUT;                                         // the lane's two best of the group
+#pragma unroll
+            for (int i = 0; i < V; i++) {
+                const int e = lane * V + i;
+                if (e >= g * width && e < (g + 1) * width) {
+                    const float v = two && !a.bias ? (l[i] == OUT ? OUT : as_key(score(l[i]))) : key[i];
+                    m2 = fmaxf(m2, fminf(m1, v));
+                    m1 = fmaxf(m1, v);
+                }
+            }
+            const float best = wave_max(m1);
+            float judged = best;
+            if (two) {
+                // the second best: the lowest lane with the best gives that one up
+                const unsigned long long has = __ballot(m1 == best);
+                const bool gives = lane == __ffsll((long long)has) - 1;
+                judged = as_key(best + wave_max(gives ? m2 : m1));
+            }
+            if (lane == g) mine = judged;
+        }
+        unsigned long long open = G == 64 ? ~0ull : (1ull << G) - 1, stays = 0;
+        for (int n = 0; n < a.rule.kept; n++) {
+            const bool here = open >> lane & 1;
+            const float best = wave_max(here ? mine : OUT);
+            const int g = __ffsll((long long)__ballot(here && mine == best)) - 1;
+            open &= ~(1ull << g);
+            stays |= 1ull << g;
+        }
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            const int e = lane * V + i;
+            if (e < E && !(stays >> (e / width) & 1)) key[i] = OUT;
+        }
+    }
+    int id = -1;                                                              // lane j: choice j
+    float chosen = OUT;
+    for (int j = 0; j < k; j++) {
+        const float m = lane_best(key);
+        const float best = wave_max(m);
+        if (best == OUT) break;
+        const int owner = __ffsll((long long)__ballot(m == best)) - 1;
+        int at = 0;
+        float value = 0.0f;
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < V; i++)
+            if (!found && key[i] == best) {
+                found = true;
+                at = i;
+                value = l[i];
+                if (lane == owner) key[i] = OUT;
+            }
+        at = __shfl(at, owner);
+        value = __shfl(value, owner);
+        if (lane == j) {
+            id = owner * V + at;
+            chosen = value;
+        }
+    }
+    float share;
+    const float largest = wave_max(chosen);                                   // (by all lanes: not inside a branch)
+    if (soft && a.rule.renormalize) share = chosen == OUT ? 0.0f : expf(chosen - largest);
+    else share = score(chosen);
+    if (id < 0) share = 0.0f;
+    if (a.rule.renormalize) {
+        const float sum = wave_sum(share);
+        share = sum > 0.0f ? share / sum : sum == 0.0f ? 0.0f : sum;
+    }
+    if (lane < k) {
+        a.ids[t * k + lane] = id;
+        a.weights[t * k + lane] = bad && id >= 0 ? __uint_as_float(0x7FC00000u) : share * a.rule.scale;
+    }
+}
+
+template <class Ty, int V> __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
+{
+    for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < a.T; t += (int64_t)gridDim.x * 4)
+        route_row<Ty, V>(a, t, threadIdx.x & 63);
+}
+
+// With the choice held fixed: w_j = c s_j or c s_j / sum of the chosen s.
+//   g_j = c dw_j                      or  (c / sum) (dw_j - sum_i dw_i s_i / sum)
+//   sigmoid: dl_j = g_j s_j (1 - s_j);  softmax: dl_e = s_e (g_e - sum_i g_i s_i), whose inner sum is 0 when renormalised
+template <class Ty, int V> __device__ __forceinline__ void route_row_backward(const RouteArgs &a, int64_t t, int lane, float *mine)
+{
+    typedef typename Ty::T T;
+    const T *row = (const T *)a.logits + t * a.stride;
+    T *out = (T *)a.d_logits + t * a.d_stride;
+    const int E = a.E, k = a.rule.k;
+    const bool soft = a.rule.score == ASGD_SCORE_SOFTMAX, renorm = a.rule.renormalize;
+    int id = lane < k ? a.ids_in[t * k + lane] : -1;
+    if (id >= E) id = -1;
+    const bool there = id >= 0;
+    const float chosen = there ? (float)row[id] : OUT;
+    const float dw = there ? a.d_weights[t * k + lane] : 0.0f;
+    float l[V], b[V];
+    const bool bad = load_logits<Ty, V>(row, a.bias, E, lane, l, b);
+    float top = 0.0f, total = 1.0f;
+    if (soft && !renorm) {
+        top = wave_max(lane_best(l));
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; i++) sum += l[i] == OUT ? 0.0f : expf(l[i] - top);
+        total = wave_sum(sum);
+    }
+    float share;
+    const float largest = wave_max(chosen);
+    if (soft && renorm) share = there ? expf(chosen - largest) : 0.0f;
+    else share = !there ? 0.0f : soft ? expf(chosen - top) / total : sigmoid(chosen);
+    float g, grad, inner = 0.0f;
+    if (renorm) {
+        const float sum = wave_sum(share);
+        const float part = sum == 0.0f ? 0.0f : share / sum;
+        g = a.rule.scale * (dw - wave_sum(dw * part));
+        if (sum == 0.0f) g = 0.0f;
+        grad = soft ? g * part : sum == 0.0f ? 0.0f : g / sum * share * (1.0f - share);
+    } else {
+        g = a.rule.scale * dw;
+        if (soft) inner = wave_sum(g * share);
+        grad = soft ? g : g * share * (1.0f - share);
+    }
+#pragma unroll
+    for (int i = 0; i < V; i++) mine[i * 64 + lane] = 0.0f;
+    __builtin_amdgcn_wave_barrier();
+    __threadfence_block();
+    if (there) mine[id] = grad;
+    __builtin_amdgcn_wave_barrier();
+    __threadfence_block();
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+        const int e = lane * V + i;
+        if (e < E) {
+            float v = mine[e];
+            if (soft && !renorm) v = l[i] == OUT ? 0.0f : expf(l[i] - top) / total * (v - inner);
+            if (bad && l[i] != OUT) v = __uint_as_float(0x7FC00000u);
+            out[e] = (T)v;
+        }
+    }
+    __builtin_amdgcn_wave_barrier();
+}
+
+template <class Ty, int V> __global__ __launch_bounds__(256) void route_backward_kernel(RouteArgs a)
+{
+    __shared__ float grads[4][64 * V];
+    const int wave = threadIdx.x >> 6;
+    for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < a.T; t += (int64_t)gridDim.x * 4)
+        route_row_backward<Ty, V>(a, t, threadIdx.x & 63, grads[wave]);
+}
+
+// ---- the order by expert --------------------------------------------------------------------------------------------
+// A counting sort that keeps the order of slots.  A chunk of CHUNK slots belongs to one wave, which walks it in order: the
+// lanes that have the same expert find each other by the bits of its number, and each learns how many lower lanes have it.
+// Three steps: count per chunk, add up over chunks and experts, place.
+constexpr int CHUNK = 1024;
+constexpr int ONE_BLOCK_CHUNKS = 16;      // up to here one workgroup does it all, its counts in the LDS
+
+__device__ __forceinline__ unsigned long long same_expert(int e)
+{
+    unsigned long long same = ~0ull;
+#pragma unroll
+    for (int bit = 0; bit < 11; bit++) {      // (E itself stands for none: 11 bits)
+        const unsigned long long set = __ballot(e >> bit & 1);
+        same &= e >> bit & 1 ? set : ~set;
+    }
+    return same;
+}
+
+__device__ __forceinline__ int expert_of(const int32_t *ids, int64_t slot, int64_t end, int E)
+{
+    const int e = slot < end ? ids[slot] : -1;
+    return (unsigned)e < (unsigned)E ? e : E;
+}
+
+// counts of a chunk, added to `count` (E + 1 words, zero before)
+__device__ void count_chunk(const int32_t *ids, int64_t begin, int64_t end, int E, int *count)
+{
+    const int lane = threadIdx.x & 63;
+    for (int64_t s = begin; s < end; s += 64) {
+        const int e = expert_of(ids, s + lane, end, E);
+        if (s + lane < end) atomicAdd(&count[e], 1);      // (whole numbers: any order gives the same)
+    }
+}
+
+// places of a chunk's slots; next[e]: the place of the next slot of expert e
+__device__ void place_chunk(const int32_t *ids, int64_t begin, int64_t end, int E, volatile int *next, int32_t *slots, int32_t *places)
+{
+    const int lane = threadIdx.x & 63;
+    for (int64_t s = begin; s < end; s += 64) {
+        const int e = expert_of(ids, s + lane, end, E);
+        const unsigned long long same = same_expert(e), before = same & ((1ull << lane) - 1);
+        const bool there = e < E;
+        int place = -1;
+        if (there) place = next[e] + __popcll(before);
+        __builtin_amdgcn_wave_barrier();
+        if (there && !before) next[e] = place + __popcll(same);
+        __builtin_amdgcn_wave_barrier();
+        if (s + lane < end) {
+            places[s + lane] = place;
+            if (there) slots[place] = (int32_t)(s + lane);
+        }
+    }
+}
+
+// Exclusive sums over the experts of their counts and of their blocks of 128, by one workgroup of 1024 (thread e has expert e).
+__device__ void sum_experts(int n, int E, int32_t *offsets, int32_t *blocks, int &offset)
+{
+    __shared__ int part[2][16];
+    const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
+    const int v0 = e < E ? n : 0, v1 = e < E ? (n + BLOCK8 - 1) / BLOCK8 : 0;
+    int s0 = v0, s1 = v1;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int u0 = __shfl_up(s0, m), u1 = __shfl_up(s1, m);
+        if (lane >= m) { s0 += u0; s1 += u1; }
+    }
+    if (lane == 63) { part[0][wave] = s0; part[1][wave] = s1; }
+    __syncthreads();
+    int b0 = 0, b1 = 0;
+    for (int w = 0; w < wave; w++) { b0 += part[0][w]; b1 += part[1][w]; }
+    offset = b0 + s0 - v0;
+    if (e < E) { offsets[e] = offset; blocks[e] = b1 + s1 - v1; }
+    if (e == E - 1) { offsets[E] = b0 + s0; blocks[E] = b1 + s1; }
+    __syncthreads();
+}
+
+__global__ __launch_bounds__(1024) void plan_one_block_kernel(const int32_t *ids, asgd_route_order o, int chunk, int chunks)
+{
+    extern __shared__ int count[];                  // [chunks][E + 1]
+    __shared__ int used;
+    const int E = o.E, wave = threadIdx.x >> 6;
+    const int64_t slots = o.T * o.k;
+    for (int i = threadIdx.x; i < chunks * (E + 1); i += blockDim.x) count[i] = 0;
+    __syncthreads();
+    const int64_t begin = (int64_t)wave * chunk, end = begin + chunk < slots ? begin + chunk : slots;
+    if (wave < chunks) count_chunk(ids, begin, end, E, count + wave * (E + 1));
+    __syncthreads();
+    int n = 0;
+    const int e = threadIdx.x;
+    if (e < E)
+        for (int c = 0; c < chunks; c++) n += count[c * (E + 1) + e];
+    int offset;
+    sum_experts(n, E, o.offsets, o.blocks, offset);
+    if (e < E)
+        for (int c = 0; c < chunks; c++) {
+            const int m = count[c * (E + 1) + e];
+            count[c * (E + 1) + e] = offset;
+            offset += m;
+        }
+    if (e == E - 1) used = offset;
+    __syncthreads();
+    if (wave < chunks) place_chunk(ids, begin, end, E, count + wave * (E + 1), o.slots, o.places);
+    for (int64_t p = used + threadIdx.x; p < slots; p += blockDim.x) o.slots[p] = -1;
+}
+
+// many slots: the counts [chunk][E] go through memory
+__global__ __launch_bounds__(64) void plan_count_kernel(const int32_t *ids, int64_t slots, int E, int *work)
+{
+    extern __shared__ int count[];                  // E + 1
+    for (int i = threadIdx.x; i <= E; i += 64) count[i] = 0;
+    __syncthreads();
+    const int64_t begin = (int64_t)blockIdx.x * CHUNK, end = begin + CHUNK < slots ? begin + CHUNK : slots;
+    count_chunk(ids, begin, end, E, count);
+    __syncthreads();
+    for (int i = threadIdx.x; i < E; i += 64) work[(int64_t)blockIdx.x * E + i] = count[i];
+}
+
+__global__ __launch_bounds__(1024) void plan_sum_kernel(asgd_route_order o, int64_t chunks, int *work)
+{
+    const int E = o.E, e = threadIdx.x;
+    int n = 0;
+    if (e < E)
+        for (int64_t c = 0; c < chunks; c++) n += work[c * E + e];
+    int offset;
+    sum_experts(n, E, o.offsets, o.blocks, offset);
+    if (e < E)
+        for (int64_t c = 0; c < chunks; c++) {
+            const int m = work[c * E + e];
+            work[c * E + e] = offset;
+            offset += m;
+        }
+}
+
+__global__ __launch_bounds__(64) void plan_place_kernel(const int32_t *ids, asgd_route_order o, const int *work)
+{
+    extern __shared__ int next[];                   // E
+    const int E = o.E;
+    const int64_t slots = o.T * o.k;
+    for (int i = threadIdx.x; i < E; i += 64) next[i] = work[(int64_t)blockIdx.x * E + i];
+    __syncthreads();
+    const int64_t begin = (int64_t)blockIdx.x * CHUNK, end = begin + CHUNK < slots ? begin + CHUNK : slots;
+    place_chunk(ids, begin, end, E, next, o.slots, o.places);
+    const int used = o.offsets[E];
+    for (int64_t p = begin + threadIdx.x; p < end; p += 64)
+        if (p >= used) o.slots[p] = -1;
+}
+
+template <class F> hipError_t with_width(int E, F f)
+{
+    if (E <= 64) return f(std::integral_constant<int, 1>{});
+    if (E <= 128) return f(std::integral_constant<int, 2>{});
+    if (E <= 256) return f(std::integral_constant<int, 4>{});
+    if (E <= 512) return f(std::integral_constant<int, 8>{});
+    return f(std::integral_constant<int, 16>{});
+}
+
+}  // namespace
+
+// four rows a workgroup, and more than once around where there are over four million
+static unsigned route_grid(int64_t T) { return (unsigned)((T + 3) / 4 < (1 << 20) ? (T + 3) / 4 : (1 << 20)); }
+
+hipError_t launch_route(const RouteArgs &a, int type, hipStream_t s)
+{
+    const unsigned grid = route_grid(a.T);
+    return with_type(type, [&](auto ty) {
+        return with_width(a.E, [&](auto v) {
+            route_kernel<decltype(ty), decltype(v)::value><<<grid, 256, 0, s>>>(a);
+            return hipGetLastError();
+        });
+    });
+}
+
+hipError_t launch_route_backward(const RouteArgs &a, int type, hipStream_t s)
+{
+    const unsigned grid = route_grid(a.T);
+    return with_type(type, [&](auto ty) {
+        return with_width(a.E, [&](auto v) {
+            route_backward_kernel<decltype(ty), decltype(v)::value><<<grid, 256, 0, s>>>(a);
+            return hipGetLastError();
+        });
+    });
+}
+
+size_t route_plan_bytes(int64_t slots, int E)
+{
+    if (slots <= (int64_t)CHUNK * ONE_BLOCK_CHUNKS) return 0;
+    return (size_t)((slots + CHUNK - 1) / CHUNK) * E * sizeof(int);
+}
+
+hipError_t launch_route_plan(const int32_t *ids, const asgd_route_order &o, void *work, hipStream_t s)
+{
+    const int64_t slots = o.T * o.k;
+    if (slots <= (int64_t)CHUNK * ONE_BLOCK_CHUNKS) {
+        // few slots: shorter chunks, so that all sixteen waves have some
+        int chunk = (int)((slots + ONE_BLOCK_CHUNKS - 1) / ONE_BLOCK_CHUNKS);
+        chunk = chunk < 64 ? 64 : (chunk + 63) / 64 * 64;
+        const int chunks = slots ? (int)((slots + chunk - 1) / chunk) : 1;
+        plan_one_block_kernel<<<1, 1024, (size_t)chunks * (o.E + 1) * sizeof(int), s>>>(ids, o, chunk, chunks);
+        return hipGetLastError();
+    }
+    const unsigned chunks = (unsigned)((slots + CHUNK - 1) / CHUNK);
+    plan_count_kernel<<<chunks, 64, (o.E + 1) * sizeof(int), s>>>(ids, slots, o.E, (int *)work);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    plan_sum_kernel<<<1, 1024, 0, s>>>(o, chunks, (int *)work);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    plan_place_kernel<<<chunks, 64, o.E * sizeof(int), s>>>(ids, o, (const int *)work);
+    return hipGetLastError();
+}
+
+}  // namespace asgd

@@ -1,0 +1,320 @@
+"""Routed experts on torch tensors: routing, products in 8-bit blocks, and the products of the experts a row was routed to.
+
+Every function checks what it is given, allocates its results and enqueues the library's kernels on the current stream of
+the tensors' device; nothing is waited for and nothing is computed here.  Rows may be strided, their elements are consecutive.
+Activations, logits and results are float32, bfloat16 or float16; what is kept in 8 bits is torch.float8_e4m3fn.
+
+    rule = Rule(k=6, score=SIGMOID, scale=2.5)
+    ids, weights = route(x @ centroids.t(), rule, bias=bias)         # the best six of the experts for every row
+    y, kept = experts(x, ids, weights, w, train=True)                # w: quantize_weights(bf16 weights [E, N, K])
+    d_x, d_w, d_weights = experts_backward(d_y, kept, w_turned)      # w_turned: quantize_weights(..., turned=True)
+    d_logits = route_backward(logits, rule, ids, d_weights, bias=bias)
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding as B
+
+SOFTMAX, SIGMOID = B.SCORE_SOFTMAX, B.SCORE_SIGMOID
+BEST, BEST_TWO = B.GROUP_BEST, B.GROUP_BEST_TWO
+BLOCK = 128
+
+_TYPES = {torch.float32: B.TYPE_F32, torch.bfloat16: B.TYPE_BF16, torch.float16: B.TYPE_F16}
+
+
+def _type(dtype):
+    code = _TYPES.get(dtype)
+    if code is None:
+        raise ValueError("float32, bfloat16 or float16 is wanted, not %s" % dtype)
+    return code
+
+
+def _stream(t):
+    if t.device.type != "cuda":
+        raise ValueError("a tensor on the GPU is wanted; there is no CPU fallback")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("the tensors are on %s, the current device is %d" % (t.device, torch.cuda.current_device()))
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _matrix(t, rows=None, cols=None, name="x"):
+    """(type, rows, cols, stride) of a matrix whose rows are runs of consecutive elements."""
+    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise ValueError("%s: a matrix%s is wanted, not %s" % (name, "" if rows is None and cols is None else " [%s, %s]" % (
+            "..." if rows is None else rows, "..." if cols is None else cols), tuple(t.shape)))
+    r, c = t.shape
+    stride = t.stride(0) if r > 1 else c
+    if (c > 1 and t.stride(1) != 1) or stride < c:
+        raise ValueError("%s: the elements of a row have to be consecutive and rows apart (strides %s)" % (name, t.stride()))
+    return _type(t.dtype), r, c, stride
+
+
+def _same_device(first, *others):
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("tensors on %s and %s" % (first.device, t.device))
+
+
+def _flat(t, shape, dtype, name):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError("%s: a contiguous %s tensor %s is wanted, not %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+
+
+class Rule:
+    """How experts are chosen: `k` of them by `score` (SOFTMAX, SIGMOID), out of the `kept` best of `groups` groups (judged by
+    their BEST key or the sum of their BEST_TWO); with renormalize a row's weights add up to `scale`, else they are scores times `scale`."""
+    __slots__ = ("k", "_c")
+
+    def __init__(self, k, score=SOFTMAX, groups=1, kept=1, group_by=BEST, renormalize=True, scale=1.0):
+        self.k = k
+        self._c = B.asgd_route_rule(k, score, groups, kept, group_by, int(renormalize), scale)
+
+
+def route(logits, rule, bias=None):
+    """(ids [T, k] int32, weights [T, k] float32) of the experts that rows of logits [T, E] are routed to; bias [E] float32 takes part in
+    the choice alone.  -infinity in logits or bias takes an expert out; ids are -1 and weights 0 where none is left."""
+    type, T, E, stride = _matrix(logits, name="logits")
+    _same_device(logits, bias)
+    if bias is not None:
+        _flat(bias, (E,), torch.float32, "bias")
+    s = _stream(logits)
+    ids = torch.empty((T, rule.k), dtype=torch.int32, device=logits.device)
+    weights = torch.empty((T, rule.k), dtype=torch.float32, device=logits.device)
+    B.asgd_route(logits.data_ptr(), type, T, E, stride, None if bias is None else bias.data_ptr(), rule._c, ids.data_ptr(),
+                 weights.data_ptr(), s)
+    return ids, weights
+
+
+def route_backward(logits, rule, ids, d_weights, bias=None):
+    """The gradient of the logits [T, E], in their type, from that of route()'s weights; the choice is held fixed."""
+    type, T, E, stride = _matrix(logits, name="logits")
+    _same_device(logits, ids, d_weights, bias)
+    _flat(ids, (T, rule.k), torch.int32, "ids")
+    _flat(d_weights, (T, rule.k), torch.float32, "d_weights")
+    if bias is not None:
+        _flat(bias, (E,), torch.float32, "bias")
+    s = _stream(logits)
+    out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+    B.asgd_route_backward(logits.data_ptr(), type, T, E, stride, None if bias is None else bias.data_ptr(), rule._c, ids.data_ptr(),
+                          d_weights.data_ptr(), out.data_ptr(), E, s)
+    return out
+
+
+class Plan:
+    """The order in which experts take their rows (plan()): offsets [E + 1] (an expert's first place), blocks [E + 1] (its first block
+    where each begins a new block of 128 places), slots [T * k] (the slot t * k + j at a place, -1: none), places [T * k] (the place of a
+    slot, -1: none)."""
+    __slots__ = ("T", "k", "E", "offsets", "blocks", "slots", "places", "_c", "_memory")
+
+    def __init__(self, T, k, E, device):
+        n = T * k
+        self.T, self.k, self.E = T, k, E
+        self._memory = m = torch.empty(2 * (E + 1) + 2 * n, dtype=torch.int32, device=device)
+        self.offsets, self.blocks, self.slots, self.places = m[:E + 1], m[E + 1:2 * E + 2], m[2 * E + 2:2 * E + 2 + n], m[2 * E + 2 + n:]
+        at = m.data_ptr()
+        self._c = B.asgd_route_order(T, k, E, at, at + 4 * (E + 1), at + 8 * (E + 1), at + 8 * (E + 1) + 4 * n)
+
+    def max_blocks(self):
+        return B.asgd_route_max_blocks(self.T, self.k, self.E)
+
+
+def plan(ids, experts):
+    """The Plan of ids [T, k] (int32; what is outside 0 .. experts - 1 has no expert)."""
+    if ids.dim() != 2:
+        raise ValueError("ids: [T, k] is wanted, not %s" % (tuple(ids.shape),))
+    _flat(ids, ids.shape, torch.int32, "ids")
+    s = _stream(ids)
+    p = Plan(ids.shape[0], ids.shape[1], experts, ids.device)
+    size = B.asgd_route_plan_bytes(p.T, p.k, p.E)
+    work = torch.empty(size, dtype=torch.uint8, device=ids.device) if size else None
+    B.asgd_route_plan(ids.data_ptr(), p._c, None if work is None else work.data_ptr(), size, s)
+    return p
+
+
+class Blocks:
+    """A matrix, or one for each expert, in 8-bit blocks: values [..., rows, 128 * ceil(cols / 128)] (float8_e4m3fn or uint8, zeros
+    from `cols` on) times scales: squares [..., ceil(rows / 128), ceil(cols / 128)], or (squares=False) [ceil(cols / 128), rows]."""
+    __slots__ = ("values", "scales", "rows", "cols", "count", "squares", "_c")
+
+    def __init__(self, values, scales, cols, squares=True):
+        kb = -(-cols // BLOCK)
+        lead, rows = values.shape[:-2], values.shape[-2] if values.dim() >= 2 else -1
+        want = (*lead, -(-rows // BLOCK), kb) if squares else (kb, rows)
+        if values.element_size() != 1 or values.dim() not in ((2, 3) if squares else (2,)) or values.shape[-1] != kb * BLOCK or not values.is_contiguous():
+            raise ValueError("values: contiguous bytes [%srows, %d] are wanted, not %s %s" % ("experts, " if squares else "", kb * BLOCK, values.dtype, tuple(values.shape)))
+        _flat(scales, want, torch.float32, "scales")
+        _same_device(values, scales)
+        self.values, self.scales, self.rows, self.cols, self.squares = values, scales, rows, cols, squares
+        self.count = lead[0] if lead else 1
+        self._c = B.asgd_blocks(values.data_ptr(), scales.data_ptr(), rows, cols, B.BLOCKS_SQUARES if squares else B.BLOCKS_ROWS, self.count, 0, 0)
+
+
+def quantize(x, turned=False, plan=None, weights=None):
+    """x [rows, cols] in 8-bit blocks of 1 x 128 (Blocks, squares=False), or with `turned` its transpose, blocks along x's rows.  With a
+    plan x has a row for each of its T rows, and what is brought to 8 bits has one for each place: x's row of the place's slot, times the
+    slot's weight (weights [T, k] float32) if given; turned, every expert's places begin a new block and the rest of its last one is zeros."""
+    type, rows, cols, stride = _matrix(x, None if plan is None else plan.T)
+    _same_device(x, weights)
+    if weights is not None:
+        if plan is None:
+            raise ValueError("weights belong to the slots of a plan")
+        _flat(weights, (plan.T, plan.k), torch.float32, "weights")
+    s = _stream(x)
+    out_rows = cols if turned else rows if plan is None else plan.T * plan.k
+    out_cols = cols if not turned else rows if plan is None else max(1, plan.max_blocks()) * BLOCK
+    kb = -(-out_cols // BLOCK)
+    out = Blocks(torch.empty((out_rows, kb * BLOCK), dtype=torch.float8_e4m3fn, device=x.device),
+                 torch.empty((kb, out_rows), dtype=torch.float32, device=x.device), out_cols, squares=False)
+    if rows:
+        B.asgd_block_quantize(x.data_ptr(), type, rows, cols, stride, int(turned), None if plan is None else plan._c,
+                              None if weights is None else weights.data_ptr(), out._c, s)
+    return out
+
+
+def quantize_weights(w, turned=False):
+    """Weights [rows, cols] or [experts, rows, cols] in 8-bit squares of 128 x 128, or with `turned` their transposes (the same values:
+    squares turn into squares), which the gradient of the activations takes."""
+    if w.dim() not in (2, 3) or not w.is_contiguous() or w.numel() == 0:
+        raise ValueError("weights: a contiguous [rows, cols] or [experts, rows, cols] is wanted, not %s" % (tuple(w.shape),))
+    type, s, lead = _type(w.dtype), _stream(w), w.shape[:-2]
+    rows, cols = w.shape[-2:]
+    out_rows, out_cols = (cols, rows) if turned else (rows, cols)
+    kb = -(-out_cols // BLOCK)
+    out = Blocks(torch.empty((*lead, out_rows, kb * BLOCK), dtype=torch.float8_e4m3fn, device=w.device),
+                 torch.empty((*lead, -(-out_rows // BLOCK), kb), dtype=torch.float32, device=w.device), out_cols)
+    B.asgd_block_quantize(w.data_ptr(), type, rows, cols, cols, int(turned), None, None, out._c, s)
+    return out
+
+
+def _exact(dtype, exact):
+    return int(dtype == torch.float32 if exact is None else exact)
+
+
+def product(a, b, dtype, plan=None, gather=False, exact=None):
+    """a b^T in `dtype` of two Blocks of the same cols.  With a plan b has a matrix for each expert, and row p of the result is that of
+    the place p with the matrix of its expert: a has a row for each place, or with `gather` one for each of the plan's T rows.  Rows at
+    places that are not in use are left as they were allocated.  exact: the products of a block are summed in 32 bits, at half the rate,
+    and not by the 8-bit matrix instruction, whose sums are off by 1.5e-5 to 7e-5 of the result (None: for float32 results)."""
+    _same_device(a.values, b.values)
+    type, s = _type(dtype), _stream(a.values)
+    rows = a.rows if plan is None else plan.T * plan.k
+    if a.cols == 0 and b.cols == 0:                                  # (a sum over nothing)
+        return torch.zeros((rows, b.rows), dtype=dtype, device=a.values.device)
+    out = torch.empty((rows, b.rows), dtype=dtype, device=a.values.device)
+    mode = B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER if gather else B.PRODUCT_PLACES
+    if rows:
+        B.asgd_block_product(a._c, b._c, mode, _exact(dtype, exact), None if plan is None else plan._c, out.data_ptr(), type, b.rows, s)
+    return out
+
+
+def product_over(a, b, plan, dtype=torch.float32, exact=None):
+    """[E, a.rows, b.rows]: for each expert a b^T over its own places alone; a and b are quantize(..., turned=True, plan=plan)."""
+    _same_device(a.values, b.values)
+    type, s = _type(dtype), _stream(a.values)
+    if plan.T == 0:
+        return torch.zeros((plan.E, a.rows, b.rows), dtype=dtype, device=a.values.device)
+    out = torch.empty((plan.E, a.rows, b.rows), dtype=dtype, device=a.values.device)
+    B.asgd_block_product(a._c, b._c, B.PRODUCT_OVER, _exact(dtype, exact), plan._c, out.data_ptr(), type, b.rows, s)
+    return out
+
+
+def _raw(x):
+    """x as an operand that the product brings to 8 bits itself."""
+    type, rows, cols, stride = _matrix(x)
+    return B.asgd_blocks(x.data_ptr(), None, rows, cols, B.BLOCKS_RAW, 1, type, stride)
+
+
+def _product_of(x, w, dtype, plan=None, exact=None):
+    """x, one row for each of the plan's T, times w."""
+    rows = x.shape[0] if plan is None else plan.T * plan.k
+    if not 0 < rows <= B.PRODUCT_RAW_ROWS:
+        return product(quantize(x), w, dtype, plan=plan, gather=plan is not None, exact=exact)
+    _same_device(x, w.values)
+    out = torch.empty((rows, w.rows), dtype=dtype, device=x.device)
+    B.asgd_block_product(_raw(x), w._c, B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER, _exact(dtype, exact), None if plan is None else plan._c,
+                         out.data_ptr(), _type(dtype), w.rows, _stream(x))
+    return out
+
+
+def experts_sum(y, plan, dtype, weights=None):
+    """[T, n] in `dtype`: the sum of each row's y [T * k, n] at the places of its slots, times weights [T, k] if given."""
+    y_type, _, n, y_stride = _matrix(y, plan.T * plan.k, name="y")
+    _same_device(y, weights)
+    if weights is not None:
+        _flat(weights, (plan.T, plan.k), torch.float32, "weights")
+    s = _stream(y)
+    out = torch.empty((plan.T, n), dtype=dtype, device=y.device)
+    B.asgd_experts_sum(y.data_ptr(), y_type, n, y_stride, plan._c, None if weights is None else weights.data_ptr(), out.data_ptr(),
+                       _type(dtype), n, s)
+    return out
+
+
+def experts_sum_backward(d_out, y, plan):
+    """The gradient [T, k] float32 of experts_sum()'s weights from that of its result [T, n]."""
+    y_type, _, n, y_stride = _matrix(y, plan.T * plan.k, name="y")
+    type, _, _, stride = _matrix(d_out, plan.T, n, "d_out")
+    _same_device(y, d_out)
+    s = _stream(y)
+    out = torch.empty((plan.T, plan.k), dtype=torch.float32, device=y.device)
+    B.asgd_experts_sum_backward(d_out.data_ptr(), type, stride, y.data_ptr(), y_type, n, y_stride, plan._c, out.data_ptr(), s)
+    return out
+
+
+def _check_weights(x, w, experts=False):
+    if not w.squares or (w.count != 1 and not experts):
+        raise ValueError("weights in squares are wanted%s" % ("" if experts else ", one matrix of them"))
+    if x.dim() != 2 or x.shape[1] != w.cols:
+        raise ValueError("x: [rows, %d] is wanted, not %s" % (w.cols, tuple(x.shape)))
+
+
+def linear(x, w, train=False):
+    """x [rows, K] times w^T, in x's type: x is brought to 8 bits on the way, w is quantize_weights() of [N, K].  train: (the result, what
+    linear_backward() needs)."""
+    _check_weights(x, w)
+    y = _product_of(x, w, x.dtype)
+    return (y, quantize(x, turned=True)) if train else y
+
+
+def linear_backward(d_out, kept, w_turned):
+    """(d_x, in d_out's type, and d_w [N, K] float32) of linear(): from d_out [rows, N], what it kept, and the turned weights."""
+    _check_weights(d_out, w_turned)
+    if d_out.shape[0] != kept.cols or w_turned.rows != kept.rows:
+        raise ValueError("d_out %s and the kept x [%d, %d] do not belong together" % (tuple(d_out.shape), kept.cols, kept.rows))
+    d_x = _product_of(d_out, w_turned, d_out.dtype)
+    return d_x, product(quantize(d_out, turned=True), kept, torch.float32)
+
+
+class Kept:
+    """What experts_backward() needs of experts()."""
+    __slots__ = ("plan", "weights", "y", "x_turned")
+
+    def __init__(self, plan, weights, y, x_turned):
+        self.plan, self.weights, self.y, self.x_turned = plan, weights, y, x_turned
+
+
+def experts(x, ids, weights, w, train=False):
+    """[T, N] in x's type: for each row of x [T, K] the sum of its experts' products with it, weights [T, k] times w[ids] x, ids as route() gives
+    them.  w is quantize_weights() of [E, N, K].  train: (the result, what experts_backward() needs)."""
+    _check_weights(x, w, experts=True)
+    _same_device(x, ids, weights, w.values)
+    if ids.dim() != 2 or ids.shape[0] != x.shape[0]:
+        raise ValueError("ids: [%d, k] is wanted, not %s" % (x.shape[0], tuple(ids.shape)))
+    _flat(weights, ids.shape, torch.float32, "weights")
+    order = plan(ids, w.count)
+    # 32-bit until the sum: one rounding to the result's type.  Beside a rounding to 16 bits the error of the 8-bit instruction does not
+    # show; the gradient of the weights is 32-bit, and y goes into it
+    y = _product_of(x, w, torch.float32, order, exact=train or x.dtype == torch.float32)
+    out = experts_sum(y, order, x.dtype, weights)
+    return (out, Kept(order, weights, y, quantize(x, turned=True, plan=order))) if train else out
+
+
+def experts_backward(d_out, kept, w_turned):
+    """(d_x [T, K] in d_out's type, d_w [E, N, K] float32, d_weights [T, k] float32) of experts(), from d_out [T, N]."""
+    _check_weights(d_out, w_turned, experts=True)
+    order = kept.plan
+    d_weights = experts_sum_backward(d_out, kept.y, order)
+    rows = product(quantize(d_out, plan=order, weights=kept.weights), w_turned, torch.float32, plan=order, exact=d_out.dtype == torch.float32)
+    d_x = experts_sum(rows, order, d_out.dtype)
+    d_w = product_over(quantize(d_out, turned=True, plan=order, weights=kept.weights), kept.x_turned, order)
+    return d_x, d_w, d_weights
