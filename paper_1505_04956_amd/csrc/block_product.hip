@@ -12,6 +12,8 @@ namespace asgd {
 
 namespace {
 
+template <int N> using One = std::integral_constant<int, N>;
+
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
@@ -55,11 +57,16 @@ __device__ __forceinline__ v4f block_product(const Operand<true> &a, const Opera
     return part;
 }
 
-// 64 lanes x 16 bytes, from an address of each lane to consecutive places of the LDS
-__device__ __forceinline__ void to_lds(const uint8_t *from, uint8_t *to)
+// 64 lanes x 16 bytes, from a base and an offset of each lane to consecutive places of the LDS; and 64 x 4 bytes
+template <class Offset> __device__ __forceinline__ void to_lds(const uint8_t *base, Offset offset, uint8_t *to)
 {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + offset),
                                      (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+__device__ __forceinline__ void to_lds4(const uint8_t *base, uint32_t offset, uint8_t *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + offset),
+                                     (__attribute__((address_space(3))) void *)to, 4, 0, 0);
 }
 
 template <class Ty> __device__ __forceinline__ void store_four(typename Ty::T *p, int64_t left, bool wide, v4f v)
@@ -73,6 +80,20 @@ template <class Ty> __device__ __forceinline__ void store_four(typename Ty::T *p
 #pragma unroll
         for (int i = 0; i < 4; i++)
             if (i < left) p[i] = (T)v[i];
+    }
+}
+
+// sixteen bytes of a row, of which `left` elements exist; wide: rows begin at a multiple of 16 bytes
+template <class T> __device__ __forceinline__ void store16(T *p, int64_t left, bool wide, uint4 v)
+{
+    constexpr int N = 16 / sizeof(T);
+    if (wide && left >= N) *(uint4 *)p = v;
+    else {
+        T u[N];
+        *(uint4 *)u = v;
+#pragma unroll
+        for (int i = 0; i < N; i++)
+            if (i < left) p[i] = u[i];
     }
 }
 
@@ -107,39 +128,54 @@ __device__ __forceinline__ bool tile_of_expert(const asgd_route_order &o, int64_
 }
 
 // Workgroups go round the eight dies; each die gets a run of neighbouring tiles, whose operands its L2 then shares.
-__device__ __forceinline__ int64_t tile_of_group(int64_t id, int64_t n)
+__device__ __forceinline__ uint32_t tile_of_group(uint32_t id, uint32_t n)
 {
-    const int64_t die = id & 7, at = id >> 3, share = n >> 3, rest = n & 7;
+    const uint32_t die = id & 7, at = id >> 3, share = n >> 3, rest = n & 7;
     return die * share + (die < rest ? die : rest) + at;
 }
 
-// A tile of TOK rows of a and WT rows of b; the waves are TOK_WAVES x WT_WAVES.  A block of the contraction of both goes to
-// the LDS (16-byte pieces of a row at their number xor the row's low bits: the lanes of a read then spread over the banks)
-// while the block before it is multiplied.
-template <int TOK, int WT, int TOK_WAVES, int WT_WAVES, bool SQUARES, bool EXACT, class Out>
-__global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES) void product_kernel(ProductArgs p, int64_t tiles_tok, int64_t tiles_wt, bool wide)
+// A tile of TOK rows of a and WT rows of b; the waves are TOK_WAVES x WT_WAVES, each with I x J pieces of 16 x 16.  Blocks of the
+// contraction of both, and their scales, go straight to one of two stages in the LDS; 16-byte pieces of a row lie at their
+// number xor the row's low bits, so that the lanes of a read spread over the banks.
+//
+// Within a block the rows of b are taken sixteen at a time: while the matrix cores work on one, the next is read from the
+// LDS and the sums of earlier ones are scaled and added.  The one barrier of a block lies before its last sixteen rows: by then a wave has
+// read all it needs of this stage, which the block after next may take, and the next block, on its way since the
+// last barrier, is there to be read while those last rows are multiplied.
+template <int TOK, int WT, bool SQUARES> struct Stage {
+    static constexpr int VALUES = (TOK + WT) * BLOCK8;                                      // bytes
+    // pieces of 64 scales: the rows' of a; the rows' of b, or for squares one for 128 rows, 64 times over
+    static constexpr int PIECES_A = (TOK + 63) / 64, PIECES_B = SQUARES ? (WT + BLOCK8 - 1) / BLOCK8 : (WT + 63) / 64, PIECES = PIECES_A + PIECES_B;
+    static constexpr int SCALES_B = VALUES + PIECES_A * 256, BYTES = VALUES + PIECES * 256;
+};
+
+template <int TOK, int WT, int TOK_WAVES, int WT_WAVES, bool SQUARES, bool EXACT, bool FAR, class Out>
+__global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_kernel(ProductArgs p, uint32_t tiles_tok, uint32_t tiles_wt, bool wide)
 {
+    typedef Stage<TOK, WT, SQUARES> S;
     constexpr int WAVES = TOK_WAVES * WT_WAVES, J = TOK / TOK_WAVES / 16, I = WT / WT_WAVES / 16;
     constexpr int SEGMENTS = (TOK + WT) / 8 / WAVES;             // of eight rows, that a wave brings
-    static_assert((TOK + WT) / 8 % WAVES == 0 && WT / WT_WAVES <= BLOCK8, "");
-    __shared__ __align__(16) uint8_t stage0[(TOK + WT) * BLOCK8];
-    __shared__ __align__(16) uint8_t stage1[(TOK + WT) * BLOCK8];
+    constexpr int PIECES = (S::PIECES + WAVES - 1) / WAVES;      // of 64 scales
+    static_assert((TOK + WT) / 8 % WAVES == 0 && WT / WT_WAVES <= BLOCK8 && TOK % (16 * TOK_WAVES) == 0 && WT % (16 * WT_WAVES) == 0, "");
+    __shared__ __align__(16) uint8_t stage0[S::BYTES];
+    __shared__ __align__(16) uint8_t stage1[S::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wave_tok = wave % TOK_WAVES * (J * 16), wave_wt = wave / TOK_WAVES * (I * 16);
 
     // which tile: strips of eight tiles of a, all tiles of b for each
-    const int64_t id = tile_of_group(blockIdx.x, gridDim.x);
-    int64_t matrix = 0, within = id;
+    const uint32_t id = tile_of_group(blockIdx.x, gridDim.x);
+    uint32_t within = id;
+    int64_t matrix = 0;
     if (p.mode == ASGD_PRODUCT_OVER) {
         matrix = id / (tiles_tok * tiles_wt);
-        within = id - matrix * tiles_tok * tiles_wt;
+        within = id - (uint32_t)matrix * tiles_tok * tiles_wt;
     }
-    const int64_t strip = within / (8 * tiles_wt), in_strip = within - strip * 8 * tiles_wt;
-    const int64_t high = tiles_tok - strip * 8 < 8 ? tiles_tok - strip * 8 : 8;
-    const int64_t tile_wt = in_strip / high, tile_tok = strip * 8 + in_strip - tile_wt * high;
+    const uint32_t strip = within / (8 * tiles_wt), in_strip = within - strip * 8 * tiles_wt;
+    const uint32_t high = min(tiles_tok - strip * 8, 8u), tile_wt = in_strip / high, tile_tok = strip * 8 + in_strip - tile_wt * high;
 
-    int64_t first = tile_tok * TOK, end = p.rows_a, k0 = 0, k1 = p.kb;
-    const int64_t first_wt = tile_wt * WT;
+    int64_t first = (int64_t)tile_tok * TOK, end = p.rows_a;
+    int k0 = 0, k1 = (int)p.kb;
+    const int64_t first_wt = (int64_t)tile_wt * WT;
     if (p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES) {
         int e;
         if (!tile_of_expert(p.order, tile_tok, TOK, e, first, end)) return;
@@ -148,36 +184,50 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES) void product_kernel(Prod
         k0 = p.order.blocks[matrix];
         k1 = p.order.blocks[matrix + 1];
     }
-    const int64_t row_bytes = p.kb * BLOCK8;
-    const uint8_t *b = p.b + (p.mode == ASGD_PRODUCT_OVER ? 0 : matrix * p.rows_b * row_bytes);
+    const int64_t row_bytes = p.kb * BLOCK8, b_matrix = p.mode == ASGD_PRODUCT_OVER ? 0 : matrix * p.rows_b;
     const auto row_of_a = [&](int64_t r) {                        // (rows beyond the last: the last again)
         r = r < end ? r : end - 1;
         return p.mode == ASGD_PRODUCT_GATHER ? (int64_t)(p.order.slots[r] / p.order.k) : r;
     };
+    const auto row_of_b = [&](int64_t r) { return r < p.rows_b ? r : p.rows_b - 1; };
 
-    const uint8_t *from[SEGMENTS];
+    // Where a lane's pieces come from, in bytes from the tile's first row.  Neighbouring rows of a tile are less than 2^32 bytes apart;
+    // gathered ones may be further (FAR)
+    typedef typename std::conditional<FAR, uint64_t, uint32_t>::type Offset;
+    Offset from[SEGMENTS];
+    const int64_t first_a = row_of_a(first);
+    const uint8_t *const a_base = p.a + first_a * row_bytes, *const b_base = p.b + (b_matrix + first_wt) * row_bytes;
 #pragma unroll
     for (int s = 0; s < SEGMENTS; s++) {
         const int row = (wave * SEGMENTS + s) * 8 + (lane >> 3), piece = (lane & 7) ^ (lane >> 3);
-        if (row < TOK) from[s] = p.a + row_of_a(first + row) * row_bytes + piece * 16;
-        else {
-            const int64_t r = first_wt + row - TOK;
-            from[s] = b + (r < p.rows_b ? r : p.rows_b - 1) * row_bytes + piece * 16;
+        const int64_t r = row < TOK ? row_of_a(first + row) - first_a : row_of_b(first_wt + row - TOK) - first_wt;
+        from[s] = (Offset)(r * row_bytes + piece * 16);
+    }
+    // and its scales: a run of 64 rows, or (squares) one number for all lanes
+    uint32_t scale_row[PIECES];                                  // bytes
+    const float *scale_from[PIECES];
+    int64_t scale_step[PIECES];                                  // from block to block
+#pragma unroll
+    for (int s = 0; s < PIECES; s++) {
+        const int piece = (wave + s * WAVES) % S::PIECES;         // (some twice: the same numbers to the same places)
+        const int64_t at = first_wt / BLOCK8 + (piece - S::PIECES_A), nb = blocks8(p.rows_b);
+        const bool of_a = piece < S::PIECES_A;
+        scale_row[s] = 4 * (uint32_t)(of_a ? row_of_a(first + piece * 64 + lane) : SQUARES ? 0 : row_of_b(first_wt + (piece - S::PIECES_A) * 64 + lane));
+        scale_from[s] = of_a ? p.sa : SQUARES ? p.sb + (matrix * nb + (at < nb ? at : nb - 1)) * p.kb : p.sb;
+        scale_step[s] = of_a ? p.rows_a : SQUARES ? 1 : p.rows_b;
+    }
+    constexpr int LOADS = SEGMENTS + PIECES, LOADING = I > 1 ? 2 : 1;  // of a wave for a block; over so many of its steps
+    const auto bring = [&](int kb, uint8_t *stage, int l) {      // the l-th of a wave's loads of a block
+        if (l < SEGMENTS) {
+            const int segment = wave * SEGMENTS + l;
+            asm volatile("" : "+v"(from[l]));                     // (else its sum with the base is kept, in twice the registers)
+            to_lds((segment * 8 < TOK ? a_base : b_base) + (int64_t)kb * BLOCK8, from[l], stage + segment * 1024);
+        } else {
+            const int s = l - SEGMENTS;
+            asm volatile("" : "+v"(scale_row[s]));
+            to_lds4((const uint8_t *)(scale_from[s] + kb * scale_step[s]), scale_row[s], stage + S::VALUES + (wave + s * WAVES) % S::PIECES * 256);
         }
-    }
-    const auto bring = [&](int64_t kb, uint8_t *stage) {
-#pragma unroll
-        for (int s = 0; s < SEGMENTS; s++) to_lds(from[s] + kb * BLOCK8, stage + (wave * SEGMENTS + s) * 1024);
     };
-
-    const float *scale_a[J];
-#pragma unroll
-    for (int j = 0; j < J; j++) scale_a[j] = p.sa + row_of_a(first + wave_tok + j * 16 + (lane & 15));
-    int64_t square = 0;
-    if (SQUARES) {
-        const int64_t nb = blocks8(p.rows_b), at = (first_wt + wave_wt) / BLOCK8;
-        square = (matrix * nb + (at < nb ? at : nb - 1)) * p.kb;
-    }
 
     v4f sum[I][J];
 #pragma unroll
@@ -185,80 +235,110 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES) void product_kernel(Prod
 #pragma unroll
         for (int j = 0; j < J; j++) sum[i][j] = {0.0f, 0.0f, 0.0f, 0.0f};
 
-    const int low = ((lane >> 4) ^ (lane & 7)) * 16, row_at = (lane & 15) * BLOCK8;
-    const auto operand = [&](const uint8_t *stage, int row) {
-        const uint8_t *at = stage + row * BLOCK8 + row_at;
-        const v4i u = *(const v4i *)(at + low), v = *(const v4i *)(at + (low ^ 64));
+    // A lane's places in a stage: its pieces of the first sixteen rows of each operand, its scales.  (Opaque, so that all reads are a
+    // register and a constant.)
+    const int low = ((lane >> 4) ^ (lane & 7)) * 16;
+    int at_a = (wave_tok + (lane & 15)) * BLOCK8 + low, at_w = (TOK + wave_wt + (lane & 15)) * BLOCK8 + low;
+    int at_sa = S::VALUES + (wave_tok + (lane & 15)) * 4, at_sb = S::SCALES_B + (SQUARES ? wave_wt / BLOCK8 * 256 + lane * 4 : wave_wt * 4 + (lane >> 4) * 16);
+    asm volatile("" : "+v"(at_a), "+v"(at_w), "+v"(at_sa), "+v"(at_sb));
+    const auto operand = [&](const uint8_t *stage, int at, int rows) {
         Operand<EXACT> o;
-        o.set(u, v);
+        o.set(*(const v4i *)(stage + at + rows * BLOCK8), *(const v4i *)(stage + (at ^ 64) + rows * BLOCK8));
         return o;
     };
-    const auto multiply = [&](int64_t kb, const uint8_t *stage) {
+    // multiplies the block in `stage` and brings block `next` to `other`
+    const auto multiply = [&](const uint8_t *stage, int next, uint8_t *other, auto bringing) {
+        constexpr bool BRING = decltype(bringing)::value;
+        constexpr int LAG = 2, N = I * J, PER = (LOADS + LOADING - 1) / LOADING;
         float s[J];
-        Operand<EXACT> a[J];
+        Operand<EXACT> a[J], w, after;
+        v4f part[LAG + 1], sb[2];
+        w = operand(stage, at_w, 0);
 #pragma unroll
         for (int j = 0; j < J; j++) {
-            s[j] = scale_a[j][kb * p.rows_a];
-            a[j] = operand(stage, wave_tok + j * 16);
+            a[j] = operand(stage, at_a, j * 16);
+            s[j] = *(const float *)(stage + at_sa + j * 64);
         }
         if (SQUARES) {
-            const float sb = p.sb[square + kb];
+            const float of_b = *(const float *)(stage + at_sb);
 #pragma unroll
-            for (int j = 0; j < J; j++) s[j] *= sb;
+            for (int j = 0; j < J; j++) s[j] *= of_b;
         }
 #pragma unroll
-        for (int i = 0; i < I; i++) {
-            const Operand<EXACT> w = operand(stage, TOK + wave_wt + i * 16);
-            v4f sb;
-            if (!SQUARES) {
-                const int64_t r = first_wt + wave_wt + i * 16 + (lane >> 4) * 4;
+        for (int q = 0; q < N + LAG; q++) {
+            if (q < N) {
+                const int i = q / J, j = q % J;
+                if (j == 0) {
+                    if (i > 0) w = after;
+                    if (i + 1 < I) after = operand(stage, at_w, (i + 1) * 16);
+                    if (!SQUARES) sb[i & 1] = *(const v4f *)(stage + at_sb + i * 64);
+                    if (BRING && i < LOADING)
 #pragma unroll
-                for (int n = 0; n < 4; n++) sb[n] = p.sb[kb * p.rows_b + (r + n < p.rows_b ? r + n : p.rows_b - 1)];
-            }
-#pragma unroll
-            for (int j = 0; j < J; j++) {
-                const v4f part = block_product(w, a[j]);
-#pragma unroll
-                for (int n = 0; n < 4; n++) {
-                    const float v = SQUARES ? part[n] : part[n] * sb[n];
-                    sum[i][j][n] = fmaf(v, s[j], sum[i][j][n]);
+                        for (int l = i * PER; l < (i + 1) * PER && l < LOADS; l++) bring(next, other, l);
                 }
+                part[q % (LAG + 1)] = block_product(w, a[j]);
             }
+            if (q >= LAG) {
+                const int i = (q - LAG) / J, j = (q - LAG) % J;
+                const v4f got = part[(q - LAG) % (LAG + 1)];
+#pragma unroll
+                for (int n = 0; n < 4; n++) sum[i][j][n] = fmaf(SQUARES ? got[n] : got[n] * sb[i & 1][n], s[j], sum[i][j][n]);
+                asm volatile("" : "+v"(sum[i][j]));               // (here, and not after the next barrier)
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
-    if (k0 < k1) bring(k0, stage0);
-    __syncthreads();
-    for (int64_t kb = k0; kb < k1; kb += 2) {
-        if (kb + 1 < k1) bring(kb + 1, stage1);
-        multiply(kb, stage0);
+    if (k0 < k1) {
+#pragma unroll
+        for (int l = 0; l < LOADS; l++) bring(k0, stage0, l);
         __syncthreads();
-        if (kb + 1 >= k1) break;
-        if (kb + 2 < k1) bring(kb + 2, stage0);
-        multiply(kb + 1, stage1);
-        __syncthreads();
+        for (int kb = k0; kb + 1 < k1; kb += 2) {
+            multiply(stage0, kb + 1, stage1, std::true_type());
+            __syncthreads();
+            multiply(stage1, min(kb + 2, k1 - 1), stage0, std::true_type());      // (the last block once more where there is none left)
+            __syncthreads();
+        }
+        if ((k1 - k0) & 1) multiply(stage0, 0, stage1, std::false_type());
     }
 
+    // Out through the LDS, sixteen rows of a at a time: there a lane has four neighbours of a row, in memory whole lines are wanted.
     typedef typename Out::T T;
+    constexpr int ROW = I * 16 * sizeof(T), PITCH = ROW + 16, PER_ROW = ROW / 16, ROWS = 64 / PER_ROW;       // bytes; lanes of a row, rows of an instruction
     T *out = (T *)p.out + (p.mode == ASGD_PRODUCT_OVER ? matrix * p.rows_a * p.stride : 0);
+    __syncthreads();
+    constexpr int HALF = (WAVES + 1) / 2;
+    static_assert(HALF * 16 * PITCH <= S::BYTES, "");
+    uint8_t *mine = (wave < HALF ? stage0 : stage1) + (wave < HALF ? wave : wave - HALF) * 16 * PITCH;
 #pragma unroll
     for (int j = 0; j < J; j++) {
-        const int64_t r = first + wave_tok + j * 16 + (lane & 15);
-        if (r < end) {
 #pragma unroll
-            for (int i = 0; i < I; i++) {
-                const int64_t c = first_wt + wave_wt + i * 16 + (lane >> 4) * 4;
-                store_four<Out>(out + r * p.stride + c, p.rows_b - c, wide, sum[i][j]);
-            }
+        for (int i = 0; i < I; i++) {
+            T u[4] = {(T)sum[i][j][0], (T)sum[i][j][1], (T)sum[i][j][2], (T)sum[i][j][3]};
+            uint8_t *to = mine + (lane & 15) * PITCH + (i * 16 + (lane >> 4) * 4) * sizeof(T);
+            if constexpr (sizeof(T) == 4) *(uint4 *)to = *(uint4 *)u;
+            else *(uint2 *)to = *(uint2 *)u;
         }
+        __builtin_amdgcn_wave_barrier();
+        __threadfence_block();
+#pragma unroll
+        for (int n = 0; n < 16 / ROWS; n++) {
+            const int row = n * ROWS + lane / PER_ROW, at = lane % PER_ROW * 16;
+            const int64_t r = first + wave_tok + j * 16 + row, c = first_wt + wave_wt + at / sizeof(T);
+            const uint4 v = *(const uint4 *)(mine + row * PITCH + at);
+            if (r < end) store16<T>(out + r * p.stride + c, p.rows_b - c, wide, v);
+        }
+        __builtin_amdgcn_wave_barrier();
+        __threadfence_block();
     }
 }
 
-// ---- few rows, not in 8 bits yet --------------------------------------------------------------------------------------
+// ---- few rows ---------------------------------------------------------------------------------------------------------
 // What counts is that the weights arrive: they go from memory to registers, sixteen rows of one block of 128 a wave and
-// instruction, and the eight waves of a workgroup share the blocks of the contraction of sixteen rows of b.  The rows of a are
-// brought to 8 bits in the registers of the lanes that need them.
-constexpr int RAW_WAVES = 8;
+// instruction, and the eight waves of a workgroup share the blocks of the contraction of sixteen rows of b, four of them on
+// their way at a time.  Rows of a, J times sixteen, come from the caches; RAW ones are brought to 8 bits in the registers of
+// the lanes that need them (up to sixteen of them: there this is less than a launch costs).
+constexpr int FEW_WAVES = 8;
 
 template <class Ty> __device__ __forceinline__ void raw_block(const typename Ty::T *row, bool there, bool wide, int64_t c, int64_t cols, float &scale, v4i &lo, v4i &hi)
 {
@@ -288,83 +368,141 @@ template <class Ty> __device__ __forceinline__ void raw_block(const typename Ty:
     }
 }
 
-// grid: strips of sixteen rows of b, and (GATHER) places
-template <class In, bool EXACT, class Out> __global__ __launch_bounds__(64 * RAW_WAVES) void product_raw_kernel(ProductArgs p, bool wide_in, bool wide)
+// In: void, or the type of a RAW a (J = 1).  grid: strips of sixteen rows of b, tiles of a
+template <class In, int J, bool SQUARES, bool EXACT, class Out> __global__ __launch_bounds__(64 * FEW_WAVES) void product_few_kernel(ProductArgs p, bool wide_in, bool wide)
 {
-    __shared__ float parts[RAW_WAVES][64][4];
+    constexpr bool RAW = !std::is_same<In, void>::value;
+    __shared__ v4f parts[FEW_WAVES][J][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t strip = blockIdx.x;
-    int64_t matrix = 0, first = 0, end = p.rows_a;
-    if (p.mode == ASGD_PRODUCT_GATHER) {
+    int64_t matrix = 0, first = (int64_t)blockIdx.y * (16 * J), end = p.rows_a;
+    if (p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES) {
         int e;
-        if (!tile_of_expert(p.order, blockIdx.y, 1, e, first, end)) return;
+        if (!tile_of_expert(p.order, blockIdx.y, 16 * J, e, first, end)) return;
         matrix = e;
-        end = first + 1;
     }
     const int tok = lane & 15, quarter = lane >> 4;
-    const bool there = first + tok < end;
-    const int64_t src = !there ? 0 : p.mode == ASGD_PRODUCT_GATHER ? p.order.slots[first + tok] / p.order.k : first + tok;
-    const typename In::T *row = (const typename In::T *)p.a + src * p.stride_raw;
+    int64_t src[J];
+#pragma unroll
+    for (int j = 0; j < J; j++) {
+        const int64_t r = first + j * 16 + tok < end ? first + j * 16 + tok : end - 1;       // (rows beyond the last: the last again)
+        src[j] = p.mode == ASGD_PRODUCT_GATHER ? p.order.slots[r] / p.order.k : r;
+    }
     const int64_t r = strip * 16 + tok, row_bytes = p.kb * BLOCK8;
     const uint8_t *b = p.b + (matrix * p.rows_b + (r < p.rows_b ? r : p.rows_b - 1)) * row_bytes + quarter * 32;
-    const float *sb = p.sb + (matrix * blocks8(p.rows_b) + strip / 8) * p.kb;
-    v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t kb = wave; kb < p.kb; kb += RAW_WAVES) {
-        const v4i u = *(const v4i *)(b + kb * BLOCK8), v = *(const v4i *)(b + kb * BLOCK8 + 16);
-        float scale;
-        v4i lo, hi;
-        raw_block<In>(row, there, wide_in, kb * BLOCK8 + quarter * 32, p.cols, scale, lo, hi);
-        scale *= sb[kb];
-        Operand<EXACT> w, a;
-        w.set(u, v);
-        a.set(lo, hi);
-        const v4f part = block_product(w, a);
+    const float *sb = SQUARES ? p.sb + (matrix * blocks8(p.rows_b) + strip / 8) * p.kb : p.sb;
+    int64_t scale_row[4];
 #pragma unroll
-        for (int n = 0; n < 4; n++) sum[n] = fmaf(part[n], scale, sum[n]);
+    for (int n = 0; n < 4; n++) scale_row[n] = strip * 16 + quarter * 4 + n < p.rows_b ? strip * 16 + quarter * 4 + n : p.rows_b - 1;
+    v4f sum[J];
+#pragma unroll
+    for (int j = 0; j < J; j++) sum[j] = {0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int AHEAD = 4;
+    for (int64_t kb0 = wave; kb0 < p.kb; kb0 += FEW_WAVES * AHEAD) {
+        v4i u[AHEAD], v[AHEAD];
+#pragma unroll
+        for (int n = 0; n < AHEAD; n++) {
+            const int64_t kb = kb0 + n * FEW_WAVES < p.kb ? kb0 + n * FEW_WAVES : kb0;
+            u[n] = *(const v4i *)(b + kb * BLOCK8);
+            v[n] = *(const v4i *)(b + kb * BLOCK8 + 16);
+        }
+#pragma unroll
+        for (int n = 0; n < AHEAD; n++) {
+            const int64_t kb = kb0 + n * FEW_WAVES;
+            if (kb >= p.kb) break;
+            Operand<EXACT> w;
+            w.set(u[n], v[n]);
+            v4f of_b;
+#pragma unroll
+            for (int i = 0; i < 4; i++) of_b[i] = SQUARES ? sb[kb] : sb[kb * p.rows_b + scale_row[i]];
+#pragma unroll
+            for (int j = 0; j < J; j++) {
+                float scale;
+                v4i lo, hi;
+                if constexpr (RAW) raw_block<In>((const typename In::T *)p.a + src[j] * p.stride_raw, first + j * 16 + tok < end, wide_in, kb * BLOCK8 + quarter * 32, p.cols, scale, lo, hi);
+                else {
+                    const uint8_t *a = p.a + src[j] * row_bytes + kb * BLOCK8 + quarter * 32;
+                    lo = *(const v4i *)a;
+                    hi = *(const v4i *)(a + 16);
+                    scale = p.sa[kb * p.rows_a + src[j]];
+                }
+                Operand<EXACT> a;
+                a.set(lo, hi);
+                const v4f part = block_product(w, a);
+#pragma unroll
+                for (int i = 0; i < 4; i++) sum[j][i] = SQUARES ? fmaf(part[i], scale * of_b[i], sum[j][i]) : fmaf(part[i] * of_b[i], scale, sum[j][i]);
+            }
+        }
     }
-    *(v4f *)parts[wave][lane] = sum;
-    __syncthreads();
-    if (wave == 0) {
 #pragma unroll
-        for (int w = 1; w < RAW_WAVES; w++) sum += *(v4f *)parts[w][lane];
-        const int64_t c = strip * 16 + quarter * 4;
-        if (there) store_four<Out>((typename Out::T *)p.out + (first + tok) * p.stride + c, p.rows_b - c, wide, sum);
+    for (int j = 0; j < J; j++) parts[wave][j][lane] = sum[j];
+    __syncthreads();
+    if (wave < J) {
+        v4f total = parts[0][wave][lane];
+#pragma unroll
+        for (int w = 1; w < FEW_WAVES; w++) total += parts[w][wave][lane];
+        const int64_t row = first + wave * 16 + tok, c = strip * 16 + quarter * 4;
+        if (row < end) store_four<Out>((typename Out::T *)p.out + row * p.stride + c, p.rows_b - c, wide, total);
     }
 }
 
 }  // namespace
 
+// places in use by `slots` slots of E experts, each expert's rounded up to whole tiles: what there can be at most, and what there will be about
+static int64_t most_tiles(int64_t slots, int64_t E, int rows) { return slots / rows + (slots < E ? slots : E); }
+
 hipError_t launch_product(const ProductArgs &p, bool squares, int type, hipStream_t s)
 {
-    constexpr int TOK = 128, WT = 128;
-    const int64_t tiles_wt = (p.rows_b + WT - 1) / WT;
-    int64_t tiles_tok = (p.rows_a + TOK - 1) / TOK, tiles = tiles_tok * tiles_wt;
-    if (p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES) {
-        const int64_t slots = p.order.T * p.order.k;
-        tiles_tok = slots / TOK + (slots < p.order.E ? slots : p.order.E);
-        tiles = tiles_tok * tiles_wt;
-    } else if (p.mode == ASGD_PRODUCT_OVER) tiles *= p.order.E;
-    const bool wide = p.stride % 4 == 0 && (uintptr_t)p.out % (4 * type_size(type)) == 0;
+    const bool grouped = p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES, over = p.mode == ASGD_PRODUCT_OVER;
+    const int64_t slots = grouped ? p.order.T * p.order.k : 0, E = p.order.E, rows = grouped ? slots : p.rows_a;
+    const bool wide4 = p.stride % 4 == 0 && (uintptr_t)p.out % (4 * type_size(type)) == 0;
+    const bool wide16 = p.stride * type_size(type) % 16 == 0 && (uintptr_t)p.out % 16 == 0;
+    const auto tiles_of = [&](int tok) { return grouped ? most_tiles(slots, E, tok) : (p.rows_a + tok - 1) / tok; };
     return with_type(type, [&](auto out) {
-        const auto go = [&](auto sq, auto exact) {
-            product_kernel<TOK, WT, 2, 2, decltype(sq)::value, decltype(exact)::value, decltype(out)><<<(unsigned)tiles, 256, 0, s>>>(p, tiles_tok, tiles_wt, wide);
+        typedef decltype(out) Out;
+        const auto few = [&](auto j, auto sq, auto exact) {
+            constexpr int J = decltype(j)::value;
+            const dim3 grid((unsigned)((p.rows_b + 15) / 16), (unsigned)tiles_of(16 * J));
+            product_few_kernel<void, J, decltype(sq)::value, decltype(exact)::value, Out><<<grid, 64 * FEW_WAVES, 0, s>>>(p, false, wide4);
             return hipGetLastError();
+        };
+        const auto tiles = [&](auto tok, auto wt, auto waves_tok, auto waves_wt, auto sq, auto exact, auto far) {
+            constexpr int TOK = decltype(tok)::value, WT = decltype(wt)::value, WAVES = decltype(waves_tok)::value * decltype(waves_wt)::value;
+            const int64_t tiles_tok = tiles_of(TOK), tiles_wt = (p.rows_b + WT - 1) / WT;
+            product_kernel<TOK, WT, decltype(waves_tok)::value, decltype(waves_wt)::value, decltype(sq)::value, decltype(exact)::value, decltype(far)::value, Out>
+                <<<(unsigned)(tiles_tok * tiles_wt * (over ? E : 1)), 64 * WAVES, 0, s>>>(p, (uint32_t)tiles_tok, (uint32_t)tiles_wt, wide16);
+            return hipGetLastError();
+        };
+        const auto choose = [&](auto sq, auto exact) {
+            const std::true_type yes;
+            const std::false_type no;
+            // (rows of a tile of an expert: what it has on average)
+            const int64_t each = grouped ? rows / E : rows;
+            if (!over && each <= 32) return each <= 16 ? few(One<1>(), sq, exact) : few(One<2>(), sq, exact);
+            if (grouped && (double)p.rows_a * p.kb * BLOCK8 >= 4294967296.0) return tiles(One<128>(), One<128>(), One<2>(), One<2>(), sq, exact, yes);
+            if constexpr (!decltype(exact)::value && decltype(sq)::value) {
+                // 256 x 256 are 1.2 times as fast as 128 x 128 where they fill the device as well: 256 of them go at a time, or 512
+                const int64_t big = (rows + (grouped ? E * 128 : 0) + 255) / 256 * ((p.rows_b + 255) / 256), small = (rows + (grouped ? E * 64 : 0) + 127) / 128 * ((p.rows_b + 127) / 128);
+                if (!over && (double)((big + 255) / 256) * 4.0 <= (double)((small + 511) / 512) * 2.0 * 1.2) return tiles(One<256>(), One<256>(), One<4>(), One<2>(), sq, exact, no);
+            }
+            return tiles(One<128>(), One<128>(), One<2>(), One<2>(), sq, exact, no);
         };
         const std::true_type yes;
         const std::false_type no;
-        return squares ? p.exact ? go(yes, yes) : go(yes, no) : p.exact ? go(no, yes) : go(no, no);
+        return squares ? p.exact ? choose(yes, yes) : choose(yes, no) : p.exact ? choose(no, yes) : choose(no, no);
     });
 }
 
 hipError_t launch_product_raw(const ProductArgs &p, int raw_type, int type, hipStream_t s)
 {
+    const bool grouped = p.mode == ASGD_PRODUCT_GATHER;
     const bool wide = p.stride % 4 == 0 && (uintptr_t)p.out % (4 * type_size(type)) == 0;
     const bool wide_in = p.stride_raw * (int64_t)type_size(raw_type) % 16 == 0 && ((uintptr_t)p.a & 15) == 0;
-    const dim3 grid((unsigned)((p.rows_b + 15) / 16), p.mode == ASGD_PRODUCT_GATHER ? (unsigned)(p.order.T * p.order.k) : 1u);
+    const dim3 grid((unsigned)((p.rows_b + 15) / 16), grouped ? (unsigned)most_tiles(p.order.T * p.order.k, p.order.E, 16) : 1u);
     return with_type(raw_type, [&](auto in) {
         return with_type(type, [&](auto out) {
-            if (p.exact) product_raw_kernel<decltype(in), true, decltype(out)><<<grid, 64 * RAW_WAVES, 0, s>>>(p, wide_in, wide);
-            else product_raw_kernel<decltype(in), false, decltype(out)><<<grid, 64 * RAW_WAVES, 0, s>>>(p, wide_in, wide);
+            if (p.exact) product_few_kernel<decltype(in), 1, true, true, decltype(out)><<<grid, 64 * FEW_WAVES, 0, s>>>(p, wide_in, wide);
+            else product_few_kernel<decltype(in), 1, true, false, decltype(out)><<<grid, 64 * FEW_WAVES, 0, s>>>(p, wide_in, wide);
             return hipGetLastError();
         });
     });

@@ -206,11 +206,11 @@ def test_offsets_beyond_32_bits(X):
     at = [0, 131_072, 262_144, 299_999]
     x[at] = data(4, cols, 8).to(torch.bfloat16).cuda()
     q = X.quantize(x)
-    few = X.quantize(x[at])
-    assert torch.equal(q.values[at].view(torch.uint8), few.values.view(torch.uint8)) and torch.equal(q.scales[:, at], few.scales)
+    few = X.quantize(x[at + list(range(1, 200))])                      # (enough rows for the same kernel: the same bits)
+    assert torch.equal(q.values[at].view(torch.uint8), few.values[:4].view(torch.uint8)) and torch.equal(q.scales[:, at], few.scales[:, :4])
     w = X.quantize_weights(data(40, cols, 9).cuda())
     y = X.product(q, w, torch.float32)
-    assert torch.equal(y[at], X.product(few, w, torch.float32)) and int((y.abs().sum(1) > 0).sum()) == 4
+    assert torch.equal(y[at], X.product(few, w, torch.float32)[:4]) and int((y.abs().sum(1) > 0).sum()) == 4
 
 
 def test_in_a_graph(X):

@@ -191,3 +191,22 @@ def test_a_clustering_becomes_a_routed_model(X):
     from paper_1505_04956_amd import clusterwise
     losses, single = clusterwise.run(samples=60_000, steps=60, batch=4096)
     assert losses[-1] < 0.75 * losses[0] and sum(losses[-5:]) / 5 < single
+
+
+def test_gathered_rows_more_than_32_bits_apart(X):
+    """Rows of one tile that lie at both ends of more than 2^32 bytes of 8-bit rows."""
+    T, K, N, E = 280_000, 16_384, 24, 3
+    free, _ = torch.cuda.mem_get_info()
+    if free < 40 << 30:
+        pytest.skip("needs 40 GB")
+    x = torch.zeros((T, K), dtype=torch.bfloat16, device="cuda")
+    at = [0, 1, 140_000, 279_998, 279_999]
+    x[at] = data(5, K, 8).to(torch.bfloat16).cuda()
+    ids = torch.zeros((T, 1), dtype=torch.int32, device="cuda")
+    ids[2:140_000] = 1
+    ids[140_001:279_998] = 1                          # expert 0: a few rows at the ends; expert 2: none
+    w, weights = X.quantize_weights(weights_of(E, N, K, 2).cuda()), torch.ones((T, 1), device="cuda")
+    y = X.experts(x, ids, weights, w)
+    few = [0, 1, 140_000, 279_998, 279_999] + list(range(2, 400))
+    part = X.experts(x[few], ids[few], weights[few], w)
+    assert torch.equal(y[at], part[:5]) and int((y.float().abs().sum(1) > 0).sum()) == 5
