@@ -398,12 +398,21 @@ int asgd_block_quantize(const void *x, int type, int64_t rows, int64_t cols, int
  *   ASGD_PRODUCT_PLACES   the same with an `a` that has a row for each place already (ROWS)
  *   ASGD_PRODUCT_OVER     a and b (ROWS) are turned quantisations over the same order: out (E x a.rows x b.rows, matrices
  *                         a.rows * stride apart) = for each expert the product over its own places alone, zeros without any
- * a RAW: at most ASGD_PRODUCT_RAW_ROWS rows (ALL) or slots (GATHER), and b SQUARES.
+ * a RAW: at most ASGD_PRODUCT_RAW_ROWS rows (ALL) or ASGD_PRODUCT_RAW_SLOTS slots (GATHER), and b SQUARES.  A matrix in 8-bit
+ * blocks has at most 2^30 rows.
  */
 enum { ASGD_PRODUCT_ALL = 0, ASGD_PRODUCT_GATHER = 1, ASGD_PRODUCT_PLACES = 2, ASGD_PRODUCT_OVER = 3 };
-enum { ASGD_PRODUCT_RAW_ROWS = 16 };
+enum { ASGD_PRODUCT_RAW_ROWS = 16, ASGD_PRODUCT_RAW_SLOTS = 4096 };
 int asgd_block_product(const asgd_blocks *a, const asgd_blocks *b, int mode, int exact, const asgd_route_order *order, void *out,
                        int type, int64_t stride, void *hip_stream);
+
+/*
+ * The experts of few rows in one launch, without an order: out[t] = sum over j of weights[t][j] * (x's row t times the
+ * matrix ids[t][j] of w), ids outside 0 .. w->count - 1 left out.  x: RAW, at most ASGD_PRODUCT_RAW_ROWS rows; w: SQUARES;
+ * ids and weights: rows x k.  Every row reads its experts' matrices for itself.
+ */
+int asgd_experts_direct(const asgd_blocks *x, const int32_t *ids, const float *weights, int k, const asgd_blocks *w, int exact,
+                        void *out, int type, int64_t stride, void *hip_stream);
 
 /*
  * out[t] = sum over j of weights[t][j] * y[place of slot (t, j)], in the order of j and 32-bit, slots without an expert left

@@ -446,6 +446,65 @@ template <class In, int J, bool SQUARES, bool EXACT, class Out> __global__ __lau
     }
 }
 
+// A row's experts without an order, for few rows: a workgroup takes sixteen rows of b of every expert of one row of a (blockIdx.y), and
+// adds what they give times its weights.  A block of the row is brought to 8 bits once for all of them; the weights of up to
+// EXPERTS of them are on their way at a time.
+template <class In, bool EXACT, class Out> __global__ __launch_bounds__(64 * FEW_WAVES) void product_direct_kernel(ProductArgs p, const int32_t *ids, const float *weights, int k, int E, bool wide_in, bool wide)
+{
+    constexpr int EXPERTS = 8;
+    __shared__ v4f parts[FEW_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tok = lane & 15, quarter = lane >> 4;
+    const int64_t t = blockIdx.y, strip = blockIdx.x, r = strip * 16 + tok, row_bytes = p.kb * BLOCK8;
+    const uint8_t *b = p.b + (r < p.rows_b ? r : p.rows_b - 1) * row_bytes + quarter * 32;
+    const float *sb = p.sb + strip / 8 * p.kb;
+    const int64_t matrix = p.rows_b * row_bytes, squares = blocks8(p.rows_b) * p.kb;
+    const typename In::T *row = (const typename In::T *)p.a + t * p.stride_raw;
+    v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int64_t kb = wave; kb < p.kb; kb += FEW_WAVES) {
+        float scale;
+        v4i lo, hi;
+        Operand<EXACT> a;
+        for (int j0 = 0; j0 < k; j0 += EXPERTS) {
+            v4i u[EXPERTS], v[EXPERTS];
+            float of_b[EXPERTS];
+#pragma unroll
+            for (int j = 0; j < EXPERTS; j++) {
+                const int e = j0 + j < k ? ids[t * k + j0 + j] : -1;
+                const bool there = (unsigned)e < (unsigned)E;
+                const int64_t m = there ? e : 0;
+                of_b[j] = there ? sb[m * squares + kb] * weights[t * k + j0 + j] : 0.0f;
+                if (there) {
+                    u[j] = *(const v4i *)(b + m * matrix + kb * BLOCK8);
+                    v[j] = *(const v4i *)(b + m * matrix + kb * BLOCK8 + 16);
+                }
+            }
+            if (j0 == 0) {
+                raw_block<In>(row, tok == 0, wide_in, kb * BLOCK8 + quarter * 32, p.cols, scale, lo, hi);
+                a.set(lo, hi);
+            }
+#pragma unroll
+            for (int j = 0; j < EXPERTS; j++) {
+                const int e = j0 + j < k ? ids[t * k + j0 + j] : -1;
+                if ((unsigned)e < (unsigned)E) {
+                    Operand<EXACT> w;
+                    w.set(u[j], v[j]);
+                    const v4f part = block_product(w, a);
+#pragma unroll
+                    for (int i = 0; i < 4; i++) sum[i] = fmaf(part[i], scale * of_b[j], sum[i]);
+                }
+            }
+        }
+    }
+    parts[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && tok == 0) {
+#pragma unroll
+        for (int w = 1; w < FEW_WAVES; w++) sum += parts[w][lane];
+        const int64_t c = strip * 16 + quarter * 4;
+        store_four<Out>((typename Out::T *)p.out + t * p.stride + c, p.rows_b - c, wide, sum);
+    }
+}
+
 }  // namespace
 
 // places in use by `slots` slots of E experts, each expert's rounded up to whole tiles: what there can be at most, and what there will be about
@@ -490,6 +549,20 @@ hipError_t launch_product(const ProductArgs &p, bool squares, int type, hipStrea
         const std::true_type yes;
         const std::false_type no;
         return squares ? p.exact ? choose(yes, yes) : choose(yes, no) : p.exact ? choose(no, yes) : choose(no, no);
+    });
+}
+
+hipError_t launch_product_direct(const ProductArgs &p, const int32_t *ids, const float *weights, int k, int E, int raw_type, int type, hipStream_t s)
+{
+    const bool wide = p.stride % 4 == 0 && (uintptr_t)p.out % (4 * type_size(type)) == 0;
+    const bool wide_in = p.stride_raw * (int64_t)type_size(raw_type) % 16 == 0 && ((uintptr_t)p.a & 15) == 0;
+    const dim3 grid((unsigned)((p.rows_b + 15) / 16), (unsigned)p.rows_a);
+    return with_type(raw_type, [&](auto in) {
+        return with_type(type, [&](auto out) {
+            if (p.exact) product_direct_kernel<decltype(in), true, decltype(out)><<<grid, 64 * FEW_WAVES, 0, s>>>(p, ids, weights, k, E, wide_in, wide);
+            else product_direct_kernel<decltype(in), false, decltype(out)><<<grid, 64 * FEW_WAVES, 0, s>>>(p, ids, weights, k, E, wide_in, wide);
+            return hipGetLastError();
+        });
     });
 }
 

@@ -5,7 +5,7 @@ using namespace asgd;
 
 namespace {
 
-constexpr int64_t MOST_ROWS = (int64_t)1 << 31;          // of an operand
+constexpr int64_t MOST_ROWS = (int64_t)1 << 30;          // of an operand: byte offsets of its scales are 32-bit
 constexpr int64_t MOST_COLS = (int64_t)1 << 24;
 constexpr int64_t MOST_SLOTS = (int64_t)1 << 30;         // places are int32
 constexpr int64_t MOST_GROUPS = (int64_t)1 << 23;        // workgroups of one launch
@@ -147,12 +147,26 @@ int asgd_block_product(const asgd_blocks *a, const asgd_blocks *b, int mode, int
     if (order) p.order = *order;
     const hipStream_t s = (hipStream_t)hip_stream;
     if (a->form == ASGD_BLOCKS_RAW) {
-        if (b->form != ASGD_BLOCKS_SQUARES || out_rows > ASGD_PRODUCT_RAW_ROWS || (mode != ASGD_PRODUCT_ALL && mode != ASGD_PRODUCT_GATHER)) return ASGD_EINVAL;
+        if (b->form != ASGD_BLOCKS_SQUARES || out_rows > (mode == ASGD_PRODUCT_ALL ? ASGD_PRODUCT_RAW_ROWS : ASGD_PRODUCT_RAW_SLOTS) || (mode != ASGD_PRODUCT_ALL && mode != ASGD_PRODUCT_GATHER)) return ASGD_EINVAL;
         p.stride_raw = a->stride;
         return done(launch_product_raw(p, a->type, type, s));
     }
     if ((double)blocks8(out_rows + (order ? (int64_t)BLOCK8 * order->E : 0)) * (mode == ASGD_PRODUCT_OVER ? order->E : 1) * blocks8(b->rows) > (double)MOST_GROUPS) return ASGD_EINVAL;
     return done(launch_product(p, b->form == ASGD_BLOCKS_SQUARES, type, s));
+}
+
+int asgd_experts_direct(const asgd_blocks *x, const int32_t *ids, const float *weights, int k, const asgd_blocks *w, int exact,
+                        void *out, int type, int64_t stride, void *hip_stream)
+{
+    if (!blocks_ok(x) || x->form != ASGD_BLOCKS_RAW || x->rows > ASGD_PRODUCT_RAW_ROWS || !blocks_ok(w) || w->form != ASGD_BLOCKS_SQUARES || w->cols != x->cols || w->rows < 1 || w->rows > MOST_COLS)
+        return ASGD_EINVAL;
+    if (k < 1 || k > ASGD_ROUTE_MAX_CHOSEN || !type_ok(type) || (exact != 0 && exact != 1)) return ASGD_EINVAL;
+    if (x->rows == 0) return ASGD_OK;
+    if (!ids || !weights || !aligned(ids, 4) || !aligned(weights, 4) || !matrix_ok(out, type, x->rows, w->rows, stride)) return ASGD_EINVAL;
+    ProductArgs p = {};
+    p.a = (const uint8_t *)x->values; p.b = (const uint8_t *)w->values; p.sb = w->scales; p.rows_a = x->rows; p.rows_b = w->rows;
+    p.kb = blocks8(x->cols); p.cols = x->cols; p.stride_raw = x->stride; p.out = out; p.stride = stride; p.exact = exact;
+    return done(launch_product_direct(p, ids, weights, k, w->count, x->type, type, (hipStream_t)hip_stream));
 }
 
 int asgd_experts_sum(const void *y, int y_type, int64_t n, int64_t y_stride, const asgd_route_order *order, const float *weights,

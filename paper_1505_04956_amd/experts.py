@@ -19,6 +19,9 @@ from . import binding as B
 SOFTMAX, SIGMOID = B.SCORE_SOFTMAX, B.SCORE_SIGMOID
 BEST, BEST_TWO = B.GROUP_BEST, B.GROUP_BEST_TWO
 BLOCK = 128
+# Up to so many bytes of weights, an expert's counted for each row that goes to it, one launch without an order is faster than an order,
+# products and sums, which take about 20 us more and read each expert's weights once.
+DIRECT_BYTES = 128 << 20
 
 _TYPES = {torch.float32: B.TYPE_F32, torch.bfloat16: B.TYPE_BF16, torch.float16: B.TYPE_F16}
 
@@ -30,12 +33,17 @@ def _type(dtype):
     return code
 
 
+# (the same number as torch.cuda.current_stream().cuda_stream, without the 3 us that its objects take)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _stream(t):
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError("a tensor on the GPU is wanted; there is no CPU fallback")
-    if t.device.index != torch.cuda.current_device():
+    index = t.get_device()
+    if index != torch.cuda.current_device():
         raise ValueError("the tensors are on %s, the current device is %d" % (t.device, torch.cuda.current_device()))
-    return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(index)
 
 
 def _matrix(t, rows=None, cols=None, name="x"):
@@ -52,7 +60,7 @@ def _matrix(t, rows=None, cols=None, name="x"):
 
 def _same_device(first, *others):
     for t in others:
-        if t is not None and t.device != first.device:
+        if t is not None and (t.get_device() != first.get_device() or t.is_cuda != first.is_cuda):
             raise ValueError("tensors on %s and %s" % (first.device, t.device))
 
 
@@ -228,7 +236,9 @@ def _raw(x):
 def _product_of(x, w, dtype, plan=None, exact=None):
     """x, one row for each of the plan's T, times w."""
     rows = x.shape[0] if plan is None else plan.T * plan.k
-    if not 0 < rows <= B.PRODUCT_RAW_ROWS:
+    # (few rows of an expert: bringing them to 8 bits again in each strip of its weights takes less than another launch)
+    raw = 0 < rows <= B.PRODUCT_RAW_ROWS if plan is None else 0 < rows <= min(B.PRODUCT_RAW_SLOTS, 16 * plan.E)
+    if not raw:
         return product(quantize(x), w, dtype, plan=plan, gather=plan is not None, exact=exact)
     _same_device(x, w.values)
     out = torch.empty((rows, w.rows), dtype=dtype, device=x.device)
@@ -301,6 +311,12 @@ def experts(x, ids, weights, w, train=False):
     if ids.dim() != 2 or ids.shape[0] != x.shape[0]:
         raise ValueError("ids: [%d, k] is wanted, not %s" % (x.shape[0], tuple(ids.shape)))
     _flat(weights, ids.shape, torch.float32, "weights")
+    if not train and 0 < x.shape[0] <= B.PRODUCT_RAW_ROWS and ids.numel() * w.rows * w.cols <= DIRECT_BYTES:
+        _flat(ids, ids.shape, torch.int32, "ids")
+        out = torch.empty((x.shape[0], w.rows), dtype=x.dtype, device=x.device)
+        B.asgd_experts_direct(_raw(x), ids.data_ptr(), weights.data_ptr(), ids.shape[1], w._c, int(x.dtype == torch.float32), out.data_ptr(),
+                              _type(x.dtype), w.rows, _stream(x))
+        return out
     order = plan(ids, w.count)
     # 32-bit until the sum: one rounding to the result's type.  Beside a rounding to 16 bits the error of the 8-bit instruction does not
     # show; the gradient of the weights is 32-bit, and y goes into it

@@ -108,7 +108,7 @@ def test_products_that_are_refused():
     raw = blocks(form=B.BLOCKS_RAW, scales=None, stride=200)
     assert product(raw, b) == B.EINVAL                                                   # raw: squares only
     assert product(blocks(form=B.BLOCKS_RAW, rows=17, stride=200), sq) == B.EINVAL
-    assert product(blocks(form=B.BLOCKS_RAW, rows=9, stride=200), three, B.PRODUCT_GATHER, o=order(T=9)) == B.EINVAL     # 18 slots
+    assert product(blocks(form=B.BLOCKS_RAW, rows=2049, stride=200), three, B.PRODUCT_GATHER, o=order(T=2049)) == B.EINVAL     # 4098 slots
     assert product(blocks(form=B.BLOCKS_RAW, stride=100), sq) == B.EINVAL
     assert product(blocks(rows=0), b) == B.OK
 
@@ -162,3 +162,13 @@ def test_the_rules_of_the_tests_hold_by_hand():
     q, s = R.to_blocks(torch.tensor([[448.0, 1.0, -17.0]]))
     assert s.tolist() == [[1.0]] and q.float()[0, 0, :3].tolist() == [448.0, 1.0, -16.0]
     assert R.order_of(torch.tensor([[2, 0], [-1, 2]]), 3) == ([0, 1, 1, 3], [0, 1, 1, 2], [1, 0, 3, -1], [1, 0, -1, 2])
+
+
+def test_direct_experts_that_are_refused():
+    x, w = blocks(form=B.BLOCKS_RAW, scales=None, stride=200, type=1), blocks(form=B.BLOCKS_SQUARES, count=3)
+
+    def go(x=x, ids=P, weights=P, k=2, w=w, exact=0, out=P, type=1, stride=8):
+        return B.lib().asgd_experts_direct(C.addressof(x), ids, weights, k, C.addressof(w), exact, out, type, stride, None)
+    for over in (dict(x=blocks()), dict(x=blocks(form=B.BLOCKS_RAW, rows=17, stride=200)), dict(x=blocks(form=B.BLOCKS_RAW, cols=199, stride=200)), dict(w=blocks()),
+                 dict(ids=None), dict(weights=P + 2), dict(k=0), dict(k=65), dict(exact=3), dict(out=None), dict(type=5), dict(stride=7)):
+        assert go(**over) == B.EINVAL
