@@ -89,17 +89,37 @@ hipError_t launch_experts_sum(const SumArgs &a, int y_type, int type, hipStream_
 hipError_t launch_experts_sum_backward(const SumArgs &a, int y_type, int type, hipStream_t s);
 
 // ---- device helpers --------------------------------------------------------------------------------------------
+// Across lanes with the instruction that does the arithmetic (DPP); a lane the pattern leaves out keeps `old`.
+template <int PATTERN, int ROWS = 0xF> __device__ __forceinline__ float from_lane(float old, float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(v), PATTERN, ROWS, 0xF, false));
+}
+constexpr int XOR1 = 0xB1, XOR2 = 0x4E, MIRROR8 = 0x141, MIRROR16 = 0x140, LANE15 = 0x142, LANE31 = 0x143;
+
+// over sixteen lanes, in all of them (each step joins two halves that hold one value each, so a mirror does for an exchange)
+__device__ __forceinline__ float row_max(float v)
+{
+    v = fmaxf(v, from_lane<XOR1>(v, v));
+    v = fmaxf(v, from_lane<XOR2>(v, v));
+    v = fmaxf(v, from_lane<MIRROR8>(v, v));
+    return fmaxf(v, from_lane<MIRROR16>(v, v));
+}
 __device__ __forceinline__ float wave_max(float v)
 {
-#pragma unroll
-    for (int m = 32; m; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
-    return v;
+    v = row_max(v);
+    v = fmaxf(v, from_lane<LANE15, 0xA>(v, v));
+    v = fmaxf(v, from_lane<LANE31, 0xC>(v, v));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 __device__ __forceinline__ float wave_sum(float v)
 {
-#pragma unroll
-    for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-    return v;
+    v += from_lane<XOR1>(0.0f, v);
+    v += from_lane<XOR2>(0.0f, v);
+    v += from_lane<MIRROR8>(0.0f, v);
+    v += from_lane<MIRROR16>(0.0f, v);
+    v += from_lane<LANE15, 0xA>(0.0f, v);
+    v += from_lane<LANE31, 0xC>(0.0f, v);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 // magnitude as an order-preserving integer: infinities and what is not a number are larger than all finite ones

@@ -1,7 +1,9 @@
 // Routing of rows to experts: scores, the best k by key, their weights; the gradient of the logits; the order by expert.
 //
-// One wave takes one row.  Lane i holds the V consecutive experts i * V .. i * V + V - 1, so that among equal keys the
-// lowest lane, and in it the lowest register, is the lowest index.
+// One wave takes a row after the other.  Lane i holds the V consecutive experts i * V .. i * V + V - 1, so that among equal keys
+// the lowest lane, and in it the lowest register, is the lowest index.  What bounds it is instructions (the row is read once): one of k
+// choices is a maximum over lanes, a ballot that finds its lane and one a register that finds its place there, the rest of which is
+// scalar work.
 #include "experts_internal.h"
 
 namespace asgd {
@@ -10,20 +12,49 @@ namespace {
 
 constexpr float OUT = -INFINITY;          // key of an expert that cannot be chosen
 
+// V consecutive elements of a row from e on, of which those before E exist
+template <class Ty, int V> struct Lane { typename Ty::T v[V]; };
+template <class Ty, int V> __device__ __forceinline__ Lane<Ty, V> load_lane(const typename Ty::T *row, int e, int E, bool wide)
+{
+    Lane<Ty, V> r;
+    constexpr int BYTES = V * sizeof(typename Ty::T), N = BYTES < 16 ? BYTES : 16;
+    if (wide) {
+        if (e < E)
+#pragma unroll
+            for (int i = 0; i < BYTES / N; i++) {
+                if constexpr (N == 16) *((uint4 *)r.v + i) = *((const uint4 *)(row + e) + i);
+                else if constexpr (N == 8) *(uint2 *)r.v = *(const uint2 *)(row + e);
+                else if constexpr (N == 4) *(uint32_t *)r.v = *(const uint32_t *)(row + e);
+                else r.v[0] = row[e];
+            }
+    } else
+#pragma unroll
+        for (int i = 0; i < V; i++)
+            if (e + i < E) r.v[i] = row[e + i];
+    return r;
+}
+template <class Ty, int V> bool rows_of_lanes(const void *p, int64_t stride, int E)
+{
+    constexpr int BYTES = V * sizeof(typename Ty::T), N = BYTES < 16 ? BYTES : 16;
+    return E % V == 0 && (uintptr_t)p % N == 0 && stride * (int64_t)sizeof(typename Ty::T) % N == 0;
+}
+
 // l of the lane's experts (out: -infinity), and whether an expert that is in has something that is not a number
 template <class Ty, int V>
-__device__ __forceinline__ bool load_logits(const typename Ty::T *row, const float *bias, int E, int lane, float (&l)[V], float (&b)[V])
+__device__ __forceinline__ bool logits_of(const Lane<Ty, V> &r, const float (&bias)[V], int E, int lane, float (&l)[V])
 {
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < V; i++) {
-        const int e = lane * V + i;
-        l[i] = e < E ? (float)row[e] : OUT;
-        b[i] = bias && e < E ? bias[e] : 0.0f;
-        if (b[i] == OUT) l[i] = OUT;
-        if (l[i] != OUT && (l[i] != l[i] || b[i] != b[i])) bad = true;
+        l[i] = lane * V + i < E && bias[i] != OUT ? (float)r.v[i] : OUT;
+        if (l[i] != OUT && (l[i] != l[i] || bias[i] != bias[i])) bad = true;
     }
     return __any(bad);
+}
+template <int V> __device__ __forceinline__ void load_bias(const float *bias, int E, int lane, float (&b)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; i++) b[i] = bias && lane * V + i < E ? bias[lane * V + i] : 0.0f;
 }
 
 // 1 / (1 + exp(-l)), in the operations of the definition
@@ -40,13 +71,20 @@ template <int V> __device__ __forceinline__ float lane_best(const float (&v)[V])
     return m;
 }
 
-template <class Ty, int V> __device__ __forceinline__ void route_row(const RouteArgs &a, int64_t t, int lane)
+// the two best of two pairs of two best
+__device__ __forceinline__ void join_best(float &m1, float &m2, float o1, float o2)
+{
+    m2 = fmaxf(fmaxf(m2, o2), fminf(m1, o1));
+    m1 = fmaxf(m1, o1);
+}
+
+template <class Ty, int V> __device__ __forceinline__ void route_row(const RouteArgs &a, int64_t t, int lane, const Lane<Ty, V> &raw, const float (&bias)[V])
 {
     const typename Ty::T *row = (const typename Ty::T *)a.logits + t * a.stride;
     const int E = a.E, k = a.rule.k;
     const bool soft = a.rule.score == ASGD_SCORE_SOFTMAX;
     float l[V], key[V];
-    const bool bad = load_logits<Ty, V>(row, a.bias, E, lane, l, key);       // key: the bias for now
+    const bool bad = logits_of<Ty, V>(raw, bias, E, lane, l);
     float top = 0.0f, total = 1.0f;
     if (soft && (!a.rule.renormalize || a.bias || (a.rule.groups > 1 && a.rule.group_by == ASGD_GROUP_BEST_TWO))) {
         top = wave_max(lane_best(l));
@@ -58,75 +96,85 @@ template <class Ty, int V> __device__ __forceinline__ void route_row(const Route
     const auto score = [&](float v) { return v == OUT ? 0.0f : soft ? expf(v - top) / total : sigmoid(v); };
     if (a.bias) {
 #pragma unroll
-        for (int i = 0; i < V; i++) key[i] = l[i] == OUT ? OUT : as_key(score(l[i]) + key[i]);
+        for (int i = 0; i < V; i++) key[i] = l[i] == OUT ? OUT : as_key(score(l[i]) + bias[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < V; i++) key[i] = as_key(l[i]);
     }
     if (a.rule.groups > 1) {
-        const int G = a.rule.groups, width = E / G;
+        const int G = a.rule.groups, width = E / G, lanes = width / V;
         const bool two = a.rule.group_by == ASGD_GROUP_BEST_TWO;
-        float mine = OUT;                                                     // lane g: how group g is judged
-        for (int g = 0; g < G; g++) {
-            float m1 = OUT, m2 = OUT;                                         // the lane's two best of the group
+        const auto by = [&](int i) { return two && !a.bias ? (l[i] == OUT ? OUT : as_key(score(l[i]))) : key[i]; };
+        unsigned long long stays = 0;
+        if (lanes * V == width && lanes <= 16 && (lanes & (lanes - 1)) == 0) {
+            // a group is 1, 2, .. 16 whole lanes next to each other: all groups at once
+            float m1 = OUT, m2 = OUT;
+#pragma unroll
+            for (int i = 0; i < V; i++) join_best(m1, m2, by(i), OUT);
+            if (lanes > 1) join_best(m1, m2, from_lane<XOR1>(m1, m1), from_lane<XOR1>(m2, m2));
+            if (lanes > 2) join_best(m1, m2, from_lane<XOR2>(m1, m1), from_lane<XOR2>(m2, m2));
+            if (lanes > 4) join_best(m1, m2, from_lane<MIRROR8>(m1, m1), from_lane<MIRROR8>(m2, m2));
+            if (lanes > 8) join_best(m1, m2, from_lane<MIRROR16>(m1, m1), from_lane<MIRROR16>(m2, m2));
+            const float mine = two ? as_key(m1 + m2) : m1;
+            const int g = lane / lanes;
+            int before = 0;                                                   // groups that are taken before the lane's
+            for (int o = 0; o < G; o++) {
+                const float other = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), o * lanes));
+                before += other > mine || (other == mine && o < g) ? 1 : 0;
+            }
+#pragma unroll
+            for (int i = 0; i < V; i++)
+                if (before >= a.rule.kept) key[i] = OUT;
+        } else {
+            float mine = OUT;                                                 // lane g: how group g is judged
+            for (int g = 0; g < G; g++) {
+                float m1 = OUT, m2 = OUT;                                     // the lane's two best of the group
+#pragma unroll
+                for (int i = 0; i < V; i++) {
+                    const int e = lane * V + i;
+                    if (e >= g * width && e < (g + 1) * width) join_best(m1, m2, by(i), OUT);
+                }
+                const float best = wave_max(m1);
+                float judged = best;
+                if (two) {
+                    // the second best: the lowest lane with the best gives that one up
+                    const unsigned long long has = __ballot(m1 == best);
+                    const bool gives = lane == __ffsll((long long)has) - 1;
+                    judged = as_key(best + wave_max(gives ? m2 : m1));
+                }
+                if (lane == g) mine = judged;
+            }
+            unsigned long long open = G == 64 ? ~0ull : (1ull << G) - 1;
+            for (int n = 0; n < a.rule.kept; n++) {
+                const bool here = open >> lane & 1;
+                const float best = wave_max(here ? mine : OUT);
+                const int g = __ffsll((long long)__ballot(here && mine == best)) - 1;
+                open &= ~(1ull << g);
+                stays |= 1ull << g;
+            }
 #pragma unroll
             for (int i = 0; i < V; i++) {
                 const int e = lane * V + i;
-                if (e >= g * width && e < (g + 1) * width) {
-                    const float v = two && !a.bias ? (l[i] == OUT ? OUT : as_key(score(l[i]))) : key[i];
-                    m2 = fmaxf(m2, fminf(m1, v));
-                    m1 = fmaxf(m1, v);
-                }
+                if (e < E && !(stays >> (e / width) & 1)) key[i] = OUT;
             }
-            const float best = wave_max(m1);
-            float judged = best;
-            if (two) {
-                // the second best: the lowest lane with the best gives that one up
-                const unsigned long long has = __ballot(m1 == best);
-                const bool gives = lane == __ffsll((long long)has) - 1;
-                judged = as_key(best + wave_max(gives ? m2 : m1));
-            }
-            if (lane == g) mine = judged;
-        }
-        unsigned long long open = G == 64 ? ~0ull : (1ull << G) - 1, stays = 0;
-        for (int n = 0; n < a.rule.kept; n++) {
-            const bool here = open >> lane & 1;
-            const float best = wave_max(here ? mine : OUT);
-            const int g = __ffsll((long long)__ballot(here && mine == best)) - 1;
-            open &= ~(1ull << g);
-            stays |= 1ull << g;
-        }
-#pragma unroll
-        for (int i = 0; i < V; i++) {
-            const int e = lane * V + i;
-            if (e < E && !(stays >> (e / width) & 1)) key[i] = OUT;
         }
     }
     int id = -1;                                                              // lane j: choice j
-    float chosen = OUT;
     for (int j = 0; j < k; j++) {
-        const float m = lane_best(key);
-        const float best = wave_max(m);
+        const float m = lane_best(key), best = wave_max(m);
         if (best == OUT) break;
         const int owner = __ffsll((long long)__ballot(m == best)) - 1;
-        int at = 0;
-        float value = 0.0f;
-        bool found = false;
+        unsigned places = 0;
+#pragma unroll
+        for (int i = 0; i < V; i++) places |= (unsigned)(__ballot(key[i] == best) >> owner & 1) << i;
+        const int place = __ffs(places) - 1;
+        const bool mine = lane == owner;
 #pragma unroll
         for (int i = 0; i < V; i++)
-            if (!found && key[i] == best) {
-                found = true;
-                at = i;
-                value = l[i];
-                if (lane == owner) key[i] = OUT;
-            }
-        at = __shfl(at, owner);
-        value = __shfl(value, owner);
-        if (lane == j) {
-            id = owner * V + at;
-            chosen = value;
-        }
+            if (mine && i == place) key[i] = OUT;
+        if (lane == j) id = owner * V + place;
     }
+    const float chosen = id >= 0 ? (float)row[id] : OUT;
     float share;
     const float largest = wave_max(chosen);                                   // (by all lanes: not inside a branch)
     if (soft && a.rule.renormalize) share = chosen == OUT ? 0.0f : expf(chosen - largest);
@@ -142,16 +190,28 @@ template <class Ty, int V> __device__ __forceinline__ void route_row(const Route
     }
 }
 
-template <class Ty, int V> __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
+template <class Ty, int V> __global__ __launch_bounds__(256) void route_kernel(RouteArgs a, bool wide)
 {
-    for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < a.T; t += (int64_t)gridDim.x * 4)
-        route_row<Ty, V>(a, t, threadIdx.x & 63);
+    const int lane = threadIdx.x & 63;
+    const int64_t step = (int64_t)gridDim.x * 4;
+    int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= a.T) return;
+    const typename Ty::T *logits = (const typename Ty::T *)a.logits;
+    Lane<Ty, V> next = load_lane<Ty, V>(logits + t * a.stride, lane * V, a.E, wide);
+    float bias[V];
+    load_bias<V>(a.bias, a.E, lane, bias);
+    for (; t < a.T; t += step) {
+        const Lane<Ty, V> now = next;
+        if (t + step < a.T) next = load_lane<Ty, V>(logits + (t + step) * a.stride, lane * V, a.E, wide);
+        route_row<Ty, V>(a, t, lane, now, bias);
+    }
 }
 
 // With the choice held fixed: w_j = c s_j or c s_j / sum of the chosen s.
 //   g_j = c dw_j                      or  (c / sum) (dw_j - sum_i dw_i s_i / sum)
 //   sigmoid: dl_j = g_j s_j (1 - s_j);  softmax: dl_e = s_e (g_e - sum_i g_i s_i), whose inner sum is 0 when renormalised
-template <class Ty, int V> __device__ __forceinline__ void route_row_backward(const RouteArgs &a, int64_t t, int lane, float *mine)
+template <class Ty, int V>
+__device__ __forceinline__ void route_row_backward(const RouteArgs &a, int64_t t, int lane, float *mine, const Lane<Ty, V> &raw, const float (&bias)[V], bool wide)
 {
     typedef typename Ty::T T;
     const T *row = (const T *)a.logits + t * a.stride;
@@ -163,8 +223,10 @@ template <class Ty, int V> __device__ __forceinline__ void route_row_backward(co
     const bool there = id >= 0;
     const float chosen = there ? (float)row[id] : OUT;
     const float dw = there ? a.d_weights[t * k + lane] : 0.0f;
-    float l[V], b[V];
-    const bool bad = load_logits<Ty, V>(row, a.bias, E, lane, l, b);
+#pragma unroll
+    for (int i = 0; i < V; i++) mine[i * 64 + lane] = 0.0f;
+    float l[V];
+    const bool bad = logits_of<Ty, V>(raw, bias, E, lane, l);
     float top = 0.0f, total = 1.0f;
     if (soft && !renorm) {
         top = wave_max(lane_best(l));
@@ -189,32 +251,52 @@ template <class Ty, int V> __device__ __forceinline__ void route_row_backward(co
         if (soft) inner = wave_sum(g * share);
         grad = soft ? g : g * share * (1.0f - share);
     }
-#pragma unroll
-    for (int i = 0; i < V; i++) mine[i * 64 + lane] = 0.0f;
     __builtin_amdgcn_wave_barrier();
     __threadfence_block();
     if (there) mine[id] = grad;
     __builtin_amdgcn_wave_barrier();
     __threadfence_block();
+    T u[V];
 #pragma unroll
     for (int i = 0; i < V; i++) {
-        const int e = lane * V + i;
-        if (e < E) {
-            float v = mine[e];
-            if (soft && !renorm) v = l[i] == OUT ? 0.0f : expf(l[i] - top) / total * (v - inner);
-            if (bad && l[i] != OUT) v = __uint_as_float(0x7FC00000u);
-            out[e] = (T)v;
-        }
+        float v = mine[lane * V + i];
+        if (soft && !renorm) v = l[i] == OUT ? 0.0f : expf(l[i] - top) / total * (v - inner);
+        if (bad && l[i] != OUT) v = __uint_as_float(0x7FC00000u);
+        u[i] = (T)v;
     }
+    if (wide) {
+        constexpr int BYTES = V * sizeof(T), N = BYTES < 16 ? BYTES : 16;
+        if (lane * V < E)
+#pragma unroll
+            for (int i = 0; i < BYTES / N; i++) {
+                if constexpr (N == 16) *((uint4 *)(out + lane * V) + i) = *((uint4 *)u + i);
+                else if constexpr (N == 8) *(uint2 *)(out + lane * V) = *(uint2 *)u;
+                else if constexpr (N == 4) *(uint32_t *)(out + lane * V) = *(uint32_t *)u;
+                else out[lane] = u[0];
+            }
+    } else
+#pragma unroll
+        for (int i = 0; i < V; i++)
+            if (lane * V + i < E) out[lane * V + i] = u[i];
     __builtin_amdgcn_wave_barrier();
 }
 
-template <class Ty, int V> __global__ __launch_bounds__(256) void route_backward_kernel(RouteArgs a)
+template <class Ty, int V> __global__ __launch_bounds__(256) void route_backward_kernel(RouteArgs a, bool wide, bool wide_out)
 {
     __shared__ float grads[4][64 * V];
-    const int wave = threadIdx.x >> 6;
-    for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < a.T; t += (int64_t)gridDim.x * 4)
-        route_row_backward<Ty, V>(a, t, threadIdx.x & 63, grads[wave]);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t step = (int64_t)gridDim.x * 4;
+    int64_t t = (int64_t)blockIdx.x * 4 + wave;
+    if (t >= a.T) return;
+    const typename Ty::T *logits = (const typename Ty::T *)a.logits;
+    Lane<Ty, V> next = load_lane<Ty, V>(logits + t * a.stride, lane * V, a.E, wide);
+    float bias[V];
+    load_bias<V>(a.bias, a.E, lane, bias);
+    for (; t < a.T; t += step) {
+        const Lane<Ty, V> now = next;
+        if (t + step < a.T) next = load_lane<Ty, V>(logits + (t + step) * a.stride, lane * V, a.E, wide);
+        route_row_backward<Ty, V>(a, t, lane, grads[wave], now, bias, wide_out);
+    }
 }
 
 // ---- the order by expert --------------------------------------------------------------------------------------------
@@ -375,15 +457,15 @@ template <class F> hipError_t with_width(int E, F f)
 
 }  // namespace
 
-// four rows a workgroup, and more than once around where there are over four million
-static unsigned route_grid(int64_t T) { return (unsigned)((T + 3) / 4 < (1 << 20) ? (T + 3) / 4 : (1 << 20)); }
+// four waves a workgroup, eight workgroups a compute unit; a wave's next row is on its way while it works on one
+static unsigned route_grid(int64_t T) { return (unsigned)((T + 3) / 4 < 2048 ? (T + 3) / 4 : 2048); }
 
 hipError_t launch_route(const RouteArgs &a, int type, hipStream_t s)
 {
     const unsigned grid = route_grid(a.T);
     return with_type(type, [&](auto ty) {
         return with_width(a.E, [&](auto v) {
-            route_kernel<decltype(ty), decltype(v)::value><<<grid, 256, 0, s>>>(a);
+            route_kernel<decltype(ty), decltype(v)::value><<<grid, 256, 0, s>>>(a, rows_of_lanes<decltype(ty), decltype(v)::value>(a.logits, a.stride, a.E));
             return hipGetLastError();
         });
     });
@@ -394,7 +476,8 @@ hipError_t launch_route_backward(const RouteArgs &a, int type, hipStream_t s)
     const unsigned grid = route_grid(a.T);
     return with_type(type, [&](auto ty) {
         return with_width(a.E, [&](auto v) {
-            route_backward_kernel<decltype(ty), decltype(v)::value><<<grid, 256, 0, s>>>(a);
+            route_backward_kernel<decltype(ty), decltype(v)::value><<<grid, 256, 0, s>>>(a, rows_of_lanes<decltype(ty), decltype(v)::value>(a.logits, a.stride, a.E),
+                                                                                         rows_of_lanes<decltype(ty), decltype(v)::value>(a.d_logits, a.d_stride, a.E));
             return hipGetLastError();
         });
     });
