@@ -368,13 +368,15 @@ template <class Ty> __device__ __forceinline__ void raw_block(const typename Ty:
     }
 }
 
-// In: void, or the type of a RAW a (J = 1).  grid: strips of sixteen rows of b, tiles of a
-template <class In, int J, bool SQUARES, bool EXACT, class Out> __global__ __launch_bounds__(64 * FEW_WAVES) void product_few_kernel(ProductArgs p, bool wide_in, bool wide)
+// In: void, or the type of a RAW a (J = 1).  A workgroup takes STRIPS times sixteen rows of b, whose loads of a block are on their way
+// together, or (one strip) those of four blocks.  grid: groups of strips, tiles of a
+template <class In, int J, int STRIPS, bool SQUARES, bool EXACT, class Out> __global__ __launch_bounds__(64 * FEW_WAVES) void product_few_kernel(ProductArgs p, bool wide_in, bool wide)
 {
     constexpr bool RAW = !std::is_same<In, void>::value;
-    __shared__ v4f parts[FEW_WAVES][J][64];
+    constexpr int AHEAD = STRIPS == 1 ? 4 : 1;
+    __shared__ v4f parts[FEW_WAVES][J * STRIPS][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t strip = blockIdx.x;
+    const int64_t strip = (int64_t)blockIdx.x * STRIPS;
     int64_t matrix = 0, first = (int64_t)blockIdx.y * (16 * J), end = p.rows_a;
     if (p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES) {
         int e;
@@ -388,60 +390,80 @@ template <class In, int J, bool SQUARES, bool EXACT, class Out> __global__ __lau
         const int64_t r = first + j * 16 + tok < end ? first + j * 16 + tok : end - 1;       // (rows beyond the last: the last again)
         src[j] = p.mode == ASGD_PRODUCT_GATHER ? p.order.slots[r] / p.order.k : r;
     }
-    const int64_t r = strip * 16 + tok, row_bytes = p.kb * BLOCK8;
-    const uint8_t *b = p.b + (matrix * p.rows_b + (r < p.rows_b ? r : p.rows_b - 1)) * row_bytes + quarter * 32;
-    const float *sb = SQUARES ? p.sb + (matrix * blocks8(p.rows_b) + strip / 8) * p.kb : p.sb;
-    int64_t scale_row[4];
+    const int64_t row_bytes = p.kb * BLOCK8, squares = blocks8(p.rows_b);
+    const uint8_t *b[STRIPS];
 #pragma unroll
-    for (int n = 0; n < 4; n++) scale_row[n] = strip * 16 + quarter * 4 + n < p.rows_b ? strip * 16 + quarter * 4 + n : p.rows_b - 1;
-    v4f sum[J];
+    for (int s = 0; s < STRIPS; s++) {
+        const int64_t r = (strip + s) * 16 + tok;
+        b[s] = p.b + (matrix * p.rows_b + (r < p.rows_b ? r : p.rows_b - 1)) * row_bytes + quarter * 32;
+    }
+    v4f sum[STRIPS][J];
 #pragma unroll
-    for (int j = 0; j < J; j++) sum[j] = {0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int AHEAD = 4;
+    for (int s = 0; s < STRIPS; s++)
+#pragma unroll
+        for (int j = 0; j < J; j++) sum[s][j] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int64_t kb0 = wave; kb0 < p.kb; kb0 += FEW_WAVES * AHEAD) {
-        v4i u[AHEAD], v[AHEAD];
+        v4i u[STRIPS][AHEAD], v[STRIPS][AHEAD];
 #pragma unroll
         for (int n = 0; n < AHEAD; n++) {
             const int64_t kb = kb0 + n * FEW_WAVES < p.kb ? kb0 + n * FEW_WAVES : kb0;
-            u[n] = *(const v4i *)(b + kb * BLOCK8);
-            v[n] = *(const v4i *)(b + kb * BLOCK8 + 16);
+#pragma unroll
+            for (int s = 0; s < STRIPS; s++) {
+                u[s][n] = *(const v4i *)(b[s] + kb * BLOCK8);
+                v[s][n] = *(const v4i *)(b[s] + kb * BLOCK8 + 16);
+            }
         }
 #pragma unroll
         for (int n = 0; n < AHEAD; n++) {
-            const int64_t kb = kb0 + n * FEW_WAVES;
-            if (kb >= p.kb) break;
-            Operand<EXACT> w;
-            w.set(u[n], v[n]);
-            v4f of_b;
-#pragma unroll
-            for (int i = 0; i < 4; i++) of_b[i] = SQUARES ? sb[kb] : sb[kb * p.rows_b + scale_row[i]];
+            // Past the last block: the first of these again, times zero.  (Not a branch around the sums: a matrix instruction whose result a path
+            // leaves unused writes registers that the path has taken for something else by then, addresses among them.)
+            const bool there = kb0 + n * FEW_WAVES < p.kb;
+            const int64_t kb = there ? kb0 + n * FEW_WAVES : kb0;
+            Operand<EXACT> a[J];
+            float scale[J];
 #pragma unroll
             for (int j = 0; j < J; j++) {
-                float scale;
                 v4i lo, hi;
-                if constexpr (RAW) raw_block<In>((const typename In::T *)p.a + src[j] * p.stride_raw, first + j * 16 + tok < end, wide_in, kb * BLOCK8 + quarter * 32, p.cols, scale, lo, hi);
+                if constexpr (RAW) raw_block<In>((const typename In::T *)p.a + src[j] * p.stride_raw, first + j * 16 + tok < end, wide_in, kb * BLOCK8 + quarter * 32, p.cols, scale[j], lo, hi);
                 else {
-                    const uint8_t *a = p.a + src[j] * row_bytes + kb * BLOCK8 + quarter * 32;
-                    lo = *(const v4i *)a;
-                    hi = *(const v4i *)(a + 16);
-                    scale = p.sa[kb * p.rows_a + src[j]];
+                    const uint8_t *at = p.a + src[j] * row_bytes + kb * BLOCK8 + quarter * 32;
+                    lo = *(const v4i *)at;
+                    hi = *(const v4i *)(at + 16);
+                    scale[j] = p.sa[kb * p.rows_a + src[j]];
                 }
-                Operand<EXACT> a;
-                a.set(lo, hi);
-                const v4f part = block_product(w, a);
+                a[j].set(lo, hi);
+                scale[j] = there ? scale[j] : 0.0f;
+            }
 #pragma unroll
-                for (int i = 0; i < 4; i++) sum[j][i] = SQUARES ? fmaf(part[i], scale * of_b[i], sum[j][i]) : fmaf(part[i] * of_b[i], scale, sum[j][i]);
+            for (int s = 0; s < STRIPS; s++) {
+                Operand<EXACT> w;
+                w.set(u[s][n], v[s][n]);
+                v4f of_b;
+                const int64_t row = (strip + s) * 16;
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    if (SQUARES) of_b[i] = p.sb[(matrix * squares + (row / BLOCK8 < squares ? row / BLOCK8 : squares - 1)) * p.kb + kb];
+                    else of_b[i] = p.sb[kb * p.rows_b + (row + quarter * 4 + i < p.rows_b ? row + quarter * 4 + i : p.rows_b - 1)];
+                }
+#pragma unroll
+                for (int j = 0; j < J; j++) {
+                    const v4f part = block_product(w, a[j]);
+#pragma unroll
+                    for (int i = 0; i < 4; i++) sum[s][j][i] = SQUARES ? fmaf(part[i], scale[j] * of_b[i], sum[s][j][i]) : fmaf(part[i] * of_b[i], scale[j], sum[s][j][i]);
+                }
             }
         }
     }
 #pragma unroll
-    for (int j = 0; j < J; j++) parts[wave][j][lane] = sum[j];
-    __syncthreads();
-    if (wave < J) {
-        v4f total = parts[0][wave][lane];
+    for (int s = 0; s < STRIPS; s++)
 #pragma unroll
-        for (int w = 1; w < FEW_WAVES; w++) total += parts[w][wave][lane];
-        const int64_t row = first + wave * 16 + tok, c = strip * 16 + quarter * 4;
+        for (int j = 0; j < J; j++) parts[wave][s * J + j][lane] = sum[s][j];
+    __syncthreads();
+    for (int n = wave; n < J * STRIPS; n += FEW_WAVES) {
+        v4f total = parts[0][n][lane];
+#pragma unroll
+        for (int w = 1; w < FEW_WAVES; w++) total += parts[w][n][lane];
+        const int64_t row = first + n % J * 16 + tok, c = (strip + n / J) * 16 + quarter * 4;
         if (row < end) store_four<Out>((typename Out::T *)p.out + row * p.stride + c, p.rows_b - c, wide, total);
     }
 }
@@ -510,6 +532,10 @@ template <class In, bool EXACT, class Out> __global__ __launch_bounds__(64 * FEW
 // places in use by `slots` slots of E experts, each expert's rounded up to whole tiles: what there can be at most, and what there will be about
 static int64_t most_tiles(int64_t slots, int64_t E, int rows) { return slots / rows + (slots < E ? slots : E); }
 
+// Four strips a workgroup (its rows of a, its place among the experts and its end are then there once for four) where that leaves more than a workgroup for
+// each of the 256 compute units, or the contraction has less than a block for each of its waves.
+static bool more_strips(const ProductArgs &p, unsigned strips, unsigned tiles) { return (int64_t)strips * tiles >= 2048 || (p.kb <= FEW_WAVES && strips >= 4); }
+
 hipError_t launch_product(const ProductArgs &p, bool squares, int type, hipStream_t s)
 {
     const bool grouped = p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES, over = p.mode == ASGD_PRODUCT_OVER;
@@ -521,8 +547,9 @@ hipError_t launch_product(const ProductArgs &p, bool squares, int type, hipStrea
         typedef decltype(out) Out;
         const auto few = [&](auto j, auto sq, auto exact) {
             constexpr int J = decltype(j)::value;
-            const dim3 grid((unsigned)((p.rows_b + 15) / 16), (unsigned)tiles_of(16 * J));
-            product_few_kernel<void, J, decltype(sq)::value, decltype(exact)::value, Out><<<grid, 64 * FEW_WAVES, 0, s>>>(p, false, wide4);
+            const unsigned strips = (unsigned)((p.rows_b + 15) / 16), tiles = (unsigned)tiles_of(16 * J);
+            if (!more_strips(p, strips, tiles)) product_few_kernel<void, J, 1, decltype(sq)::value, decltype(exact)::value, Out><<<dim3(strips, tiles), 64 * FEW_WAVES, 0, s>>>(p, false, wide4);
+            else product_few_kernel<void, J, 4, decltype(sq)::value, decltype(exact)::value, Out><<<dim3((strips + 3) / 4, tiles), 64 * FEW_WAVES, 0, s>>>(p, false, wide4);
             return hipGetLastError();
         };
         const auto tiles = [&](auto tok, auto wt, auto waves_tok, auto waves_wt, auto sq, auto exact, auto far) {
@@ -571,12 +598,18 @@ hipError_t launch_product_raw(const ProductArgs &p, int raw_type, int type, hipS
     const bool grouped = p.mode == ASGD_PRODUCT_GATHER;
     const bool wide = p.stride % 4 == 0 && (uintptr_t)p.out % (4 * type_size(type)) == 0;
     const bool wide_in = p.stride_raw * (int64_t)type_size(raw_type) % 16 == 0 && ((uintptr_t)p.a & 15) == 0;
-    const dim3 grid((unsigned)((p.rows_b + 15) / 16), grouped ? (unsigned)most_tiles(p.order.T * p.order.k, p.order.E, 16) : 1u);
+    const unsigned strips = (unsigned)((p.rows_b + 15) / 16), tiles = grouped ? (unsigned)most_tiles(p.order.T * p.order.k, p.order.E, 16) : 1u;
+    const bool more = more_strips(p, strips, tiles);
+    const dim3 grid(more ? (strips + 3) / 4 : strips, tiles);
     return with_type(raw_type, [&](auto in) {
         return with_type(type, [&](auto out) {
-            if (p.exact) product_few_kernel<decltype(in), 1, true, true, decltype(out)><<<grid, 64 * FEW_WAVES, 0, s>>>(p, wide_in, wide);
-            else product_few_kernel<decltype(in), 1, true, false, decltype(out)><<<grid, 64 * FEW_WAVES, 0, s>>>(p, wide_in, wide);
-            return hipGetLastError();
+            const auto go = [&](auto n, auto exact) {
+                product_few_kernel<decltype(in), 1, decltype(n)::value, true, decltype(exact)::value, decltype(out)><<<grid, 64 * FEW_WAVES, 0, s>>>(p, wide_in, wide);
+                return hipGetLastError();
+            };
+            const std::true_type yes;
+            const std::false_type no;
+            return more ? p.exact ? go(One<4>(), yes) : go(One<4>(), no) : p.exact ? go(One<1>(), yes) : go(One<1>(), no);
         });
     });
 }

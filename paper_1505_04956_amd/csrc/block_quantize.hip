@@ -61,16 +61,19 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_rows_kernel(
     }
 }
 
-// The transpose: a workgroup takes 128 rows of x (a block of the result) and 64 columns (rows of the result).  A thread has one column
-// and 32 of the rows in registers, four threads a block; it writes 32 bytes in a row, the four of them a whole line.
-template <class Ty> __global__ __launch_bounds__(256) void quantize_turned_kernel(QuantArgs q)
+// The transpose: a workgroup takes 128 rows of x (a block of the result) and 64 columns (rows of the result).  A thread has eight
+// neighbouring columns of four rows, so that loads are wide; it gives four neighbours of each of eight rows of the result, which go
+// through the LDS to be written as whole lines.
+template <class Ty> __global__ __launch_bounds__(256) void quantize_turned_kernel(QuantArgs q, bool wide)
 {
     typedef typename Ty::T T;
-    __shared__ uint32_t tops[4][64];
+    constexpr int PITCH = BLOCK8 + 4;
+    __shared__ uint32_t tops[32][64];
+    __shared__ uint32_t lines[64 * PITCH / 4];
     __shared__ int64_t source[BLOCK8];
     __shared__ float factor[BLOCK8];
     const int64_t rb = blockIdx.x;
-    const int c0 = threadIdx.x & 63, quarter = threadIdx.x >> 6;
+    const int part = threadIdx.x & 7, rows = threadIdx.x >> 3;
     if (q.order.offsets) {
         const int E = q.order.E;
         if (rb >= q.order.blocks[E]) return;
@@ -94,32 +97,51 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_turned_kerne
     }
     __syncthreads();
     for (int64_t cb = blockIdx.y; cb * 64 < q.cols; cb += gridDim.y) {
-        const int64_t c = cb * 64 + c0;
-        const bool inside = c < q.cols;
-        float v[32];
-        uint32_t top = 0;
+        const int64_t c = cb * 64 + part * 8;
+        float v[4][8];
+        uint32_t top[8] = {};
 #pragma unroll
-        for (int i = 0; i < 32; i++) {
-            const int64_t r = source[quarter * 32 + i];
-            v[i] = inside && r >= 0 ? (float)((const T *)q.x)[r * q.stride + c] : 0.0f;
-            if (q.weights) v[i] *= r >= 0 ? factor[quarter * 32 + i] : 0.0f;
-            top = max(top, magnitude_bits(v[i]));
-        }
-        tops[quarter][c0] = top;
-        __syncthreads();
-        top = max(max(tops[0][c0], tops[1][c0]), max(tops[2][c0], tops[3][c0]));
-        __syncthreads();
-        float scale, inverse;
-        block_scale(top, scale, inverse);
-        if (inside) {
-            uint32_t o[8];
+        for (int i = 0; i < 4; i++) {
+            const int64_t r = source[rows * 4 + i];
+            if (r >= 0) load8<Ty>((const T *)q.x + r * q.stride + c, q.cols - c, wide, v[i]);
+            else
 #pragma unroll
-            for (int i = 0; i < 8; i++) o[i] = eight_bits(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inverse);
-            uint4 *to = (uint4 *)(q.values + (c * q.out_blocks + rb) * BLOCK8 + quarter * 32);
-            to[0] = make_uint4(o[0], o[1], o[2], o[3]);
-            to[1] = make_uint4(o[4], o[5], o[6], o[7]);
-            if (quarter == 0) q.scales[rb * q.out_rows + c] = scale;
+                for (int n = 0; n < 8; n++) v[i][n] = 0.0f;
         }
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const float w = q.weights ? factor[rows * 4 + i] : 1.0f;
+#pragma unroll
+            for (int n = 0; n < 8; n++) {
+                if (q.weights) v[i][n] *= w;
+                top[n] = max(top[n], magnitude_bits(v[i][n]));
+            }
+        }
+        *(uint4 *)&tops[rows][part * 8] = make_uint4(top[0], top[1], top[2], top[3]);
+        *(uint4 *)&tops[rows][part * 8 + 4] = make_uint4(top[4], top[5], top[6], top[7]);
+        __syncthreads();
+        if (threadIdx.x < 64) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int n = 0; n < 32; n++) m = max(m, tops[n][threadIdx.x]);
+            float scale, inverse;
+            block_scale(m, scale, inverse);
+            if (cb * 64 + threadIdx.x < q.cols) q.scales[rb * q.out_rows + cb * 64 + threadIdx.x] = scale;
+            tops[0][threadIdx.x] = __float_as_uint(inverse);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < 8; n++)
+            lines[((part * 8 + n) * PITCH) / 4 + rows] = eight_bits(v[0][n], v[1][n], v[2][n], v[3][n], __uint_as_float(tops[0][part * 8 + n]));
+        __syncthreads();
+        const int line = threadIdx.x >> 2, quarter = threadIdx.x & 3;
+        if (cb * 64 + line < q.cols) {
+            const uint32_t *from = lines + line * (PITCH / 4) + quarter * 8;
+            uint4 *to = (uint4 *)(q.values + ((cb * 64 + line) * q.out_blocks + rb) * BLOCK8 + quarter * 32);
+            to[0] = make_uint4(from[0], from[1], from[2], from[3]);
+            to[1] = make_uint4(from[4], from[5], from[6], from[7]);
+        }
+        __syncthreads();
     }
 }
 
@@ -179,7 +201,7 @@ hipError_t launch_quantize_turned(const QuantArgs &q, int type, hipStream_t s)
     const int64_t strips = (q.cols + 63) / 64;
     const dim3 grid((unsigned)q.out_blocks, (unsigned)(strips < 1024 ? strips : 1024));
     return with_type(type, [&](auto ty) {
-        quantize_turned_kernel<decltype(ty)><<<grid, 256, 0, s>>>(q);
+        quantize_turned_kernel<decltype(ty)><<<grid, 256, 0, s>>>(q, rows_are_wide(q, type));
         return hipGetLastError();
     });
 }

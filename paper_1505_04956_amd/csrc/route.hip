@@ -300,61 +300,37 @@ template <class Ty, int V> __global__ __launch_bounds__(256) void route_backward
 }
 
 // ---- the order by expert --------------------------------------------------------------------------------------------
-// A counting sort that keeps the order of slots.  A chunk of CHUNK slots belongs to one wave, which walks it in order: the
-// lanes that have the same expert find each other by the bits of its number, and each learns how many lower lanes have it.
-// Three steps: count per chunk, add up over chunks and experts, place.
-constexpr int CHUNK = 1024;
-constexpr int ONE_BLOCK_CHUNKS = 16;      // up to here one workgroup does it all, its counts in the LDS
+// A counting sort that keeps the order of slots.  Lanes that have the same expert find each other by the bits of its number, and each
+// learns how many lower lanes have it.  A workgroup takes 4096 slots at a time, 256 a wave, whose ids it holds in registers:
+// counts of each wave, sums over the waves, places.  Where there are more slots, chunks of them are counted first, and every
+// workgroup adds up for itself what lies before its chunk.
+constexpr int HELD = 4, WAVE_SLOTS = 64 * HELD, BLOCK_SLOTS = 16 * WAVE_SLOTS, MOST_CHUNKS = 256;
 
-__device__ __forceinline__ unsigned long long same_expert(int e)
+__device__ __forceinline__ unsigned long long same_expert(int e, int bits)
 {
     unsigned long long same = ~0ull;
-#pragma unroll
-    for (int bit = 0; bit < 11; bit++) {      // (E itself stands for none: 11 bits)
+    for (int bit = 0; bit < bits; bit++) {
         const unsigned long long set = __ballot(e >> bit & 1);
         same &= e >> bit & 1 ? set : ~set;
     }
     return same;
 }
 
-__device__ __forceinline__ int expert_of(const int32_t *ids, int64_t slot, int64_t end, int E)
-{
-    const int e = slot < end ? ids[slot] : -1;
-    return (unsigned)e < (unsigned)E ? e : E;
-}
-
-// counts of a chunk, added to `count` (E + 1 words, zero before)
-__device__ void count_chunk(const int32_t *ids, int64_t begin, int64_t end, int E, int *count)
+// a wave's ids from `begin` on; E: none
+__device__ __forceinline__ void load_ids(const int32_t *ids, int64_t begin, int64_t end, int E, int (&e)[HELD])
 {
     const int lane = threadIdx.x & 63;
-    for (int64_t s = begin; s < end; s += 64) {
-        const int e = expert_of(ids, s + lane, end, E);
-        if (s + lane < end) atomicAdd(&count[e], 1);      // (whole numbers: any order gives the same)
+#pragma unroll
+    for (int r = 0; r < HELD; r++) {
+        const int64_t s = begin + r * 64 + lane;
+        e[r] = s < end ? ids[s] : -1;
     }
-}
-
-// places of a chunk's slots; next[e]: the place of the next slot of expert e
-__device__ void place_chunk(const int32_t *ids, int64_t begin, int64_t end, int E, volatile int *next, int32_t *slots, int32_t *places)
-{
-    const int lane = threadIdx.x & 63;
-    for (int64_t s = begin; s < end; s += 64) {
-        const int e = expert_of(ids, s + lane, end, E);
-        const unsigned long long same = same_expert(e), before = same & ((1ull << lane) - 1);
-        const bool there = e < E;
-        int place = -1;
-        if (there) place = next[e] + __popcll(before);
-        __builtin_amdgcn_wave_barrier();
-        if (there && !before) next[e] = place + __popcll(same);
-        __builtin_amdgcn_wave_barrier();
-        if (s + lane < end) {
-            places[s + lane] = place;
-            if (there) slots[place] = (int32_t)(s + lane);
-        }
-    }
+#pragma unroll
+    for (int r = 0; r < HELD; r++) e[r] = (unsigned)e[r] < (unsigned)E ? e[r] : E;
 }
 
 // Exclusive sums over the experts of their counts and of their blocks of 128, by one workgroup of 1024 (thread e has expert e).
-__device__ void sum_experts(int n, int E, int32_t *offsets, int32_t *blocks, int &offset)
+__device__ int sum_experts(int n, int E, int32_t *offsets, int32_t *blocks, bool write)
 {
     __shared__ int part[2][16];
     const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
@@ -369,82 +345,126 @@ __device__ void sum_experts(int n, int E, int32_t *offsets, int32_t *blocks, int
     __syncthreads();
     int b0 = 0, b1 = 0;
     for (int w = 0; w < wave; w++) { b0 += part[0][w]; b1 += part[1][w]; }
-    offset = b0 + s0 - v0;
-    if (e < E) { offsets[e] = offset; blocks[e] = b1 + s1 - v1; }
-    if (e == E - 1) { offsets[E] = b0 + s0; blocks[E] = b1 + s1; }
-    __syncthreads();
+    if (write) {
+        if (e < E) { offsets[e] = b0 + s0 - v0; blocks[e] = b1 + s1 - v1; }
+        if (e == E - 1) { offsets[E] = b0 + s0; blocks[E] = b1 + s1; }
+    }
+    return b0 + s0 - v0;
 }
 
-__global__ __launch_bounds__(1024) void plan_one_block_kernel(const int32_t *ids, asgd_route_order o, int chunk, int chunks)
+// table[chunk][e]: the slots of expert e in a chunk of `chunk` slots
+__global__ __launch_bounds__(1024) void plan_count_kernel(const int32_t *ids, int64_t slots, int64_t chunk, int E, int bits, int *table)
 {
-    extern __shared__ int count[];                  // [chunks][E + 1]
+    __shared__ int count[ASGD_ROUTE_MAX_EXPERTS + 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int i = threadIdx.x; i <= E; i += 1024) count[i] = 0;
+    __syncthreads();
+    const int64_t begin = blockIdx.x * chunk, end = begin + chunk < slots ? begin + chunk : slots;
+    for (int64_t s = begin + wave * WAVE_SLOTS; s < end; s += BLOCK_SLOTS) {
+        int e[HELD];
+        load_ids(ids, s, end, E, e);
+#pragma unroll
+        for (int r = 0; r < HELD; r++) {
+            const unsigned long long same = same_expert(e[r], bits);
+            if (!(same & ((1ull << lane) - 1))) atomicAdd(&count[e[r]], __popcll(same));      // (whole numbers: any order gives the same)
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < E; i += 1024) table[(int64_t)blockIdx.x * E + i] = count[i];
+}
+
+// chunks = 1: no table
+__global__ __launch_bounds__(1024) void plan_place_kernel(const int32_t *ids, asgd_route_order o, int64_t chunk, int chunks, int bits, const int *table)
+{
+    extern __shared__ unsigned short ranks[];       // [16][E + 1]: of a wave, then slots of the expert in the waves before it
+    __shared__ int next[ASGD_ROUTE_MAX_EXPERTS], total[ASGD_ROUTE_MAX_EXPERTS];
     __shared__ int used;
-    const int E = o.E, wave = threadIdx.x >> 6;
-    const int64_t slots = o.T * o.k;
-    for (int i = threadIdx.x; i < chunks * (E + 1); i += blockDim.x) count[i] = 0;
-    __syncthreads();
-    const int64_t begin = (int64_t)wave * chunk, end = begin + chunk < slots ? begin + chunk : slots;
-    if (wave < chunks) count_chunk(ids, begin, end, E, count + wave * (E + 1));
-    __syncthreads();
-    int n = 0;
-    const int e = threadIdx.x;
-    if (e < E)
-        for (int c = 0; c < chunks; c++) n += count[c * (E + 1) + e];
-    int offset;
-    sum_experts(n, E, o.offsets, o.blocks, offset);
-    if (e < E)
-        for (int c = 0; c < chunks; c++) {
-            const int m = count[c * (E + 1) + e];
-            count[c * (E + 1) + e] = offset;
-            offset += m;
+    const int E = o.E, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, me = threadIdx.x;
+    const int64_t slots = o.T * o.k, begin = blockIdx.x * chunk, end = begin + chunk < slots ? begin + chunk : slots;
+    unsigned short *mine = ranks + wave * (E + 1);
+    int e[HELD];
+    const auto count = [&](int64_t s) {
+        for (int i = lane; i <= E; i += 64) mine[i] = 0;
+        __threadfence_block();
+        load_ids(ids, s + wave * WAVE_SLOTS, end, E, e);
+#pragma unroll
+        for (int r = 0; r < HELD; r++) {
+            const unsigned long long same = same_expert(e[r], bits);
+            if (!(same & ((1ull << lane) - 1))) mine[e[r]] += (unsigned short)__popcll(same);
+            __builtin_amdgcn_wave_barrier();
+            __threadfence_block();
         }
-    if (e == E - 1) used = offset;
-    __syncthreads();
-    if (wave < chunks) place_chunk(ids, begin, end, E, count + wave * (E + 1), o.slots, o.places);
-    for (int64_t p = used + threadIdx.x; p < slots; p += blockDim.x) o.slots[p] = -1;
-}
-
-// many slots: the counts [chunk][E] go through memory
-__global__ __launch_bounds__(64) void plan_count_kernel(const int32_t *ids, int64_t slots, int E, int *work)
-{
-    extern __shared__ int count[];                  // E + 1
-    for (int i = threadIdx.x; i <= E; i += 64) count[i] = 0;
-    __syncthreads();
-    const int64_t begin = (int64_t)blockIdx.x * CHUNK, end = begin + CHUNK < slots ? begin + CHUNK : slots;
-    count_chunk(ids, begin, end, E, count);
-    __syncthreads();
-    for (int i = threadIdx.x; i < E; i += 64) work[(int64_t)blockIdx.x * E + i] = count[i];
-}
-
-__global__ __launch_bounds__(1024) void plan_sum_kernel(asgd_route_order o, int64_t chunks, int *work)
-{
-    const int E = o.E, e = threadIdx.x;
-    int n = 0;
-    if (e < E)
-        for (int64_t c = 0; c < chunks; c++) n += work[c * E + e];
-    int offset;
-    sum_experts(n, E, o.offsets, o.blocks, offset);
-    if (e < E)
-        for (int64_t c = 0; c < chunks; c++) {
-            const int m = work[c * E + e];
-            work[c * E + e] = offset;
-            offset += m;
+        __syncthreads();
+    };
+    if (chunks > 1) {
+        // what all chunks have, and those before this one: the threads of an expert take a part of the chunks each
+        if (me < E) next[me] = total[me] = 0;
+        __syncthreads();
+        const int parts = 1024 / E, part = me / E, mine_e = me - part * E;
+        int all = 0, before = 0;
+        if (part < parts)
+            for (int c = part; c < chunks; c += parts) {
+                const int n = table[(int64_t)c * E + mine_e];
+                all += n;
+                before += c < (int)blockIdx.x ? n : 0;
+            }
+        if (part < parts) {
+            atomicAdd(&total[mine_e], all);
+            atomicAdd(&next[mine_e], before);
         }
-}
-
-__global__ __launch_bounds__(64) void plan_place_kernel(const int32_t *ids, asgd_route_order o, const int *work)
-{
-    extern __shared__ int next[];                   // E
-    const int E = o.E;
-    const int64_t slots = o.T * o.k;
-    for (int i = threadIdx.x; i < E; i += 64) next[i] = work[(int64_t)blockIdx.x * E + i];
+        __syncthreads();
+    } else {
+        count(begin);
+        if (me < E) {
+            int n = 0;
+            for (int w = 0; w < 16; w++) n += ranks[w * (E + 1) + me];
+            total[me] = n;
+            next[me] = 0;
+        }
+        __syncthreads();
+    }
+    const int n = me < E ? total[me] : 0, offset = sum_experts(n, E, o.offsets, o.blocks, blockIdx.x == 0);
+    if (me < E) next[me] += offset;
+    if (me == E - 1) used = offset + n;
     __syncthreads();
-    const int64_t begin = (int64_t)blockIdx.x * CHUNK, end = begin + CHUNK < slots ? begin + CHUNK : slots;
-    place_chunk(ids, begin, end, E, next, o.slots, o.places);
-    const int used = o.offsets[E];
-    for (int64_t p = begin + threadIdx.x; p < end; p += 64)
+    for (int64_t s = begin; s < end; s += BLOCK_SLOTS) {
+        if (chunks > 1) count(s);
+        int sum = 0;
+        if (me < E)
+            for (int w = 0; w < 16; w++) {
+                const int m = ranks[w * (E + 1) + me];
+                ranks[w * (E + 1) + me] = (unsigned short)sum;
+                sum += m;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < HELD; r++) {
+            const int64_t slot = s + wave * WAVE_SLOTS + r * 64 + lane;
+            const unsigned long long same = same_expert(e[r], bits), before = same & ((1ull << lane) - 1);
+            const bool there = e[r] < E;
+            int rank = 0;
+            if (there) rank = mine[e[r]] + __popcll(before);
+            __builtin_amdgcn_wave_barrier();
+            __threadfence_block();
+            if (there && !before) mine[e[r]] = (unsigned short)(rank + __popcll(same));
+            __builtin_amdgcn_wave_barrier();
+            __threadfence_block();
+            if (slot < end) {
+                const int place = there ? next[e[r]] + rank : -1;
+                o.places[slot] = place;
+                if (there) o.slots[place] = (int32_t)slot;
+            }
+        }
+        __syncthreads();
+        if (me < E) next[me] += sum;
+        __syncthreads();
+    }
+    for (int64_t p = begin + me; p < end; p += 1024)
         if (p >= used) o.slots[p] = -1;
 }
+
+// slots of a chunk: one workgroup's where that gives few chunks
+int64_t plan_chunk(int64_t slots) { return BLOCK_SLOTS * ((slots + (int64_t)BLOCK_SLOTS * MOST_CHUNKS - 1) / ((int64_t)BLOCK_SLOTS * MOST_CHUNKS)); }
 
 template <class F> hipError_t with_width(int E, F f)
 {
@@ -485,29 +505,23 @@ hipError_t launch_route_backward(const RouteArgs &a, int type, hipStream_t s)
 
 size_t route_plan_bytes(int64_t slots, int E)
 {
-    if (slots <= (int64_t)CHUNK * ONE_BLOCK_CHUNKS) return 0;
-    return (size_t)((slots + CHUNK - 1) / CHUNK) * E * sizeof(int);
+    if (slots <= BLOCK_SLOTS) return 0;
+    const int64_t chunk = plan_chunk(slots);
+    return (size_t)((slots + chunk - 1) / chunk) * E * sizeof(int);
 }
 
 hipError_t launch_route_plan(const int32_t *ids, const asgd_route_order &o, void *work, hipStream_t s)
 {
-    const int64_t slots = o.T * o.k;
-    if (slots <= (int64_t)CHUNK * ONE_BLOCK_CHUNKS) {
-        // few slots: shorter chunks, so that all sixteen waves have some
-        int chunk = (int)((slots + ONE_BLOCK_CHUNKS - 1) / ONE_BLOCK_CHUNKS);
-        chunk = chunk < 64 ? 64 : (chunk + 63) / 64 * 64;
-        const int chunks = slots ? (int)((slots + chunk - 1) / chunk) : 1;
-        plan_one_block_kernel<<<1, 1024, (size_t)chunks * (o.E + 1) * sizeof(int), s>>>(ids, o, chunk, chunks);
-        return hipGetLastError();
+    const int64_t slots = o.T * o.k, chunk = slots ? plan_chunk(slots) : BLOCK_SLOTS;
+    const int chunks = slots ? (int)((slots + chunk - 1) / chunk) : 1;
+    int bits = 0;
+    while (o.E >> bits) bits++;                       // (E itself stands for none)
+    if (chunks > 1) {
+        plan_count_kernel<<<chunks, 1024, 0, s>>>(ids, slots, chunk, o.E, bits, (int *)work);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
     }
-    const unsigned chunks = (unsigned)((slots + CHUNK - 1) / CHUNK);
-    plan_count_kernel<<<chunks, 64, (o.E + 1) * sizeof(int), s>>>(ids, slots, o.E, (int *)work);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    plan_sum_kernel<<<1, 1024, 0, s>>>(o, chunks, (int *)work);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    plan_place_kernel<<<chunks, 64, o.E * sizeof(int), s>>>(ids, o, (const int *)work);
+    plan_place_kernel<<<chunks, 1024, (size_t)16 * (o.E + 1) * sizeof(unsigned short), s>>>(ids, o, chunk, chunks, bits, (const int *)work);
     return hipGetLastError();
 }
 
