@@ -340,33 +340,40 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_kernel(P
 // the lanes that need them (up to sixteen of them: there this is less than a launch costs).
 constexpr int FEW_WAVES = 8;
 
-template <class Ty> __device__ __forceinline__ void raw_block(const typename Ty::T *row, bool there, bool wide, int64_t c, int64_t cols, float &scale, v4i &lo, v4i &hi)
-{
-    typedef typename Ty::T T;
-    float v[32];
-    if (there && wide && c + 32 <= cols) {
-        T u[32];
+// a lane's 32 elements of a block of a row: fetched early, brought to 8 bits when they are there
+template <class Ty> struct RawBlock {
+    typename Ty::T u[32];
+    __device__ __forceinline__ void load(const typename Ty::T *row, bool there, bool wide, int64_t c, int64_t cols)
+    {
+        if (wide && c + 32 <= cols) {
+            if (there)
 #pragma unroll
-        for (int n = 0; n < (int)(32 * sizeof(T) / 16); n++) *((uint4 *)u + n) = *((const uint4 *)(row + c) + n);
+                for (int n = 0; n < (int)(32 * sizeof(typename Ty::T) / 16); n++) *((uint4 *)u + n) = *((const uint4 *)(row + c) + n);
+        } else
 #pragma unroll
-        for (int i = 0; i < 32; i++) v[i] = (float)u[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; i++) v[i] = there && c + i < cols ? (float)row[c + i] : 0.0f;
+            for (int i = 0; i < 32; i++) u[i] = there && c + i < cols ? row[c + i] : (typename Ty::T)0.0f;
     }
-    uint32_t top = 0;
+    __device__ __forceinline__ void set(bool there, float &scale, v4i &lo, v4i &hi) const
+    {
+        float v[32];
+        uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 32; i++) top = max(top, magnitude_bits(v[i]));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-    float inverse;
-    block_scale(top, scale, inverse);
+        for (int i = 0; i < 32; i++) {
+            v[i] = there ? (float)u[i] : 0.0f;
+            top = max(top, magnitude_bits(v[i]));
+        }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        float inverse;
+        block_scale(top, scale, inverse);
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        lo[i] = (int)eight_bits(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inverse);
-        hi[i] = (int)eight_bits(v[4 * i + 16], v[4 * i + 17], v[4 * i + 18], v[4 * i + 19], inverse);
+        for (int i = 0; i < 4; i++) {
+            lo[i] = (int)eight_bits(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inverse);
+            hi[i] = (int)eight_bits(v[4 * i + 16], v[4 * i + 17], v[4 * i + 18], v[4 * i + 19], inverse);
+        }
     }
-}
+};
+template <> struct RawBlock<void> {};
 
 // In: void, or the type of a RAW a (J = 1).  A workgroup takes STRIPS times sixteen rows of b, whose loads of a block are on their way
 // together, or (one strip) those of four blocks.  grid: groups of strips, tiles of a
@@ -404,9 +411,11 @@ template <class In, int J, int STRIPS, bool SQUARES, bool EXACT, class Out> __gl
         for (int j = 0; j < J; j++) sum[s][j] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int64_t kb0 = wave; kb0 < p.kb; kb0 += FEW_WAVES * AHEAD) {
         v4i u[STRIPS][AHEAD], v[STRIPS][AHEAD];
+        RawBlock<In> raw[AHEAD];
 #pragma unroll
         for (int n = 0; n < AHEAD; n++) {
             const int64_t kb = kb0 + n * FEW_WAVES < p.kb ? kb0 + n * FEW_WAVES : kb0;
+            if constexpr (RAW) raw[n].load((const typename In::T *)p.a + src[0] * p.stride_raw, first + tok < end, wide_in, kb * BLOCK8 + quarter * 32, p.cols);
 #pragma unroll
             for (int s = 0; s < STRIPS; s++) {
                 u[s][n] = *(const v4i *)(b[s] + kb * BLOCK8);
@@ -424,7 +433,7 @@ template <class In, int J, int STRIPS, bool SQUARES, bool EXACT, class Out> __gl
 #pragma unroll
             for (int j = 0; j < J; j++) {
                 v4i lo, hi;
-                if constexpr (RAW) raw_block<In>((const typename In::T *)p.a + src[j] * p.stride_raw, first + j * 16 + tok < end, wide_in, kb * BLOCK8 + quarter * 32, p.cols, scale[j], lo, hi);
+                if constexpr (RAW) raw[n].set(first + tok < end, scale[j], lo, hi);
                 else {
                     const uint8_t *at = p.a + src[j] * row_bytes + kb * BLOCK8 + quarter * 32;
                     lo = *(const v4i *)at;
@@ -471,10 +480,12 @@ template <class In, int J, int STRIPS, bool SQUARES, bool EXACT, class Out> __gl
 // A row's experts without an order, for few rows: a workgroup takes sixteen rows of b of every expert of one row of a (blockIdx.y), and
 // adds what they give times its weights.  A block of the row is brought to 8 bits once for all of them; the weights of up to
 // EXPERTS of them are on their way at a time.
-template <class In, bool EXACT, class Out> __global__ __launch_bounds__(64 * FEW_WAVES) void product_direct_kernel(ProductArgs p, const int32_t *ids, const float *weights, int k, int E, bool wide_in, bool wide)
+constexpr int DIRECT_WAVES = 16;
+
+template <class In, bool EXACT, class Out> __global__ __launch_bounds__(64 * DIRECT_WAVES) void product_direct_kernel(ProductArgs p, const int32_t *ids, const float *weights, int k, int E, bool wide_in, bool wide)
 {
-    constexpr int EXPERTS = 8;
-    __shared__ v4f parts[FEW_WAVES][64];
+    constexpr int EXPERTS = 4;
+    __shared__ v4f parts[DIRECT_WAVES][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tok = lane & 15, quarter = lane >> 4;
     const int64_t t = blockIdx.y, strip = blockIdx.x, r = strip * 16 + tok, row_bytes = p.kb * BLOCK8;
     const uint8_t *b = p.b + (r < p.rows_b ? r : p.rows_b - 1) * row_bytes + quarter * 32;
@@ -482,10 +493,12 @@ template <class In, bool EXACT, class Out> __global__ __launch_bounds__(64 * FEW
     const int64_t matrix = p.rows_b * row_bytes, squares = blocks8(p.rows_b) * p.kb;
     const typename In::T *row = (const typename In::T *)p.a + t * p.stride_raw;
     v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t kb = wave; kb < p.kb; kb += FEW_WAVES) {
+    for (int64_t kb = wave; kb < p.kb; kb += DIRECT_WAVES) {
         float scale;
         v4i lo, hi;
         Operand<EXACT> a;
+        RawBlock<In> raw;
+        raw.load(row, tok == 0, wide_in, kb * BLOCK8 + quarter * 32, p.cols);
         for (int j0 = 0; j0 < k; j0 += EXPERTS) {
             v4i u[EXPERTS], v[EXPERTS];
             float of_b[EXPERTS];
@@ -501,7 +514,7 @@ template <class In, bool EXACT, class Out> __global__ __launch_bounds__(64 * FEW
                 }
             }
             if (j0 == 0) {
-                raw_block<In>(row, tok == 0, wide_in, kb * BLOCK8 + quarter * 32, p.cols, scale, lo, hi);
+                raw.set(tok == 0, scale, lo, hi);
                 a.set(lo, hi);
             }
 #pragma unroll
@@ -521,7 +534,7 @@ template <class In, bool EXACT, class Out> __global__ __launch_bounds__(64 * FEW
     __syncthreads();
     if (wave == 0 && tok == 0) {
 #pragma unroll
-        for (int w = 1; w < FEW_WAVES; w++) sum += parts[w][lane];
+        for (int w = 1; w < DIRECT_WAVES; w++) sum += parts[w][lane];
         const int64_t c = strip * 16 + quarter * 4;
         store_four<Out>((typename Out::T *)p.out + t * p.stride + c, p.rows_b - c, wide, sum);
     }
@@ -586,8 +599,8 @@ hipError_t launch_product_direct(const ProductArgs &p, const int32_t *ids, const
     const dim3 grid((unsigned)((p.rows_b + 15) / 16), (unsigned)p.rows_a);
     return with_type(raw_type, [&](auto in) {
         return with_type(type, [&](auto out) {
-            if (p.exact) product_direct_kernel<decltype(in), true, decltype(out)><<<grid, 64 * FEW_WAVES, 0, s>>>(p, ids, weights, k, E, wide_in, wide);
-            else product_direct_kernel<decltype(in), false, decltype(out)><<<grid, 64 * FEW_WAVES, 0, s>>>(p, ids, weights, k, E, wide_in, wide);
+            if (p.exact) product_direct_kernel<decltype(in), true, decltype(out)><<<grid, 64 * DIRECT_WAVES, 0, s>>>(p, ids, weights, k, E, wide_in, wide);
+            else product_direct_kernel<decltype(in), false, decltype(out)><<<grid, 64 * DIRECT_WAVES, 0, s>>>(p, ids, weights, k, E, wide_in, wide);
             return hipGetLastError();
         });
     });
