@@ -127,6 +127,25 @@ __device__ __forceinline__ bool tile_of_expert(const asgd_route_order &o, int64_
     return false;
 }
 
+// The same for tiles of 128 places, whose number before each expert the order holds.
+__device__ __forceinline__ bool block_of_expert(const asgd_route_order &o, int tile, int &expert, int64_t &first, int64_t &end)
+{
+    const int lane = threadIdx.x & 63;
+    for (int e0 = 0; e0 < o.E; e0 += 64) {
+        const int e = e0 + lane < o.E ? e0 + lane : o.E - 1;
+        const int stop = o.blocks[e + 1], begin = o.blocks[e], place = o.offsets[e], last = o.offsets[e + 1];
+        const unsigned long long past = __ballot(stop > tile);
+        if (past) {
+            const int at = __ffsll((long long)past) - 1;
+            expert = e0 + at;
+            first = __builtin_amdgcn_readlane(place, at) + (tile - __builtin_amdgcn_readlane(begin, at)) * BLOCK8;
+            end = __builtin_amdgcn_readlane(last, at);
+            return true;
+        }
+    }
+    return false;
+}
+
 // Workgroups go round the eight dies; each die gets a run of neighbouring tiles, whose operands its L2 then shares.
 __device__ __forceinline__ uint32_t tile_of_group(uint32_t id, uint32_t n)
 {
@@ -149,7 +168,7 @@ template <int TOK, int WT, bool SQUARES> struct Stage {
     static constexpr int SCALES_B = VALUES + PIECES_A * 256, BYTES = VALUES + PIECES * 256;
 };
 
-template <int TOK, int WT, int TOK_WAVES, int WT_WAVES, bool SQUARES, bool EXACT, bool FAR, class Out>
+template <int TOK, int WT, int TOK_WAVES, int WT_WAVES, int STAGES, bool SQUARES, bool EXACT, bool FAR, class Out>
 __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_kernel(ProductArgs p, uint32_t tiles_tok, uint32_t tiles_wt, bool wide)
 {
     typedef Stage<TOK, WT, SQUARES> S;
@@ -159,11 +178,18 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_kernel(P
     static_assert((TOK + WT) / 8 % WAVES == 0 && WT / WT_WAVES <= BLOCK8 && TOK % (16 * TOK_WAVES) == 0 && WT % (16 * WT_WAVES) == 0, "");
     __shared__ __align__(16) uint8_t stage0[S::BYTES];
     __shared__ __align__(16) uint8_t stage1[S::BYTES];
+    __shared__ __align__(16) uint8_t stage2[STAGES > 2 ? S::BYTES : 16];
+    __shared__ __align__(16) uint8_t stage3[STAGES > 3 ? S::BYTES : 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wave_tok = wave % TOK_WAVES * (J * 16), wave_wt = wave / TOK_WAVES * (I * 16);
 
-    // which tile: strips of eight tiles of a, all tiles of b for each
-    const uint32_t id = tile_of_group(blockIdx.x, gridDim.x);
+    // which tile: strips of eight tiles of a, all tiles of b for each.  (The host knows how many tiles experts can have at most; shared among
+    // the dies are those that they have.)
+    const bool grouped = p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES;
+    if (grouped && TOK == BLOCK8) tiles_tok = p.order.blocks[p.order.E];
+    const uint32_t all = grouped && TOK == BLOCK8 ? tiles_tok * tiles_wt : gridDim.x;
+    if (blockIdx.x >= all) return;
+    const uint32_t id = tile_of_group(blockIdx.x, all);
     uint32_t within = id;
     int64_t matrix = 0;
     if (p.mode == ASGD_PRODUCT_OVER) {
@@ -176,9 +202,9 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_kernel(P
     int64_t first = (int64_t)tile_tok * TOK, end = p.rows_a;
     int k0 = 0, k1 = (int)p.kb;
     const int64_t first_wt = (int64_t)tile_wt * WT;
-    if (p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES) {
+    if (grouped) {
         int e;
-        if (!tile_of_expert(p.order, tile_tok, TOK, e, first, end)) return;
+        if (!(TOK == BLOCK8 ? block_of_expert(p.order, tile_tok, e, first, end) : tile_of_expert(p.order, tile_tok, TOK, e, first, end))) return;
         matrix = e;
     } else if (p.mode == ASGD_PRODUCT_OVER) {
         k0 = p.order.blocks[matrix];
@@ -289,17 +315,37 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_kernel(P
         }
     };
 
+    // Step n of a round multiplies stage n and fills the one that was multiplied before it with the block STAGES - 1 further on (the last
+    // block once more where there is none left).  Before that a wave's loads of this block have arrived, those of later ones need not have,
+    // and all waves are done with the stage that is filled.
+    const auto step = [&](int kb, auto at) {
+        constexpr int N = decltype(at)::value % STAGES, FREE = (N + STAGES - 1) % STAGES;
+        uint8_t *const stages[4] = {stage0, stage1, stage2, stage3};
+        constexpr int FLYING = (STAGES - 2) * LOADS;
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt((FLYING & 15) | 7 << 4 | 15 << 8 | FLYING >> 4 << 14);       // (vmcnt alone)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        multiply(stages[N], min(kb + STAGES - 1, k1 - 1), stages[FREE], std::true_type());
+    };
     if (k0 < k1) {
+        uint8_t *const stages[4] = {stage0, stage1, stage2, stage3};
 #pragma unroll
-        for (int l = 0; l < LOADS; l++) bring(k0, stage0, l);
-        __syncthreads();
-        for (int kb = k0; kb + 1 < k1; kb += 2) {
-            multiply(stage0, kb + 1, stage1, std::true_type());
-            __syncthreads();
-            multiply(stage1, min(kb + 2, k1 - 1), stage0, std::true_type());      // (the last block once more where there is none left)
-            __syncthreads();
+        for (int n = 0; n < STAGES - 1; n++)
+#pragma unroll
+            for (int l = 0; l < LOADS; l++) bring(min(k0 + n, k1 - 1), stages[n], l);
+        int kb = k0;
+        for (; kb + STAGES - 1 < k1; kb += STAGES) {
+            step(kb, One<0>());
+            step(kb + 1, One<1>());
+            if constexpr (STAGES > 2) step(kb + 2, One<2>());
+            if constexpr (STAGES > 3) step(kb + 3, One<3>());
         }
-        if ((k1 - k0) & 1) multiply(stage0, 0, stage1, std::false_type());
+        if (kb < k1) step(kb, One<0>());
+        if constexpr (STAGES > 2)
+            if (kb + 1 < k1) step(kb + 1, One<1>());
+        if constexpr (STAGES > 3)
+            if (kb + 2 < k1) step(kb + 2, One<2>());
     }
 
     // Out through the LDS, sixteen rows of a at a time: there a lane has four neighbours of a row, in memory whole lines are wanted.
@@ -545,6 +591,12 @@ template <class In, bool EXACT, class Out> __global__ __launch_bounds__(64 * DIR
 // places in use by `slots` slots of E experts, each expert's rounded up to whole tiles: what there can be at most, and what there will be about
 static int64_t most_tiles(int64_t slots, int64_t E, int rows) { return slots / rows + (slots < E ? slots : E); }
 
+// Which tile: us of a block of the contraction for n tiles on 256 compute units, from what one tile takes with a unit to itself and what each takes where
+// there are many.  Measured (8-bit instruction, squares): 64 x 64 0.31 and 0.223 (8192^3: 916 us), 128 x 128 0.66 and 0.63 (645 us), 256 x 256
+// 2.1 (539 us).  At 777 x 1001 x 1152: 5.4, 9.5 and 18.8 us; 256 x 4096 x 4096: 10.9, 22, 48; 2048^3: 17.5, 15.7, 29; 4096 x 4096 x 2048: 66, 42, 38.  Sums in
+// 32 bits take about twice as long in each, and have no 256 x 256 (registers).
+static double tiles_time(int64_t n, double alone, double among) { return n <= 256 ? alone : alone > (double)((n + 255) / 256) * among ? alone : (double)((n + 255) / 256) * among; }
+
 // Four strips a workgroup (its rows of a, its place among the experts and its end are then there once for four) where that leaves more than a workgroup for
 // each of the 256 compute units, or the contraction has less than a block for each of its waves.
 static bool more_strips(const ProductArgs &p, unsigned strips, unsigned tiles) { return (int64_t)strips * tiles >= 2048 || (p.kb <= FEW_WAVES && strips >= 4); }
@@ -565,26 +617,27 @@ hipError_t launch_product(const ProductArgs &p, bool squares, int type, hipStrea
             else product_few_kernel<void, J, 4, decltype(sq)::value, decltype(exact)::value, Out><<<dim3((strips + 3) / 4, tiles), 64 * FEW_WAVES, 0, s>>>(p, false, wide4);
             return hipGetLastError();
         };
-        const auto tiles = [&](auto tok, auto wt, auto waves_tok, auto waves_wt, auto sq, auto exact, auto far) {
+        const auto tiles = [&](auto tok, auto wt, auto waves_tok, auto waves_wt, auto stages, auto sq, auto exact, auto far) {
             constexpr int TOK = decltype(tok)::value, WT = decltype(wt)::value, WAVES = decltype(waves_tok)::value * decltype(waves_wt)::value;
             const int64_t tiles_tok = tiles_of(TOK), tiles_wt = (p.rows_b + WT - 1) / WT;
-            product_kernel<TOK, WT, decltype(waves_tok)::value, decltype(waves_wt)::value, decltype(sq)::value, decltype(exact)::value, decltype(far)::value, Out>
+            product_kernel<TOK, WT, decltype(waves_tok)::value, decltype(waves_wt)::value, decltype(stages)::value, decltype(sq)::value, decltype(exact)::value, decltype(far)::value, Out>
                 <<<(unsigned)(tiles_tok * tiles_wt * (over ? E : 1)), 64 * WAVES, 0, s>>>(p, (uint32_t)tiles_tok, (uint32_t)tiles_wt, wide16);
             return hipGetLastError();
         };
         const auto choose = [&](auto sq, auto exact) {
             const std::true_type yes;
             const std::false_type no;
-            // (rows of a tile of an expert: what it has on average)
+            // few rows (of an expert, on average)
             const int64_t each = grouped ? rows / E : rows;
             if (!over && each <= 32) return each <= 16 ? few(One<1>(), sq, exact) : few(One<2>(), sq, exact);
-            if (grouped && (double)p.rows_a * p.kb * BLOCK8 >= 4294967296.0) return tiles(One<128>(), One<128>(), One<2>(), One<2>(), sq, exact, yes);
-            if constexpr (!decltype(exact)::value && decltype(sq)::value) {
-                // 256 x 256 are 1.2 times as fast as 128 x 128 where they fill the device as well: 256 of them go at a time, or 512
-                const int64_t big = (rows + (grouped ? E * 128 : 0) + 255) / 256 * ((p.rows_b + 255) / 256), small = (rows + (grouped ? E * 64 : 0) + 127) / 128 * ((p.rows_b + 127) / 128);
-                if (!over && (double)((big + 255) / 256) * 4.0 <= (double)((small + 511) / 512) * 2.0 * 1.2) return tiles(One<256>(), One<256>(), One<4>(), One<2>(), sq, exact, no);
+            if (grouped && (double)p.rows_a * p.kb * BLOCK8 >= 4294967296.0) return tiles(One<128>(), One<128>(), One<2>(), One<2>(), One<2>(), sq, exact, yes);
+            if (!grouped && !over) {
+                const double t64 = tiles_time(tiles_of(64) * ((p.rows_b + 63) / 64), 0.31, 0.223), t128 = tiles_time(tiles_of(128) * ((p.rows_b + 127) / 128), 0.66, 0.63);
+                if (t64 < t128) return tiles(One<64>(), One<64>(), One<2>(), One<2>(), One<4>(), sq, exact, no);
+                if constexpr (!decltype(exact)::value && decltype(sq)::value)
+                    if (tiles_time(tiles_of(256) * ((p.rows_b + 255) / 256), 2.1, 2.1) < t128) return tiles(One<256>(), One<256>(), One<4>(), One<2>(), One<2>(), sq, exact, no);
             }
-            return tiles(One<128>(), One<128>(), One<2>(), One<2>(), sq, exact, no);
+            return tiles(One<128>(), One<128>(), One<2>(), One<2>(), One<2>(), sq, exact, no);
         };
         const std::true_type yes;
         const std::false_type no;

@@ -382,17 +382,20 @@ __global__ __launch_bounds__(1024) void plan_place_kernel(const int32_t *ids, as
     const int E = o.E, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, me = threadIdx.x;
     const int64_t slots = o.T * o.k, begin = blockIdx.x * chunk, end = begin + chunk < slots ? begin + chunk : slots;
     unsigned short *mine = ranks + wave * (E + 1);
+    const int waves = end - begin >= BLOCK_SLOTS ? 16 : (int)((end - begin + WAVE_SLOTS - 1) / WAVE_SLOTS);       // that have slots
     int e[HELD];
     const auto count = [&](int64_t s) {
-        for (int i = lane; i <= E; i += 64) mine[i] = 0;
-        __threadfence_block();
-        load_ids(ids, s + wave * WAVE_SLOTS, end, E, e);
-#pragma unroll
-        for (int r = 0; r < HELD; r++) {
-            const unsigned long long same = same_expert(e[r], bits);
-            if (!(same & ((1ull << lane) - 1))) mine[e[r]] += (unsigned short)__popcll(same);
-            __builtin_amdgcn_wave_barrier();
+        if (wave < waves) {
+            for (int i = lane; i <= E; i += 64) mine[i] = 0;
             __threadfence_block();
+            load_ids(ids, s + wave * WAVE_SLOTS, end, E, e);
+#pragma unroll
+            for (int r = 0; r < HELD; r++) {
+                const unsigned long long same = same_expert(e[r], bits);
+                if (!(same & ((1ull << lane) - 1))) mine[e[r]] += (unsigned short)__popcll(same);
+                __builtin_amdgcn_wave_barrier();
+                __threadfence_block();
+            }
         }
         __syncthreads();
     };
@@ -417,7 +420,7 @@ __global__ __launch_bounds__(1024) void plan_place_kernel(const int32_t *ids, as
         count(begin);
         if (me < E) {
             int n = 0;
-            for (int w = 0; w < 16; w++) n += ranks[w * (E + 1) + me];
+            for (int w = 0; w < waves; w++) n += ranks[w * (E + 1) + me];
             total[me] = n;
             next[me] = 0;
         }
@@ -431,30 +434,31 @@ __global__ __launch_bounds__(1024) void plan_place_kernel(const int32_t *ids, as
         if (chunks > 1) count(s);
         int sum = 0;
         if (me < E)
-            for (int w = 0; w < 16; w++) {
+            for (int w = 0; w < waves; w++) {
                 const int m = ranks[w * (E + 1) + me];
                 ranks[w * (E + 1) + me] = (unsigned short)sum;
                 sum += m;
             }
         __syncthreads();
+        if (wave < waves)
 #pragma unroll
-        for (int r = 0; r < HELD; r++) {
-            const int64_t slot = s + wave * WAVE_SLOTS + r * 64 + lane;
-            const unsigned long long same = same_expert(e[r], bits), before = same & ((1ull << lane) - 1);
-            const bool there = e[r] < E;
-            int rank = 0;
-            if (there) rank = mine[e[r]] + __popcll(before);
-            __builtin_amdgcn_wave_barrier();
-            __threadfence_block();
-            if (there && !before) mine[e[r]] = (unsigned short)(rank + __popcll(same));
-            __builtin_amdgcn_wave_barrier();
-            __threadfence_block();
-            if (slot < end) {
-                const int place = there ? next[e[r]] + rank : -1;
-                o.places[slot] = place;
-                if (there) o.slots[place] = (int32_t)slot;
+            for (int r = 0; r < HELD; r++) {
+                const int64_t slot = s + wave * WAVE_SLOTS + r * 64 + lane;
+                const unsigned long long same = same_expert(e[r], bits), before = same & ((1ull << lane) - 1);
+                const bool there = e[r] < E;
+                int rank = 0;
+                if (there) rank = mine[e[r]] + __popcll(before);
+                __builtin_amdgcn_wave_barrier();
+                __threadfence_block();
+                if (there && !before) mine[e[r]] = (unsigned short)(rank + __popcll(same));
+                __builtin_amdgcn_wave_barrier();
+                __threadfence_block();
+                if (slot < end) {
+                    const int place = there ? next[e[r]] + rank : -1;
+                    o.places[slot] = place;
+                    if (there) o.slots[place] = (int32_t)slot;
+                }
             }
-        }
         __syncthreads();
         if (me < E) next[me] += sum;
         __syncthreads();
