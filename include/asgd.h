@@ -384,6 +384,11 @@ typedef struct asgd_blocks {
 int asgd_block_quantize(const void *x, int type, int64_t rows, int64_t cols, int64_t stride, int turned,
                         const asgd_route_order *order, const float *weights, const asgd_blocks *out, void *hip_stream);
 
+/* asgd_block_quantize() of the same x twice, not turned into `out` and turned into `out_turned` (both ASGD_BLOCKS_ROWS), from one
+   reading of x: what a training step takes of its activations and gradients. */
+int asgd_block_quantize_both(const void *x, int type, int64_t rows, int64_t cols, int64_t stride, const asgd_route_order *order,
+                             const float *weights, const asgd_blocks *out, const asgd_blocks *out_turned, void *hip_stream);
+
 /*
  * out[i][j] = sum over the blocks of the contraction of (scale of a) * (scale of b) * (sum of a block's products of values); a and b
  * have the same cols.  out: `type`, rows `stride` elements apart.  Scales are applied and blocks added in 32 bits.

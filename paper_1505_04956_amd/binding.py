@@ -34,7 +34,7 @@ SYMBOLS = (
     "asgd_schedule_peer", "asgd_schedule_peer_n", "asgd_last_hip_error", "asgd_destroy", "asgd_strerror",
     "asgd_quant_error_noalloc", "asgd_get_exchange", "asgd_set_exchange", "asgd_last_run_form",
     "asgd_route", "asgd_route_backward", "asgd_route_plan_bytes", "asgd_route_plan", "asgd_route_max_blocks",
-    "asgd_block_quantize", "asgd_block_product", "asgd_experts_direct", "asgd_experts_sum", "asgd_experts_sum_backward",
+    "asgd_block_quantize", "asgd_block_quantize_both", "asgd_block_product", "asgd_experts_direct", "asgd_experts_sum", "asgd_experts_sum_backward",
 )
 
 
@@ -118,6 +118,7 @@ def lib():
             "asgd_route_plan": (C.c_int, [vp, vp, vp, C.c_size_t, vp]),
             "asgd_route_max_blocks": (i64, [i64, C.c_int, C.c_int]),
             "asgd_block_quantize": (C.c_int, [vp, C.c_int, i64, i64, i64, C.c_int, vp, vp, vp, vp]),
+            "asgd_block_quantize_both": (C.c_int, [vp, C.c_int, i64, i64, i64, vp, vp, vp, vp, vp]),
             "asgd_block_product": (C.c_int, [vp, vp, C.c_int, C.c_int, vp, vp, C.c_int, i64, vp]),
             "asgd_experts_direct": (C.c_int, [vp, vp, vp, C.c_int, vp, C.c_int, vp, C.c_int, i64, vp]),
             "asgd_experts_sum": (C.c_int, [vp, C.c_int, i64, i64, vp, vp, vp, C.c_int, i64, vp]),
@@ -270,6 +271,11 @@ def asgd_route_max_blocks(T, k, E) -> int:
 def asgd_block_quantize(x_ptr, type, rows, cols, stride, turned, order, weights_ptr, out, stream=0):
     _check(lib().asgd_block_quantize(x_ptr, type, rows, cols, stride, turned, None if order is None else C.addressof(order), weights_ptr,
                                      C.addressof(out), stream), "asgd_block_quantize")
+
+
+def asgd_block_quantize_both(x_ptr, type, rows, cols, stride, order, weights_ptr, out, out_turned, stream=0):
+    _check(lib().asgd_block_quantize_both(x_ptr, type, rows, cols, stride, None if order is None else C.addressof(order), weights_ptr,
+                                          C.addressof(out), C.addressof(out_turned), stream), "asgd_block_quantize_both")
 
 
 def asgd_block_product(a, b, mode, exact, order, out_ptr, type, stride, stream=0):

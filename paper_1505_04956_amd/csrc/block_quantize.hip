@@ -61,6 +61,17 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_rows_kernel(
     }
 }
 
+// the expert whose blocks hold block rb: the last one that begins at or before it (and is not empty)
+__device__ __forceinline__ int expert_of_block(const asgd_route_order &o, int64_t rb)
+{
+    int lo = 0, hi = o.E;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (o.blocks[mid] <= rb) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
 // The transpose: a workgroup takes 128 rows of x (a block of the result) and 64 columns (rows of the result).  A thread has eight
 // neighbouring columns of four rows, so that loads are wide; it gives four neighbours of each of eight rows of the result, which go
 // through the LDS to be written as whole lines.
@@ -75,17 +86,11 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_turned_kerne
     const int64_t rb = blockIdx.x;
     const int part = threadIdx.x & 7, rows = threadIdx.x >> 3;
     if (q.order.offsets) {
-        const int E = q.order.E;
-        if (rb >= q.order.blocks[E]) return;
-        // the expert whose blocks hold rb: the last one that begins at or before it and is not empty
-        int lo = 0, hi = E;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (q.order.blocks[mid] <= rb) lo = mid; else hi = mid;
-        }
+        if (rb >= q.order.blocks[q.order.E]) return;
+        const int e = expert_of_block(q.order, rb);
         if (threadIdx.x < BLOCK8) {
-            const int64_t p = q.order.offsets[lo] + (rb - q.order.blocks[lo]) * BLOCK8 + threadIdx.x;
-            const bool there = p < q.order.offsets[lo + 1];
+            const int64_t p = q.order.offsets[e] + (rb - q.order.blocks[e]) * BLOCK8 + threadIdx.x;
+            const bool there = p < q.order.offsets[e + 1];
             const int slot = there ? q.order.slots[p] : -1;
             source[threadIdx.x] = there ? slot / q.order.k : -1;
             factor[threadIdx.x] = there && q.weights ? q.weights[slot] : 1.0f;
@@ -140,6 +145,102 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_turned_kerne
             uint4 *to = (uint4 *)(q.values + ((cb * 64 + line) * q.out_blocks + rb) * BLOCK8 + quarter * 32);
             to[0] = make_uint4(from[0], from[1], from[2], from[3]);
             to[1] = make_uint4(from[4], from[5], from[6], from[7]);
+        }
+        __syncthreads();
+    }
+}
+
+// Both at once, for training: the rows (of places) and the transpose, from one reading of x.  A workgroup takes a square of 128 x 128, a
+// thread eight neighbouring columns of eight rows: sixteen lanes hold a row's block, sixteen threads of different waves a column's.
+template <class Ty> __global__ __launch_bounds__(256) void quantize_both_kernel(QuantArgs q, uint8_t *rows_values, float *rows_scales, int64_t rows_out, int64_t rows_blocks, bool wide)
+{
+    typedef typename Ty::T T;
+    constexpr int PITCH = BLOCK8 + 4;
+    __shared__ __align__(16) uint32_t tops[16][BLOCK8];
+    __shared__ uint32_t lines[BLOCK8 * PITCH / 4];
+    __shared__ int64_t source[BLOCK8], target[BLOCK8];
+    __shared__ float factor[BLOCK8];
+    const int64_t rb = blockIdx.x;
+    const int part = threadIdx.x & 15, rows = threadIdx.x >> 4;
+    if (q.order.offsets) {
+        if (rb >= q.order.blocks[q.order.E]) return;
+        const int e = expert_of_block(q.order, rb);
+        if (threadIdx.x < BLOCK8) {
+            const int64_t p = q.order.offsets[e] + (rb - q.order.blocks[e]) * BLOCK8 + threadIdx.x;
+            const bool there = p < q.order.offsets[e + 1];
+            const int slot = there ? q.order.slots[p] : -1;
+            source[threadIdx.x] = there ? slot / q.order.k : -1;
+            target[threadIdx.x] = p;
+            factor[threadIdx.x] = there && q.weights ? q.weights[slot] : 1.0f;
+        }
+    } else if (threadIdx.x < BLOCK8) {
+        const int64_t r = rb * BLOCK8 + threadIdx.x;
+        source[threadIdx.x] = r < q.rows ? r : -1;
+        target[threadIdx.x] = r;
+        factor[threadIdx.x] = 1.0f;
+    }
+    __syncthreads();
+    for (int64_t cb = blockIdx.y; cb * BLOCK8 < q.cols; cb += gridDim.y) {
+        const int64_t c = cb * BLOCK8 + part * 8;
+        float v[8][8];
+        uint32_t top[8] = {};
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const int64_t r = source[rows * 8 + i];
+            if (r >= 0) load8<Ty>((const T *)q.x + r * q.stride + c, q.cols - c, wide, v[i]);
+            else
+#pragma unroll
+                for (int n = 0; n < 8; n++) v[i][n] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const int row = rows * 8 + i;
+            uint32_t mine = 0;
+#pragma unroll
+            for (int n = 0; n < 8; n++) {
+                if (q.weights) v[i][n] *= factor[row];
+                const uint32_t m = magnitude_bits(v[i][n]);
+                top[n] = max(top[n], m);
+                mine = max(mine, m);
+            }
+#pragma unroll
+            for (int m = 8; m; m >>= 1) mine = max(mine, (uint32_t)__shfl_xor((int)mine, m));
+            float scale, inverse;
+            block_scale(mine, scale, inverse);
+            if (source[row] >= 0) {
+                uint2 o;
+                o.x = eight_bits(v[i][0], v[i][1], v[i][2], v[i][3], inverse);
+                o.y = eight_bits(v[i][4], v[i][5], v[i][6], v[i][7], inverse);
+                *(uint2 *)(rows_values + (target[row] * rows_blocks + cb) * BLOCK8 + part * 8) = o;
+                if (part == 0) rows_scales[cb * rows_out + target[row]] = scale;
+            }
+        }
+        *(uint4 *)&tops[rows][part * 8] = make_uint4(top[0], top[1], top[2], top[3]);
+        *(uint4 *)&tops[rows][part * 8 + 4] = make_uint4(top[4], top[5], top[6], top[7]);
+        __syncthreads();
+        if (threadIdx.x < BLOCK8) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int n = 0; n < 16; n++) m = max(m, tops[n][threadIdx.x]);
+            float scale, inverse;
+            block_scale(m, scale, inverse);
+            if (cb * BLOCK8 + threadIdx.x < q.cols) q.scales[rb * q.out_rows + cb * BLOCK8 + threadIdx.x] = scale;
+            tops[0][threadIdx.x] = __float_as_uint(inverse);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < 8; n++) {
+            const float inverse = __uint_as_float(tops[0][part * 8 + n]);
+            lines[(part * 8 + n) * (PITCH / 4) + rows * 2] = eight_bits(v[0][n], v[1][n], v[2][n], v[3][n], inverse);
+            lines[(part * 8 + n) * (PITCH / 4) + rows * 2 + 1] = eight_bits(v[4][n], v[5][n], v[6][n], v[7][n], inverse);
+        }
+        __syncthreads();
+        const int line = threadIdx.x >> 1, half = threadIdx.x & 1;
+        if (cb * BLOCK8 + line < q.cols) {
+            const uint32_t *from = lines + line * (PITCH / 4) + half * 16;
+            uint4 *to = (uint4 *)(q.values + ((cb * BLOCK8 + line) * q.out_blocks + rb) * BLOCK8 + half * 64);
+#pragma unroll
+            for (int n = 0; n < 4; n++) to[n] = make_uint4(from[4 * n], from[4 * n + 1], from[4 * n + 2], from[4 * n + 3]);
         }
         __syncthreads();
     }
@@ -202,6 +303,16 @@ hipError_t launch_quantize_turned(const QuantArgs &q, int type, hipStream_t s)
     const dim3 grid((unsigned)q.out_blocks, (unsigned)(strips < 1024 ? strips : 1024));
     return with_type(type, [&](auto ty) {
         quantize_turned_kernel<decltype(ty)><<<grid, 256, 0, s>>>(q, rows_are_wide(q, type));
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_quantize_both(const QuantArgs &q, const asgd_blocks &rows, int type, hipStream_t s)
+{
+    const int64_t strips = blocks8(q.cols);
+    const dim3 grid((unsigned)q.out_blocks, (unsigned)(strips < 1024 ? strips : 1024));
+    return with_type(type, [&](auto ty) {
+        quantize_both_kernel<decltype(ty)><<<grid, 256, 0, s>>>(q, (uint8_t *)rows.values, rows.scales, rows.rows, blocks8(rows.cols), rows_are_wide(q, type));
         return hipGetLastError();
     });
 }

@@ -120,6 +120,24 @@ int asgd_block_quantize(const void *x, int type, int64_t rows, int64_t cols, int
     return done(turned ? launch_quantize_turned(q, type, s) : launch_quantize_rows(q, type, s));
 }
 
+int asgd_block_quantize_both(const void *x, int type, int64_t rows, int64_t cols, int64_t stride, const asgd_route_order *order,
+                             const float *weights, const asgd_blocks *out, const asgd_blocks *out_turned, void *hip_stream)
+{
+    if (!type_ok(type) || rows < 0 || !blocks_ok(out) || !blocks_ok(out_turned) || out->form != ASGD_BLOCKS_ROWS || out_turned->form != ASGD_BLOCKS_ROWS) return ASGD_EINVAL;
+    if (order && (!order_ok(order) || rows != order->T)) return ASGD_EINVAL;
+    if (weights && (!order || !aligned(weights, 4))) return ASGD_EINVAL;
+    if (rows == 0) return ASGD_OK;
+    if (!matrix_ok(x, type, rows, cols, stride)) return ASGD_EINVAL;
+    if (out->rows != (order ? order->T * order->k : rows) || out->cols != cols || out_turned->rows != cols || out_turned->cols != (order ? BLOCK8 * asgd_route_max_blocks(order->T, order->k, order->E) : rows))
+        return ASGD_EINVAL;
+    QuantArgs q = {};
+    q.x = x; q.rows = rows; q.cols = cols; q.stride = stride; q.count = 1; q.values = (uint8_t *)out_turned->values; q.scales = out_turned->scales;
+    q.out_rows = out_turned->rows; q.out_blocks = blocks8(out_turned->cols); q.weights = weights;
+    if (order) q.order = *order;
+    if (q.out_blocks > MOST_GROUPS) return ASGD_EINVAL;
+    return done(launch_quantize_both(q, *out, type, (hipStream_t)hip_stream));
+}
+
 int asgd_block_product(const asgd_blocks *a, const asgd_blocks *b, int mode, int exact, const asgd_route_order *order, void *out,
                        int type, int64_t stride, void *hip_stream)
 {

@@ -59,6 +59,7 @@ struct QuantArgs {
 };
 hipError_t launch_quantize_rows(const QuantArgs &q, int type, hipStream_t s);
 hipError_t launch_quantize_turned(const QuantArgs &q, int type, hipStream_t s);
+hipError_t launch_quantize_both(const QuantArgs &q, const asgd_blocks &rows, int type, hipStream_t s);
 hipError_t launch_quantize_squares(const QuantArgs &q, int type, bool turned, hipStream_t s);
 
 struct ProductArgs {

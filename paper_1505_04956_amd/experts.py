@@ -33,39 +33,44 @@ def _type(dtype):
     return code
 
 
-# (the same number as torch.cuda.current_stream().cuda_stream, without the 3 us that its objects take)
+# (the same numbers as torch.cuda.current_stream().cuda_stream and torch.cuda.current_device(), without the 3 us that their objects take)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _stream(t):
     if not t.is_cuda:
         raise ValueError("a tensor on the GPU is wanted; there is no CPU fallback")
     index = t.get_device()
-    if index != torch.cuda.current_device():
-        raise ValueError("the tensors are on %s, the current device is %d" % (t.device, torch.cuda.current_device()))
+    if index != _device():
+        raise ValueError("the tensors are on %s, the current device is %d" % (t.device, _device()))
     return _raw_stream(index)
 
 
 def _matrix(t, rows=None, cols=None, name="x"):
     """(type, rows, cols, stride) of a matrix whose rows are runs of consecutive elements."""
-    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+    shape = t.shape
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
         raise ValueError("%s: a matrix%s is wanted, not %s" % (name, "" if rows is None and cols is None else " [%s, %s]" % (
-            "..." if rows is None else rows, "..." if cols is None else cols), tuple(t.shape)))
-    r, c = t.shape
-    stride = t.stride(0) if r > 1 else c
-    if (c > 1 and t.stride(1) != 1) or stride < c:
+            "..." if rows is None else rows, "..." if cols is None else cols), tuple(shape)))
+    r, c = shape
+    stride, inner = t.stride()
+    if r <= 1:
+        stride = c
+    if (c > 1 and inner != 1) or stride < c:
         raise ValueError("%s: the elements of a row have to be consecutive and rows apart (strides %s)" % (name, t.stride()))
     return _type(t.dtype), r, c, stride
 
 
 def _same_device(first, *others):
+    index = first.get_device()                                      # (-1: the CPU)
     for t in others:
-        if t is not None and (t.get_device() != first.get_device() or t.is_cuda != first.is_cuda):
+        if t is not None and t.get_device() != index:
             raise ValueError("tensors on %s and %s" % (first.device, t.device))
 
 
 def _flat(t, shape, dtype, name):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s: a contiguous %s tensor %s is wanted, not %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
 
 
@@ -87,8 +92,8 @@ def route(logits, rule, bias=None):
     if bias is not None:
         _flat(bias, (E,), torch.float32, "bias")
     s = _stream(logits)
-    ids = torch.empty((T, rule.k), dtype=torch.int32, device=logits.device)
-    weights = torch.empty((T, rule.k), dtype=torch.float32, device=logits.device)
+    ids = logits.new_empty((T, rule.k), dtype=torch.int32)
+    weights = torch.empty_like(ids, dtype=torch.float32)
     B.asgd_route(logits.data_ptr(), type, T, E, stride, None if bias is None else bias.data_ptr(), rule._c, ids.data_ptr(),
                  weights.data_ptr(), s)
     return ids, weights
@@ -146,32 +151,76 @@ class Blocks:
     __slots__ = ("values", "scales", "rows", "cols", "count", "squares", "_c")
 
     def __init__(self, values, scales, cols, squares=True):
-        kb = -(-cols // BLOCK)
-        lead, rows = values.shape[:-2], values.shape[-2] if values.dim() >= 2 else -1
-        want = (*lead, -(-rows // BLOCK), kb) if squares else (kb, rows)
-        if values.element_size() != 1 or values.dim() not in ((2, 3) if squares else (2,)) or values.shape[-1] != kb * BLOCK or not values.is_contiguous():
-            raise ValueError("values: contiguous bytes [%srows, %d] are wanted, not %s %s" % ("experts, " if squares else "", kb * BLOCK, values.dtype, tuple(values.shape)))
-        _flat(scales, want, torch.float32, "scales")
+        kb, shape, dims = -(-cols // BLOCK), values.shape, values.dim()
+        if values.element_size() != 1 or not (dims == 2 or (squares and dims == 3)) or shape[-1] != kb * BLOCK or not values.is_contiguous():
+            raise ValueError("values: contiguous bytes [%srows, %d] are wanted, not %s %s" % ("experts, " if squares else "", kb * BLOCK, values.dtype, tuple(shape)))
+        rows, count = shape[-2], shape[0] if dims == 3 else 1
+        _flat(scales, (kb, rows) if not squares else (-(-rows // BLOCK), kb) if dims == 2 else (count, -(-rows // BLOCK), kb), torch.float32, "scales")
         _same_device(values, scales)
-        self.values, self.scales, self.rows, self.cols, self.squares = values, scales, rows, cols, squares
-        self.count = lead[0] if lead else 1
-        self._c = B.asgd_blocks(values.data_ptr(), scales.data_ptr(), rows, cols, B.BLOCKS_SQUARES if squares else B.BLOCKS_ROWS, self.count, 0, 0)
+        self.values, self.scales, self.rows, self.cols, self.squares, self.count = values, scales, rows, cols, squares, count
+        self._c = B.asgd_blocks(values.data_ptr(), scales.data_ptr(), rows, cols, B.BLOCKS_SQUARES if squares else B.BLOCKS_ROWS, count, 0, 0)
+
+
+def _sizes(x, turned, plan):
+    """(rows, cols, blocks) of x in 8 bits."""
+    rows, cols = x.shape
+    if turned:
+        out_rows, out_cols = cols, rows if plan is None else max(1, plan.max_blocks()) * BLOCK
+    else:
+        out_rows, out_cols = rows if plan is None else plan.T * plan.k, cols
+    return out_rows, out_cols, -(-out_cols // BLOCK)
+
+
+def _check_rows(x, plan, weights):
+    """_matrix() of what is brought to 8 bits."""
+    if weights is not None:
+        if plan is None:
+            raise ValueError("weights belong to the slots of a plan")
+        _flat(weights, (plan.T, plan.k), torch.float32, "weights")
+        _same_device(x, weights)
+    return _matrix(x, None if plan is None else plan.T)
+
+
+class _Rows:
+    """8-bit blocks of 1 x 128 that stay inside: one piece of memory, and the library's structure for it."""
+    __slots__ = ("memory", "rows", "cols", "_c")
+
+    def __init__(self, x, turned, plan):
+        self.rows, self.cols, kb = _sizes(x, turned, plan)
+        n = self.rows * kb * BLOCK
+        self.memory = torch.empty(n + 4 * kb * self.rows, dtype=torch.uint8, device=x.device)
+        at = self.memory.data_ptr()
+        self._c = B.asgd_blocks(at, at + n, self.rows, self.cols, B.BLOCKS_ROWS, 1, 0, 0)
+
+
+def _quantized(x, turned=False, plan=None, weights=None):
+    type, rows, cols, stride = _check_rows(x, plan, weights)
+    s = _stream(x)
+    out = _Rows(x, turned, plan)
+    if rows:
+        B.asgd_block_quantize(x.data_ptr(), type, rows, cols, stride, int(turned), None if plan is None else plan._c,
+                              None if weights is None else weights.data_ptr(), out._c, s)
+    return out
+
+
+def _quantized_both(x, plan=None, weights=None):
+    """(not turned, turned) from one reading of x."""
+    type, rows, cols, stride = _check_rows(x, plan, weights)
+    s = _stream(x)
+    out, turned = _Rows(x, False, plan), _Rows(x, True, plan)
+    if rows:
+        B.asgd_block_quantize_both(x.data_ptr(), type, rows, cols, stride, None if plan is None else plan._c,
+                                   None if weights is None else weights.data_ptr(), out._c, turned._c, s)
+    return out, turned
 
 
 def quantize(x, turned=False, plan=None, weights=None):
     """x [rows, cols] in 8-bit blocks of 1 x 128 (Blocks, squares=False), or with `turned` its transpose, blocks along x's rows.  With a
     plan x has a row for each of its T rows, and what is brought to 8 bits has one for each place: x's row of the place's slot, times the
     slot's weight (weights [T, k] float32) if given; turned, every expert's places begin a new block and the rest of its last one is zeros."""
-    type, rows, cols, stride = _matrix(x, None if plan is None else plan.T)
-    _same_device(x, weights)
-    if weights is not None:
-        if plan is None:
-            raise ValueError("weights belong to the slots of a plan")
-        _flat(weights, (plan.T, plan.k), torch.float32, "weights")
+    type, rows, cols, stride = _check_rows(x, plan, weights)
     s = _stream(x)
-    out_rows = cols if turned else rows if plan is None else plan.T * plan.k
-    out_cols = cols if not turned else rows if plan is None else max(1, plan.max_blocks()) * BLOCK
-    kb = -(-out_cols // BLOCK)
+    out_rows, out_cols, kb = _sizes(x, turned, plan)
     out = Blocks(torch.empty((out_rows, kb * BLOCK), dtype=torch.float8_e4m3fn, device=x.device),
                  torch.empty((kb, out_rows), dtype=torch.float32, device=x.device), out_cols, squares=False)
     if rows:
@@ -199,32 +248,41 @@ def _exact(dtype, exact):
     return int(dtype == torch.float32 if exact is None else exact)
 
 
+def _product(a, b, dtype, plan, mode, exact, device):
+    rows = a.rows if plan is None else plan.T * plan.k
+    type, s = _type(dtype), _raw_stream(device.index)
+    if a.cols == 0 and b.cols == 0:                                  # (a sum over nothing)
+        return torch.zeros((rows, b.rows), dtype=dtype, device=device)
+    out = torch.empty((rows, b.rows), dtype=dtype, device=device)
+    if rows:
+        B.asgd_block_product(a._c, b._c, mode, _exact(dtype, exact), None if plan is None else plan._c, out.data_ptr(), type, b.rows, s)
+    return out
+
+
+def _product_over(a, b, plan, dtype, exact, device):
+    shape = (plan.E, a.rows, b.rows)
+    if plan.T == 0:
+        return torch.zeros(shape, dtype=dtype, device=device)
+    out = torch.empty(shape, dtype=dtype, device=device)
+    B.asgd_block_product(a._c, b._c, B.PRODUCT_OVER, _exact(dtype, exact), plan._c, out.data_ptr(), _type(dtype), b.rows, _raw_stream(device.index))
+    return out
+
+
 def product(a, b, dtype, plan=None, gather=False, exact=None):
     """a b^T in `dtype` of two Blocks of the same cols.  With a plan b has a matrix for each expert, and row p of the result is that of
     the place p with the matrix of its expert: a has a row for each place, or with `gather` one for each of the plan's T rows.  Rows at
     places that are not in use are left as they were allocated.  exact: the products of a block are summed in 32 bits, at half the rate,
     and not by the 8-bit matrix instruction, whose sums are off by 1.5e-5 to 7e-5 of the result (None: for float32 results)."""
     _same_device(a.values, b.values)
-    type, s = _type(dtype), _stream(a.values)
-    rows = a.rows if plan is None else plan.T * plan.k
-    if a.cols == 0 and b.cols == 0:                                  # (a sum over nothing)
-        return torch.zeros((rows, b.rows), dtype=dtype, device=a.values.device)
-    out = torch.empty((rows, b.rows), dtype=dtype, device=a.values.device)
-    mode = B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER if gather else B.PRODUCT_PLACES
-    if rows:
-        B.asgd_block_product(a._c, b._c, mode, _exact(dtype, exact), None if plan is None else plan._c, out.data_ptr(), type, b.rows, s)
-    return out
+    _stream(a.values)
+    return _product(a, b, dtype, plan, B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER if gather else B.PRODUCT_PLACES, exact, a.values.device)
 
 
 def product_over(a, b, plan, dtype=torch.float32, exact=None):
     """[E, a.rows, b.rows]: for each expert a b^T over its own places alone; a and b are quantize(..., turned=True, plan=plan)."""
     _same_device(a.values, b.values)
-    type, s = _type(dtype), _stream(a.values)
-    if plan.T == 0:
-        return torch.zeros((plan.E, a.rows, b.rows), dtype=dtype, device=a.values.device)
-    out = torch.empty((plan.E, a.rows, b.rows), dtype=dtype, device=a.values.device)
-    B.asgd_block_product(a._c, b._c, B.PRODUCT_OVER, _exact(dtype, exact), plan._c, out.data_ptr(), type, b.rows, s)
-    return out
+    _stream(a.values)
+    return _product_over(a, b, plan, dtype, exact, a.values.device)
 
 
 def _raw(x):
@@ -236,14 +294,14 @@ def _raw(x):
 def _product_of(x, w, dtype, plan=None, exact=None):
     """x, one row for each of the plan's T, times w."""
     rows = x.shape[0] if plan is None else plan.T * plan.k
-    # (few rows of an expert: bringing them to 8 bits again in each strip of its weights takes less than another launch)
-    raw = 0 < rows <= B.PRODUCT_RAW_ROWS if plan is None else 0 < rows <= min(B.PRODUCT_RAW_SLOTS, 16 * plan.E)
-    if not raw:
-        return product(quantize(x), w, dtype, plan=plan, gather=plan is not None, exact=exact)
+    mode = B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER
     _same_device(x, w.values)
+    s = _stream(x)
+    # (few rows of an expert: bringing them to 8 bits again in each strip of its weights takes less than another launch)
+    if not 0 < rows <= (B.PRODUCT_RAW_ROWS if plan is None else min(B.PRODUCT_RAW_SLOTS, 16 * plan.E)):
+        return _product(_quantized(x), w, dtype, plan, mode, exact, x.device)
     out = torch.empty((rows, w.rows), dtype=dtype, device=x.device)
-    B.asgd_block_product(_raw(x), w._c, B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER, _exact(dtype, exact), None if plan is None else plan._c,
-                         out.data_ptr(), _type(dtype), w.rows, _stream(x))
+    B.asgd_block_product(_raw(x), w._c, mode, _exact(dtype, exact), None if plan is None else plan._c, out.data_ptr(), _type(dtype), w.rows, s)
     return out
 
 
@@ -282,8 +340,11 @@ def linear(x, w, train=False):
     """x [rows, K] times w^T, in x's type: x is brought to 8 bits on the way, w is quantize_weights() of [N, K].  train: (the result, what
     linear_backward() needs)."""
     _check_weights(x, w)
-    y = _product_of(x, w, x.dtype)
-    return (y, quantize(x, turned=True)) if train else y
+    if not train:
+        return _product_of(x, w, x.dtype)
+    _same_device(x, w.values)
+    rows, turned = _quantized_both(x)
+    return _product(rows, w, x.dtype, None, B.PRODUCT_ALL, None, x.device), turned
 
 
 def linear_backward(d_out, kept, w_turned):
@@ -291,8 +352,10 @@ def linear_backward(d_out, kept, w_turned):
     _check_weights(d_out, w_turned)
     if d_out.shape[0] != kept.cols or w_turned.rows != kept.rows:
         raise ValueError("d_out %s and the kept x [%d, %d] do not belong together" % (tuple(d_out.shape), kept.cols, kept.rows))
-    d_x = _product_of(d_out, w_turned, d_out.dtype)
-    return d_x, product(quantize(d_out, turned=True), kept, torch.float32)
+    _same_device(d_out, w_turned.values, kept.memory)
+    rows, turned = _quantized_both(d_out)
+    return (_product(rows, w_turned, d_out.dtype, None, B.PRODUCT_ALL, None, d_out.device),
+            _product(turned, kept, torch.float32, None, B.PRODUCT_ALL, None, d_out.device))
 
 
 class Kept:
@@ -308,29 +371,35 @@ def experts(x, ids, weights, w, train=False):
     them.  w is quantize_weights() of [E, N, K].  train: (the result, what experts_backward() needs)."""
     _check_weights(x, w, experts=True)
     _same_device(x, ids, weights, w.values)
-    if ids.dim() != 2 or ids.shape[0] != x.shape[0]:
-        raise ValueError("ids: [%d, k] is wanted, not %s" % (x.shape[0], tuple(ids.shape)))
+    T = x.shape[0]
+    if ids.dim() != 2 or ids.shape[0] != T:
+        raise ValueError("ids: [%d, k] is wanted, not %s" % (T, tuple(ids.shape)))
+    _flat(ids, ids.shape, torch.int32, "ids")
     _flat(weights, ids.shape, torch.float32, "weights")
-    if not train and 0 < x.shape[0] <= B.PRODUCT_RAW_ROWS and ids.numel() * w.rows * w.cols <= DIRECT_BYTES:
-        _flat(ids, ids.shape, torch.int32, "ids")
-        out = torch.empty((x.shape[0], w.rows), dtype=x.dtype, device=x.device)
-        B.asgd_experts_direct(_raw(x), ids.data_ptr(), weights.data_ptr(), ids.shape[1], w._c, int(x.dtype == torch.float32), out.data_ptr(),
-                              _type(x.dtype), w.rows, _stream(x))
+    if not train and 0 < T <= B.PRODUCT_RAW_ROWS and ids.numel() * w.rows * w.cols <= DIRECT_BYTES:
+        s = _stream(x)
+        out = torch.empty((T, w.rows), dtype=x.dtype, device=x.device)
+        B.asgd_experts_direct(_raw(x), ids.data_ptr(), weights.data_ptr(), ids.shape[1], w._c, int(x.dtype is torch.float32), out.data_ptr(),
+                              _type(x.dtype), w.rows, s)
         return out
     order = plan(ids, w.count)
     # 32-bit until the sum: one rounding to the result's type.  Beside a rounding to 16 bits the error of the 8-bit instruction does not
     # show; the gradient of the weights is 32-bit, and y goes into it
     y = _product_of(x, w, torch.float32, order, exact=train or x.dtype == torch.float32)
     out = experts_sum(y, order, x.dtype, weights)
-    return (out, Kept(order, weights, y, quantize(x, turned=True, plan=order))) if train else out
+    return (out, Kept(order, weights, y, _quantized(x, turned=True, plan=order))) if train else out
 
 
 def experts_backward(d_out, kept, w_turned):
     """(d_x [T, K] in d_out's type, d_w [E, N, K] float32, d_weights [T, k] float32) of experts(), from d_out [T, N]."""
     _check_weights(d_out, w_turned, experts=True)
-    order = kept.plan
+    order, x_turned = kept.plan, kept.x_turned
+    if d_out.shape[0] != order.T or w_turned.rows != x_turned.rows or w_turned.count != order.E:
+        raise ValueError("d_out %s and weights of %d experts [%d, %d] do not belong to what was kept" % (
+            tuple(d_out.shape), w_turned.count, w_turned.rows, w_turned.cols))
+    _same_device(d_out, w_turned.values, kept.y)
     d_weights = experts_sum_backward(d_out, kept.y, order)
-    rows = product(quantize(d_out, plan=order, weights=kept.weights), w_turned, torch.float32, plan=order, exact=d_out.dtype == torch.float32)
-    d_x = experts_sum(rows, order, d_out.dtype)
-    d_w = product_over(quantize(d_out, turned=True, plan=order, weights=kept.weights), kept.x_turned, order)
-    return d_x, d_w, d_weights
+    rows, turned = _quantized_both(d_out, order, kept.weights)
+    d_rows = _product(rows, w_turned, torch.float32, order, B.PRODUCT_PLACES, d_out.dtype == torch.float32, d_out.device)
+    d_x = experts_sum(d_rows, order, d_out.dtype)
+    return d_x, _product_over(turned, x_turned, order, torch.float32, True, d_out.device), d_weights

@@ -52,6 +52,19 @@ def test_to_eight_bits(X, rows, cols, dtype):
     assert same_bits(got.values, q) and same_scales(got.scales, s)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 128), (5, 129), (128, 64), (130, 257), (257, 200)])
+def test_both_ways_at_once(X, rows, cols, dtype):
+    """What a training step takes of a matrix: the rows' and the transpose's blocks, as they are one by one."""
+    base = data(rows, cols + 24, rows, dtype).cuda()
+    for x in (base[:, :cols], base[:, :cols].contiguous()):
+        a, b = X._quantized_both(x)
+        for got, want in ((a, X.quantize(x)), (b, X.quantize(x, turned=True))):
+            n = want.values.numel()
+            assert torch.equal(got.memory[:n], want.values.view(torch.uint8).reshape(-1))
+            assert torch.equal(got.memory[n:].view(torch.float32), want.scales.reshape(-1))
+
+
 def test_turned_squares_are_the_same_numbers(X):
     w = data(3 * 200, 300, 2).view(3, 200, 300)
     a, b = X.quantize_weights(w.cuda()), X.quantize_weights(w.cuda(), turned=True)

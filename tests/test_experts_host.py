@@ -89,6 +89,15 @@ def test_bringing_to_eight_bits_that_is_refused():
     assert quantize(blocks(rows=200, cols=128), turned=1, o=o) == B.EINVAL               # 3 blocks
 
 
+def test_both_ways_that_are_refused():
+    def go(out=None, turned=None, x=P, type=1, rows=8, cols=200, stride=200, o=None, weights=None):
+        out, turned = out or blocks(), turned or blocks(rows=200, cols=8)
+        return B.lib().asgd_block_quantize_both(x, type, rows, cols, stride, None if o is None else C.addressof(o), weights, C.addressof(out), C.addressof(turned), None)
+    for over in (dict(out=blocks(rows=9)), dict(out=blocks(form=B.BLOCKS_SQUARES)), dict(turned=blocks(rows=200, cols=9)), dict(turned=blocks(rows=199, cols=8)),
+                 dict(turned=blocks(rows=200, cols=8, values=None)), dict(x=None), dict(type=7), dict(rows=-1), dict(stride=199), dict(weights=P), dict(o=order(T=8, k=2, E=3))):
+        assert go(**over) == B.EINVAL
+
+
 def product(a, b, mode=B.PRODUCT_ALL, exact=0, o=None, out=P, type=0, stride=8):
     return B.lib().asgd_block_product(C.addressof(a), C.addressof(b), mode, exact, None if o is None else C.addressof(o), out, type, stride, None)
 
