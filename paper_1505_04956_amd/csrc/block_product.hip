@@ -267,51 +267,72 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_kernel(P
     int at_a = (wave_tok + (lane & 15)) * BLOCK8 + low, at_w = (TOK + wave_wt + (lane & 15)) * BLOCK8 + low;
     int at_sa = S::VALUES + (wave_tok + (lane & 15)) * 4, at_sb = S::SCALES_B + (SQUARES ? wave_wt / BLOCK8 * 256 + lane * 4 : wave_wt * 4 + (lane >> 4) * 16);
     asm volatile("" : "+v"(at_a), "+v"(at_w), "+v"(at_sa), "+v"(at_sb));
+    struct Raw { v4i u, v; };
     const auto operand = [&](const uint8_t *stage, int at, int rows) {
-        Operand<EXACT> o;
-        o.set(*(const v4i *)(stage + at + rows * BLOCK8), *(const v4i *)(stage + (at ^ 64) + rows * BLOCK8));
-        return o;
+        return Raw{*(const v4i *)(stage + at + rows * BLOCK8), *(const v4i *)(stage + (at ^ 64) + rows * BLOCK8)};
     };
     // multiplies the block in `stage` and brings block `next` to `other`
     const auto multiply = [&](const uint8_t *stage, int next, uint8_t *other, auto bringing) {
         constexpr bool BRING = decltype(bringing)::value;
         constexpr int LAG = 2, N = I * J, PER = (LOADS + LOADING - 1) / LOADING;
         float s[J];
-        Operand<EXACT> a[J], w, after;
+        Operand<EXACT> a[J], w;
+        Raw raw[J], after = operand(stage, at_w, 0);              // (converted where it is used: not to wait for it where it is read)
         v4f part[LAG + 1], sb[2];
-        w = operand(stage, at_w, 0);
 #pragma unroll
         for (int j = 0; j < J; j++) {
-            a[j] = operand(stage, at_a, j * 16);
+            raw[j] = operand(stage, at_a, j * 16);
             s[j] = *(const float *)(stage + at_sa + j * 64);
         }
+#pragma unroll
+        for (int j = 0; j < J; j++) a[j].set(raw[j].u, raw[j].v);
         if (SQUARES) {
             const float of_b = *(const float *)(stage + at_sb);
 #pragma unroll
             for (int j = 0; j < J; j++) s[j] *= of_b;
         }
+        const auto row = [&](int i) {                             // begins sixteen rows of b
+            w.set(after.u, after.v);
+            if (i + 1 < I) after = operand(stage, at_w, (i + 1) * 16);
+            if (!SQUARES) sb[i & 1] = *(const v4f *)(stage + at_sb + i * 64);
+            if (BRING && i < LOADING)
 #pragma unroll
-        for (int q = 0; q < N + LAG; q++) {
-            if (q < N) {
-                const int i = q / J, j = q % J;
-                if (j == 0) {
-                    if (i > 0) w = after;
-                    if (i + 1 < I) after = operand(stage, at_w, (i + 1) * 16);
-                    if (!SQUARES) sb[i & 1] = *(const v4f *)(stage + at_sb + i * 64);
-                    if (BRING && i < LOADING)
+                for (int l = i * PER; l < (i + 1) * PER && l < LOADS; l++) bring(next, other, l);
+        };
+        if constexpr (EXACT) {
+            // a quarter of a block for all J, then the next: each instruction adds to what the one J before it gives; one sum of the rows before beside each
+            v4f parts[2][J];
 #pragma unroll
-                        for (int l = i * PER; l < (i + 1) * PER && l < LOADS; l++) bring(next, other, l);
+            for (int q = 0; q < (I + 1) * 4 * J; q++) {
+                const int i = q / (4 * J), n = q / J % 4, j = q % J;
+                if (i < I) {
+                    if (q % (4 * J) == 0) row(i);
+                    const v4f zero = {0.0f, 0.0f, 0.0f, 0.0f};
+                    parts[i & 1][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.v[n], a[j].v[n], n == 0 ? zero : parts[i & 1][j], 0, 0, 0);
                 }
-                part[q % (LAG + 1)] = block_product(w, a[j]);
+                if (i > 0) {
+                    const float got = parts[(i - 1) & 1][j][n];
+                    sum[i - 1][j][n] = fmaf(SQUARES ? got : got * sb[(i - 1) & 1][n], s[j], sum[i - 1][j][n]);
+                    if (n == 3) asm volatile("" : "+v"(sum[i - 1][j]));     // (here, and not after the next barrier)
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if (q >= LAG) {
-                const int i = (q - LAG) / J, j = (q - LAG) % J;
-                const v4f got = part[(q - LAG) % (LAG + 1)];
+        } else {
 #pragma unroll
-                for (int n = 0; n < 4; n++) sum[i][j][n] = fmaf(SQUARES ? got[n] : got[n] * sb[i & 1][n], s[j], sum[i][j][n]);
-                asm volatile("" : "+v"(sum[i][j]));               // (here, and not after the next barrier)
+            for (int q = 0; q < N + LAG; q++) {
+                if (q < N) {
+                    if (q % J == 0) row(q / J);
+                    part[q % (LAG + 1)] = block_product(w, a[q % J]);
+                }
+                if (q >= LAG) {
+                    const int i = (q - LAG) / J, j = (q - LAG) % J;
+                    const v4f got = part[(q - LAG) % (LAG + 1)];
+#pragma unroll
+                    for (int n = 0; n < 4; n++) sum[i][j][n] = fmaf(SQUARES ? got[n] : got[n] * sb[i & 1][n], s[j], sum[i][j][n]);
+                    asm volatile("" : "+v"(sum[i][j]));
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
