@@ -97,21 +97,27 @@ template <int PATTERN, int ROWS = 0xF> __device__ __forceinline__ float from_lan
 }
 constexpr int XOR1 = 0xB1, XOR2 = 0x4E, MIRROR8 = 0x141, MIRROR16 = 0x140, LANE15 = 0x142, LANE31 = 0x143;
 
-// over sixteen lanes, in all of them (each step joins two halves that hold one value each, so a mirror does for an exchange)
-__device__ __forceinline__ float row_max(float v)
+// a pattern that leaves no lane out
+template <int PATTERN> __device__ __forceinline__ float across(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), PATTERN, 0xF, 0xF, true)); }
+template <int PATTERN> __device__ __forceinline__ int across(int v) { return __builtin_amdgcn_mov_dpp(v, PATTERN, 0xF, 0xF, true); }
+
+// a number as an integer of the same order (minus zero before zero), and back
+__device__ __forceinline__ int as_integer(float v) { return __float_as_int(v) ^ (__float_as_int(v) >> 31 & 0x7FFFFFFF); }
+__device__ __forceinline__ float as_number(int v) { return __int_as_float(v ^ (v >> 31 & 0x7FFFFFFF)); }
+
+// The largest, in all lanes (each step joins two halves that hold one value each, so a mirror does for an exchange).  Of integers a
+// step is one instruction; of floats it would be four, since operands that may be signalling are made quiet first.
+__device__ __forceinline__ int wave_max(int v)
 {
-    v = fmaxf(v, from_lane<XOR1>(v, v));
-    v = fmaxf(v, from_lane<XOR2>(v, v));
-    v = fmaxf(v, from_lane<MIRROR8>(v, v));
-    return fmaxf(v, from_lane<MIRROR16>(v, v));
+    v = max(v, across<XOR1>(v));
+    v = max(v, across<XOR2>(v));
+    v = max(v, across<MIRROR8>(v));
+    v = max(v, across<MIRROR16>(v));
+    v = max(v, __builtin_amdgcn_update_dpp((int)0x80000000, v, LANE15, 0xA, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp((int)0x80000000, v, LANE31, 0xC, 0xF, false));
+    return __builtin_amdgcn_readlane(v, 63);
 }
-__device__ __forceinline__ float wave_max(float v)
-{
-    v = row_max(v);
-    v = fmaxf(v, from_lane<LANE15, 0xA>(v, v));
-    v = fmaxf(v, from_lane<LANE31, 0xC>(v, v));
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
-}
+__device__ __forceinline__ float wave_max(float v) { return as_number(wave_max(as_integer(v))); }
 __device__ __forceinline__ float wave_sum(float v)
 {
     v += from_lane<XOR1>(0.0f, v);

@@ -47,7 +47,7 @@ __device__ __forceinline__ bool logits_of(const Lane<Ty, V> &r, const float (&bi
 #pragma unroll
     for (int i = 0; i < V; i++) {
         l[i] = lane * V + i < E && bias[i] != OUT ? (float)r.v[i] : OUT;
-        if (l[i] != OUT && (l[i] != l[i] || bias[i] != bias[i])) bad = true;
+        bad |= (l[i] != l[i]) | ((l[i] != OUT) & (bias[i] != bias[i]));
     }
     return __any(bad);
 }
@@ -63,11 +63,11 @@ __device__ __forceinline__ float sigmoid(float l) { return 1.0f / (1.0f + expf(-
 // an order among numbers: what is not one comes last of those that are in
 __device__ __forceinline__ float as_key(float v) { return v == v ? v : -3.402823466e38f; }
 
-template <int V> __device__ __forceinline__ float lane_best(const float (&v)[V])
+template <class T, int V> __device__ __forceinline__ T lane_best(const T (&v)[V])
 {
-    float m = v[0];
+    T m = v[0];
 #pragma unroll
-    for (int i = 1; i < V; i++) m = fmaxf(m, v[i]);
+    for (int i = 1; i < V; i++) m = max(m, v[i]);
     return m;
 }
 
@@ -78,7 +78,7 @@ __device__ __forceinline__ void join_best(float &m1, float &m2, float o1, float 
     m1 = fmaxf(m1, o1);
 }
 
-template <class Ty, int V> __device__ __forceinline__ void route_row(const RouteArgs &a, int64_t t, int lane, const Lane<Ty, V> &raw, const float (&bias)[V])
+template <class Ty, int V, bool SORTED> __device__ __forceinline__ void route_row(const RouteArgs &a, int64_t t, int lane, const Lane<Ty, V> &raw, const float (&bias)[V])
 {
     const typename Ty::T *row = (const typename Ty::T *)a.logits + t * a.stride;
     const int E = a.E, k = a.rule.k;
@@ -93,28 +93,38 @@ template <class Ty, int V> __device__ __forceinline__ void route_row(const Route
         for (int i = 0; i < V; i++) sum += l[i] == OUT ? 0.0f : expf(l[i] - top);
         total = wave_sum(sum);
     }
-    const auto score = [&](float v) { return v == OUT ? 0.0f : soft ? expf(v - top) / total : sigmoid(v); };
+    const bool two = a.rule.groups > 1 && a.rule.group_by == ASGD_GROUP_BEST_TWO;
+    float score[V];
+    if (a.bias || two) {
+        if (soft)
+#pragma unroll
+            for (int i = 0; i < V; i++) score[i] = expf(l[i] - top) / total;
+        else
+#pragma unroll
+            for (int i = 0; i < V; i++) score[i] = sigmoid(l[i]);
+#pragma unroll
+        for (int i = 0; i < V; i++) score[i] = l[i] == OUT ? OUT : as_key(score[i] + bias[i]);       // (no bias: plus zero)
+    }
     if (a.bias) {
 #pragma unroll
-        for (int i = 0; i < V; i++) key[i] = l[i] == OUT ? OUT : as_key(score(l[i]) + bias[i]);
+        for (int i = 0; i < V; i++) key[i] = score[i];
     } else {
 #pragma unroll
         for (int i = 0; i < V; i++) key[i] = as_key(l[i]);
     }
     if (a.rule.groups > 1) {
         const int G = a.rule.groups, width = E / G, lanes = width / V;
-        const bool two = a.rule.group_by == ASGD_GROUP_BEST_TWO;
-        const auto by = [&](int i) { return two && !a.bias ? (l[i] == OUT ? OUT : as_key(score(l[i]))) : key[i]; };
+        const auto by = [&](int i) { return two ? score[i] : key[i]; };
         unsigned long long stays = 0;
         if (lanes * V == width && lanes <= 16 && (lanes & (lanes - 1)) == 0) {
             // a group is 1, 2, .. 16 whole lanes next to each other: all groups at once
             float m1 = OUT, m2 = OUT;
 #pragma unroll
             for (int i = 0; i < V; i++) join_best(m1, m2, by(i), OUT);
-            if (lanes > 1) join_best(m1, m2, from_lane<XOR1>(m1, m1), from_lane<XOR1>(m2, m2));
-            if (lanes > 2) join_best(m1, m2, from_lane<XOR2>(m1, m1), from_lane<XOR2>(m2, m2));
-            if (lanes > 4) join_best(m1, m2, from_lane<MIRROR8>(m1, m1), from_lane<MIRROR8>(m2, m2));
-            if (lanes > 8) join_best(m1, m2, from_lane<MIRROR16>(m1, m1), from_lane<MIRROR16>(m2, m2));
+            if (lanes > 1) join_best(m1, m2, across<XOR1>(m1), across<XOR1>(m2));
+            if (lanes > 2) join_best(m1, m2, across<XOR2>(m1), across<XOR2>(m2));
+            if (lanes > 4) join_best(m1, m2, across<MIRROR8>(m1), across<MIRROR8>(m2));
+            if (lanes > 8) join_best(m1, m2, across<MIRROR16>(m1), across<MIRROR16>(m2));
             const float mine = two ? as_key(m1 + m2) : m1;
             const int g = lane / lanes;
             int before = 0;                                                   // groups that are taken before the lane's
@@ -160,26 +170,64 @@ template <class Ty, int V> __device__ __forceinline__ void route_row(const Route
         }
     }
     int id = -1;                                                              // lane j: choice j
+    const int none = as_integer(OUT);
+    int order[V];
+#pragma unroll
+    for (int i = 0; i < V; i++) order[i] = as_integer(key[i] + 0.0f);
+    // SORTED: a lane's experts are put in order first (largest key first, of equal ones the lower index): its first is then all that can be
+    // chosen next, and the lane that it is chosen from gives it up.  Else a choice is looked for among all V again.
+    uint64_t places = 0;                                                      // four bits each, in that order
+    if constexpr (SORTED) {
+        int at[V];
+#pragma unroll
+        for (int i = 0; i < V; i++) at[i] = i;
+#pragma unroll
+        for (int i = 1; i < V; i++)
+#pragma unroll
+            for (int n = i; n > 0; n--) {
+                const bool swap = order[n] > order[n - 1];
+                const int u = order[n], w = order[n - 1];
+                const int p = at[n], q = at[n - 1];
+                order[n] = swap ? w : u;
+                order[n - 1] = swap ? u : w;
+                at[n] = swap ? q : p;
+                at[n - 1] = swap ? p : q;
+            }
+#pragma unroll
+        for (int i = 0; i < V; i++) places |= (uint64_t)at[i] << 4 * i;
+    }
     for (int j = 0; j < k; j++) {
-        const float m = lane_best(key), best = wave_max(m);
-        if (best == OUT) break;
+        const int m = SORTED ? order[0] : lane_best(order), best = wave_max(m);
+        if (best == none) break;
         const int owner = __ffsll((long long)__ballot(m == best)) - 1;
-        unsigned places = 0;
-#pragma unroll
-        for (int i = 0; i < V; i++) places |= (unsigned)(__ballot(key[i] == best) >> owner & 1) << i;
-        const int place = __ffs(places) - 1;
         const bool mine = lane == owner;
+        int place;
+        if constexpr (SORTED) {
+            place = __builtin_amdgcn_readlane((int)(uint32_t)places, owner) & 15;
 #pragma unroll
-        for (int i = 0; i < V; i++)
-            if (mine && i == place) key[i] = OUT;
+            for (int i = 0; i < V; i++) {
+                const int now = order[i], then = i + 1 < V ? order[i + 1 < V ? i + 1 : i] : none;
+                order[i] = mine ? then : now;
+            }
+            places = mine ? places >> 4 : places;
+        } else {
+            unsigned has = 0;
+#pragma unroll
+            for (int i = 0; i < V; i++) has |= (unsigned)(__ballot(order[i] == best) >> owner & 1) << i;
+            place = __ffs(has) - 1;
+#pragma unroll
+            for (int i = 0; i < V; i++)
+                if (mine && i == place) order[i] = none;
+        }
         if (lane == j) id = owner * V + place;
     }
     const float chosen = id >= 0 ? (float)row[id] : OUT;
     float share;
-    const float largest = wave_max(chosen);                                   // (by all lanes: not inside a branch)
-    if (soft && a.rule.renormalize) share = chosen == OUT ? 0.0f : expf(chosen - largest);
-    else share = score(chosen);
-    if (id < 0) share = 0.0f;
+    if (soft && a.rule.renormalize) {                                         // (all lanes or none)
+        const float largest = wave_max(chosen);
+        share = expf(chosen - largest);
+    } else share = soft ? expf(chosen - top) / total : sigmoid(chosen);
+    if (chosen == OUT) share = 0.0f;
     if (a.rule.renormalize) {
         const float sum = wave_sum(share);
         share = sum > 0.0f ? share / sum : sum == 0.0f ? 0.0f : sum;
@@ -190,7 +238,7 @@ template <class Ty, int V> __device__ __forceinline__ void route_row(const Route
     }
 }
 
-template <class Ty, int V> __global__ __launch_bounds__(256) void route_kernel(RouteArgs a, bool wide)
+template <class Ty, int V, bool SORTED> __global__ __launch_bounds__(256) void route_kernel(RouteArgs a, bool wide)
 {
     const int lane = threadIdx.x & 63;
     const int64_t step = (int64_t)gridDim.x * 4;
@@ -203,7 +251,7 @@ template <class Ty, int V> __global__ __launch_bounds__(256) void route_kernel(R
     for (; t < a.T; t += step) {
         const Lane<Ty, V> now = next;
         if (t + step < a.T) next = load_lane<Ty, V>(logits + (t + step) * a.stride, lane * V, a.E, wide);
-        route_row<Ty, V>(a, t, lane, now, bias);
+        route_row<Ty, V, SORTED>(a, t, lane, now, bias);
     }
 }
 
@@ -484,12 +532,25 @@ template <class F> hipError_t with_width(int E, F f)
 // four waves a workgroup, eight workgroups a compute unit; a wave's next row is on its way while it works on one
 static unsigned route_grid(int64_t T) { return (unsigned)((T + 3) / 4 < 2048 ? (T + 3) / 4 : 2048); }
 
+// In order or not, us of float32 softmax over 65536 rows (512: 32768, 1024: 16384) for 1, 2, 4, 8 choices:
+//    64   16.4 18.0 21.9 29.6   not   16.9 18.8 23.2 32.4
+//   128   19.4 21.4 26.1 35.2   not   19.4 22.2 28.1 39.9
+//   256   23.7 26.1 30.8 41.0   not   22.7 26.7 35.1 53.7
+//   512   25.3 26.9 30.1 36.5   not   19.3 22.3 29.5 45.2
+//  1024   25.5 26.7 29.3 33.8   not   22.1 25.8 33.5 48.7
 hipError_t launch_route(const RouteArgs &a, int type, hipStream_t s)
 {
     const unsigned grid = route_grid(a.T);
     return with_type(type, [&](auto ty) {
         return with_width(a.E, [&](auto v) {
-            route_kernel<decltype(ty), decltype(v)::value><<<grid, 256, 0, s>>>(a, rows_of_lanes<decltype(ty), decltype(v)::value>(a.logits, a.stride, a.E));
+            constexpr int V = decltype(v)::value;
+            const bool wide = rows_of_lanes<decltype(ty), V>(a.logits, a.stride, a.E);
+            if constexpr (V >= 8)
+                if (a.rule.k < 4) {
+                    route_kernel<decltype(ty), V, false><<<grid, 256, 0, s>>>(a, wide);
+                    return hipGetLastError();
+                }
+            route_kernel<decltype(ty), V, true><<<grid, 256, 0, s>>>(a, wide);
             return hipGetLastError();
         });
     });

@@ -36,7 +36,8 @@ def weight_bound(E):
 
 
 SHAPES = [(1, 1, 1, 1, 1), (1, 64, 6, 1, 1), (3, 7, 7, 1, 1), (65, 65, 4, 5, 2), (130, 160, 6, 8, 3), (33, 256, 8, 8, 4), (9, 500, 12, 4, 4),
-          (5, 1000, 32, 1, 1), (4, 1024, 64, 64, 64), (6, 1024, 9, 64, 1), (17, 128, 2, 64, 1), (2, 72, 40, 3, 2)]
+          (5, 1000, 32, 1, 1), (4, 1024, 64, 64, 64), (6, 1024, 9, 64, 1), (17, 128, 2, 64, 1), (2, 72, 40, 3, 2),
+          (9, 1000, 3, 10, 2), (7, 512, 2, 1, 1)]
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
