@@ -185,14 +185,15 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_kernel(P
 
     // which tile: strips of eight tiles of a, all tiles of b for each.  (The host knows how many tiles experts can have at most; shared among
     // the dies are those that they have.)
-    const bool grouped = p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES;
-    if (grouped && TOK == BLOCK8) tiles_tok = p.order.blocks[p.order.E];
-    const uint32_t all = grouped && TOK == BLOCK8 ? tiles_tok * tiles_wt : gridDim.x;
+    const bool grouped = SQUARES && TOK == BLOCK8 && (p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES);
+    const bool over = !SQUARES && TOK == BLOCK8 && p.mode == ASGD_PRODUCT_OVER;
+    if (grouped) tiles_tok = p.order.blocks[p.order.E];
+    const uint32_t all = grouped ? tiles_tok * tiles_wt : gridDim.x;
     if (blockIdx.x >= all) return;
     const uint32_t id = tile_of_group(blockIdx.x, all);
     uint32_t within = id;
     int64_t matrix = 0;
-    if (p.mode == ASGD_PRODUCT_OVER) {
+    if (over) {
         matrix = id / (tiles_tok * tiles_wt);
         within = id - (uint32_t)matrix * tiles_tok * tiles_wt;
     }
@@ -204,16 +205,16 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_kernel(P
     const int64_t first_wt = (int64_t)tile_wt * WT;
     if (grouped) {
         int e;
-        if (!(TOK == BLOCK8 ? block_of_expert(p.order, tile_tok, e, first, end) : tile_of_expert(p.order, tile_tok, TOK, e, first, end))) return;
+        if (!block_of_expert(p.order, tile_tok, e, first, end)) return;
         matrix = e;
-    } else if (p.mode == ASGD_PRODUCT_OVER) {
+    } else if (over) {
         k0 = p.order.blocks[matrix];
         k1 = p.order.blocks[matrix + 1];
     }
-    const int64_t row_bytes = p.kb * BLOCK8, b_matrix = p.mode == ASGD_PRODUCT_OVER ? 0 : matrix * p.rows_b;
+    const int64_t row_bytes = p.kb * BLOCK8, b_matrix = over ? 0 : matrix * p.rows_b;
     const auto row_of_a = [&](int64_t r) {                        // (rows beyond the last: the last again)
         r = r < end ? r : end - 1;
-        return p.mode == ASGD_PRODUCT_GATHER ? (int64_t)(p.order.slots[r] / p.order.k) : r;
+        return grouped && p.mode == ASGD_PRODUCT_GATHER ? (int64_t)(p.order.slots[r] / p.order.k) : r;
     };
     const auto row_of_b = [&](int64_t r) { return r < p.rows_b ? r : p.rows_b - 1; };
 
@@ -372,7 +373,7 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_kernel(P
     // Out through the LDS, sixteen rows of a at a time: there a lane has four neighbours of a row, in memory whole lines are wanted.
     typedef typename Out::T T;
     constexpr int ROW = I * 16 * sizeof(T), PITCH = ROW + 16, PER_ROW = ROW / 16, ROWS = 64 / PER_ROW;       // bytes; lanes of a row, rows of an instruction
-    T *out = (T *)p.out + (p.mode == ASGD_PRODUCT_OVER ? matrix * p.rows_a * p.stride : 0);
+    T *out = (T *)p.out + (over ? matrix * p.rows_a * p.stride : 0);
     __syncthreads();
     constexpr int HALF = (WAVES + 1) / 2;
     static_assert(HALF * 16 * PITCH <= S::BYTES, "");
@@ -651,7 +652,8 @@ hipError_t launch_product(const ProductArgs &p, bool squares, int type, hipStrea
             // few rows (of an expert, on average)
             const int64_t each = grouped ? rows / E : rows;
             if (!over && each <= 32) return each <= 16 ? few(One<1>(), sq, exact) : few(One<2>(), sq, exact);
-            if (grouped && (double)p.rows_a * p.kb * BLOCK8 >= 4294967296.0) return tiles(One<128>(), One<128>(), One<2>(), One<2>(), One<2>(), sq, exact, yes);
+            if constexpr (decltype(sq)::value)
+                if (grouped && (double)p.rows_a * p.kb * BLOCK8 >= 4294967296.0) return tiles(One<128>(), One<128>(), One<2>(), One<2>(), One<2>(), sq, exact, yes);
             if (!grouped && !over) {
                 const double t64 = tiles_time(tiles_of(64) * ((p.rows_b + 63) / 64), 0.31, 0.223), t128 = tiles_time(tiles_of(128) * ((p.rows_b + 127) / 128), 0.66, 0.63);
                 if (t64 < t128) return tiles(One<64>(), One<64>(), One<2>(), One<2>(), One<4>(), sq, exact, no);

@@ -169,7 +169,7 @@ int asgd_block_product(const asgd_blocks *a, const asgd_blocks *b, int mode, int
         p.stride_raw = a->stride;
         return done(launch_product_raw(p, a->type, type, s));
     }
-    if ((double)blocks8(out_rows + (order ? (int64_t)BLOCK8 * order->E : 0)) * (mode == ASGD_PRODUCT_OVER ? order->E : 1) * blocks8(b->rows) > (double)MOST_GROUPS) return ASGD_EINVAL;
+    if ((double)blocks8(out_rows + (order ? (int64_t)BLOCK8 * order->E : 0)) * (mode == ASGD_PRODUCT_OVER ? order->E : 1) * blocks8(b->rows) > (double)(MOST_GROUPS / 2)) return ASGD_EINVAL;      // (of 128 x 128: where thin, twice as many of 64 x 64)
     return done(launch_product(p, b->form == ASGD_BLOCKS_SQUARES, type, s));
 }
 
