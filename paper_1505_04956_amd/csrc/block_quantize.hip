@@ -246,25 +246,34 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_both_kernel(
     }
 }
 
-// Squares: a workgroup of 256 takes one, in two passes over its 128 x 128 elements (the second from the caches).  Rows of the
-// result beyond out_rows do not exist; columns beyond the data are zeros.
-template <class Ty> __global__ __launch_bounds__(256) void quantize_squares_kernel(QuantArgs q, bool turned)
+// Squares: a workgroup of 256 takes one, a thread eight neighbouring columns of eight rows, which stay in registers until the largest of all is
+// known.  The transposed square goes through the LDS to be written as whole lines.  Rows of the result beyond out_rows do not exist; columns
+// beyond the data are zeros.
+template <class Ty, bool TURNED> __global__ __launch_bounds__(256) void quantize_squares_kernel(QuantArgs q, bool wide)
 {
     typedef typename Ty::T T;
+    constexpr int PITCH = BLOCK8 + 4;
     __shared__ uint32_t tops[4];
+    __shared__ uint32_t lines[TURNED ? BLOCK8 * PITCH / 4 : 1];
+    const int part = threadIdx.x & 15, rows = threadIdx.x >> 4;
     const int64_t nb = blocks8(q.out_rows), kb = q.out_blocks, square = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
     if (square >= nb * kb * q.count) return;
     const int64_t m = square / (nb * kb), ib = square / kb % nb, jb = square % kb;
     const T *x = (const T *)q.x + m * q.rows * q.stride;
-    const auto at = [&](int i, int j) {
-        const int64_t r = ib * BLOCK8 + i, c = jb * BLOCK8 + j, xr = turned ? c : r, xc = turned ? r : c;
-        return xr < q.rows && xc < q.cols ? (float)x[xr * q.stride + xc] : 0.0f;
-    };
-    uint32_t top = 0;
-    for (int n = threadIdx.x; n < BLOCK8 * BLOCK8; n += 256) {
-        const int u = n >> 7, v = n & 127;                       // v: along x's rows, so that neighbours read neighbours
-        top = max(top, magnitude_bits(turned ? at(v, u) : at(u, v)));
+    const int64_t r0 = (TURNED ? jb : ib) * BLOCK8 + rows * 8, c = (TURNED ? ib : jb) * BLOCK8 + part * 8;
+    float v[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        if (r0 + i < q.rows) load8<Ty>(x + (r0 + i) * q.stride + c, q.cols - c, wide, v[i]);
+        else
+#pragma unroll
+            for (int n = 0; n < 8; n++) v[i][n] = 0.0f;
     }
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+#pragma unroll
+        for (int n = 0; n < 8; n++) top = max(top, magnitude_bits(v[i][n]));
 #pragma unroll
     for (int s = 32; s; s >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, s));
     if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
@@ -272,13 +281,32 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_squares_kern
     top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
     float scale, inverse;
     block_scale(top, scale, inverse);
-    for (int n = threadIdx.x; n < BLOCK8 * BLOCK8 / 4; n += 256) {
-        const int i = turned ? n & 127 : n >> 5, j = (turned ? n >> 7 : n & 31) * 4;
-        if (ib * BLOCK8 + i < q.out_rows)
-            *(uint32_t *)(q.values + ((m * q.out_rows + ib * BLOCK8 + i) * kb + jb) * BLOCK8 + j) =
-                eight_bits(at(i, j), at(i, j + 1), at(i, j + 2), at(i, j + 3), inverse);
-    }
     if (threadIdx.x == 0) q.scales[square] = scale;
+    uint8_t *out = q.values + (m * q.out_rows * kb + jb) * BLOCK8;
+    if constexpr (TURNED) {
+#pragma unroll
+        for (int n = 0; n < 8; n++) {
+            lines[(part * 8 + n) * (PITCH / 4) + rows * 2] = eight_bits(v[0][n], v[1][n], v[2][n], v[3][n], inverse);
+            lines[(part * 8 + n) * (PITCH / 4) + rows * 2 + 1] = eight_bits(v[4][n], v[5][n], v[6][n], v[7][n], inverse);
+        }
+        __syncthreads();
+        const int line = threadIdx.x >> 1, half = threadIdx.x & 1;
+        if (ib * BLOCK8 + line < q.out_rows) {
+            const uint32_t *from = lines + line * (PITCH / 4) + half * 16;
+            uint4 *to = (uint4 *)(out + (ib * BLOCK8 + line) * kb * BLOCK8 + half * 64);
+#pragma unroll
+            for (int n = 0; n < 4; n++) to[n] = make_uint4(from[4 * n], from[4 * n + 1], from[4 * n + 2], from[4 * n + 3]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (r0 + i < q.out_rows) {
+                uint2 o;
+                o.x = eight_bits(v[i][0], v[i][1], v[i][2], v[i][3], inverse);
+                o.y = eight_bits(v[i][4], v[i][5], v[i][6], v[i][7], inverse);
+                *(uint2 *)(out + (r0 + i) * kb * BLOCK8 + part * 8) = o;
+            }
+    }
 }
 
 bool rows_are_wide(const QuantArgs &q, int type)
@@ -322,7 +350,9 @@ hipError_t launch_quantize_squares(const QuantArgs &q, int type, bool turned, hi
     const int64_t squares = blocks8(q.out_rows) * q.out_blocks * q.count, across = squares < (1 << 16) ? squares : (1 << 16);
     const dim3 grid((unsigned)across, (unsigned)((squares + across - 1) / across));
     return with_type(type, [&](auto ty) {
-        quantize_squares_kernel<decltype(ty)><<<grid, 256, 0, s>>>(q, turned);
+        const bool wide = rows_are_wide(q, type);
+        if (turned) quantize_squares_kernel<decltype(ty), true><<<grid, 256, 0, s>>>(q, wide);
+        else quantize_squares_kernel<decltype(ty), false><<<grid, 256, 0, s>>>(q, wide);
         return hipGetLastError();
     });
 }
