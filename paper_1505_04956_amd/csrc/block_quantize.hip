@@ -1,5 +1,7 @@
-// To 8 bits in blocks of 128: rows, the transpose's rows, squares.  All three read x once and write a byte an element, so memory
-// bounds them; the largest magnitude of a block is found among the lanes that hold it.
+// To 8 bits in blocks of 128: rows, the transpose's rows, both, squares.  With m the largest magnitude of a block (at least 1e-30) its scale is
+// m / 448 and an element v becomes e4m3(v * 448 / m), each factor rounded once.  All read x once and write a byte an element (both: two), so memory
+// bounds them; the largest magnitude of a block is found among the lanes that hold it.  8192 x 8192 in bfloat16: rows 39 us (5.2 TB/s),
+// transpose 38 (5.3), both 65 (4.1), squares 34 (5.9), transposed 43 (4.7).  (A large copy reaches 4.7; part of x stays in the last cache.)
 #include "experts_internal.h"
 
 namespace asgd {
@@ -49,8 +51,7 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_rows_kernel(
             if (q.weights) v[i] *= w;
             top = max(top, magnitude_bits(v[i]));
         }
-#pragma unroll
-        for (int m = 8; m; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+        top = (uint32_t)row_max((int)top);
         float scale, inverse;
         block_scale(top, scale, inverse);
         uint2 o;
@@ -74,7 +75,8 @@ __device__ __forceinline__ int expert_of_block(const asgd_route_order &o, int64_
 
 // The transpose: a workgroup takes 128 rows of x (a block of the result) and 64 columns (rows of the result).  A thread has eight
 // neighbouring columns of four rows, so that loads are wide; it gives four neighbours of each of eight rows of the result, which go
-// through the LDS to be written as whole lines.
+// through the LDS to be written as whole lines.  (Two bytes a load, 8192 rows of 1024
+// at 32768 places: 52 us; so, 24.)
 template <class Ty> __global__ __launch_bounds__(256) void quantize_turned_kernel(QuantArgs q, bool wide)
 {
     typedef typename Ty::T T;
@@ -150,13 +152,13 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_turned_kerne
     }
 }
 
-// Both at once, for training: the rows (of places) and the transpose, from one reading of x.  A workgroup takes a square of 128 x 128, a
-// thread eight neighbouring columns of eight rows: sixteen lanes hold a row's block, sixteen threads of different waves a column's.
-template <class Ty> __global__ __launch_bounds__(256) void quantize_both_kernel(QuantArgs q, uint8_t *rows_values, float *rows_scales, int64_t rows_out, int64_t rows_blocks, bool wide)
+// Both at once, for training: the rows (of places) and the transpose, from one reading of x.  (8192 x 8192: 65 us, one after the other 39 and 38; with eight
+// rows a thread, and half the waves, 78.)  A workgroup takes a square of 128 x 128, a thread eight neighbouring columns of four rows: sixteen lanes hold a row's block, 32 threads of different waves a column's.
+template <class Ty> __global__ __launch_bounds__(512) void quantize_both_kernel(QuantArgs q, uint8_t *rows_values, float *rows_scales, int64_t rows_out, int64_t rows_blocks, bool wide)
 {
     typedef typename Ty::T T;
     constexpr int PITCH = BLOCK8 + 4;
-    __shared__ __align__(16) uint32_t tops[16][BLOCK8];
+    __shared__ __align__(16) uint32_t tops[32][BLOCK8];
     __shared__ uint32_t lines[BLOCK8 * PITCH / 4];
     __shared__ int64_t source[BLOCK8], target[BLOCK8];
     __shared__ float factor[BLOCK8];
@@ -182,19 +184,19 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_both_kernel(
     __syncthreads();
     for (int64_t cb = blockIdx.y; cb * BLOCK8 < q.cols; cb += gridDim.y) {
         const int64_t c = cb * BLOCK8 + part * 8;
-        float v[8][8];
+        float v[4][8];
         uint32_t top[8] = {};
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const int64_t r = source[rows * 8 + i];
+        for (int i = 0; i < 4; i++) {
+            const int64_t r = source[rows * 4 + i];
             if (r >= 0) load8<Ty>((const T *)q.x + r * q.stride + c, q.cols - c, wide, v[i]);
             else
 #pragma unroll
                 for (int n = 0; n < 8; n++) v[i][n] = 0.0f;
         }
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const int row = rows * 8 + i;
+        for (int i = 0; i < 4; i++) {
+            const int row = rows * 4 + i;
             uint32_t mine = 0;
 #pragma unroll
             for (int n = 0; n < 8; n++) {
@@ -203,8 +205,7 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_both_kernel(
                 top[n] = max(top[n], m);
                 mine = max(mine, m);
             }
-#pragma unroll
-            for (int m = 8; m; m >>= 1) mine = max(mine, (uint32_t)__shfl_xor((int)mine, m));
+            mine = (uint32_t)row_max((int)mine);
             float scale, inverse;
             block_scale(mine, scale, inverse);
             if (source[row] >= 0) {
@@ -221,7 +222,7 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_both_kernel(
         if (threadIdx.x < BLOCK8) {
             uint32_t m = 0;
 #pragma unroll
-            for (int n = 0; n < 16; n++) m = max(m, tops[n][threadIdx.x]);
+            for (int n = 0; n < 32; n++) m = max(m, tops[n][threadIdx.x]);
             float scale, inverse;
             block_scale(m, scale, inverse);
             if (cb * BLOCK8 + threadIdx.x < q.cols) q.scales[rb * q.out_rows + cb * BLOCK8 + threadIdx.x] = scale;
@@ -229,25 +230,23 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_both_kernel(
         }
         __syncthreads();
 #pragma unroll
-        for (int n = 0; n < 8; n++) {
-            const float inverse = __uint_as_float(tops[0][part * 8 + n]);
-            lines[(part * 8 + n) * (PITCH / 4) + rows * 2] = eight_bits(v[0][n], v[1][n], v[2][n], v[3][n], inverse);
-            lines[(part * 8 + n) * (PITCH / 4) + rows * 2 + 1] = eight_bits(v[4][n], v[5][n], v[6][n], v[7][n], inverse);
-        }
+        for (int n = 0; n < 8; n++)
+            lines[(part * 8 + n) * (PITCH / 4) + rows] = eight_bits(v[0][n], v[1][n], v[2][n], v[3][n], __uint_as_float(tops[0][part * 8 + n]));
         __syncthreads();
-        const int line = threadIdx.x >> 1, half = threadIdx.x & 1;
+        const int line = threadIdx.x >> 2, quarter = threadIdx.x & 3;
         if (cb * BLOCK8 + line < q.cols) {
-            const uint32_t *from = lines + line * (PITCH / 4) + half * 16;
-            uint4 *to = (uint4 *)(q.values + ((cb * BLOCK8 + line) * q.out_blocks + rb) * BLOCK8 + half * 64);
+            const uint32_t *from = lines + line * (PITCH / 4) + quarter * 8;
+            uint4 *to = (uint4 *)(q.values + ((cb * BLOCK8 + line) * q.out_blocks + rb) * BLOCK8 + quarter * 32);
 #pragma unroll
-            for (int n = 0; n < 4; n++) to[n] = make_uint4(from[4 * n], from[4 * n + 1], from[4 * n + 2], from[4 * n + 3]);
+            for (int n = 0; n < 2; n++) to[n] = make_uint4(from[4 * n], from[4 * n + 1], from[4 * n + 2], from[4 * n + 3]);
         }
         __syncthreads();
     }
 }
 
 // Squares: a workgroup of 256 takes one, a thread eight neighbouring columns of eight rows, which stay in registers until the largest of all is
-// known.  The transposed square goes through the LDS to be written as whole lines.  Rows of the result beyond out_rows do not exist; columns
+// known.  (Read twice, the second time from the caches, an element a load: 116 us and transposed 184 for 8192 x 8192, where this takes 34 and 43.)
+// The transposed square goes through the LDS to be written as whole lines.  Rows of the result beyond out_rows do not exist; columns
 // beyond the data are zeros.
 template <class Ty, bool TURNED> __global__ __launch_bounds__(256) void quantize_squares_kernel(QuantArgs q, bool wide)
 {
@@ -274,8 +273,7 @@ template <class Ty, bool TURNED> __global__ __launch_bounds__(256) void quantize
     for (int i = 0; i < 8; i++)
 #pragma unroll
         for (int n = 0; n < 8; n++) top = max(top, magnitude_bits(v[i][n]));
-#pragma unroll
-    for (int s = 32; s; s >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, s));
+    top = (uint32_t)wave_max((int)top);
     if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
     __syncthreads();
     top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
@@ -340,7 +338,7 @@ hipError_t launch_quantize_both(const QuantArgs &q, const asgd_blocks &rows, int
     const int64_t strips = blocks8(q.cols);
     const dim3 grid((unsigned)q.out_blocks, (unsigned)(strips < 1024 ? strips : 1024));
     return with_type(type, [&](auto ty) {
-        quantize_both_kernel<decltype(ty)><<<grid, 256, 0, s>>>(q, (uint8_t *)rows.values, rows.scales, rows.rows, blocks8(rows.cols), rows_are_wide(q, type));
+        quantize_both_kernel<decltype(ty)><<<grid, 512, 0, s>>>(q, (uint8_t *)rows.values, rows.scales, rows.rows, blocks8(rows.cols), rows_are_wide(q, type));
         return hipGetLastError();
     });
 }

@@ -107,12 +107,16 @@ __device__ __forceinline__ float as_number(int v) { return __int_as_float(v ^ (v
 
 // The largest, in all lanes (each step joins two halves that hold one value each, so a mirror does for an exchange).  Of integers a
 // step is one instruction; of floats it would be four, since operands that may be signalling are made quiet first.
-__device__ __forceinline__ int wave_max(int v)
+__device__ __forceinline__ int row_max(int v)                     // over sixteen lanes
 {
     v = max(v, across<XOR1>(v));
     v = max(v, across<XOR2>(v));
     v = max(v, across<MIRROR8>(v));
-    v = max(v, across<MIRROR16>(v));
+    return max(v, across<MIRROR16>(v));
+}
+__device__ __forceinline__ int wave_max(int v)
+{
+    v = row_max(v);
     v = max(v, __builtin_amdgcn_update_dpp((int)0x80000000, v, LANE15, 0xA, 0xF, false));
     v = max(v, __builtin_amdgcn_update_dpp((int)0x80000000, v, LANE31, 0xC, 0xF, false));
     return __builtin_amdgcn_readlane(v, 63);

@@ -1,4 +1,5 @@
-// The weighted sum of a row's experts and the gradient of its weights: both read every row of y once.
+// The weighted sum of a row's experts, out[t] = sum_j w[t, j] y[place(t, j)], and the gradient of its weights, dw[t, j] = d_out[t] . y[place(t, j)]:
+// both read every row of y once, in 32 bits, and memory bounds them.  4096 rows of four experts, 2048 columns: 33 us, 4.6 TB/s, and 31 us, 4.9 TB/s.
 #include "experts_internal.h"
 
 namespace asgd {
