@@ -1,5 +1,5 @@
-// Products of matrices in 8-bit blocks on the matrix cores (v_mfma_f32_16x16x128_f8f6f4: one instruction is one block of
-// the contraction).  out^T = b a^T is what is formed: rows of b are the instruction's rows, rows of a its columns, so that a
+// Products of matrices in 8-bit blocks, out[m, n] = sum over blocks kb of sa[kb, m] sb[kb, n] sum over the block's 128 k of a[m, k] b[n, k], on the
+// matrix cores (v_mfma_f32_16x16x128_f8f6f4: one instruction is one block of the contraction); sums and scales are 32-bit.  out^T = b a^T is what is formed: rows of b are the instruction's rows, rows of a its columns, so that a
 // lane holds four neighbours of one row of out, and the scale of its row of a is one number a lane.
 //
 // The order of the 128 bytes of a block among the lanes is free as long as both operands have the same: lane l holds the
@@ -102,27 +102,23 @@ template <class T> __device__ __forceinline__ void store16(T *p, int64_t left, b
 __device__ __forceinline__ bool tile_of_expert(const asgd_route_order &o, int64_t tile, int rows, int &expert, int64_t &first, int64_t &end)
 {
     const int lane = threadIdx.x & 63;
-    int64_t before = 0;
+    int before = 0, begin = o.offsets[min(lane, o.E)], stop = o.offsets[min(lane + 1, o.E)];
     for (int e0 = 0; e0 < o.E; e0 += 64) {
-        const int e = e0 + lane;
-        const int begin = e < o.E ? o.offsets[e] : 0, stop = e < o.E ? o.offsets[e + 1] : 0;
-        const int tiles = (stop - begin + rows - 1) / rows;
-        int sum = tiles;
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const int u = __shfl_up(sum, m);
-            if (lane >= m) sum += u;
+        const int from = begin, to = stop;
+        if (e0 + 64 < o.E) {                                      // (the next are on their way meanwhile)
+            begin = o.offsets[min(e0 + 64 + lane, o.E)];
+            stop = o.offsets[min(e0 + 65 + lane, o.E)];
         }
-        const unsigned long long past = __ballot(before + sum > tile);
+        const int tiles = (int)((unsigned)(to - from + rows - 1) / (unsigned)rows), sum = wave_scan(tiles);
+        const unsigned long long past = __ballot(before + sum > (int)tile);
         if (past) {
-            const int at = __ffsll((long long)past) - 1;
-            expert = __builtin_amdgcn_readfirstlane(e0 + at);
-            const int mine = __shfl(begin, at), last = __shfl(stop, at), done = __shfl(sum - tiles, at);
-            first = __builtin_amdgcn_readfirstlane((int)(mine + (tile - before - done) * rows));
-            end = __builtin_amdgcn_readfirstlane(last);
+            const int at = __ffsll((long long)past) - 1, done = before + __builtin_amdgcn_readlane(sum - tiles, at);
+            expert = e0 + at;
+            first = __builtin_amdgcn_readlane(from, at) + ((int)tile - done) * rows;
+            end = __builtin_amdgcn_readlane(to, at);
             return true;
         }
-        before += __shfl(sum, 63);
+        before += __builtin_amdgcn_readlane(sum, 63);
     }
     return false;
 }
@@ -153,6 +149,11 @@ __device__ __forceinline__ uint32_t tile_of_group(uint32_t id, uint32_t n)
     return die * share + (die < rest ? die : rest) + at;
 }
 
+// Many rows.  8192^3 to bfloat16: 455 to 475 us, 2.3 to 2.4 PFLOP/s, where the power that the card may draw holds its clock at 1.6 to 1.8 GHz (a
+// library product with one scale for all reaches 2.65).  With 32-bit sums (EXACT) 8192^3 takes 940 us, 1.17 PFLOP/s; 65536 x 1024 x 128 to float32, 64 us:
+// its 302 MB at what a large copy reaches.  4096 rows of four of 64 experts, 2048 x 2048: 180 us, 0.76 PFLOP/s at 2.4 GHz, where a wave waits for data of the
+// LDS or of the other waves half of the time: experts' last tiles are part empty, and sixteen blocks are soon over.
+//
 // A tile of TOK rows of a and WT rows of b; the waves are TOK_WAVES x WT_WAVES, each with I x J pieces of 16 x 16.  Blocks of the
 // contraction of both, and their scales, go straight to one of two stages in the LDS; 16-byte pieces of a row lie at their
 // number xor the row's low bits, so that the lanes of a read spread over the banks.
@@ -405,7 +406,8 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_kernel(P
 // What counts is that the weights arrive: they go from memory to registers, sixteen rows of one block of 128 a wave and
 // instruction, and the eight waves of a workgroup share the blocks of the contraction of sixteen rows of b, four of them on
 // their way at a time.  Rows of a, J times sixteen, come from the caches; RAW ones are brought to 8 bits in the registers of
-// the lanes that need them (up to sixteen of them: there this is less than a launch costs).
+// the lanes that need them (up to sixteen of them: there this is less than a launch costs).  One row times 4096 x 4096: 9.0 us, 1.9
+// TB/s; 120 rows of 100 experts, 33 of which have rows, 1000 x 1100: 17 us, 2.2 TB/s.  The weights' way from memory bounds it, one round of loads a wave at few strips.
 constexpr int FEW_WAVES = 8;
 
 // a lane's 32 elements of a block of a row: fetched early, brought to 8 bits when they are there
@@ -547,7 +549,8 @@ template <class In, int J, int STRIPS, bool SQUARES, bool EXACT, class Out> __gl
 
 // A row's experts without an order, for few rows: a workgroup takes sixteen rows of b of every expert of one row of a (blockIdx.y), and
 // adds what they give times its weights.  A block of the row is brought to 8 bits once for all of them; the weights of up to
-// EXPERTS of them are on their way at a time.
+// EXPERTS of them are on their way at a time.  Six experts of 2048 x 2048: 9.8 us, 2.6 TB/s.  Sixteen waves, since a round of loads then
+// is all that each has of 2048 columns, and its latency is what counts (eight: 10.4).
 constexpr int DIRECT_WAVES = 16;
 
 template <class In, bool EXACT, class Out> __global__ __launch_bounds__(64 * DIRECT_WAVES) void product_direct_kernel(ProductArgs p, const int32_t *ids, const float *weights, int k, int E, bool wide_in, bool wide)
