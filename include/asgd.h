@@ -404,7 +404,7 @@ int asgd_block_quantize_both(const void *x, int type, int64_t rows, int64_t cols
  *   ASGD_PRODUCT_OVER     a and b (ROWS) are turned quantisations over the same order: out (E x a.rows x b.rows, matrices
  *                         a.rows * stride apart) = for each expert the product over its own places alone, zeros without any
  * a RAW: at most ASGD_PRODUCT_RAW_ROWS rows (ALL) or ASGD_PRODUCT_RAW_SLOTS slots (GATHER), and b SQUARES.  A matrix in 8-bit
- * blocks has at most 2^30 rows.
+ * blocks has at most 2^30 rows and 2^24 columns, b at most 2^24 rows, out at most 2^22 tiles of 128 x 128.
  */
 enum { ASGD_PRODUCT_ALL = 0, ASGD_PRODUCT_GATHER = 1, ASGD_PRODUCT_PLACES = 2, ASGD_PRODUCT_OVER = 3 };
 enum { ASGD_PRODUCT_RAW_ROWS = 16, ASGD_PRODUCT_RAW_SLOTS = 4096 };
