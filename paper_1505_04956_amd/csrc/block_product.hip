@@ -83,14 +83,16 @@ template <class Ty> __device__ __forceinline__ void store_four(typename Ty::T *p
     }
 }
 
-// sixteen bytes of a row, of which `left` elements exist; wide: rows begin at a multiple of 16 bytes
-template <class T> __device__ __forceinline__ void store16(T *p, int64_t left, bool wide, uint4 v)
+// sixteen bytes of a row, of which `left` elements exist; wide: rows begin at a multiple of 16 bytes.  They pass by the second cache, whose
+// place belongs to the operands (65536 x 1024 x 128 to float32, bringing a to 8 bits included: 61 us; kept there, 71; the sum of experts that
+// reads 129 MB of them next loses nothing by it)
+template <class T> __device__ __forceinline__ void store16(T *p, int64_t left, bool wide, v4i v)
 {
     constexpr int N = 16 / sizeof(T);
-    if (wide && left >= N) *(uint4 *)p = v;
+    if (wide && left >= N) __builtin_nontemporal_store(v, (v4i *)p);
     else {
         T u[N];
-        *(uint4 *)u = v;
+        *(v4i *)u = v;
 #pragma unroll
         for (int i = 0; i < N; i++)
             if (i < left) p[i] = u[i];
@@ -149,9 +151,9 @@ __device__ __forceinline__ uint32_t tile_of_group(uint32_t id, uint32_t n)
     return die * share + (die < rest ? die : rest) + at;
 }
 
-// Many rows.  8192^3 to bfloat16: 455 to 475 us, 2.3 to 2.4 PFLOP/s, where the power that the card may draw holds its clock at 1.6 to 1.8 GHz (a
-// library product with one scale for all reaches 2.65).  With 32-bit sums (EXACT) 8192^3 takes 940 us, 1.17 PFLOP/s; 65536 x 1024 x 128 to float32, 64 us:
-// its 302 MB at what a large copy reaches.  4096 rows of four of 64 experts, 2048 x 2048: 180 us, 0.76 PFLOP/s at 2.4 GHz, where a wave waits for data of the
+// Many rows.  8192^3 to bfloat16: 453 us, 2.4 PFLOP/s, where the power that the card may draw holds its clock at 1.6 to 1.8 GHz (a
+// library product with one scale for all reaches 2.65).  With 32-bit sums (EXACT) 8192^3 takes 898 us, 1.22 PFLOP/s; 65536 x 1024 x 128 to float32 is
+// bound by memory, its 277 MB.  4096 rows of four of 64 experts, 2048 x 2048: 159 us, 0.86 PFLOP/s at 2.4 GHz, where a wave waits for data of the
 // LDS or of the other waves half of the time: experts' last tiles are part empty, and sixteen blocks are soon over.
 //
 // A tile of TOK rows of a and WT rows of b; the waves are TOK_WAVES x WT_WAVES, each with I x J pieces of 16 x 16.  Blocks of the
@@ -394,7 +396,7 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_kernel(P
         for (int n = 0; n < 16 / ROWS; n++) {
             const int row = n * ROWS + lane / PER_ROW, at = lane % PER_ROW * 16;
             const int64_t r = first + wave_tok + j * 16 + row, c = first_wt + wave_wt + at / sizeof(T);
-            const uint4 v = *(const uint4 *)(mine + row * PITCH + at);
+            const v4i v = *(const v4i *)(mine + row * PITCH + at);
             if (r < end) store16<T>(out + r * p.stride + c, p.rows_b - c, wide, v);
         }
         __builtin_amdgcn_wave_barrier();

@@ -1,7 +1,7 @@
 // To 8 bits in blocks of 128: rows, the transpose's rows, both, squares.  With m the largest magnitude of a block (at least 1e-30) its scale is
 // m * (1 / 448) and an element v becomes e4m3(v * (448 * (1 / m))), every operation rounded.  All read x once and write a byte an element (both: two), so memory
-// bounds them; the largest magnitude of a block is found among the lanes that hold it.  8192 x 8192 in bfloat16: rows 39 us (5.2 TB/s),
-// transpose 38 (5.3), both 65 (4.1), squares 34 (5.9), transposed 43 (4.7).  (A large copy reaches 4.7; part of x stays in the last cache.)
+// bounds them; the largest magnitude of a block is found among the lanes that hold it.  8192 x 8192 in bfloat16: rows 38 us (5.3 TB/s),
+// transpose 38 (5.3), both 64 (4.2), squares 34 (5.9), transposed 42 (4.8).  (A large copy reaches 4.7; part of x stays in the last cache.)
 #include "experts_internal.h"
 
 namespace asgd {
