@@ -619,9 +619,10 @@ template <class In, bool EXACT, class Out> __global__ __launch_bounds__(64 * DIR
 static int64_t most_tiles(int64_t slots, int64_t E, int rows) { return slots / rows + (slots < E ? slots : E); }
 
 // Which tile: us of a block of the contraction for n tiles on 256 compute units, from what one tile takes with a unit to itself and what each takes where
-// there are many.  Measured (8-bit instruction, squares): 64 x 64 0.31 and 0.223 (8192^3: 916 us), 128 x 128 0.66 and 0.63 (645 us), 256 x 256
-// 2.1 (539 us).  At 777 x 1001 x 1152: 5.4, 9.5 and 18.8 us; 256 x 4096 x 4096: 10.9, 22, 48; 2048^3: 17.5, 15.7, 29; 4096 x 4096 x 2048: 66, 42, 38.  Sums in
-// 32 bits take about twice as long in each, and have no 256 x 256 (registers).
+// there are many, the writing of results included (8-bit instruction, squares): 64 x 64 0.31 and 0.223, 128 x 128 0.66 and 0.63, 256 x 256 2.1.  What
+// each takes, and so what the rule decides between, in that order: 777 x 1001 x 1152 7.2, 11.4, 29.4 us; 256 x 4096 x 4096 11.1, 21.6, 46.4; 2048^3
+// 17.6, 14.7, 28.0; 4096 x 4096 x 2048 67, 46.5, 41.4; 8192^3 821, 542, 453.  Sums in 32 bits take about twice as long in each, and have no
+// 256 x 256 (registers).
 static double tiles_time(int64_t n, double alone, double among) { return n <= 256 ? alone : alone > (double)((n + 255) / 256) * among ? alone : (double)((n + 255) / 256) * among; }
 
 // Four strips a workgroup (its rows of a, its place among the experts and its end are then there once for four) where that leaves more than a workgroup for
