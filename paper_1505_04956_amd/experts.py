@@ -245,7 +245,9 @@ def quantize_weights(w, turned=False):
 
 
 def _exact(dtype, exact):
-    return int(dtype == torch.float32 if exact is None else exact)
+    """Beside a rounding to bfloat16 what the 8-bit instruction drops does not show (4096^3: an error of 1.6602e-3 for 1.6599e-3, in half the
+    time); beside one to float16 it does (2.096e-4 for 2.075e-4)."""
+    return int(dtype != torch.bfloat16 if exact is None else exact)
 
 
 def _product(a, b, dtype, plan, mode, exact, device):
@@ -271,8 +273,9 @@ def _product_over(a, b, plan, dtype, exact, device):
 def product(a, b, dtype, plan=None, gather=False, exact=None):
     """a b^T in `dtype` of two Blocks of the same cols.  With a plan b has a matrix for each expert, and row p of the result is that of
     the place p with the matrix of its expert: a has a row for each place, or with `gather` one for each of the plan's T rows.  Rows at
-    places that are not in use are left as they were allocated.  exact: the products of a block are summed in 32 bits, at half the rate,
-    and not by the 8-bit matrix instruction, whose sums are off by 1.5e-5 to 7e-5 of the result (None: for float32 results)."""
+    places that are not in use are left as they were allocated.  exact: the products of a block are summed in 32 bits, at half the rate, and
+    not by the 8-bit matrix instruction, whose sums are off by some 2e-5 to 1e-4 of the result, more where large products cancel (None: in 32
+    bits, but for bfloat16 results)."""
     _same_device(a.values, b.values)
     _stream(a.values)
     return _product(a, b, dtype, plan, B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER if gather else B.PRODUCT_PLACES, exact, a.values.device)
@@ -336,26 +339,27 @@ def _check_weights(x, w, experts=False):
         raise ValueError("x: [rows, %d] is wanted, not %s" % (w.cols, tuple(x.shape)))
 
 
-def linear(x, w, train=False):
+def linear(x, w, train=False, exact=None):
     """x [rows, K] times w^T, in x's type: x is brought to 8 bits on the way, w is quantize_weights() of [N, K].  train: (the result, what
-    linear_backward() needs)."""
+    linear_backward() needs); the result is the same.  exact: as in product()."""
     _check_weights(x, w)
     if not train:
-        return _product_of(x, w, x.dtype)
+        return _product_of(x, w, x.dtype, exact=exact)
     _same_device(x, w.values)
     rows, turned = _quantized_both(x)
-    return _product(rows, w, x.dtype, None, B.PRODUCT_ALL, None, x.device), turned
+    return _product(rows, w, x.dtype, None, B.PRODUCT_ALL, exact, x.device), turned
 
 
-def linear_backward(d_out, kept, w_turned):
-    """(d_x, in d_out's type, and d_w [N, K] float32) of linear(): from d_out [rows, N], what it kept, and the turned weights."""
+def linear_backward(d_out, kept, w_turned, exact=None):
+    """(d_x, in d_out's type, and d_w [N, K] float32) of linear(): from d_out [rows, N], what it kept, and the turned weights.  exact, as in
+    product(), is for d_x; d_w is summed in 32 bits."""
     _check_weights(d_out, w_turned)
     if d_out.shape[0] != kept.cols or w_turned.rows != kept.rows:
         raise ValueError("d_out %s and the kept x [%d, %d] do not belong together" % (tuple(d_out.shape), kept.cols, kept.rows))
     _same_device(d_out, w_turned.values, kept.memory)
     rows, turned = _quantized_both(d_out)
-    return (_product(rows, w_turned, d_out.dtype, None, B.PRODUCT_ALL, None, d_out.device),
-            _product(turned, kept, torch.float32, None, B.PRODUCT_ALL, None, d_out.device))
+    return (_product(rows, w_turned, d_out.dtype, None, B.PRODUCT_ALL, exact, d_out.device),
+            _product(turned, kept, torch.float32, None, B.PRODUCT_ALL, True, d_out.device))
 
 
 class Kept:
@@ -366,9 +370,11 @@ class Kept:
         self.plan, self.weights, self.y, self.x_turned = plan, weights, y, x_turned
 
 
-def experts(x, ids, weights, w, train=False):
+def experts(x, ids, weights, w, train=False, exact=None):
     """[T, N] in x's type: for each row of x [T, K] the sum of its experts' products with it, weights [T, k] times w[ids] x, ids as route() gives
-    them.  w is quantize_weights() of [E, N, K].  train: (the result, what experts_backward() needs)."""
+    them.  w is quantize_weights() of [E, N, K].  train: (the result, what experts_backward() needs).  The result is the same with it and
+    without, but for up to 16 rows the order in which 32-bit sums are added.  exact: as in product(), but None is in 32 bits for every type,
+    since the gradient of the weights, which is 32-bit, is formed from the products."""
     _check_weights(x, w, experts=True)
     _same_device(x, ids, weights, w.values)
     T = x.shape[0]
@@ -376,22 +382,23 @@ def experts(x, ids, weights, w, train=False):
         raise ValueError("ids: [%d, k] is wanted, not %s" % (T, tuple(ids.shape)))
     _flat(ids, ids.shape, torch.int32, "ids")
     _flat(weights, ids.shape, torch.float32, "weights")
+    exact = exact is None or bool(exact)
     if not train and 0 < T <= B.PRODUCT_RAW_ROWS and ids.numel() * w.rows * w.cols <= DIRECT_BYTES:
         s = _stream(x)
         out = torch.empty((T, w.rows), dtype=x.dtype, device=x.device)
-        B.asgd_experts_direct(_raw(x), ids.data_ptr(), weights.data_ptr(), ids.shape[1], w._c, int(x.dtype is torch.float32), out.data_ptr(),
+        B.asgd_experts_direct(_raw(x), ids.data_ptr(), weights.data_ptr(), ids.shape[1], w._c, int(exact), out.data_ptr(),
                               _type(x.dtype), w.rows, s)
         return out
     order = plan(ids, w.count)
-    # 32-bit until the sum: one rounding to the result's type.  Beside a rounding to 16 bits the error of the 8-bit instruction does not
-    # show; the gradient of the weights is 32-bit, and y goes into it
-    y = _product_of(x, w, torch.float32, order, exact=train or x.dtype == torch.float32)
+    # 32-bit until the sum: one rounding to the result's type
+    y = _product_of(x, w, torch.float32, order, exact=exact)
     out = experts_sum(y, order, x.dtype, weights)
     return (out, Kept(order, weights, y, _quantized(x, turned=True, plan=order))) if train else out
 
 
-def experts_backward(d_out, kept, w_turned):
-    """(d_x [T, K] in d_out's type, d_w [E, N, K] float32, d_weights [T, k] float32) of experts(), from d_out [T, N]."""
+def experts_backward(d_out, kept, w_turned, exact=None):
+    """(d_x [T, K] in d_out's type, d_w [E, N, K] float32, d_weights [T, k] float32) of experts(), from d_out [T, N].  exact, as in
+    product(), is for d_x; d_w is summed in 32 bits."""
     _check_weights(d_out, w_turned, experts=True)
     order, x_turned = kept.plan, kept.x_turned
     if d_out.shape[0] != order.T or w_turned.rows != x_turned.rows or w_turned.count != order.E:
@@ -400,6 +407,6 @@ def experts_backward(d_out, kept, w_turned):
     _same_device(d_out, w_turned.values, kept.y)
     d_weights = experts_sum_backward(d_out, kept.y, order)
     rows, turned = _quantized_both(d_out, order, kept.weights)
-    d_rows = _product(rows, w_turned, torch.float32, order, B.PRODUCT_PLACES, d_out.dtype == torch.float32, d_out.device)
+    d_rows = _product(rows, w_turned, torch.float32, order, B.PRODUCT_PLACES, _exact(d_out.dtype, exact), d_out.device)
     d_x = experts_sum(d_rows, order, d_out.dtype)
     return d_x, _product_over(turned, x_turned, order, torch.float32, True, d_out.device), d_weights
