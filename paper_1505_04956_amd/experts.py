@@ -23,6 +23,7 @@ BLOCK = 128
 # products and sums, which take about 20 us more and read each expert's weights once.
 DIRECT_BYTES = 128 << 20
 
+_BYTES = (torch.float8_e4m3fn, torch.uint8)
 _TYPES = {torch.float32: B.TYPE_F32, torch.bfloat16: B.TYPE_BF16, torch.float16: B.TYPE_F16}
 
 
@@ -152,8 +153,8 @@ class Blocks:
 
     def __init__(self, values, scales, cols, squares=True):
         kb, shape, dims = -(-cols // BLOCK), values.shape, values.dim()
-        if values.element_size() != 1 or not (dims == 2 or (squares and dims == 3)) or shape[-1] != kb * BLOCK or not values.is_contiguous():
-            raise ValueError("values: contiguous bytes [%srows, %d] are wanted, not %s %s" % ("experts, " if squares else "", kb * BLOCK, values.dtype, tuple(shape)))
+        if values.dtype not in _BYTES or not (dims == 2 or (squares and dims == 3)) or shape[-1] != kb * BLOCK or not values.is_contiguous():
+            raise ValueError("values: contiguous float8_e4m3fn or uint8 [%srows, %d] are wanted, not %s %s" % ("experts, " if squares else "", kb * BLOCK, values.dtype, tuple(shape)))
         rows, count = shape[-2], shape[0] if dims == 3 else 1
         _flat(scales, (kb, rows) if not squares else (-(-rows // BLOCK), kb) if dims == 2 else (count, -(-rows // BLOCK), kb), torch.float32, "scales")
         _same_device(values, scales)
