@@ -12,6 +12,8 @@ Activations, logits and results are float32, bfloat16 or float16; what is kept i
 """
 from __future__ import annotations
 
+from operator import attrgetter
+
 import torch
 
 from . import binding as B
@@ -75,13 +77,19 @@ def _flat(t, shape, dtype, name):
         raise ValueError("%s: a contiguous %s tensor %s is wanted, not %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
 
 
+def _fixed(*names):
+    """Attributes to be read: what the library is handed was made from them, and would not follow a change."""
+    return (property(attrgetter("_" + name)) for name in names)
+
+
 class Rule:
     """How experts are chosen: `k` of them by `score` (SOFTMAX, SIGMOID), out of the `kept` best of `groups` groups (judged by
     their BEST key or the sum of their BEST_TWO); with renormalize a row's weights add up to `scale`, else they are scores times `scale`."""
-    __slots__ = ("k", "_c")
+    __slots__ = ("_k", "_c")
+    k, = _fixed("k")
 
     def __init__(self, k, score=SOFTMAX, groups=1, kept=1, group_by=BEST, renormalize=True, scale=1.0):
-        self.k = k
+        self._k = k
         self._c = B.asgd_route_rule(k, score, groups, kept, group_by, int(renormalize), scale)
 
 
@@ -119,13 +127,14 @@ class Plan:
     """The order in which experts take their rows (plan()): offsets [E + 1] (an expert's first place), blocks [E + 1] (its first block
     where each begins a new block of 128 places), slots [T * k] (the slot t * k + j at a place, -1: none), places [T * k] (the place of a
     slot, -1: none)."""
-    __slots__ = ("T", "k", "E", "offsets", "blocks", "slots", "places", "_c", "_memory")
+    __slots__ = ("_T", "_k", "_E", "_offsets", "_blocks", "_slots", "_places", "_c", "_memory")
+    T, k, E, offsets, blocks, slots, places = _fixed("T", "k", "E", "offsets", "blocks", "slots", "places")
 
     def __init__(self, T, k, E, device):
         n = T * k
-        self.T, self.k, self.E = T, k, E
+        self._T, self._k, self._E = T, k, E
         self._memory = m = torch.empty(2 * (E + 1) + 2 * n, dtype=torch.int32, device=device)
-        self.offsets, self.blocks, self.slots, self.places = m[:E + 1], m[E + 1:2 * E + 2], m[2 * E + 2:2 * E + 2 + n], m[2 * E + 2 + n:]
+        self._offsets, self._blocks, self._slots, self._places = m[:E + 1], m[E + 1:2 * E + 2], m[2 * E + 2:2 * E + 2 + n], m[2 * E + 2 + n:]
         at = m.data_ptr()
         self._c = B.asgd_route_order(T, k, E, at, at + 4 * (E + 1), at + 8 * (E + 1), at + 8 * (E + 1) + 4 * n)
 
@@ -149,7 +158,8 @@ def plan(ids, experts):
 class Blocks:
     """A matrix, or one for each expert, in 8-bit blocks: values [..., rows, 128 * ceil(cols / 128)] (float8_e4m3fn or uint8, zeros
     from `cols` on) times scales: squares [..., ceil(rows / 128), ceil(cols / 128)], or (squares=False) [ceil(cols / 128), rows]."""
-    __slots__ = ("values", "scales", "rows", "cols", "count", "squares", "_c")
+    __slots__ = ("_values", "_scales", "_rows", "_cols", "_count", "_squares", "_c")
+    values, scales, rows, cols, count, squares = _fixed("values", "scales", "rows", "cols", "count", "squares")
 
     def __init__(self, values, scales, cols, squares=True):
         kb, shape, dims = -(-cols // BLOCK), values.shape, values.dim()
@@ -158,7 +168,7 @@ class Blocks:
         rows, count = shape[-2], shape[0] if dims == 3 else 1
         _flat(scales, (kb, rows) if not squares else (-(-rows // BLOCK), kb) if dims == 2 else (count, -(-rows // BLOCK), kb), torch.float32, "scales")
         _same_device(values, scales)
-        self.values, self.scales, self.rows, self.cols, self.squares, self.count = values, scales, rows, cols, squares, count
+        self._values, self._scales, self._rows, self._cols, self._squares, self._count = values, scales, rows, cols, squares, count
         self._c = B.asgd_blocks(values.data_ptr(), scales.data_ptr(), rows, cols, B.BLOCKS_SQUARES if squares else B.BLOCKS_ROWS, count, 0, 0)
 
 
@@ -184,14 +194,16 @@ def _check_rows(x, plan, weights):
 
 class _Rows:
     """8-bit blocks of 1 x 128 that stay inside: one piece of memory, and the library's structure for it."""
-    __slots__ = ("memory", "rows", "cols", "_c")
+    __slots__ = ("_memory", "_rows", "_cols", "_c")
+    memory, rows, cols = _fixed("memory", "rows", "cols")
 
     def __init__(self, x, turned, plan):
-        self.rows, self.cols, kb = _sizes(x, turned, plan)
-        n = self.rows * kb * BLOCK
-        self.memory = torch.empty(n + 4 * kb * self.rows, dtype=torch.uint8, device=x.device)
-        at = self.memory.data_ptr()
-        self._c = B.asgd_blocks(at, at + n, self.rows, self.cols, B.BLOCKS_ROWS, 1, 0, 0)
+        rows, cols, kb = _sizes(x, turned, plan)
+        self._rows, self._cols = rows, cols
+        n = rows * kb * BLOCK
+        self._memory = torch.empty(n + 4 * kb * rows, dtype=torch.uint8, device=x.device)
+        at = self._memory.data_ptr()
+        self._c = B.asgd_blocks(at, at + n, rows, cols, B.BLOCKS_ROWS, 1, 0, 0)
 
 
 def _quantized(x, turned=False, plan=None, weights=None):
@@ -365,10 +377,11 @@ def linear_backward(d_out, kept, w_turned, exact=None):
 
 class Kept:
     """What experts_backward() needs of experts()."""
-    __slots__ = ("plan", "weights", "y", "x_turned")
+    __slots__ = ("_plan", "_weights", "_y", "_x_turned")
+    plan, weights, y, x_turned = _fixed("plan", "weights", "y", "x_turned")
 
     def __init__(self, plan, weights, y, x_turned):
-        self.plan, self.weights, self.y, self.x_turned = plan, weights, y, x_turned
+        self._plan, self._weights, self._y, self._x_turned = plan, weights, y, x_turned
 
 
 def experts(x, ids, weights, w, train=False, exact=None):
