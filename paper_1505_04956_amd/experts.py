@@ -188,7 +188,8 @@ def _check_rows(x, plan, weights):
         if plan is None:
             raise ValueError("weights belong to the slots of a plan")
         _flat(weights, (plan.T, plan.k), torch.float32, "weights")
-        _same_device(x, weights)
+    if plan is not None:
+        _same_device(x, plan._memory, weights)
     return _matrix(x, None if plan is None else plan.T)
 
 
@@ -289,14 +290,14 @@ def product(a, b, dtype, plan=None, gather=False, exact=None):
     places that are not in use are left as they were allocated.  exact: the products of a block are summed in 32 bits, at half the rate, and
     not by the 8-bit matrix instruction, whose sums are off by some 2e-5 to 1e-4 of the result, more where large products cancel (None: in 32
     bits, but for bfloat16 results)."""
-    _same_device(a.values, b.values)
+    _same_device(a.values, b.values, None if plan is None else plan._memory)
     _stream(a.values)
     return _product(a, b, dtype, plan, B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER if gather else B.PRODUCT_PLACES, exact, a.values.device)
 
 
 def product_over(a, b, plan, dtype=torch.float32, exact=None):
     """[E, a.rows, b.rows]: for each expert a b^T over its own places alone; a and b are quantize(..., turned=True, plan=plan)."""
-    _same_device(a.values, b.values)
+    _same_device(a.values, b.values, plan._memory)
     _stream(a.values)
     return _product_over(a, b, plan, dtype, exact, a.values.device)
 
@@ -324,7 +325,7 @@ def _product_of(x, w, dtype, plan=None, exact=None):
 def experts_sum(y, plan, dtype, weights=None):
     """[T, n] in `dtype`: the sum of each row's y [T * k, n] at the places of its slots, times weights [T, k] if given."""
     y_type, _, n, y_stride = _matrix(y, plan.T * plan.k, name="y")
-    _same_device(y, weights)
+    _same_device(y, plan._memory, weights)
     if weights is not None:
         _flat(weights, (plan.T, plan.k), torch.float32, "weights")
     s = _stream(y)
@@ -338,7 +339,7 @@ def experts_sum_backward(d_out, y, plan):
     """The gradient [T, k] float32 of experts_sum()'s weights from that of its result [T, n]."""
     y_type, _, n, y_stride = _matrix(y, plan.T * plan.k, name="y")
     type, _, _, stride = _matrix(d_out, plan.T, n, "d_out")
-    _same_device(y, d_out)
+    _same_device(y, plan._memory, d_out)
     s = _stream(y)
     out = torch.empty((plan.T, plan.k), dtype=torch.float32, device=y.device)
     B.asgd_experts_sum_backward(d_out.data_ptr(), type, stride, y.data_ptr(), y_type, n, y_stride, plan._c, out.data_ptr(), s)

@@ -37,3 +37,37 @@ def test_structures_do_not_change():
             thing.other = 1
     assert (rule.k, plan.T, plan.k, plan.E, w.rows, w.cols, w.count, w.squares) == (4, 5, 2, 3, 4, 100, 2, True)
     assert plan.offsets.numel() == plan.blocks.numel() == 4 and plan.slots.numel() == plan.places.numel() == 10
+
+
+class Elsewhere(torch.Tensor):
+    """A tensor on the CPU that says it is on the GPU, or (`there`) on another one."""
+    there = 0
+
+    def get_device(self):
+        return self.there
+
+
+class OnAnother(Elsewhere):
+    there = 1
+
+
+def test_a_plan_on_another_device_is_refused(monkeypatch):
+    """Its addresses would be read by kernels of the tensors' device.  (Nothing gets as far as a kernel here: what calls the library is replaced.)"""
+    for name in ("asgd_block_quantize", "asgd_block_quantize_both", "asgd_block_product", "asgd_experts_sum", "asgd_experts_sum_backward"):
+        monkeypatch.setattr(B, name, lambda *a: None)
+    monkeypatch.setattr(X, "_stream", lambda t: 0)
+    monkeypatch.setattr(X, "_raw_stream", lambda index: 0)
+    with monkeypatch.context() as m:
+        empty = torch.empty
+        m.setattr(torch, "empty", lambda *a, **k: empty(*a, **k).as_subclass(OnAnother))
+        plan = X.Plan(8, 2, 3, "cpu")
+    assert plan.offsets.get_device() == 1
+    here = lambda *shape, dtype=torch.float32: torch.zeros(shape, dtype=dtype).as_subclass(Elsewhere)  # noqa: E731
+    x, y, d = here(8, 200), here(16, 40), here(8, 40)
+    w = X.Blocks(here(3, 40, 256, dtype=torch.uint8), here(3, 1, 2), 200)
+    a, turned = X.Blocks(here(16, 256, dtype=torch.uint8), here(2, 16), 200, squares=False), X.Blocks(here(40, 384, dtype=torch.uint8), here(3, 40), 384, squares=False)
+    for call in (lambda: X.quantize(x, plan=plan), lambda: X.quantize(x, turned=True, plan=plan), lambda: X._quantized(x, plan=plan), lambda: X._quantized_both(x, plan),
+                 lambda: X.product(a, w, torch.float32, plan), lambda: X.product_over(turned, turned, plan), lambda: X.experts_sum(y, plan, torch.float32),
+                 lambda: X.experts_sum_backward(d, y, plan)):
+        with pytest.raises(ValueError, match="tensors on"):
+            call()
