@@ -1,7 +1,8 @@
 """Routed experts on torch tensors: routing, products in 8-bit blocks, and the products of the experts a row was routed to.
 
 Every function checks what it is given, allocates its results and enqueues the library's kernels on the current stream of
-the tensors' device; nothing is waited for and nothing is computed here.  Rows may be strided, their elements are consecutive.
+the tensors' device; nothing is waited for and nothing is computed here.  Results have no history: tensors that want a gradient are refused
+where gradients are recorded, and the *_backward calls form them.  Rows may be strided, their elements are consecutive.
 Activations, logits and results are float32, bfloat16 or float16; what is kept in 8 bits is torch.float8_e4m3fn.
 
     rule = Rule(k=6, score=SIGMOID, scale=2.5)
@@ -15,6 +16,7 @@ from __future__ import annotations
 from operator import attrgetter
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding as B
 
@@ -50,8 +52,17 @@ def _stream(t):
     return _raw_stream(index)
 
 
+def _no_history(t, name):
+    """Results have no history: what wants a gradient would lose it without a word.  (Under vmap and the transforms of torch.func tensors
+    have no memory, which torch itself says.)"""
+    if (t.requires_grad and torch.is_grad_enabled()) or (forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None):
+        raise ValueError("%s wants a gradient, which would be lost: detach it or call under torch.no_grad(), and use the *_backward calls" % name)
+
+
 def _matrix(t, rows=None, cols=None, name="x"):
     """(type, rows, cols, stride) of a matrix whose rows are runs of consecutive elements."""
+    if t.requires_grad or forward_ad._current_level >= 0:
+        _no_history(t, name)
     shape = t.shape
     if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
         raise ValueError("%s: a matrix%s is wanted, not %s" % (name, "" if rows is None and cols is None else " [%s, %s]" % (
@@ -73,6 +84,8 @@ def _same_device(first, *others):
 
 
 def _flat(t, shape, dtype, name):
+    if t.requires_grad or forward_ad._current_level >= 0:
+        _no_history(t, name)
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s: a contiguous %s tensor %s is wanted, not %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
 
@@ -101,7 +114,7 @@ def route(logits, rule, bias=None):
     if bias is not None:
         _flat(bias, (E,), torch.float32, "bias")
     s = _stream(logits)
-    ids = logits.new_empty((T, rule.k), dtype=torch.int32)
+    ids = logits.new_empty((T, rule._k), dtype=torch.int32)
     weights = torch.empty_like(ids, dtype=torch.float32)
     B.asgd_route(logits.data_ptr(), type, T, E, stride, None if bias is None else bias.data_ptr(), rule._c, ids.data_ptr(),
                  weights.data_ptr(), s)
@@ -112,8 +125,8 @@ def route_backward(logits, rule, ids, d_weights, bias=None):
     """The gradient of the logits [T, E], in their type, from that of route()'s weights; the choice is held fixed."""
     type, T, E, stride = _matrix(logits, name="logits")
     _same_device(logits, ids, d_weights, bias)
-    _flat(ids, (T, rule.k), torch.int32, "ids")
-    _flat(d_weights, (T, rule.k), torch.float32, "d_weights")
+    _flat(ids, (T, rule._k), torch.int32, "ids")
+    _flat(d_weights, (T, rule._k), torch.float32, "d_weights")
     if bias is not None:
         _flat(bias, (E,), torch.float32, "bias")
     s = _stream(logits)
@@ -149,7 +162,7 @@ def plan(ids, experts):
     _flat(ids, ids.shape, torch.int32, "ids")
     s = _stream(ids)
     p = Plan(ids.shape[0], ids.shape[1], experts, ids.device)
-    size = B.asgd_route_plan_bytes(p.T, p.k, p.E)
+    size = B.asgd_route_plan_bytes(p._T, p._k, p._E)
     work = torch.empty(size, dtype=torch.uint8, device=ids.device) if size else None
     B.asgd_route_plan(ids.data_ptr(), p._c, None if work is None else work.data_ptr(), size, s)
     return p
@@ -178,7 +191,7 @@ def _sizes(x, turned, plan):
     if turned:
         out_rows, out_cols = cols, rows if plan is None else max(1, plan.max_blocks()) * BLOCK
     else:
-        out_rows, out_cols = rows if plan is None else plan.T * plan.k, cols
+        out_rows, out_cols = rows if plan is None else plan._T * plan._k, cols
     return out_rows, out_cols, -(-out_cols // BLOCK)
 
 
@@ -187,10 +200,10 @@ def _check_rows(x, plan, weights):
     if weights is not None:
         if plan is None:
             raise ValueError("weights belong to the slots of a plan")
-        _flat(weights, (plan.T, plan.k), torch.float32, "weights")
+        _flat(weights, (plan._T, plan._k), torch.float32, "weights")
     if plan is not None:
         _same_device(x, plan._memory, weights)
-    return _matrix(x, None if plan is None else plan.T)
+    return _matrix(x, None if plan is None else plan._T)
 
 
 class _Rows:
@@ -248,6 +261,8 @@ def quantize_weights(w, turned=False):
     squares turn into squares), which the gradient of the activations takes."""
     if w.dim() not in (2, 3) or not w.is_contiguous() or w.numel() == 0:
         raise ValueError("weights: a contiguous [rows, cols] or [experts, rows, cols] is wanted, not %s" % (tuple(w.shape),))
+    if w.requires_grad or forward_ad._current_level >= 0:
+        _no_history(w, "weights")
     type, s, lead = _type(w.dtype), _stream(w), w.shape[:-2]
     rows, cols = w.shape[-2:]
     out_rows, out_cols = (cols, rows) if turned else (rows, cols)
@@ -265,22 +280,22 @@ def _exact(dtype, exact):
 
 
 def _product(a, b, dtype, plan, mode, exact, device):
-    rows = a.rows if plan is None else plan.T * plan.k
+    rows = a._rows if plan is None else plan._T * plan._k
     type, s = _type(dtype), _raw_stream(device.index)
-    if a.cols == 0 and b.cols == 0:                                  # (a sum over nothing)
-        return torch.zeros((rows, b.rows), dtype=dtype, device=device)
-    out = torch.empty((rows, b.rows), dtype=dtype, device=device)
+    if a._cols == 0 and b._cols == 0:                                  # (a sum over nothing)
+        return torch.zeros((rows, b._rows), dtype=dtype, device=device)
+    out = torch.empty((rows, b._rows), dtype=dtype, device=device)
     if rows:
-        B.asgd_block_product(a._c, b._c, mode, _exact(dtype, exact), None if plan is None else plan._c, out.data_ptr(), type, b.rows, s)
+        B.asgd_block_product(a._c, b._c, mode, _exact(dtype, exact), None if plan is None else plan._c, out.data_ptr(), type, b._rows, s)
     return out
 
 
 def _product_over(a, b, plan, dtype, exact, device):
-    shape = (plan.E, a.rows, b.rows)
-    if plan.T == 0:
+    shape = (plan._E, a._rows, b._rows)
+    if plan._T == 0:
         return torch.zeros(shape, dtype=dtype, device=device)
     out = torch.empty(shape, dtype=dtype, device=device)
-    B.asgd_block_product(a._c, b._c, B.PRODUCT_OVER, _exact(dtype, exact), plan._c, out.data_ptr(), _type(dtype), b.rows, _raw_stream(device.index))
+    B.asgd_block_product(a._c, b._c, B.PRODUCT_OVER, _exact(dtype, exact), plan._c, out.data_ptr(), _type(dtype), b._rows, _raw_stream(device.index))
     return out
 
 
@@ -290,16 +305,16 @@ def product(a, b, dtype, plan=None, gather=False, exact=None):
     places that are not in use are left as they were allocated.  exact: the products of a block are summed in 32 bits, at half the rate, and
     not by the 8-bit matrix instruction, whose sums are off by some 2e-5 to 1e-4 of the result, more where large products cancel (None: in 32
     bits, but for bfloat16 results)."""
-    _same_device(a.values, b.values, None if plan is None else plan._memory)
-    _stream(a.values)
-    return _product(a, b, dtype, plan, B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER if gather else B.PRODUCT_PLACES, exact, a.values.device)
+    _same_device(a._values, b._values, None if plan is None else plan._memory)
+    _stream(a._values)
+    return _product(a, b, dtype, plan, B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER if gather else B.PRODUCT_PLACES, exact, a._values.device)
 
 
 def product_over(a, b, plan, dtype=torch.float32, exact=None):
     """[E, a.rows, b.rows]: for each expert a b^T over its own places alone; a and b are quantize(..., turned=True, plan=plan)."""
-    _same_device(a.values, b.values, plan._memory)
-    _stream(a.values)
-    return _product_over(a, b, plan, dtype, exact, a.values.device)
+    _same_device(a._values, b._values, plan._memory)
+    _stream(a._values)
+    return _product_over(a, b, plan, dtype, exact, a._values.device)
 
 
 def _raw(x):
@@ -310,26 +325,26 @@ def _raw(x):
 
 def _product_of(x, w, dtype, plan=None, exact=None):
     """x, one row for each of the plan's T, times w."""
-    rows = x.shape[0] if plan is None else plan.T * plan.k
+    rows = x.shape[0] if plan is None else plan._T * plan._k
     mode = B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER
-    _same_device(x, w.values)
-    s = _stream(x)
+    _same_device(x, w._values)
     # (few rows of an expert: bringing them to 8 bits again in each strip of its weights takes less than another launch)
-    if not 0 < rows <= (B.PRODUCT_RAW_ROWS if plan is None else min(B.PRODUCT_RAW_SLOTS, 16 * plan.E)):
+    if not 0 < rows <= (B.PRODUCT_RAW_ROWS if plan is None else min(B.PRODUCT_RAW_SLOTS, 16 * plan._E)):
         return _product(_quantized(x), w, dtype, plan, mode, exact, x.device)
-    out = torch.empty((rows, w.rows), dtype=dtype, device=x.device)
-    B.asgd_block_product(_raw(x), w._c, mode, _exact(dtype, exact), None if plan is None else plan._c, out.data_ptr(), _type(dtype), w.rows, s)
+    raw, s = _raw(x), _stream(x)
+    out = torch.empty((rows, w._rows), dtype=dtype, device=x.device)
+    B.asgd_block_product(raw, w._c, mode, _exact(dtype, exact), None if plan is None else plan._c, out.data_ptr(), _type(dtype), w._rows, s)
     return out
 
 
 def experts_sum(y, plan, dtype, weights=None):
     """[T, n] in `dtype`: the sum of each row's y [T * k, n] at the places of its slots, times weights [T, k] if given."""
-    y_type, _, n, y_stride = _matrix(y, plan.T * plan.k, name="y")
+    y_type, _, n, y_stride = _matrix(y, plan._T * plan._k, name="y")
     _same_device(y, plan._memory, weights)
     if weights is not None:
-        _flat(weights, (plan.T, plan.k), torch.float32, "weights")
+        _flat(weights, (plan._T, plan._k), torch.float32, "weights")
     s = _stream(y)
-    out = torch.empty((plan.T, n), dtype=dtype, device=y.device)
+    out = torch.empty((plan._T, n), dtype=dtype, device=y.device)
     B.asgd_experts_sum(y.data_ptr(), y_type, n, y_stride, plan._c, None if weights is None else weights.data_ptr(), out.data_ptr(),
                        _type(dtype), n, s)
     return out
@@ -337,20 +352,20 @@ def experts_sum(y, plan, dtype, weights=None):
 
 def experts_sum_backward(d_out, y, plan):
     """The gradient [T, k] float32 of experts_sum()'s weights from that of its result [T, n]."""
-    y_type, _, n, y_stride = _matrix(y, plan.T * plan.k, name="y")
-    type, _, _, stride = _matrix(d_out, plan.T, n, "d_out")
+    y_type, _, n, y_stride = _matrix(y, plan._T * plan._k, name="y")
+    type, _, _, stride = _matrix(d_out, plan._T, n, "d_out")
     _same_device(y, plan._memory, d_out)
     s = _stream(y)
-    out = torch.empty((plan.T, plan.k), dtype=torch.float32, device=y.device)
+    out = torch.empty((plan._T, plan._k), dtype=torch.float32, device=y.device)
     B.asgd_experts_sum_backward(d_out.data_ptr(), type, stride, y.data_ptr(), y_type, n, y_stride, plan._c, out.data_ptr(), s)
     return out
 
 
 def _check_weights(x, w, experts=False):
-    if not w.squares or (w.count != 1 and not experts):
+    if not w._squares or (w._count != 1 and not experts):
         raise ValueError("weights in squares are wanted%s" % ("" if experts else ", one matrix of them"))
-    if x.dim() != 2 or x.shape[1] != w.cols:
-        raise ValueError("x: [rows, %d] is wanted, not %s" % (w.cols, tuple(x.shape)))
+    if x.dim() != 2 or x.shape[1] != w._cols:
+        raise ValueError("x: [rows, %d] is wanted, not %s" % (w._cols, tuple(x.shape)))
 
 
 def linear(x, w, train=False, exact=None):
@@ -359,7 +374,7 @@ def linear(x, w, train=False, exact=None):
     _check_weights(x, w)
     if not train:
         return _product_of(x, w, x.dtype, exact=exact)
-    _same_device(x, w.values)
+    _same_device(x, w._values)
     rows, turned = _quantized_both(x)
     return _product(rows, w, x.dtype, None, B.PRODUCT_ALL, exact, x.device), turned
 
@@ -368,9 +383,9 @@ def linear_backward(d_out, kept, w_turned, exact=None):
     """(d_x, in d_out's type, and d_w [N, K] float32) of linear(): from d_out [rows, N], what it kept, and the turned weights.  exact, as in
     product(), is for d_x; d_w is summed in 32 bits."""
     _check_weights(d_out, w_turned)
-    if d_out.shape[0] != kept.cols or w_turned.rows != kept.rows:
-        raise ValueError("d_out %s and the kept x [%d, %d] do not belong together" % (tuple(d_out.shape), kept.cols, kept.rows))
-    _same_device(d_out, w_turned.values, kept.memory)
+    if d_out.shape[0] != kept._cols or w_turned._rows != kept._rows:
+        raise ValueError("d_out %s and the kept x [%d, %d] do not belong together" % (tuple(d_out.shape), kept._cols, kept._rows))
+    _same_device(d_out, w_turned._values, kept._memory)
     rows, turned = _quantized_both(d_out)
     return (_product(rows, w_turned, d_out.dtype, None, B.PRODUCT_ALL, exact, d_out.device),
             _product(turned, kept, torch.float32, None, B.PRODUCT_ALL, True, d_out.device))
@@ -391,20 +406,21 @@ def experts(x, ids, weights, w, train=False, exact=None):
     without, but for up to 16 rows the order in which 32-bit sums are added.  exact: as in product(), but None is in 32 bits for every type,
     since the gradient of the weights, which is 32-bit, is formed from the products."""
     _check_weights(x, w, experts=True)
-    _same_device(x, ids, weights, w.values)
+    _same_device(x, ids, weights, w._values)
     T = x.shape[0]
     if ids.dim() != 2 or ids.shape[0] != T:
         raise ValueError("ids: [%d, k] is wanted, not %s" % (T, tuple(ids.shape)))
     _flat(ids, ids.shape, torch.int32, "ids")
     _flat(weights, ids.shape, torch.float32, "weights")
     exact = exact is None or bool(exact)
-    if not train and 0 < T <= B.PRODUCT_RAW_ROWS and ids.numel() * w.rows * w.cols <= DIRECT_BYTES:
-        s = _stream(x)
-        out = torch.empty((T, w.rows), dtype=x.dtype, device=x.device)
-        B.asgd_experts_direct(_raw(x), ids.data_ptr(), weights.data_ptr(), ids.shape[1], w._c, int(exact), out.data_ptr(),
-                              _type(x.dtype), w.rows, s)
+    if not train and 0 < T <= B.PRODUCT_RAW_ROWS and ids.numel() * w._rows * w._cols <= DIRECT_BYTES:
+        raw, s = _raw(x), _stream(x)
+        out = torch.empty((T, w._rows), dtype=x.dtype, device=x.device)
+        B.asgd_experts_direct(raw, ids.data_ptr(), weights.data_ptr(), ids.shape[1], w._c, int(exact), out.data_ptr(),
+                              _type(x.dtype), w._rows, s)
         return out
-    order = plan(ids, w.count)
+    _matrix(x)
+    order = plan(ids, w._count)
     # 32-bit until the sum: one rounding to the result's type
     y = _product_of(x, w, torch.float32, order, exact=exact)
     out = experts_sum(y, order, x.dtype, weights)
@@ -415,13 +431,13 @@ def experts_backward(d_out, kept, w_turned, exact=None):
     """(d_x [T, K] in d_out's type, d_w [E, N, K] float32, d_weights [T, k] float32) of experts(), from d_out [T, N].  exact, as in
     product(), is for d_x; d_w is summed in 32 bits."""
     _check_weights(d_out, w_turned, experts=True)
-    order, x_turned = kept.plan, kept.x_turned
-    if d_out.shape[0] != order.T or w_turned.rows != x_turned.rows or w_turned.count != order.E:
+    order, x_turned = kept._plan, kept._x_turned
+    if d_out.shape[0] != order._T or w_turned._rows != x_turned._rows or w_turned._count != order._E:
         raise ValueError("d_out %s and weights of %d experts [%d, %d] do not belong to what was kept" % (
-            tuple(d_out.shape), w_turned.count, w_turned.rows, w_turned.cols))
-    _same_device(d_out, w_turned.values, kept.y)
-    d_weights = experts_sum_backward(d_out, kept.y, order)
-    rows, turned = _quantized_both(d_out, order, kept.weights)
+            tuple(d_out.shape), w_turned._count, w_turned._rows, w_turned._cols))
+    _same_device(d_out, w_turned._values, kept._y)
+    d_weights = experts_sum_backward(d_out, kept._y, order)
+    rows, turned = _quantized_both(d_out, order, kept._weights)
     d_rows = _product(rows, w_turned, torch.float32, order, B.PRODUCT_PLACES, _exact(d_out.dtype, exact), d_out.device)
     d_x = experts_sum(d_rows, order, d_out.dtype)
     return d_x, _product_over(turned, x_turned, order, torch.float32, True, d_out.device), d_weights

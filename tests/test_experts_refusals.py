@@ -71,3 +71,46 @@ def test_a_plan_on_another_device_is_refused(monkeypatch):
                  lambda: X.experts_sum_backward(d, y, plan)):
         with pytest.raises(ValueError, match="tensors on"):
             call()
+
+
+def calls_that_lose_gradients(wanted):
+    """Every call with each of its inputs that can have a gradient; wanted(t) gives it one."""
+    x, l, i = torch.zeros(4, 128), torch.zeros(4, 8), torch.zeros(4, 2, dtype=torch.int32)
+    c, rule, plan = torch.zeros(4, 2), X.Rule(2), X.Plan(4, 2, 3, "cpu")
+    w = X.Blocks(torch.zeros(3, 6, 128, dtype=torch.uint8), torch.zeros(3, 1, 1), 128)
+    one = X.Blocks(torch.zeros(6, 128, dtype=torch.uint8), torch.zeros(1, 1), 128)
+    back, all_back = X.Blocks(torch.zeros(128, 128, dtype=torch.uint8), torch.zeros(1, 1), 6), X.Blocks(torch.zeros(3, 128, 128, dtype=torch.uint8), torch.zeros(3, 1, 1), 6)
+    y, d = torch.zeros(8, 6), torch.zeros(4, 6)
+    of_x = X._Rows(x, True, None)
+    kept = X.Kept(plan, c, y, X._Rows(x, True, plan))
+    return [lambda: X.route(wanted(l), rule), lambda: X.route(l, rule, bias=wanted(torch.zeros(8))), lambda: X.route_backward(wanted(l), rule, i, c),
+            lambda: X.route_backward(l, rule, i, wanted(c)), lambda: X.route_backward(l, rule, i, c, bias=wanted(torch.zeros(8))),
+            lambda: X.Blocks(torch.zeros(6, 128, dtype=torch.uint8), wanted(torch.zeros(1, 1)), 128),
+            lambda: X.quantize(wanted(x)), lambda: X.quantize(x, plan=plan, weights=wanted(c)), lambda: X.quantize_weights(wanted(x)),
+            lambda: X.quantize_weights(wanted(torch.zeros(2, 3, 4)), turned=True), lambda: X.experts_sum(wanted(y), plan, torch.float32),
+            lambda: X.experts_sum(y, plan, torch.float32, weights=wanted(c)), lambda: X.experts_sum_backward(wanted(d), y, plan),
+            lambda: X.experts_sum_backward(d, wanted(y), plan), lambda: X.linear(wanted(x), one), lambda: X.linear(wanted(x), one, train=True),
+            lambda: X.linear(wanted(torch.zeros(40, 128)), one), lambda: X.linear_backward(wanted(d), of_x, back), lambda: X.experts(wanted(x), i, c, w),
+            lambda: X.experts(x, i, wanted(c), w), lambda: X.experts(wanted(x), i, c, w, train=True), lambda: X.experts_backward(wanted(d), kept, all_back)]
+
+
+def test_gradients_that_would_be_lost_are_refused():
+    """The results have no history: a tensor that wants a gradient is to be detached, or used where none are recorded."""
+    for call in calls_that_lose_gradients(lambda t: t.clone().requires_grad_(True)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    with torch.no_grad():
+        for call in calls_that_lose_gradients(lambda t: t.clone().requires_grad_(True))[:5]:
+            with pytest.raises(ValueError, match="no CPU fallback"):
+                call()
+    for call in calls_that_lose_gradients(lambda t: t.clone().requires_grad_(True).detach())[:5]:
+        with pytest.raises(ValueError, match="no CPU fallback"):
+            call()
+
+
+def test_tangents_that_would_be_lost_are_refused():
+    from torch.autograd import forward_ad
+    with forward_ad.dual_level():
+        for call in calls_that_lose_gradients(lambda t: forward_ad.make_dual(t, torch.ones_like(t))):
+            with pytest.raises(ValueError, match="gradient"):
+                call()
