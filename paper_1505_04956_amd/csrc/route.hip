@@ -290,17 +290,18 @@ __device__ __forceinline__ void route_row_backward(const RouteArgs &a, int64_t t
     const float largest = wave_max(chosen);
     if (soft && renorm) share = there ? expf(chosen - largest) : 0.0f;
     else share = !there ? 0.0f : soft ? expf(chosen - top) / total : sigmoid(chosen);
+    const float rest = sigmoid(-chosen);           // 1 - s of a sigmoid (not by that difference, which loses a confident expert's gradient)
     float g, grad, inner = 0.0f;
     if (renorm) {
         const float sum = wave_sum(share);
         const float part = sum == 0.0f ? 0.0f : share / sum;
         g = a.rule.scale * (dw - wave_sum(dw * part));
         if (sum == 0.0f) g = 0.0f;
-        grad = soft ? g * part : sum == 0.0f ? 0.0f : g / sum * share * (1.0f - share);
+        grad = soft ? g * part : sum == 0.0f ? 0.0f : g / sum * share * rest;
     } else {
         g = a.rule.scale * dw;
         if (soft) inner = wave_sum(g * share);
-        grad = soft ? g : g * share * (1.0f - share);
+        grad = soft ? g : g * share * rest;
     }
     __builtin_amdgcn_wave_barrier();
     __threadfence_block();
