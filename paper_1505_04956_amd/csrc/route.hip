@@ -297,7 +297,7 @@ __device__ __forceinline__ void route_row_backward(const RouteArgs &a, int64_t t
         const float part = sum == 0.0f ? 0.0f : share / sum;
         g = a.rule.scale * (dw - wave_sum(dw * part));
         if (sum == 0.0f) g = 0.0f;
-        grad = soft ? g * part : sum == 0.0f ? 0.0f : g / sum * share * rest;
+        grad = soft ? g * part : g * part * rest;              // (and not g / sum * share, beyond 32 bits where scores are small)
     } else {
         g = a.rule.scale * dw;
         if (soft) inner = wave_sum(g * share);
