@@ -259,6 +259,9 @@ template <class Ty, int V, bool SORTED> __global__ __launch_bounds__(256) void r
 // With the choice held fixed: w_j = c s_j or c s_j / sum of the chosen s.
 //   g_j = c dw_j                      or  (c / sum) (dw_j - sum_i dw_i s_i / sum)
 //   sigmoid: dl_j = g_j s_j (1 - s_j);  softmax: dl_e = s_e (g_e - sum_i g_i s_i), whose inner sum is 0 when renormalised
+// Both differences stay what they are when all dw, or all g, are lessened by the same number, since the shares they are weighed by add up to
+// one.  That number is the one of the largest share: next to a share of one its own difference would cancel, and the gradient of a confident
+// router with it.
 // The k gradients are scattered over a row in the LDS and leave as whole lines.  Memory bounds it: 65536 rows of 256 in float32 take 29 us, 4.9
 // TB/s of logits read and gradients written, what a large copy reaches.
 template <class Ty, int V>
@@ -274,33 +277,44 @@ __device__ __forceinline__ void route_row_backward(const RouteArgs &a, int64_t t
     const bool there = id >= 0;
     const float chosen = there ? (float)row[id] : OUT;
     const float dw = there ? a.d_weights[t * k + lane] : 0.0f;
+    const auto fill = [&](float v) {
 #pragma unroll
-    for (int i = 0; i < V; i++) mine[i * 64 + lane] = 0.0f;
+        for (int i = 0; i < V; i++) mine[i * 64 + lane] = v;
+    };
+    if (!soft || renorm) fill(0.0f);
     float l[V];
     const bool bad = logits_of<Ty, V>(raw, bias, E, lane, l);
-    float top = 0.0f, total = 1.0f;
+    float top = 0.0f, total = 1.0f, score[V];
     if (soft && !renorm) {
         top = wave_max(lane_best(l));
         float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < V; i++) sum += l[i] == OUT ? 0.0f : expf(l[i] - top);
+        for (int i = 0; i < V; i++) sum += score[i] = l[i] == OUT ? 0.0f : expf(l[i] - top);
         total = wave_sum(sum);
+#pragma unroll
+        for (int i = 0; i < V; i++) score[i] = l[i] == OUT ? 0.0f : score[i] / total;
     }
     float share;
     const float largest = wave_max(chosen);
     if (soft && renorm) share = there ? expf(chosen - largest) : 0.0f;
     else share = !there ? 0.0f : soft ? expf(chosen - top) / total : sigmoid(chosen);
-    const float rest = sigmoid(-chosen);           // 1 - s of a sigmoid (not by that difference, which loses a confident expert's gradient)
-    float g, grad, inner = 0.0f;
+    const float rest = soft ? 0.0f : sigmoid(-chosen);         // 1 - s of a sigmoid (not by that difference, which loses a confident expert's gradient)
+    const auto of_first = [&](bool which, float v) {           // v of the first such lane, 0 without any
+        const unsigned long long has = __ballot(which);
+        return has ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), __ffsll((long long)has) - 1)) : 0.0f;
+    };
+    float g, grad;
     if (renorm) {
         const float sum = wave_sum(share);
         const float part = sum == 0.0f ? 0.0f : share / sum;
-        g = a.rule.scale * (dw - wave_sum(dw * part));
+        const float off = dw - of_first(there && chosen == largest, dw);
+        g = a.rule.scale * (off - wave_sum(off * part));
         if (sum == 0.0f) g = 0.0f;
         grad = soft ? g * part : g * part * rest;              // (and not g / sum * share, beyond 32 bits where scores are small)
     } else {
-        g = a.rule.scale * dw;
-        if (soft) inner = wave_sum(g * share);
+        const float base = soft ? of_first(there && chosen == top, dw) : 0.0f;
+        if (soft) fill(-a.rule.scale * base);                                 // (an expert that is not chosen: dw = 0)
+        g = a.rule.scale * (dw - base);
         grad = soft ? g : g * share * rest;
     }
     __builtin_amdgcn_wave_barrier();
@@ -308,11 +322,20 @@ __device__ __forceinline__ void route_row_backward(const RouteArgs &a, int64_t t
     if (there) mine[id] = grad;
     __builtin_amdgcn_wave_barrier();
     __threadfence_block();
+    float d[V], inner = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; i++) d[i] = mine[lane * V + i];
+    if (soft && !renorm) {
+#pragma unroll
+        for (int i = 0; i < V; i++) inner = fmaf(score[i], d[i], inner);
+        inner = wave_sum(inner);
+#pragma unroll
+        for (int i = 0; i < V; i++) d[i] = l[i] == OUT ? 0.0f : score[i] * (d[i] - inner);
+    }
     T u[V];
 #pragma unroll
     for (int i = 0; i < V; i++) {
-        float v = mine[lane * V + i];
-        if (soft && !renorm) v = l[i] == OUT ? 0.0f : expf(l[i] - top) / total * (v - inner);
+        float v = d[i];
         if (bad && l[i] != OUT) v = __uint_as_float(0x7FC00000u);
         u[i] = (T)v;
     }

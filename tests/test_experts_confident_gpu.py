@@ -57,3 +57,61 @@ def test_sigmoid_renormalised_far_below(X, dtype, rest):
     # every share is off by 24 roundings (exponential at 88, sum, division, the score's own), and by as many what they weigh
     size = 2.0 * p * (d.abs() + (p * d.abs()).sum(1, keepdim=True))
     assert ((gradient(X, l, rule, ids, dw) - want).abs() <= 2 * 32 * 2 * R.U * size + rest * want.abs()).all()
+
+
+def confident(T, E, low, high, seed, dtype):
+    """One expert of each row lies `low` to `high` above the best of the others."""
+    g = torch.Generator().manual_seed(seed)
+    l = torch.randn(T, E, generator=g) * 1.5
+    lead = torch.randint(0, E, (T,), generator=g)
+    l[torch.arange(T), lead] = l.amax(1) + low + (high - low) * torch.rand(T, generator=g)
+    return l.to(dtype)
+
+
+def exps(E):
+    """Relative, of a share: logits up to 30 and their difference in the exponent, exponential, sum over E, division."""
+    return (30 + 2 + E / 64 + 6 + 14 + 8) * 2 * R.U
+
+
+def pairwise(p, h):
+    """p_e sum_i p_i (h_e - h_i), and the sum of its terms' magnitudes."""
+    diff = h[:, :, None] - h[:, None, :]
+    return p * (p[:, None, :] * diff).sum(2), p * (p[:, None, :] * diff.abs()).sum(2)
+
+
+@pytest.mark.parametrize("dtype,rest", TYPES)
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,k", [(8, 2), (100, 6), (300, 8)])
+def test_renormalised_shares_next_to_one(X, E, k, score, dtype, rest):
+    """g = c share (dw - sum of share dw) = c share_j sum_i share_i (dw_j - dw_i): the leader's is as small as the others' shares, and the
+    differences of dw are all that enters it."""
+    l = confident(50, E, 6.0, 18.0, E, dtype)
+    if score == "sigmoid":
+        l = l - l.amax(1, keepdim=True) - 2.0           # (where it falls like an exponential)
+    rule, dw = rule_of(X, k, score, scale=1.5), torch.randn(50, k, generator=torch.Generator().manual_seed(k))
+    ids = X.route(l.cuda(), rule)[0].cpu()
+    want, size = pairwise(share_of(l, ids, score), dw.double())
+    if score == "sigmoid":
+        away = torch.sigmoid(-torch.gather(l.double(), 1, ids.long()))
+        want, size = want * away, size * away
+    # (a share next to one: what the others' roundings are worth of it is theirs alone; 6: see the sum over differences from the leader's)
+    assert ((gradient(X, l, rule, ids, dw) - 1.5 * want).abs() <= 6 * exps(k) * 1.5 * size + rest * 1.5 * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype,rest", TYPES)
+@pytest.mark.parametrize("chosen", [True, False])
+@pytest.mark.parametrize("E,k", [(8, 2), (100, 6), (300, 8), (1000, 3)])
+def test_softmax_scores_next_to_one(X, E, k, chosen, dtype, rest):
+    """dl_e = s_e sum_i s_i (g_e - g_i) over all experts, whether the leader is among the chosen or not."""
+    T = 50
+    l = confident(T, E, 6.0, 18.0, E + 1, dtype)
+    rule, g = rule_of(X, k, "softmax", renormalize=False, scale=1.5), torch.Generator().manual_seed(k)
+    ids = X.route(l.cuda(), rule)[0].cpu()
+    if not chosen:
+        order = torch.argsort(l.double(), 1, descending=True)
+        ids = order[:, 1:k + 1].int().contiguous()
+    dw = torch.randn(T, k, generator=g)
+    h = torch.zeros(T, E, dtype=torch.float64).scatter_(1, ids.long(), 1.5 * dw.double())
+    want, size = pairwise(torch.softmax(l.double(), 1), h)
+    got = X.route_backward(l.cuda(), rule, ids.cuda(), dw.cuda()).cpu().double()
+    assert ((got - want).abs() <= 6 * exps(E) * size + rest * want.abs() + 1e-40).all()
