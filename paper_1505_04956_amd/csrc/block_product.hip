@@ -377,6 +377,8 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_kernel(P
     typedef typename Out::T T;
     constexpr int ROW = I * 16 * sizeof(T), PITCH = ROW + 16, PER_ROW = ROW / 16, ROWS = 64 / PER_ROW;       // bytes; lanes of a row, rows of an instruction
     T *out = (T *)p.out + (over ? matrix * p.rows_a * p.stride : 0);
+    // (the last steps brought the last block once more: to stages that results go to now, so it has to be there before any wave's barrier)
+    __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);                 // (vmcnt alone, to zero)
     __syncthreads();
     constexpr int HALF = (WAVES + 1) / 2;
     static_assert(HALF * 16 * PITCH <= S::BYTES, "");
