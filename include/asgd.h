@@ -413,6 +413,12 @@ enum { ASGD_PRODUCT_RAW_ROWS = 16, ASGD_PRODUCT_RAW_SLOTS = 4096 };
 int asgd_block_product(const asgd_blocks *a, const asgd_blocks *b, int mode, int exact, const asgd_route_order *order, void *out,
                        int type, int64_t stride, void *hip_stream);
 
+/* The kernel that asgd_block_product() takes, from sizes and forms alone (host arithmetic): few rows, whose weights go from memory
+   to registers, or tiles of so many rows of a and of b (FAR: of a gathered a of 2^32 bytes and more).  NONE: refused, or nothing to do. */
+enum { ASGD_PRODUCT_FORM_NONE = 0, ASGD_PRODUCT_FORM_FEW = 1, ASGD_PRODUCT_FORM_TILES_64 = 2, ASGD_PRODUCT_FORM_TILES_128 = 3,
+       ASGD_PRODUCT_FORM_TILES_128_FAR = 4, ASGD_PRODUCT_FORM_TILES_256 = 5 };
+int asgd_block_product_form(const asgd_blocks *a, const asgd_blocks *b, int mode, int exact, const asgd_route_order *order);
+
 /*
  * The experts of few rows in one launch, without an order: out[t] = sum over j of weights[t][j] * (x's row t times the
  * matrix ids[t][j] of w), ids outside 0 .. w->count - 1 left out.  x: RAW, at most ASGD_PRODUCT_RAW_ROWS rows; w: SQUARES;

@@ -25,6 +25,7 @@ GROUP_BEST, GROUP_BEST_TWO = 0, 1
 BLOCKS_ROWS, BLOCKS_SQUARES, BLOCKS_RAW = range(3)
 PRODUCT_ALL, PRODUCT_GATHER, PRODUCT_PLACES, PRODUCT_OVER = range(4)
 PRODUCT_RAW_ROWS, PRODUCT_RAW_SLOTS = 16, 4096
+PRODUCT_FORM_NONE, PRODUCT_FORM_FEW, PRODUCT_FORM_TILES_64, PRODUCT_FORM_TILES_128, PRODUCT_FORM_TILES_128_FAR, PRODUCT_FORM_TILES_256 = range(6)
 
 # every symbol include/asgd.h declares
 SYMBOLS = (
@@ -34,7 +35,7 @@ SYMBOLS = (
     "asgd_schedule_peer", "asgd_schedule_peer_n", "asgd_last_hip_error", "asgd_destroy", "asgd_strerror",
     "asgd_quant_error_noalloc", "asgd_get_exchange", "asgd_set_exchange", "asgd_last_run_form",
     "asgd_route", "asgd_route_backward", "asgd_route_plan_bytes", "asgd_route_plan", "asgd_route_max_blocks",
-    "asgd_block_quantize", "asgd_block_quantize_both", "asgd_block_product", "asgd_experts_direct", "asgd_experts_sum", "asgd_experts_sum_backward",
+    "asgd_block_quantize", "asgd_block_quantize_both", "asgd_block_product", "asgd_block_product_form", "asgd_experts_direct", "asgd_experts_sum", "asgd_experts_sum_backward",
 )
 
 
@@ -120,6 +121,7 @@ def lib():
             "asgd_block_quantize": (C.c_int, [vp, C.c_int, i64, i64, i64, C.c_int, vp, vp, vp, vp]),
             "asgd_block_quantize_both": (C.c_int, [vp, C.c_int, i64, i64, i64, vp, vp, vp, vp, vp]),
             "asgd_block_product": (C.c_int, [vp, vp, C.c_int, C.c_int, vp, vp, C.c_int, i64, vp]),
+            "asgd_block_product_form": (C.c_int, [vp, vp, C.c_int, C.c_int, vp]),
             "asgd_experts_direct": (C.c_int, [vp, vp, vp, C.c_int, vp, C.c_int, vp, C.c_int, i64, vp]),
             "asgd_experts_sum": (C.c_int, [vp, C.c_int, i64, i64, vp, vp, vp, C.c_int, i64, vp]),
             "asgd_experts_sum_backward": (C.c_int, [vp, C.c_int, i64, vp, C.c_int, i64, i64, vp, vp, vp]),
@@ -281,6 +283,10 @@ def asgd_block_quantize_both(x_ptr, type, rows, cols, stride, order, weights_ptr
 def asgd_block_product(a, b, mode, exact, order, out_ptr, type, stride, stream=0):
     _check(lib().asgd_block_product(C.addressof(a), C.addressof(b), mode, exact, None if order is None else C.addressof(order), out_ptr, type,
                                     stride, stream), "asgd_block_product")
+
+
+def asgd_block_product_form(a, b, mode, exact, order) -> int:
+    return int(lib().asgd_block_product_form(C.addressof(a), C.addressof(b), mode, exact, None if order is None else C.addressof(order)))
 
 
 def asgd_experts_direct(x, ids_ptr, weights_ptr, k, w, exact, out_ptr, type, stride, stream=0):

@@ -631,10 +631,28 @@ static double tiles_time(int64_t n, double alone, double among) { return n <= 25
 // each of the 256 compute units, or the contraction has less than a block for each of its waves.
 static bool more_strips(const ProductArgs &p, unsigned strips, unsigned tiles) { return (int64_t)strips * tiles >= 2048 || (p.kb <= FEW_WAVES && strips >= 4); }
 
+static bool experts_rows(const ProductArgs &p) { return p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES; }
+
+// rows of a (of an expert, on average)
+static int64_t rows_each(const ProductArgs &p) { return experts_rows(p) ? p.order.T * p.order.k / p.order.E : p.rows_a; }
+
+int product_form(const ProductArgs &p, bool squares)
+{
+    const bool over = p.mode == ASGD_PRODUCT_OVER;
+    if (!over && rows_each(p) <= 32) return ASGD_PRODUCT_FORM_FEW;
+    if (experts_rows(p)) return (double)p.rows_a * p.kb * BLOCK8 >= 4294967296.0 ? ASGD_PRODUCT_FORM_TILES_128_FAR : ASGD_PRODUCT_FORM_TILES_128;
+    if (over) return ASGD_PRODUCT_FORM_TILES_128;
+    const auto tiles = [&](int n) { return ((p.rows_a + n - 1) / n) * ((p.rows_b + n - 1) / n); };
+    const double t64 = tiles_time(tiles(64), 0.31, 0.223), t128 = tiles_time(tiles(128), 0.66, 0.63);
+    if (t64 < t128) return ASGD_PRODUCT_FORM_TILES_64;
+    return squares && !p.exact && tiles_time(tiles(256), 2.1, 2.1) < t128 ? ASGD_PRODUCT_FORM_TILES_256 : ASGD_PRODUCT_FORM_TILES_128;
+}
+
 hipError_t launch_product(const ProductArgs &p, bool squares, int type, hipStream_t s)
 {
-    const bool grouped = p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES, over = p.mode == ASGD_PRODUCT_OVER;
-    const int64_t slots = grouped ? p.order.T * p.order.k : 0, E = p.order.E, rows = grouped ? slots : p.rows_a;
+    const bool grouped = experts_rows(p), over = p.mode == ASGD_PRODUCT_OVER;
+    const int64_t slots = grouped ? p.order.T * p.order.k : 0, E = p.order.E;
+    const int form = product_form(p, squares);
     const bool wide4 = p.stride % 4 == 0 && (uintptr_t)p.out % (4 * type_size(type)) == 0;
     const bool wide16 = p.stride * type_size(type) % 16 == 0 && (uintptr_t)p.out % 16 == 0;
     const auto tiles_of = [&](int tok) { return grouped ? most_tiles(slots, E, tok) : (p.rows_a + tok - 1) / tok; };
@@ -657,17 +675,12 @@ hipError_t launch_product(const ProductArgs &p, bool squares, int type, hipStrea
         const auto choose = [&](auto sq, auto exact) {
             const std::true_type yes;
             const std::false_type no;
-            // few rows (of an expert, on average)
-            const int64_t each = grouped ? rows / E : rows;
-            if (!over && each <= 32) return each <= 16 ? few(One<1>(), sq, exact) : few(One<2>(), sq, exact);
-            if constexpr (decltype(sq)::value)
-                if (grouped && (double)p.rows_a * p.kb * BLOCK8 >= 4294967296.0) return tiles(One<128>(), One<128>(), One<2>(), One<2>(), One<2>(), sq, exact, yes);
-            if (!grouped && !over) {
-                const double t64 = tiles_time(tiles_of(64) * ((p.rows_b + 63) / 64), 0.31, 0.223), t128 = tiles_time(tiles_of(128) * ((p.rows_b + 127) / 128), 0.66, 0.63);
-                if (t64 < t128) return tiles(One<64>(), One<64>(), One<2>(), One<2>(), One<4>(), sq, exact, no);
-                if constexpr (!decltype(exact)::value && decltype(sq)::value)
-                    if (tiles_time(tiles_of(256) * ((p.rows_b + 255) / 256), 2.1, 2.1) < t128) return tiles(One<256>(), One<256>(), One<4>(), One<2>(), One<2>(), sq, exact, no);
-            }
+            if (form == ASGD_PRODUCT_FORM_FEW) return rows_each(p) <= 16 ? few(One<1>(), sq, exact) : few(One<2>(), sq, exact);
+            if constexpr (decltype(sq)::value)                    // (experts' weights are squares)
+                if (form == ASGD_PRODUCT_FORM_TILES_128_FAR) return tiles(One<128>(), One<128>(), One<2>(), One<2>(), One<2>(), sq, exact, yes);
+            if (form == ASGD_PRODUCT_FORM_TILES_64) return tiles(One<64>(), One<64>(), One<2>(), One<2>(), One<4>(), sq, exact, no);
+            if constexpr (!decltype(exact)::value && decltype(sq)::value)
+                if (form == ASGD_PRODUCT_FORM_TILES_256) return tiles(One<256>(), One<256>(), One<4>(), One<2>(), One<2>(), sq, exact, no);
             return tiles(One<128>(), One<128>(), One<2>(), One<2>(), One<2>(), sq, exact, no);
         };
         const std::true_type yes;

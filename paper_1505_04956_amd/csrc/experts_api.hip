@@ -43,6 +43,37 @@ bool blocks_ok(const asgd_blocks *m)
     return m->scales && aligned(m->values, 16) && aligned(m->scales, 4) && (m->form == ASGD_BLOCKS_SQUARES || m->count == 1) && m->count <= ASGD_ROUTE_MAX_EXPERTS;
 }
 
+// A product but for its result: p and the rows of the result, or false.
+bool product_ok(const asgd_blocks *a, const asgd_blocks *b, int mode, int exact, const asgd_route_order *order, ProductArgs &p, int64_t &out_rows)
+{
+    if (!blocks_ok(a) || !blocks_ok(b) || a->cols != b->cols || b->rows < 1 || b->rows > MOST_COLS || b->form == ASGD_BLOCKS_RAW || a->form == ASGD_BLOCKS_SQUARES || (exact != 0 && exact != 1))
+        return false;
+    out_rows = a->rows;
+    if (mode == ASGD_PRODUCT_ALL) {
+        if (order || b->count != 1) return false;
+    } else {
+        if (!order_ok(order)) return false;
+        const int64_t slots = order->T * order->k;
+        if (mode == ASGD_PRODUCT_GATHER || mode == ASGD_PRODUCT_PLACES) {
+            if (b->form != ASGD_BLOCKS_SQUARES || b->count != order->E) return false;
+            if (a->rows != (mode == ASGD_PRODUCT_GATHER ? order->T : slots)) return false;
+            out_rows = slots;
+        } else if (mode == ASGD_PRODUCT_OVER) {
+            if (a->form != ASGD_BLOCKS_ROWS || b->form != ASGD_BLOCKS_ROWS || a->cols != BLOCK8 * asgd_route_max_blocks(order->T, order->k, order->E)) return false;
+        } else return false;
+    }
+    p = {};
+    p.a = (const uint8_t *)a->values; p.b = (const uint8_t *)b->values; p.sa = a->scales; p.sb = b->scales;
+    p.rows_a = a->rows; p.rows_b = b->rows; p.kb = blocks8(a->cols); p.cols = a->cols; p.mode = mode; p.exact = exact;
+    if (order) p.order = *order;
+    if (out_rows == 0) return true;
+    if (a->form == ASGD_BLOCKS_RAW) {
+        p.stride_raw = a->stride;
+        return b->form == ASGD_BLOCKS_SQUARES && out_rows <= (mode == ASGD_PRODUCT_ALL ? ASGD_PRODUCT_RAW_ROWS : ASGD_PRODUCT_RAW_SLOTS) && (mode == ASGD_PRODUCT_ALL || mode == ASGD_PRODUCT_GATHER);
+    }
+    return !((double)blocks8(out_rows + (order ? (int64_t)BLOCK8 * order->E : 0)) * (mode == ASGD_PRODUCT_OVER ? order->E : 1) * blocks8(b->rows) > (double)(MOST_GROUPS / 2));      // (of 128 x 128: where thin, twice as many of 64 x 64)
+}
+
 int done(hipError_t e) { return e == hipSuccess ? ASGD_OK : ASGD_EHIP; }
 
 }  // namespace
@@ -141,36 +172,22 @@ int asgd_block_quantize_both(const void *x, int type, int64_t rows, int64_t cols
 int asgd_block_product(const asgd_blocks *a, const asgd_blocks *b, int mode, int exact, const asgd_route_order *order, void *out,
                        int type, int64_t stride, void *hip_stream)
 {
-    if (!blocks_ok(a) || !blocks_ok(b) || !type_ok(type) || a->cols != b->cols || b->rows < 1 || b->rows > MOST_COLS || b->form == ASGD_BLOCKS_RAW || a->form == ASGD_BLOCKS_SQUARES || (exact != 0 && exact != 1))
-        return ASGD_EINVAL;
-    int64_t out_rows = a->rows;
-    if (mode == ASGD_PRODUCT_ALL) {
-        if (order || b->count != 1) return ASGD_EINVAL;
-    } else {
-        if (!order_ok(order)) return ASGD_EINVAL;
-        const int64_t slots = order->T * order->k;
-        if (mode == ASGD_PRODUCT_GATHER || mode == ASGD_PRODUCT_PLACES) {
-            if (b->form != ASGD_BLOCKS_SQUARES || b->count != order->E) return ASGD_EINVAL;
-            if (a->rows != (mode == ASGD_PRODUCT_GATHER ? order->T : slots)) return ASGD_EINVAL;
-            out_rows = slots;
-        } else if (mode == ASGD_PRODUCT_OVER) {
-            if (a->form != ASGD_BLOCKS_ROWS || b->form != ASGD_BLOCKS_ROWS || a->cols != BLOCK8 * asgd_route_max_blocks(order->T, order->k, order->E)) return ASGD_EINVAL;
-        } else return ASGD_EINVAL;
-    }
+    ProductArgs p;
+    int64_t out_rows;
+    if (!type_ok(type) || !product_ok(a, b, mode, exact, order, p, out_rows)) return ASGD_EINVAL;
     if (out_rows == 0) return ASGD_OK;
     if (!matrix_ok(out, type, out_rows, b->rows, stride) || (mode == ASGD_PRODUCT_OVER && stride < b->rows)) return ASGD_EINVAL;
-    ProductArgs p = {};
-    p.a = (const uint8_t *)a->values; p.b = (const uint8_t *)b->values; p.sa = a->scales; p.sb = b->scales;
-    p.rows_a = a->rows; p.rows_b = b->rows; p.kb = blocks8(a->cols); p.cols = a->cols; p.out = out; p.stride = stride; p.mode = mode; p.exact = exact;
-    if (order) p.order = *order;
+    p.out = out; p.stride = stride;
     const hipStream_t s = (hipStream_t)hip_stream;
-    if (a->form == ASGD_BLOCKS_RAW) {
-        if (b->form != ASGD_BLOCKS_SQUARES || out_rows > (mode == ASGD_PRODUCT_ALL ? ASGD_PRODUCT_RAW_ROWS : ASGD_PRODUCT_RAW_SLOTS) || (mode != ASGD_PRODUCT_ALL && mode != ASGD_PRODUCT_GATHER)) return ASGD_EINVAL;
-        p.stride_raw = a->stride;
-        return done(launch_product_raw(p, a->type, type, s));
-    }
-    if ((double)blocks8(out_rows + (order ? (int64_t)BLOCK8 * order->E : 0)) * (mode == ASGD_PRODUCT_OVER ? order->E : 1) * blocks8(b->rows) > (double)(MOST_GROUPS / 2)) return ASGD_EINVAL;      // (of 128 x 128: where thin, twice as many of 64 x 64)
-    return done(launch_product(p, b->form == ASGD_BLOCKS_SQUARES, type, s));
+    return done(a->form == ASGD_BLOCKS_RAW ? launch_product_raw(p, a->type, type, s) : launch_product(p, b->form == ASGD_BLOCKS_SQUARES, type, s));
+}
+
+int asgd_block_product_form(const asgd_blocks *a, const asgd_blocks *b, int mode, int exact, const asgd_route_order *order)
+{
+    ProductArgs p;
+    int64_t out_rows;
+    if (!product_ok(a, b, mode, exact, order, p, out_rows) || out_rows == 0) return ASGD_PRODUCT_FORM_NONE;
+    return a->form == ASGD_BLOCKS_RAW ? ASGD_PRODUCT_FORM_FEW : product_form(p, b->form == ASGD_BLOCKS_SQUARES);
 }
 
 int asgd_experts_direct(const asgd_blocks *x, const int32_t *ids, const float *weights, int k, const asgd_blocks *w, int exact,

@@ -74,6 +74,7 @@ struct ProductArgs {
     int mode;
     int exact;
 };
+int product_form(const ProductArgs &p, bool squares);      // ASGD_PRODUCT_FORM_* that launch_product() takes
 hipError_t launch_product(const ProductArgs &p, bool squares, int type, hipStream_t s);
 hipError_t launch_product_direct(const ProductArgs &p, const int32_t *ids, const float *weights, int k, int E, int raw_type, int type, hipStream_t s);
 hipError_t launch_product_raw(const ProductArgs &p, int raw_type, int type, hipStream_t s);

@@ -114,3 +114,30 @@ def test_tangents_that_would_be_lost_are_refused():
         for call in calls_that_lose_gradients(lambda t: forward_ad.make_dual(t, torch.ones_like(t))):
             with pytest.raises(ValueError, match="gradient"):
                 call()
+
+
+def test_which_kernel_a_product_takes():
+    """From sizes and forms alone: nothing is enqueued, addresses are not used."""
+    def blocks(rows, cols, form=B.BLOCKS_ROWS, count=1, **over):
+        return B.asgd_blocks(1 << 20, None if form == B.BLOCKS_RAW else 1 << 20, rows, cols, form, count, over.get("type", 0), over.get("stride", 0))
+
+    def form(rows, outs, cols, exact=0, squares=B.BLOCKS_SQUARES):
+        return B.asgd_block_product_form(blocks(rows, cols), blocks(outs, cols, squares), B.PRODUCT_ALL, exact, None)
+    assert form(32, 4096, 4096) == B.PRODUCT_FORM_FEW and form(33, 4096, 4096) == B.PRODUCT_FORM_TILES_64
+    assert form(777, 1001, 1100) == B.PRODUCT_FORM_TILES_64 and form(65536, 1024, 128, 1) == B.PRODUCT_FORM_TILES_128
+    assert form(8192, 8192, 8192) == B.PRODUCT_FORM_TILES_256 and form(8192, 8192, 8192, 1) == B.PRODUCT_FORM_TILES_128
+    assert form(8192, 8192, 8192, 0, B.BLOCKS_ROWS) == B.PRODUCT_FORM_TILES_128
+    assert form(0, 8, 8) == B.PRODUCT_FORM_NONE and form(8, 0, 8) == B.PRODUCT_FORM_NONE and form(8, 8, 8, 2) == B.PRODUCT_FORM_NONE
+    raw = blocks(16, 200, B.BLOCKS_RAW, stride=200)
+    assert B.asgd_block_product_form(raw, blocks(8, 200, B.BLOCKS_SQUARES), B.PRODUCT_ALL, 0, None) == B.PRODUCT_FORM_FEW
+    assert B.asgd_block_product_form(raw, blocks(8, 200), B.PRODUCT_ALL, 0, None) == B.PRODUCT_FORM_NONE
+
+    def experts(T, k, E, cols, mode=B.PRODUCT_GATHER):
+        o = B.asgd_route_order(T, k, E, *[1 << 20] * 4)
+        if mode == B.PRODUCT_OVER:
+            cols = X.BLOCK * B.asgd_route_max_blocks(T, k, E)
+            return B.asgd_block_product_form(blocks(64, cols), blocks(96, cols), mode, 1, o)
+        return B.asgd_block_product_form(blocks(T if mode == B.PRODUCT_GATHER else T * k, cols), blocks(96, cols, B.BLOCKS_SQUARES, E), mode, 0, o)
+    assert experts(24, 5, 100, 1000) == B.PRODUCT_FORM_FEW and experts(4093, 4, 64, 2048) == B.PRODUCT_FORM_TILES_128
+    assert experts(280_000, 1, 3, 16_384) == B.PRODUCT_FORM_TILES_128_FAR and experts(4093, 4, 64, 2048, B.PRODUCT_PLACES) == B.PRODUCT_FORM_TILES_128
+    assert experts(4, 1, 64, 0, B.PRODUCT_OVER) == B.PRODUCT_FORM_TILES_128
