@@ -116,3 +116,10 @@ def test_from_logits_to_gradients(X, T, k, E):
     y2, kept = X.experts(some[1], ids, w, X.quantize_weights(mats.cuda()), train=True)
     back = X.experts_backward(some[2], kept, X.quantize_weights(mats.cuda(), turned=True))
     assert torch.equal(y[real.cuda()], y2) and torch.equal(d_x[real.cuda()], back[0]) and torch.equal(d_w, back[1]) and torch.equal(d_weights[real.cuda()], back[2])
+
+
+def test_a_clustering_with_a_map_for_all(X):
+    """The example with --shared: routing, experts and a layer that every row passes through, each with its gradient, in one training loop."""
+    from paper_1505_04956_amd import clusterwise
+    losses, single = clusterwise.run(samples=60_000, steps=60, batch=4096, shared=True)
+    assert losses[-1] < 0.75 * losses[0] and sum(losses[-5:]) / 5 < single
