@@ -84,8 +84,8 @@ template <class Ty> __device__ __forceinline__ void store_four(typename Ty::T *p
 }
 
 // sixteen bytes of a row, of which `left` elements exist; wide: rows begin at a multiple of 16 bytes.  They pass by the second cache, whose
-// place belongs to the operands (65536 x 1024 x 128 to float32, bringing a to 8 bits included: 61 us; kept there, 71; the sum of experts that
-// reads 129 MB of them next loses nothing by it)
+// place belongs to the operands (65536 x 1024 x 128 to float32, bringing a to 8 bits included: 61 us; kept there, 65; gradients of 64 experts' weights of
+// 2048 x 2048 306 and 395; the sum of experts that reads 129 MB of them next loses nothing by it)
 template <class T> __device__ __forceinline__ void store16(T *p, int64_t left, bool wide, v4i v)
 {
     constexpr int N = 16 / sizeof(T);
@@ -153,17 +153,18 @@ __device__ __forceinline__ uint32_t tile_of_group(uint32_t id, uint32_t n)
 
 // Many rows.  8192^3 to bfloat16: 453 us, 2.4 PFLOP/s, where the power that the card may draw holds its clock at 1.6 to 1.8 GHz (a
 // library product with one scale for all reaches 2.65).  With 32-bit sums (EXACT) 8192^3 takes 898 us, 1.22 PFLOP/s; 65536 x 1024 x 128 to float32 is
-// bound by memory, its 277 MB.  4096 rows of four of 64 experts, 2048 x 2048: 159 us, 0.86 PFLOP/s at 2.4 GHz, where a wave waits for data of the
-// LDS or of the other waves half of the time: experts' last tiles are part empty, and sixteen blocks are soon over.
+// bound by memory, its 277 MB.  4096 rows of four of 64 experts, 2048 x 2048: 144 us, 0.95 PFLOP/s at 2.4 GHz, with 32-bit sums 182, 0.75;
+// a wave waits for data of the LDS or of the other waves half of the time: a block begins with waits (below), experts' last tiles are part empty,
+// and sixteen blocks are soon over.
 //
 // A tile of TOK rows of a and WT rows of b; the waves are TOK_WAVES x WT_WAVES, each with I x J pieces of 16 x 16.  Blocks of the
-// contraction of both, and their scales, go straight to one of two stages in the LDS; 16-byte pieces of a row lie at their
+// contraction of both, and their scales, go straight to one of two or four (STAGES) stages in the LDS; 16-byte pieces of a row lie at their
 // number xor the row's low bits, so that the lanes of a read spread over the banks.
 //
 // Within a block the rows of b are taken sixteen at a time: while the matrix cores work on one, the next is read from the
-// LDS and the sums of earlier ones are scaled and added.  The one barrier of a block lies before its last sixteen rows: by then a wave has
-// read all it needs of this stage, which the block after next may take, and the next block, on its way since the
-// last barrier, is there to be read while those last rows are multiplied.
+// LDS and the sums of earlier ones are scaled and added.  The one barrier of a block lies at its begin: by then its own loads have arrived and
+// all waves are done with the block before, whose stage the block STAGES - 1 further on takes, loaded while the first of this one's rows
+// are multiplied.  Nothing is read across the barrier, so a block's first rows of b, and its rows of a, are waited for.
 template <int TOK, int WT, bool SQUARES> struct Stage {
     static constexpr int VALUES = (TOK + WT) * BLOCK8;                                      // bytes
     // pieces of 64 scales: the rows' of a; the rows' of b, or for squares one for 128 rows, 64 times over
@@ -411,7 +412,7 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_kernel(P
 // instruction, and the eight waves of a workgroup share the blocks of the contraction of sixteen rows of b, four of them on
 // their way at a time.  Rows of a, J times sixteen, come from the caches; RAW ones are brought to 8 bits in the registers of
 // the lanes that need them (up to sixteen of them: there this is less than a launch costs).  One row times 4096 x 4096: 9.0 us, 1.9
-// TB/s; 120 rows of 100 experts, 33 of which have rows, 1000 x 1100: 17 us, 2.2 TB/s.  The weights' way from memory bounds it, one round of loads a wave at few strips.
+// TB/s; 120 rows of 100 experts, 33 of which have rows, 1000 x 1100: 18 us, 2.1 TB/s.  The weights' way from memory bounds it, one round of loads a wave at few strips.
 constexpr int FEW_WAVES = 8;
 
 // a lane's 32 elements of a block of a row: fetched early, brought to 8 bits when they are there
@@ -553,7 +554,7 @@ template <class In, int J, int STRIPS, bool SQUARES, bool EXACT, class Out> __gl
 
 // A row's experts without an order, for few rows: a workgroup takes sixteen rows of b of every expert of one row of a (blockIdx.y), and
 // adds what they give times its weights.  A block of the row is brought to 8 bits once for all of them; the weights of up to
-// EXPERTS of them are on their way at a time.  Six experts of 2048 x 2048: 9.8 us, 2.6 TB/s.  Sixteen waves, since a round of loads then
+// EXPERTS of them are on their way at a time.  Six experts of 2048 x 2048: 10.0 us, 2.5 TB/s.  Sixteen waves, since a round of loads then
 // is all that each has of 2048 columns, and its latency is what counts (eight: 10.4).
 constexpr int DIRECT_WAVES = 16;
 
