@@ -392,12 +392,17 @@ def linear_backward(d_out, kept, w_turned, exact=None):
 
 
 class Kept:
-    """What experts_backward() needs of experts()."""
-    __slots__ = ("_plan", "_weights", "_y", "_x_turned")
+    """What experts_backward() needs of experts(): the plan, the weights themselves, not a copy, the experts' products y and x in 8 bits."""
+    __slots__ = ("_plan", "_weights", "_y", "_x_turned", "_version")
     plan, weights, y, x_turned = _fixed("plan", "weights", "y", "x_turned")
 
     def __init__(self, plan, weights, y, x_turned):
         self._plan, self._weights, self._y, self._x_turned = plan, weights, y, x_turned
+        self._version = self._written()
+
+    def _written(self):
+        """How often the weights were written to (tensors of inference mode do not count that)."""
+        return None if self._weights.is_inference() else self._weights._version
 
 
 def experts(x, ids, weights, w, train=False, exact=None):
@@ -435,6 +440,8 @@ def experts_backward(d_out, kept, w_turned, exact=None):
     if d_out.shape[0] != order._T or w_turned._rows != x_turned._rows or w_turned._count != order._E:
         raise ValueError("d_out %s and weights of %d experts [%d, %d] do not belong to what was kept" % (
             tuple(d_out.shape), w_turned._count, w_turned._rows, w_turned._cols))
+    if kept._version != kept._written():
+        raise ValueError("the weights have changed since experts() was called with them")
     _same_device(d_out, w_turned._values, kept._y)
     d_weights = experts_sum_backward(d_out, kept._y, order)
     rows, turned = _quantized_both(d_out, order, kept._weights)

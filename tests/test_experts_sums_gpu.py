@@ -94,3 +94,20 @@ def test_what_the_8_bit_instruction_costs(X):
         for exact, limit in ((False, most), (True, 2e-7)):
             off = X.product(a, b, torch.float32, exact=exact).cpu().double() - want
             assert off.square().mean().sqrt() <= limit * want.square().mean().sqrt()
+
+
+def test_weights_that_changed_since(X):
+    """The weights are kept, not copied: gradients from others than the result was formed with are refused."""
+    ids, w = routed(40, 2, 3, 1)
+    x, d, mats = data(40, 100, 1).cuda(), data(40, 60, 2).cuda(), weights_of(3, 60, 100, 3).cuda()
+    q, t, w = X.quantize_weights(mats), X.quantize_weights(mats, turned=True), w.cuda()
+    _, kept = X.experts(x, ids.cuda(), w, q, train=True)
+    first = X.experts_backward(d, kept, t)
+    assert all(torch.equal(a, b) for a, b in zip(first, X.experts_backward(d, kept, t)))
+    w *= 2
+    with pytest.raises(ValueError, match="changed"):
+        X.experts_backward(d, kept, t)
+    with torch.inference_mode():
+        v = w.clone()
+        _, kept = X.experts(x, ids.cuda(), v, q, train=True)
+        assert len(X.experts_backward(d, kept, t)) == 3
