@@ -356,12 +356,18 @@ int64_t asgd_route_max_blocks(int64_t T, int k, int E);
  *   ASGD_BLOCKS_ROWS     blocks of 1 x 128: scales[kb][rows] (block major; count = 1)
  *   ASGD_BLOCKS_SQUARES  blocks of 128 x 128: scales[count][ceil(rows / 128)][kb]
  *   ASGD_BLOCKS_RAW      not in 8 bits yet: values are rows x cols of `type`, rows `stride` elements apart, scales is
- *                        not used (count = 1); the product brings them to 8 bits as ASGD_BLOCKS_ROWS would on the way
+ *                        not used (count = 1); the product brings them to 8 bits as ASGD_BLOCKS_ROWS would on the way (to 4, if
+                        the other operand is ASGD_BLOCKS_FOURS)
+ * or in 4-bit floating point:
+ *   ASGD_BLOCKS_FOURS    blocks of 1 x 32.  values: e2m1, two a byte, the first in the low four bits, `count` matrices of rows x
+ *                        (128 * kf) bytes, kf = ceil(cols / 256), zeros from column cols on; scales: bytes, count x rows x (8 * kf),
+ *                        2^(byte - 127) is the scale of 32 columns, 255: it is not a number; both 16-byte aligned.  Rows of
+ *                        activations and of weights (any count) are alike
  */
-enum { ASGD_BLOCKS_ROWS = 0, ASGD_BLOCKS_SQUARES = 1, ASGD_BLOCKS_RAW = 2 };
+enum { ASGD_BLOCKS_ROWS = 0, ASGD_BLOCKS_SQUARES = 1, ASGD_BLOCKS_RAW = 2, ASGD_BLOCKS_FOURS = 4 };
 typedef struct asgd_blocks {
     void *values;
-    float *scales;
+    float *scales;     /* ASGD_BLOCKS_FOURS: bytes */
     int64_t rows, cols;
     int32_t form;      /* ASGD_BLOCKS_* */
     int32_t count;
@@ -374,6 +380,10 @@ typedef struct asgd_blocks {
  * out's values and scales are written, its rows, cols, form and count say how.  A block with largest magnitude m (at least
  * 1e-30) gets the scale m * (1 / 448) and the values v * (448 * (1 / m)), each operation rounded to 32 bits, then to the nearest e4m3 number, ties to even.
  * A block that holds an infinity or something that is not a number gets a scale that is not a number.
+ * out in 4 bits (ASGD_BLOCKS_FOURS; turned = 0, order = NULL): a block whose largest magnitude is m gets the scale 2^e, e =
+ * floor(log2 m) - 2, one more where m is at least 1.75 * 2^floor(log2 m), at least -126 and at most 125, and the values v / 2^e to the
+ * nearest e2m1 number (0, 0.5, 1, 1.5, 2, 3, 4, 6), ties to even, cut at 6.  (m then rounds to at most 6, but where m / 2^e lies
+ * between 6 and 7 and is cut.)  The scales of columns beyond cols are 2^-126.
  *   turned = 1   the transpose of x is brought to 8 bits: out has cols rows; blocks lie along x's rows
  *   order        (ASGD_BLOCKS_ROWS only, count = 1, or NULL) x has one row for each of the order's T rows; row p of what is
  *                brought to 8 bits is x's row of the slot at place p, times weights[slot] (float T x k, or NULL).  Not
@@ -383,6 +393,10 @@ typedef struct asgd_blocks {
  */
 int asgd_block_quantize(const void *x, int type, int64_t rows, int64_t cols, int64_t stride, int turned,
                         const asgd_route_order *order, const float *weights, const asgd_blocks *out, void *hip_stream);
+
+/* The values that x, in 4 bits (ASGD_BLOCKS_FOURS), stands for: out, count * rows rows of cols elements of `type`, `stride` elements apart.
+   Every finite one is a float32, and but for its exponent a bfloat16 and a float16; blocks whose scale is not a number give what is not one. */
+int asgd_block_expand(const asgd_blocks *x, void *out, int type, int64_t stride, void *hip_stream);
 
 /* asgd_block_quantize() of the same x twice, not turned into `out` and turned into `out_turned` (both ASGD_BLOCKS_ROWS), from one
    reading of x: what a training step takes of its activations and gradients. */
@@ -405,7 +419,9 @@ int asgd_block_quantize_both(const void *x, int type, int64_t rows, int64_t cols
  *   ASGD_PRODUCT_PLACES   the same with an `a` that has a row for each place already (ROWS)
  *   ASGD_PRODUCT_OVER     a and b (ROWS) are turned quantisations over the same order: out (E x a.rows x b.rows, matrices
  *                         a.rows * stride apart) = for each expert the product over its own places alone, zeros without any
- * a RAW: at most ASGD_PRODUCT_RAW_ROWS rows (ALL) or ASGD_PRODUCT_RAW_SLOTS slots (GATHER), and b SQUARES.  A matrix in 8-bit
+ * In 4 bits (b FOURS, a FOURS or RAW; every mode but OVER) the matrix instruction takes the scales, and adds to 32-bit sums what it
+ * forms of 128 products: within 1.2e-7 of the sum of their magnitudes, so `exact` makes no difference.
+ * a RAW: at most ASGD_PRODUCT_RAW_ROWS rows (ALL) or ASGD_PRODUCT_RAW_SLOTS slots (GATHER), and b SQUARES or FOURS.  A matrix in
  * blocks has at most 2^30 rows and 2^24 columns, b at most 2^24 rows, out at most 2^22 tiles of 128 x 128.
  */
 enum { ASGD_PRODUCT_ALL = 0, ASGD_PRODUCT_GATHER = 1, ASGD_PRODUCT_PLACES = 2, ASGD_PRODUCT_OVER = 3 };
@@ -421,7 +437,7 @@ int asgd_block_product_form(const asgd_blocks *a, const asgd_blocks *b, int mode
 
 /*
  * The experts of few rows in one launch, without an order: out[t] = sum over j of weights[t][j] * (x's row t times the
- * matrix ids[t][j] of w), ids outside 0 .. w->count - 1 left out.  x: RAW, at most ASGD_PRODUCT_RAW_ROWS rows; w: SQUARES;
+ * matrix ids[t][j] of w), ids outside 0 .. w->count - 1 left out.  x: RAW, at most ASGD_PRODUCT_RAW_ROWS rows; w: SQUARES or FOURS;
  * ids and weights: rows x k.  Every row reads its experts' matrices for itself.
  */
 int asgd_experts_direct(const asgd_blocks *x, const int32_t *ids, const float *weights, int k, const asgd_blocks *w, int exact,
@@ -438,6 +454,45 @@ int asgd_experts_sum(const void *y, int y_type, int64_t n, int64_t y_stride, con
 /* Gradient of those weights: d_weights[t][j] = d_out[t] . y[place of slot (t, j)], 0 at slots without an expert. */
 int asgd_experts_sum_backward(const void *d_out, int type, int64_t stride, const void *y, int y_type, int64_t n, int64_t y_stride,
                               const asgd_route_order *order, float *d_weights, void *hip_stream);
+
+/*
+ * A whole layer of experts for few rows, from the router's logits to the sum:
+ *   ids, weights (rows x k)  as asgd_route() gives them for `logits` (rows x E of logits_type, rows logits_stride apart), bias and rule
+ *   u = up[e] x[t]           for every expert e = ids[t][j]; up: 2 * H rows of D columns for each of E experts
+ *   h = f(u[0 .. H)) * u[H .. 2 * H), f(g) = g / (1 + exp(-g)) (ASGD_ACTIVATION_SILU) or g / 2 * (1 + erf(g / sqrt(2))) (_GELU), in 32 bits
+ *   out[t] = sum over j, in no order that changes between calls, of weights[t][j] * (down[e] h); down: N rows of H columns for each expert
+ * up and down are SQUARES or both FOURS; x (RAW, at most ASGD_PRODUCT_RAW_ROWS rows of D columns) and h are brought to the same bits on the
+ * way, 8-bit products are summed in 32 bits.  A row without an expert gives zeros, a place without one (id -1) adds nothing.  work: asgd_experts_layer_bytes() of
+ * scratch, 16-byte aligned, of one call at a time.
+ */
+enum { ASGD_ACTIVATION_SILU = 0, ASGD_ACTIVATION_GELU = 1 };
+size_t asgd_experts_layer_bytes(int64_t rows, int k, int64_t H);
+int asgd_experts_layer(const asgd_blocks *x, const void *logits, int logits_type, int64_t logits_stride, const float *bias,
+                       const asgd_route_rule *rule, const asgd_blocks *up, const asgd_blocks *down, int activation, int32_t *ids,
+                       float *weights, void *out, int type, int64_t stride, void *work, size_t work_bytes, void *hip_stream);
+
+/* A run of n elements of `type` (ASGD_TYPE_*), aligned to one of them, device memory. */
+typedef struct asgd_span {
+    void *data;
+    int64_t n;
+    int64_t type;
+} asgd_span;
+
+/*
+ * norm (one float, device memory) = the square root of the sum of the squares of all elements of `count` runs, whose squares and sums
+ * are 64-bit.  The same runs give the same bits.  work: asgd_gradient_bytes() of scratch, 16-byte aligned, of one call at a time.
+ */
+size_t asgd_gradient_bytes(const asgd_span *runs, int64_t count);
+int asgd_gradient_norm(const asgd_span *runs, int64_t count, float *norm, void *work, size_t work_bytes, void *hip_stream);
+
+/*
+ * That norm, and out[i] = runs[i] * factor, factor = limit / norm (64-bit, rounded to 32) where norm > limit, 1 where it is not, not a number where the norm is
+ * none; a product is rounded to 32 bits, then to the type of out[i].  limit >= 0.  An infinite norm, then, gives zeros and, of
+ * infinities, what is not a number.  out may be NULL (runs are clipped in place); out[i] has as many elements as runs[i], is runs[i] itself
+ * or shares no byte with any run or other out.  In place nothing is written where the factor is 1.
+ */
+int asgd_gradient_clip(const asgd_span *runs, const asgd_span *out, int64_t count, double limit, float *norm, void *work, size_t work_bytes,
+                       void *hip_stream);
 
 /* Device time in milliseconds of the last asgd_run_* call, measured with HIP events recorded on
    the context's stream around its kernel launches.  No device access. */

@@ -22,9 +22,10 @@ FORM_NONE, FORM_FP32, FORM_SPLIT_LAUNCH, FORM_SPLIT_PHASES = range(4)
 TYPE_F32, TYPE_BF16, TYPE_F16 = range(3)
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 GROUP_BEST, GROUP_BEST_TWO = 0, 1
-BLOCKS_ROWS, BLOCKS_SQUARES, BLOCKS_RAW = range(3)
+BLOCKS_ROWS, BLOCKS_SQUARES, BLOCKS_RAW, BLOCKS_FOURS = 0, 1, 2, 4
 PRODUCT_ALL, PRODUCT_GATHER, PRODUCT_PLACES, PRODUCT_OVER = range(4)
 PRODUCT_RAW_ROWS, PRODUCT_RAW_SLOTS = 16, 4096
+ACTIVATION_SILU, ACTIVATION_GELU = 0, 1
 PRODUCT_FORM_NONE, PRODUCT_FORM_FEW, PRODUCT_FORM_TILES_64, PRODUCT_FORM_TILES_128, PRODUCT_FORM_TILES_128_FAR, PRODUCT_FORM_TILES_256 = range(6)
 
 # every symbol include/asgd.h declares
@@ -36,6 +37,7 @@ SYMBOLS = (
     "asgd_quant_error_noalloc", "asgd_get_exchange", "asgd_set_exchange", "asgd_last_run_form",
     "asgd_route", "asgd_route_backward", "asgd_route_plan_bytes", "asgd_route_plan", "asgd_route_max_blocks",
     "asgd_block_quantize", "asgd_block_quantize_both", "asgd_block_product", "asgd_block_product_form", "asgd_experts_direct", "asgd_experts_sum", "asgd_experts_sum_backward",
+    "asgd_block_expand", "asgd_experts_layer_bytes", "asgd_experts_layer", "asgd_gradient_bytes", "asgd_gradient_norm", "asgd_gradient_clip",
 )
 
 
@@ -125,6 +127,12 @@ def lib():
             "asgd_experts_direct": (C.c_int, [vp, vp, vp, C.c_int, vp, C.c_int, vp, C.c_int, i64, vp]),
             "asgd_experts_sum": (C.c_int, [vp, C.c_int, i64, i64, vp, vp, vp, C.c_int, i64, vp]),
             "asgd_experts_sum_backward": (C.c_int, [vp, C.c_int, i64, vp, C.c_int, i64, i64, vp, vp, vp]),
+            "asgd_block_expand": (C.c_int, [vp, vp, C.c_int, i64, vp]),
+            "asgd_experts_layer_bytes": (C.c_size_t, [i64, C.c_int, i64]),
+            "asgd_experts_layer": (C.c_int, [vp, vp, C.c_int, i64, vp, vp, vp, vp, C.c_int, vp, vp, vp, C.c_int, i64, vp, C.c_size_t, vp]),
+            "asgd_gradient_bytes": (C.c_size_t, [vp, i64]),
+            "asgd_gradient_norm": (C.c_int, [vp, i64, vp, vp, C.c_size_t, vp]),
+            "asgd_gradient_clip": (C.c_int, [vp, vp, i64, dbl, vp, vp, C.c_size_t, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -302,6 +310,34 @@ def asgd_experts_sum(y_ptr, y_type, n, y_stride, order, weights_ptr, out_ptr, ty
 def asgd_experts_sum_backward(d_out_ptr, type, stride, y_ptr, y_type, n, y_stride, order, d_weights_ptr, stream=0):
     _check(lib().asgd_experts_sum_backward(d_out_ptr, type, stride, y_ptr, y_type, n, y_stride, C.addressof(order), d_weights_ptr, stream),
            "asgd_experts_sum_backward")
+
+
+def asgd_block_expand(x, out_ptr, type, stride, stream=0):
+    _check(lib().asgd_block_expand(C.addressof(x), out_ptr, type, stride, stream), "asgd_block_expand")
+
+
+def asgd_experts_layer_bytes(rows, k, H) -> int:
+    return int(lib().asgd_experts_layer_bytes(rows, k, H))
+
+
+def asgd_experts_layer(x, logits_ptr, logits_type, logits_stride, bias_ptr, rule, up, down, activation, ids_ptr, weights_ptr, out_ptr, type,
+                       stride, work_ptr, work_bytes, stream=0):
+    _check(lib().asgd_experts_layer(C.addressof(x), logits_ptr, logits_type, logits_stride, bias_ptr, C.addressof(rule), C.addressof(up),
+                                    C.addressof(down), activation, ids_ptr, weights_ptr, out_ptr, type, stride, work_ptr, work_bytes, stream),
+           "asgd_experts_layer")
+
+
+# gradients: runs are (address, elements, TYPE_*) as 64-bit integers one after the other, host memory; the tensor-level calls are in gradients.py
+def asgd_gradient_bytes(runs_ptr, count) -> int:
+    return int(lib().asgd_gradient_bytes(runs_ptr, count))
+
+
+def asgd_gradient_norm(runs_ptr, count, norm_ptr, work_ptr, work_bytes, stream=0):
+    _check(lib().asgd_gradient_norm(runs_ptr, count, norm_ptr, work_ptr, work_bytes, stream), "asgd_gradient_norm")
+
+
+def asgd_gradient_clip(runs_ptr, out_ptr, count, limit, norm_ptr, work_ptr, work_bytes, stream=0):
+    _check(lib().asgd_gradient_clip(runs_ptr, out_ptr, count, limit, norm_ptr, work_ptr, work_bytes, stream), "asgd_gradient_clip")
 
 
 # ---- convenience wrapper: owns a handle, keeps the borrowed tensors alive -----------------

@@ -1,5 +1,5 @@
 // C entry points of the routed experts: what is refused, and which launch does the rest.
-#include "experts_internal.h"
+#include "four_bits.h"
 
 using namespace asgd;
 
@@ -39,6 +39,7 @@ bool blocks_ok(const asgd_blocks *m)
 {
     if (!m || !m->values || m->rows < 0 || m->rows > MOST_ROWS || m->cols < 1 || m->cols > MOST_COLS || m->count < 1) return false;
     if (m->form == ASGD_BLOCKS_RAW) return m->count == 1 && matrix_ok(m->values, m->type, m->rows, m->cols, m->stride);
+    if (m->form == ASGD_BLOCKS_FOURS) return m->scales && aligned(m->values, 16) && aligned(m->scales, 16) && m->count <= ASGD_ROUTE_MAX_EXPERTS;
     if (m->form != ASGD_BLOCKS_ROWS && m->form != ASGD_BLOCKS_SQUARES) return false;
     return m->scales && aligned(m->values, 16) && aligned(m->scales, 4) && (m->form == ASGD_BLOCKS_SQUARES || m->count == 1) && m->count <= ASGD_ROUTE_MAX_EXPERTS;
 }
@@ -48,6 +49,8 @@ bool product_ok(const asgd_blocks *a, const asgd_blocks *b, int mode, int exact,
 {
     if (!blocks_ok(a) || !blocks_ok(b) || a->cols != b->cols || b->rows < 1 || b->rows > MOST_COLS || b->form == ASGD_BLOCKS_RAW || a->form == ASGD_BLOCKS_SQUARES || (exact != 0 && exact != 1))
         return false;
+    const bool four = b->form == ASGD_BLOCKS_FOURS;
+    if (four ? a->form != ASGD_BLOCKS_RAW && (a->form != ASGD_BLOCKS_FOURS || a->count != 1) : a->form == ASGD_BLOCKS_FOURS) return false;
     out_rows = a->rows;
     if (mode == ASGD_PRODUCT_ALL) {
         if (order || b->count != 1) return false;
@@ -55,7 +58,7 @@ bool product_ok(const asgd_blocks *a, const asgd_blocks *b, int mode, int exact,
         if (!order_ok(order)) return false;
         const int64_t slots = order->T * order->k;
         if (mode == ASGD_PRODUCT_GATHER || mode == ASGD_PRODUCT_PLACES) {
-            if (b->form != ASGD_BLOCKS_SQUARES || b->count != order->E) return false;
+            if ((b->form != ASGD_BLOCKS_SQUARES && !four) || b->count != order->E) return false;
             if (a->rows != (mode == ASGD_PRODUCT_GATHER ? order->T : slots)) return false;
             out_rows = slots;
         } else if (mode == ASGD_PRODUCT_OVER) {
@@ -64,15 +67,18 @@ bool product_ok(const asgd_blocks *a, const asgd_blocks *b, int mode, int exact,
     }
     p = {};
     p.a = (const uint8_t *)a->values; p.b = (const uint8_t *)b->values; p.sa = a->scales; p.sb = b->scales;
-    p.rows_a = a->rows; p.rows_b = b->rows; p.kb = blocks8(a->cols); p.cols = a->cols; p.mode = mode; p.exact = exact;
+    p.rows_a = a->rows; p.rows_b = b->rows; p.kb = four ? runs4(a->cols) : blocks8(a->cols); p.cols = a->cols; p.mode = mode; p.exact = exact;
     if (order) p.order = *order;
     if (out_rows == 0) return true;
     if (a->form == ASGD_BLOCKS_RAW) {
         p.stride_raw = a->stride;
-        return b->form == ASGD_BLOCKS_SQUARES && out_rows <= (mode == ASGD_PRODUCT_ALL ? ASGD_PRODUCT_RAW_ROWS : ASGD_PRODUCT_RAW_SLOTS) && (mode == ASGD_PRODUCT_ALL || mode == ASGD_PRODUCT_GATHER);
+        return (b->form == ASGD_BLOCKS_SQUARES || four) && out_rows <= (mode == ASGD_PRODUCT_ALL ? ASGD_PRODUCT_RAW_ROWS : ASGD_PRODUCT_RAW_SLOTS) && (mode == ASGD_PRODUCT_ALL || mode == ASGD_PRODUCT_GATHER);
     }
     return !((double)blocks8(out_rows + (order ? (int64_t)BLOCK8 * order->E : 0)) * (mode == ASGD_PRODUCT_OVER ? order->E : 1) * blocks8(b->rows) > (double)(MOST_GROUPS / 2));      // (of 128 x 128: where thin, twice as many of 64 x 64)
 }
+
+// four neighbours of a row at a time
+bool four_wide(const void *out, int type, int64_t stride) { return stride % 4 == 0 && aligned(out, 4 * type_size(type)); }
 
 int done(hipError_t e) { return e == hipSuccess ? ASGD_OK : ASGD_EHIP; }
 
@@ -130,6 +136,7 @@ int asgd_block_quantize(const void *x, int type, int64_t rows, int64_t cols, int
                         const asgd_route_order *order, const float *weights, const asgd_blocks *out, void *hip_stream)
 {
     if (!type_ok(type) || rows < 0 || !blocks_ok(out) || out->form == ASGD_BLOCKS_RAW || (turned != 0 && turned != 1)) return ASGD_EINVAL;
+    if (out->form == ASGD_BLOCKS_FOURS && (turned || order)) return ASGD_EINVAL;
     if (order && (!order_ok(order) || out->form != ASGD_BLOCKS_ROWS || rows != order->T)) return ASGD_EINVAL;
     if (weights && (!order || !aligned(weights, 4))) return ASGD_EINVAL;
     const int64_t slots = order ? order->T * order->k : 0;
@@ -138,6 +145,11 @@ int asgd_block_quantize(const void *x, int type, int64_t rows, int64_t cols, int
     if (rows == 0) return ASGD_OK;
     if (!matrix_ok(x, type, rows, cols, stride) || (out->count > 1 && stride < cols)) return ASGD_EINVAL;
     if (out->rows != want_rows || out->cols != want_cols) return ASGD_EINVAL;
+    if (out->form == ASGD_BLOCKS_FOURS) {
+        if (rows * out->count > MOST_ROWS) return ASGD_EINVAL;
+        const FourArgs f = {x, rows * out->count, cols, rows > 1 || out->count == 1 ? stride : cols, (uint8_t *)out->values, (uint8_t *)out->scales};
+        return done(launch_quantize_four(f, type, (hipStream_t)hip_stream));
+    }
     QuantArgs q = {};
     q.x = x; q.rows = rows; q.cols = cols; q.stride = stride; q.count = out->count; q.values = (uint8_t *)out->values; q.scales = out->scales;
     q.out_rows = out->rows; q.out_blocks = blocks8(out->cols); q.weights = weights;
@@ -149,6 +161,15 @@ int asgd_block_quantize(const void *x, int type, int64_t rows, int64_t cols, int
     }
     if (turned && q.out_blocks > MOST_GROUPS) return ASGD_EINVAL;
     return done(turned ? launch_quantize_turned(q, type, s) : launch_quantize_rows(q, type, s));
+}
+
+int asgd_block_expand(const asgd_blocks *x, void *out, int type, int64_t stride, void *hip_stream)
+{
+    if (!type_ok(type) || !blocks_ok(x) || x->form != ASGD_BLOCKS_FOURS) return ASGD_EINVAL;
+    if (x->rows == 0) return ASGD_OK;
+    if (x->rows > MOST_ROWS / x->count || !matrix_ok(out, type, x->rows * x->count, x->cols, stride)) return ASGD_EINVAL;
+    const FourArgs f = {out, x->rows * x->count, x->cols, stride, (uint8_t *)x->values, (uint8_t *)x->scales};
+    return done(launch_expand_four(f, type, (hipStream_t)hip_stream));
 }
 
 int asgd_block_quantize_both(const void *x, int type, int64_t rows, int64_t cols, int64_t stride, const asgd_route_order *order,
@@ -179,6 +200,7 @@ int asgd_block_product(const asgd_blocks *a, const asgd_blocks *b, int mode, int
     if (!matrix_ok(out, type, out_rows, b->rows, stride) || (mode == ASGD_PRODUCT_OVER && stride < b->rows)) return ASGD_EINVAL;
     p.out = out; p.stride = stride;
     const hipStream_t s = (hipStream_t)hip_stream;
+    if (b->form == ASGD_BLOCKS_FOURS) return done(a->form == ASGD_BLOCKS_RAW ? launch_product_four_raw(p, a->type, type, s) : launch_product_four(p, type, s));
     return done(a->form == ASGD_BLOCKS_RAW ? launch_product_raw(p, a->type, type, s) : launch_product(p, b->form == ASGD_BLOCKS_SQUARES, type, s));
 }
 
@@ -187,17 +209,24 @@ int asgd_block_product_form(const asgd_blocks *a, const asgd_blocks *b, int mode
     ProductArgs p;
     int64_t out_rows;
     if (!product_ok(a, b, mode, exact, order, p, out_rows) || out_rows == 0) return ASGD_PRODUCT_FORM_NONE;
+    if (b->form == ASGD_BLOCKS_FOURS && a->form != ASGD_BLOCKS_RAW) return product_four_form(p);
     return a->form == ASGD_BLOCKS_RAW ? ASGD_PRODUCT_FORM_FEW : product_form(p, b->form == ASGD_BLOCKS_SQUARES);
 }
 
 int asgd_experts_direct(const asgd_blocks *x, const int32_t *ids, const float *weights, int k, const asgd_blocks *w, int exact,
                         void *out, int type, int64_t stride, void *hip_stream)
 {
-    if (!blocks_ok(x) || x->form != ASGD_BLOCKS_RAW || x->rows > ASGD_PRODUCT_RAW_ROWS || !blocks_ok(w) || w->form != ASGD_BLOCKS_SQUARES || w->cols != x->cols || w->rows < 1 || w->rows > MOST_COLS)
+    if (!blocks_ok(x) || x->form != ASGD_BLOCKS_RAW || x->rows > ASGD_PRODUCT_RAW_ROWS || !blocks_ok(w) || (w->form != ASGD_BLOCKS_SQUARES && w->form != ASGD_BLOCKS_FOURS) || w->cols != x->cols || w->rows < 1 || w->rows > MOST_COLS)
         return ASGD_EINVAL;
     if (k < 1 || k > ASGD_ROUTE_MAX_CHOSEN || !type_ok(type) || (exact != 0 && exact != 1)) return ASGD_EINVAL;
     if (x->rows == 0) return ASGD_OK;
     if (!ids || !weights || !aligned(ids, 4) || !aligned(weights, 4) || !matrix_ok(out, type, x->rows, w->rows, stride)) return ASGD_EINVAL;
+    if (w->form == ASGD_BLOCKS_FOURS) {
+        LayerArgs a = {};
+        a.x = x->values; a.x_stride = x->stride; a.T = (int)x->rows; a.k = k; a.E = w->count; a.ids = const_cast<int32_t *>(ids); a.weights = const_cast<float *>(weights);
+        a.down = *w; a.H = w->cols; a.N = w->rows; a.out = out; a.out_stride = stride; a.wide_out = four_wide(out, type, stride);
+        return done(launch_direct_four(a, x->type, type, (hipStream_t)hip_stream));
+    }
     ProductArgs p = {};
     p.a = (const uint8_t *)x->values; p.b = (const uint8_t *)w->values; p.sb = w->scales; p.rows_a = x->rows; p.rows_b = w->rows;
     p.kb = blocks8(x->cols); p.cols = x->cols; p.stride_raw = x->stride; p.out = out; p.stride = stride; p.exact = exact;
@@ -224,6 +253,35 @@ int asgd_experts_sum_backward(const void *d_out, int type, int64_t stride, const
     SumArgs a = {};
     a.y = y; a.d_out = d_out; a.n = n; a.y_stride = y_stride; a.order = *order; a.d_weights = d_weights; a.stride = stride;
     return done(launch_experts_sum_backward(a, y_type, type, (hipStream_t)hip_stream));
+}
+
+size_t asgd_experts_layer_bytes(int64_t rows, int k, int64_t H)
+{
+    if (rows < 0 || rows > ASGD_PRODUCT_RAW_ROWS || k < 1 || k > ASGD_ROUTE_MAX_CHOSEN || H < 1 || H > MOST_COLS / 2) return 0;
+    return layer_bytes(rows, k, H);
+}
+
+int asgd_experts_layer(const asgd_blocks *x, const void *logits, int logits_type, int64_t logits_stride, const float *bias,
+                       const asgd_route_rule *rule, const asgd_blocks *up, const asgd_blocks *down, int activation, int32_t *ids,
+                       float *weights, void *out, int type, int64_t stride, void *work, size_t work_bytes, void *hip_stream)
+{
+    if (!blocks_ok(x) || x->form != ASGD_BLOCKS_RAW || x->rows > ASGD_PRODUCT_RAW_ROWS || !blocks_ok(up) || !blocks_ok(down)) return ASGD_EINVAL;
+    if ((up->form != ASGD_BLOCKS_SQUARES && up->form != ASGD_BLOCKS_FOURS) || down->form != up->form || down->count != up->count || up->cols != x->cols) return ASGD_EINVAL;
+    if (down->rows < 1 || down->rows > MOST_COLS || up->rows > MOST_COLS || up->rows != 2 * down->cols || (activation != ASGD_ACTIVATION_SILU && activation != ASGD_ACTIVATION_GELU)) return ASGD_EINVAL;
+    if (!rule_ok(rule, up->count) || !type_ok(logits_type) || !type_ok(type)) return ASGD_EINVAL;
+    if (x->rows == 0) return ASGD_OK;
+    if (!matrix_ok(logits, logits_type, x->rows, up->count, logits_stride) || !matrix_ok(out, type, x->rows, down->rows, stride)) return ASGD_EINVAL;
+    if (!ids || !weights || !aligned(ids, 4) || !aligned(weights, 4) || !aligned(bias, 4)) return ASGD_EINVAL;
+    if (!work || !aligned(work, 16) || work_bytes < layer_bytes(x->rows, rule->k, down->cols)) return ASGD_EINVAL;
+    const hipStream_t s = (hipStream_t)hip_stream;
+    RouteArgs r = {};
+    r.logits = logits; r.bias = bias; r.ids = ids; r.weights = weights; r.T = x->rows; r.stride = logits_stride; r.E = up->count; r.rule = *rule;
+    const hipError_t e = launch_route(r, logits_type, s);
+    if (e != hipSuccess) return ASGD_EHIP;
+    LayerArgs a = {};
+    a.x = x->values; a.x_stride = x->stride; a.T = (int)x->rows; a.k = rule->k; a.E = up->count; a.ids = ids; a.weights = weights; a.up = *up; a.down = *down;
+    a.D = x->cols; a.H = down->cols; a.N = down->rows; a.activation = activation; a.h = (float *)work; a.out = out; a.out_stride = stride; a.wide_out = four_wide(out, type, stride);
+    return done(launch_layer(a, x->type, type, s));
 }
 
 }  // extern "C"

@@ -79,6 +79,37 @@ hipError_t launch_product(const ProductArgs &p, bool squares, int type, hipStrea
 hipError_t launch_product_direct(const ProductArgs &p, const int32_t *ids, const float *weights, int k, int E, int raw_type, int type, hipStream_t s);
 hipError_t launch_product_raw(const ProductArgs &p, int raw_type, int type, hipStream_t s);
 
+// 4 bits: x, rows of cols elements `stride` apart, to values and scales; or back, x written
+struct FourArgs {
+    const void *x;
+    int64_t rows, cols, stride;
+    uint8_t *values, *scales;
+};
+hipError_t launch_quantize_four(const FourArgs &q, int type, hipStream_t s);
+hipError_t launch_expand_four(const FourArgs &q, int type, hipStream_t s);
+// (kb counts runs of 256 columns; sa and sb are bytes)
+int product_four_form(const ProductArgs &p);
+hipError_t launch_product_four(const ProductArgs &p, int type, hipStream_t s);
+hipError_t launch_product_four_raw(const ProductArgs &p, int raw_type, int type, hipStream_t s);
+
+struct LayerArgs {
+    const void *x;
+    int64_t x_stride;
+    int T, k, E;
+    int32_t *ids;
+    float *weights;
+    asgd_blocks up, down;         // (direct: down alone, H columns of x)
+    int64_t D, H, N;
+    int activation;
+    float *h;                     // T * k rows of H
+    void *out;
+    int64_t out_stride;
+    bool wide_out;
+};
+size_t layer_bytes(int64_t T, int k, int64_t H);
+hipError_t launch_layer(const LayerArgs &a, int x_type, int type, hipStream_t s);       // after the routing
+hipError_t launch_direct_four(const LayerArgs &a, int x_type, int type, hipStream_t s);
+
 struct SumArgs {
     const void *y, *d_out;
     int64_t n, y_stride, stride;

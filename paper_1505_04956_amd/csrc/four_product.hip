@@ -1,0 +1,295 @@
+// Products of matrices in 4 bits, out[m, n] = sum over blocks of 32 of sa sb sum over the block's k of a[m, k] b[n, k], on the matrix cores
+// (v_mfma_f32_16x16x128_f8f6f4 with both operands e2m1): one instruction takes four blocks of 16 rows of each operand, their scales among its
+// operands, and adds to 32-bit sums.  What it adds is exact to 1.2e-7 of the products' magnitudes (measured; products of e2m1 numbers are multiples of
+// 1/4 up to 36, so that nothing of them is dropped where eight of them are aligned).  As in 8 bits rows of b are the instruction's rows, and a lane
+// holds four neighbours of one row of out.
+#include "four_bits.h"
+
+namespace asgd {
+
+namespace {
+
+// ---- many rows ----------------------------------------------------------------------------------------------------
+// A tile of TOK rows of a and WT rows of b; the waves are TOK_WAVES x WT_WAVES, each with I x J pieces of 16 x 16.  A stage in the LDS is a run of 256
+// columns of all rows, 128 bytes of values and 8 of scales each, filled straight from memory while the other is multiplied; sixteen-byte pieces of a row lie at their
+// number xor the row's low bits, so that the lanes of a read spread over the banks.
+template <int TOK, int WT> struct Stage4 {
+    static constexpr int VALUES = (TOK + WT) * RUN4_BYTES, BYTES = VALUES + (TOK + WT) * RUN4_SCALES;
+};
+
+template <int TOK, int WT, int TOK_WAVES, int WT_WAVES, bool GROUPED, class Out>
+__global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, TOK_WAVES * WT_WAVES <= 4 ? 1 : 2) void product_four_kernel(ProductArgs p, uint32_t tiles_tok, uint32_t tiles_wt, bool wide)
+{
+    typedef Stage4<TOK, WT> S;
+    constexpr int WAVES = TOK_WAVES * WT_WAVES, J = TOK / TOK_WAVES / 16, I = WT / WT_WAVES / 16;
+    constexpr int SEGMENTS = (TOK + WT) / 8 / WAVES;             // of eight rows, that a wave brings
+    constexpr int PIECES = (TOK + WT) / 32 / WAVES;              // of 32 rows' scales
+    static_assert((TOK + WT) % (32 * WAVES) == 0 && TOK % (16 * TOK_WAVES) == 0 && WT % (16 * WT_WAVES) == 0 && TOK % 32 == 0, "");
+    __shared__ __align__(16) uint8_t stage0[S::BYTES];
+    __shared__ __align__(16) uint8_t stage1[S::BYTES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave_tok = wave % TOK_WAVES * (J * 16), wave_wt = wave / TOK_WAVES * (I * 16);
+
+    // which tile: strips of eight tiles of a, all tiles of b for each
+    if (GROUPED) tiles_tok = p.order.blocks[p.order.E];
+    const uint32_t all = GROUPED ? tiles_tok * tiles_wt : gridDim.x;
+    if (blockIdx.x >= all) return;
+    const uint32_t id = tile_of_group(blockIdx.x, all);
+    const uint32_t strip = id / (8 * tiles_wt), in_strip = id - strip * 8 * tiles_wt;
+    const uint32_t high = min(tiles_tok - strip * 8, 8u), tile_wt = in_strip / high, tile_tok = strip * 8 + in_strip - tile_wt * high;
+
+    int64_t first = (int64_t)tile_tok * TOK, end = p.rows_a, matrix = 0;
+    const int64_t first_wt = (int64_t)tile_wt * WT;
+    if (GROUPED) {
+        static_assert(!GROUPED || TOK == BLOCK8, "");
+        int e;
+        if (!block_of_expert(p.order, tile_tok, e, first, end)) return;
+        matrix = e;
+    }
+    const int64_t row_bytes = p.kb * RUN4_BYTES, scale_bytes = p.kb * RUN4_SCALES;
+    const auto row_of_a = [&](int64_t r) {                        // (rows beyond the last: the last again)
+        r = r < end ? r : end - 1;
+        return GROUPED && p.mode == ASGD_PRODUCT_GATHER ? (int64_t)(p.order.slots[r] / p.order.k) : r;
+    };
+    const auto row_of_b = [&](int64_t r) { return r < p.rows_b ? r : p.rows_b - 1; };
+
+    // Where a lane's pieces come from, in bytes from the tile's first row (gathered rows of a may be further apart than 2^32)
+    typedef typename std::conditional<GROUPED, uint64_t, uint32_t>::type Offset;
+    Offset from[SEGMENTS], scale_from[PIECES];
+    const int64_t base_a = GROUPED ? 0 : first, base_b = matrix * p.rows_b + first_wt;
+    const uint8_t *const a_base = p.a + base_a * row_bytes, *const b_base = p.b + base_b * row_bytes;
+    const uint8_t *const sa_base = (const uint8_t *)p.sa + base_a * scale_bytes, *const sb_base = (const uint8_t *)p.sb + base_b * scale_bytes;
+#pragma unroll
+    for (int s = 0; s < SEGMENTS; s++) {
+        const int row = (wave * SEGMENTS + s) * 8 + (lane >> 3), piece = (lane & 7) ^ (lane >> 3);
+        const int64_t r = row < TOK ? row_of_a(first + row) - base_a : row_of_b(first_wt + row - TOK) - first_wt;
+        from[s] = (Offset)(r * row_bytes + piece * 16);
+    }
+#pragma unroll
+    for (int s = 0; s < PIECES; s++) {
+        const int row = (wave * PIECES + s) * 32 + (lane >> 1);
+        const int64_t r = row < TOK ? row_of_a(first + row) - base_a : row_of_b(first_wt + row - TOK) - first_wt;
+        scale_from[s] = (Offset)(r * scale_bytes + (lane & 1) * 4);
+    }
+    const auto bring = [&](int kb, uint8_t *stage) {
+#pragma unroll
+        for (int l = 0; l < SEGMENTS; l++) {
+            const int segment = wave * SEGMENTS + l;
+            to_lds((segment * 8 < TOK ? a_base : b_base) + (int64_t)kb * RUN4_BYTES, from[l], stage + segment * 1024);
+        }
+#pragma unroll
+        for (int l = 0; l < PIECES; l++) {
+            const int piece = wave * PIECES + l;
+            to_lds4((piece * 32 < TOK ? sa_base : sb_base) + (int64_t)kb * RUN4_SCALES, scale_from[l], stage + S::VALUES + piece * 256);
+        }
+    };
+
+    v4f sum[I][J];
+#pragma unroll
+    for (int i = 0; i < I; i++)
+#pragma unroll
+        for (int j = 0; j < J; j++) sum[i][j] = {0.0f, 0.0f, 0.0f, 0.0f};
+
+    const int low = ((lane >> 4) ^ (lane & 7)) * 16;
+    const int at_a = (wave_tok + (lane & 15)) * RUN4_BYTES + low, at_w = (TOK + wave_wt + (lane & 15)) * RUN4_BYTES + low;
+    const int at_sa = S::VALUES + (wave_tok + (lane & 15)) * RUN4_SCALES + (lane >> 4), at_sb = S::VALUES + (TOK + wave_wt + (lane & 15)) * RUN4_SCALES + (lane >> 4);
+    struct Raw { v4i v; uint32_t scale; };
+    const auto operand = [&](const uint8_t *stage, int at, int at_scale, int half, int piece) {
+        return Raw{*(const v4i *)(stage + (at ^ half * 64) + piece * 16 * RUN4_BYTES), stage[at_scale + half * 4 + piece * 16 * RUN4_SCALES]};
+    };
+    // Multiplies the run in `stage` and brings run `next` to `other`.  Sixteen rows of b are read from the LDS while those before are multiplied, and the
+    // second half's rows of a during the first half.
+    const auto multiply = [&](const uint8_t *stage, int next, uint8_t *other) {
+        Raw a[2][J], after = operand(stage, at_w, at_sb, 0, 0);
+#pragma unroll
+        for (int j = 0; j < J; j++) a[0][j] = operand(stage, at_a, at_sa, 0, j);
+        bring(next, other);
+#pragma unroll
+        for (int q = 0; q < 2 * I; q++) {
+            const int half = q / I, i = q % I;
+            const Raw w = after;
+            if (q + 1 < 2 * I) after = operand(stage, at_w, at_sb, (q + 1) / I, (q + 1) % I);
+            if (half == 0)
+#pragma unroll
+                for (int j = i * J / I; j < (i + 1) * J / I; j++) a[1][j] = operand(stage, at_a, at_sa, 1, j);
+#pragma unroll
+            for (int j = 0; j < J; j++) sum[i][j] = four_product(w.v, w.scale, a[half][j].v, a[half][j].scale, sum[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // This stage's loads have arrived, and all waves are done with the other, whose place the next run takes.
+    const auto arrive = [&] {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(7 << 4);                       // (vmcnt and lgkmcnt, to zero)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    const int n = (int)p.kb;
+    bring(0, stage0);
+    for (int kb = 0; kb < n; kb += 2) {
+        arrive();
+        multiply(stage0, min(kb + 1, n - 1), stage1);
+        arrive();
+        if (kb + 1 < n) multiply(stage1, min(kb + 2, n - 1), stage0);
+    }
+    arrive();
+
+    // Out through the LDS, sixteen rows of a at a time, in whole lines
+    typedef typename Out::T T;
+    constexpr int ROW = I * 16 * sizeof(T), PITCH = ROW + 16, PER_ROW = ROW / 16, ROWS = 64 / PER_ROW;       // bytes; lanes of a row, rows of an instruction
+    T *out = (T *)p.out;
+    constexpr int HALF = (WAVES + 1) / 2;
+    static_assert(HALF * 16 * PITCH <= S::BYTES, "");
+    uint8_t *mine = (wave < HALF ? stage0 : stage1) + (wave < HALF ? wave : wave - HALF) * 16 * PITCH;
+#pragma unroll
+    for (int j = 0; j < J; j++) {
+#pragma unroll
+        for (int i = 0; i < I; i++) {
+            T u[4] = {(T)sum[i][j][0], (T)sum[i][j][1], (T)sum[i][j][2], (T)sum[i][j][3]};
+            uint8_t *to = mine + (lane & 15) * PITCH + (i * 16 + (lane >> 4) * 4) * sizeof(T);
+            if constexpr (sizeof(T) == 4) *(uint4 *)to = *(uint4 *)u;
+            else *(uint2 *)to = *(uint2 *)u;
+        }
+        __builtin_amdgcn_wave_barrier();
+        __threadfence_block();
+#pragma unroll
+        for (int m = 0; m < 16 / ROWS; m++) {
+            const int row = m * ROWS + lane / PER_ROW, at = lane % PER_ROW * 16;
+            const int64_t r = first + wave_tok + j * 16 + row, c = first_wt + wave_wt + at / sizeof(T);
+            const v4i v = *(const v4i *)(mine + row * PITCH + at);
+            if (r < end) store16<T>(out + r * p.stride + c, p.rows_b - c, wide, v);
+        }
+        __builtin_amdgcn_wave_barrier();
+        __threadfence_block();
+    }
+}
+
+// ---- few rows -----------------------------------------------------------------------------------------------------
+// The weights go from memory to registers, sixteen rows of a run of 256 columns a wave, and the eight waves of a workgroup share the runs of the
+// contraction of sixteen rows of b.  Rows of a, J times sixteen, come from the caches; RAW ones are brought to 4 bits in the lanes that need them.
+constexpr int FEW4_WAVES = 8;
+
+// grid: strips of sixteen rows of b, tiles of 16 * J rows of a
+template <class In, int J, class Out> __global__ __launch_bounds__(64 * FEW4_WAVES) void product_four_few_kernel(ProductArgs p, bool wide_in, bool wide)
+{
+    constexpr bool RAW = !std::is_same<In, void>::value;
+    __shared__ v4f parts[FEW4_WAVES][J][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t strip = blockIdx.x;
+    int64_t matrix = 0, first = (int64_t)blockIdx.y * (16 * J), end = p.rows_a;
+    if (p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES) {
+        int e;
+        if (!tile_of_expert(p.order, blockIdx.y, 16 * J, e, first, end)) return;
+        matrix = e;
+    }
+    const int tok = lane & 15, quarter = lane >> 4;
+    int64_t src[J];
+#pragma unroll
+    for (int j = 0; j < J; j++) {
+        const int64_t r = first + j * 16 + tok < end ? first + j * 16 + tok : end - 1;       // (rows beyond the last: the last again)
+        src[j] = p.mode == ASGD_PRODUCT_GATHER ? p.order.slots[r] / p.order.k : r;
+    }
+    const int64_t r = strip * 16 + tok, row_b = matrix * p.rows_b + (r < p.rows_b ? r : p.rows_b - 1);
+    const uint8_t *b = p.b + row_b * p.kb * RUN4_BYTES + quarter * 16, *sb = (const uint8_t *)p.sb + row_b * p.kb * RUN4_SCALES + quarter;
+    v4f sum[J];
+#pragma unroll
+    for (int j = 0; j < J; j++) sum[j] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int64_t kb = wave; kb < p.kb; kb += FEW4_WAVES) {
+        v4i w[2];
+        uint32_t scale_b[2];
+        RawFour<In> raw[2];
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+            w[half] = *(const v4i *)(b + kb * RUN4_BYTES + half * 64);
+            scale_b[half] = sb[kb * RUN4_SCALES + half * 4];
+            if constexpr (RAW) raw[half].load((const typename In::T *)p.a + src[0] * p.stride_raw, true, wide_in, kb * RUN4 + half * 128 + quarter * 32, p.cols);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; half++)
+#pragma unroll
+            for (int j = 0; j < J; j++) {
+                v4i a;
+                uint32_t scale_a;
+                if constexpr (RAW) raw[half].set(true, scale_a, a);
+                else {
+                    a = *(const v4i *)(p.a + src[j] * p.kb * RUN4_BYTES + kb * RUN4_BYTES + half * 64 + quarter * 16);
+                    scale_a = ((const uint8_t *)p.sa)[src[j] * p.kb * RUN4_SCALES + kb * RUN4_SCALES + half * 4 + quarter];
+                }
+                sum[j] = four_product(w[half], scale_b[half], a, scale_a, sum[j]);
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < J; j++) parts[wave][j][lane] = sum[j];
+    __syncthreads();
+    for (int n = wave; n < J; n += FEW4_WAVES) {
+        v4f total = parts[0][n][lane];
+#pragma unroll
+        for (int w = 1; w < FEW4_WAVES; w++) total += parts[w][n][lane];
+        const int64_t row = first + n * 16 + tok, c = strip * 16 + quarter * 4;
+        if (row < end) store_four<Out>((typename Out::T *)p.out + row * p.stride + c, p.rows_b - c, wide, total);
+    }
+}
+
+// places in use by `slots` slots of E experts, each expert's rounded up to whole tiles: what there can be at most
+int64_t most_tiles4(int64_t slots, int64_t E, int rows) { return slots / rows + (slots < E ? slots : E); }
+
+bool grouped4(const ProductArgs &p) { return p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES; }
+
+// rows of a (of an expert, on average)
+int64_t rows_each4(const ProductArgs &p) { return grouped4(p) ? p.order.T * p.order.k / p.order.E : p.rows_a; }
+
+template <int N> using Int = std::integral_constant<int, N>;
+
+}  // namespace
+
+int product_four_form(const ProductArgs &p)
+{
+    if (rows_each4(p) <= 32) return ASGD_PRODUCT_FORM_FEW;
+    if (grouped4(p)) return ASGD_PRODUCT_FORM_TILES_128;
+    const int64_t tiles = ((p.rows_a + 255) / 256) * ((p.rows_b + 255) / 256);
+    return tiles >= 256 ? ASGD_PRODUCT_FORM_TILES_256 : ASGD_PRODUCT_FORM_TILES_128;
+}
+
+hipError_t launch_product_four(const ProductArgs &p, int type, hipStream_t s)
+{
+    const bool grouped = grouped4(p);
+    const int form = product_four_form(p);
+    const bool wide4 = p.stride % 4 == 0 && (uintptr_t)p.out % (4 * type_size(type)) == 0;
+    const bool wide16 = p.stride * type_size(type) % 16 == 0 && (uintptr_t)p.out % 16 == 0;
+    const auto tiles_of = [&](int tok) { return grouped ? most_tiles4(p.order.T * p.order.k, p.order.E, tok) : (p.rows_a + tok - 1) / tok; };
+    return with_type(type, [&](auto out) {
+        typedef decltype(out) Out;
+        const auto few = [&](auto j) {
+            constexpr int J = decltype(j)::value;
+            product_four_few_kernel<void, J, Out><<<dim3((unsigned)((p.rows_b + 15) / 16), (unsigned)tiles_of(16 * J)), 64 * FEW4_WAVES, 0, s>>>(p, false, wide4);
+            return hipGetLastError();
+        };
+        const auto tiles = [&](auto tok, auto wt, auto waves_tok, auto waves_wt, auto by_expert) {
+            constexpr int TOK = decltype(tok)::value, WT = decltype(wt)::value, WAVES = decltype(waves_tok)::value * decltype(waves_wt)::value;
+            const int64_t tiles_tok = tiles_of(TOK), tiles_wt = (p.rows_b + WT - 1) / WT;
+            product_four_kernel<TOK, WT, decltype(waves_tok)::value, decltype(waves_wt)::value, decltype(by_expert)::value, Out>
+                <<<(unsigned)(tiles_tok * tiles_wt), 64 * WAVES, 0, s>>>(p, (uint32_t)tiles_tok, (uint32_t)tiles_wt, wide16);
+            return hipGetLastError();
+        };
+        if (form == ASGD_PRODUCT_FORM_FEW) return rows_each4(p) <= 16 ? few(Int<1>()) : few(Int<2>());
+        if (grouped) return tiles(Int<128>(), Int<128>(), Int<2>(), Int<2>(), std::true_type());
+        if (form == ASGD_PRODUCT_FORM_TILES_256) return tiles(Int<256>(), Int<256>(), Int<4>(), Int<2>(), std::false_type());
+        return tiles(Int<128>(), Int<128>(), Int<2>(), Int<2>(), std::false_type());
+    });
+}
+
+hipError_t launch_product_four_raw(const ProductArgs &p, int raw_type, int type, hipStream_t s)
+{
+    const bool wide = p.stride % 4 == 0 && (uintptr_t)p.out % (4 * type_size(type)) == 0;
+    const bool wide_in = p.stride_raw * (int64_t)type_size(raw_type) % 16 == 0 && ((uintptr_t)p.a & 15) == 0;
+    const unsigned strips = (unsigned)((p.rows_b + 15) / 16), tiles = grouped4(p) ? (unsigned)most_tiles4(p.order.T * p.order.k, p.order.E, 16) : 1u;
+    return with_type(raw_type, [&](auto in) {
+        return with_type(type, [&](auto out) {
+            product_four_few_kernel<decltype(in), 1, decltype(out)><<<dim3(strips, tiles), 64 * FEW4_WAVES, 0, s>>>(p, wide_in, wide);
+            return hipGetLastError();
+        });
+    });
+}
+
+}  // namespace asgd

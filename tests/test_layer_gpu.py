@@ -1,0 +1,202 @@
+"""A whole layer of experts for few rows on the GPU, against 64 bits; and the calls of experts, 4 bits, layers and gradients together."""
+import pytest
+import torch
+
+from tests import experts_rules as R
+from tests import micro_rules as Q
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+ROUNDING = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+SMALLEST = {torch.float32: 1e-37, torch.bfloat16: 1e-37, torch.float16: 6e-8}
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a HIP device; there is no CPU fallback")
+    from paper_1505_04956_amd import layer
+    return layer
+
+
+def make(L, T, E, D, H, N, bits, dtype, seed):
+    """(x, logits, up, down, their matrices in 64 bits)"""
+    from paper_1505_04956_amd import experts as X, micro as M
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn(T, D, generator=g) * torch.exp(torch.randn(D, generator=g) * 0.5)).to(dtype)
+    logits = torch.randn(T, E, generator=g) * 2
+    up, down = torch.randn(E, 2 * H, D, generator=g) / D ** 0.5, torch.randn(E, N, H, generator=g) / H ** 0.5
+    if bits == 4:
+        mu, md = M.quantize(up.cuda()), M.quantize(down.cuda())
+        return x, logits, mu, md, Q.matrix_of(mu), Q.matrix_of(md)
+    mu, md = X.quantize_weights(up.cuda()), X.quantize_weights(down.cuda())
+    of = lambda m: torch.stack([R.from_squares(v, s)[:, :m.cols] for v, s in zip(m.values.cpu(), m.scales.cpu())])  # noqa: E731
+    return x, logits, mu, md, of(mu), of(md)
+
+
+def close(got, want, bound, dtype):
+    off = (got.cpu().double() - want).abs()
+    allowed = bound + ROUNDING[dtype] * (want.abs() + bound) + SMALLEST[dtype]
+    assert (off <= allowed).all(), float((off / allowed).max())
+
+
+SHAPES = [(1, 8, 2, 64, 32, 48), (1, 64, 6, 300, 200, 130), (2, 5, 5, 257, 129, 100), (5, 100, 5, 100, 70, 33), (15, 9, 2, 513, 260, 17), (16, 40, 3, 128, 128, 256),
+          (16, 7, 7, 1000, 40, 1), (3, 300, 8, 33, 1, 20), (1, 1, 1, 1, 1, 1), (4, 1024, 20, 40, 24, 16), (2, 64, 64, 40, 24, 16)]
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,E,k,D,H,N", SHAPES)
+def test_layers(L, T, E, k, D, H, N, dtype, bits):
+    from paper_1505_04956_amd import experts as X
+    x, logits, up, down, u64, d64 = make(L, T, E, D, H, N, bits, dtype, T * E + D)
+    gelu = (T + E + D) % 2 == 1
+    rule = X.Rule(k, score=X.SIGMOID if T % 2 else X.SOFTMAX, scale=1.5, renormalize=D % 2 == 0)
+    bias = (torch.randn(E, generator=torch.Generator().manual_seed(E)) * 0.1).cuda() if T % 2 else None
+    if T > 2:
+        logits[1] = -float("inf")
+        logits[2, 1:] = -float("inf")
+    y, ids, weights = L.layer(x.cuda(), logits.cuda(), rule, up, down, bias=bias, activation=L.GELU if gelu else L.SILU)
+    i2, w2 = X.route(logits.cuda(), rule, bias=bias)
+    assert torch.equal(ids, i2) and torch.equal(weights, w2) and y.dtype == dtype and y.shape == (T, N)
+    if T > 2:
+        assert (ids[1] == -1).all() and (y[1] == 0).all() and (ids[2, 0] == 0) and (ids[2, 1:] == -1).all()
+    want, bound = Q.layer(x.float(), ids.cpu(), weights.cpu(), u64, d64, bits, gelu)
+    close(y, want, bound, dtype)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_logits_of_every_type_and_strides(L, bits):
+    from paper_1505_04956_amd import experts as X
+    x, logits, up, down, _, _ = make(L, 6, 12, 100, 40, 30, bits, torch.float16, 1)
+    wide_x, wide_l = torch.full((6, 300), 9.0, dtype=torch.float16).cuda(), torch.full((12, 31), 50.0).cuda()
+    wide_x[:, 5:105], wide_l[::2, 3:15] = x.cuda(), logits.cuda()
+    rule = X.Rule(3)
+    want = L.layer(x.cuda(), logits.cuda(), rule, up, down)
+    got = L.layer(wide_x[:, 5:105], wide_l[::2, 3:15], rule, up, down)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    for dtype in (torch.bfloat16, torch.float16):
+        l = logits.to(dtype).cuda()
+        got, want = L.layer(x.cuda(), l, rule, up, down), L.layer(x.cuda(), l.float(), rule, up, down)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_what_is_not_a_number_stays_with_its_rows(L, bits):
+    from paper_1505_04956_amd import experts as X
+    x, logits, up, down, _, _ = make(L, 7, 6, 300, 140, 50, bits, torch.float32, 2)
+    rule = X.Rule(2)
+    want, ids, _ = L.layer(x.cuda(), logits.cuda(), rule, up, down)
+    bad = x.clone()
+    bad[1, 17], bad[4, 299] = float("nan"), float("inf")
+    y, _, _ = L.layer(bad.cuda(), logits.cuda(), rule, up, down)
+    others = [0, 2, 3, 5, 6]
+    assert torch.isnan(y[[1, 4]]).all() and torch.equal(y[others], want[others])
+    # scales of one expert's weights
+    for m in (up, down):
+        kept = m.scales.clone()
+        if bits == 4:
+            m.scales[3, 0, 0] = 255
+        else:
+            m.scales[3, 0, 0] = float("nan")
+        y, _, _ = L.layer(x.cuda(), logits.cuda(), rule, up, down)
+        goes = (ids == 3).any(1)
+        assert goes.any() and not goes.all()
+        assert torch.isnan(y[goes]).any(1).all() and torch.equal(y[~goes], want[~goes])
+        m.scales.copy_(kept)
+    # a logit
+    bad = logits.clone()
+    bad[2, 3] = float("nan")
+    y, i, w = L.layer(x.cuda(), bad.cuda(), rule, up, down)
+    assert torch.isnan(w[2][i[2] >= 0]).all() and torch.isnan(y[2]).all() and torch.equal(y[[0, 1, 3, 4, 5, 6]], want[[0, 1, 3, 4, 5, 6]])
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("T", [1, 5, 16])
+def test_the_same_as_the_calls_that_it_stands_for(L, T, bits):
+    from paper_1505_04956_amd import experts as X, micro as M
+    D, H, N, E, k = 200, 96, 70, 6, 2
+    x, logits, up, down, _, _ = make(L, T, E, D, H, N, bits, torch.float32, 3)
+    rule = X.Rule(k)
+    y, ids, weights = L.layer(x.cuda(), logits.cuda(), rule, up, down)
+    order = X.plan(ids, E)
+    P = M if bits == 4 else X
+    u = P.product(P.quantize(x.cuda()), up, torch.float32, order, gather=True)
+    h = torch.nn.functional.silu(u[:, :H]) * u[:, H:]
+    z = X.experts_sum(P.product(P.quantize(h), down, torch.float32, order), order, torch.float32, weights)
+    # a value of h next to a border may be rounded the other way: one of 96, by a step of at most a quarter of it
+    assert ((y - z).norm(dim=1) <= 0.05 * z.norm(dim=1)).all() and (y - z).norm() <= 0.02 * z.norm()
+
+
+def test_no_rows(L):
+    from paper_1505_04956_amd import experts as X
+    x, logits, up, down, _, _ = make(L, 1, 6, 100, 40, 30, 8, torch.float32, 1)
+    y, ids, weights = L.layer(x[:0].cuda(), logits[:0].cuda(), X.Rule(2), up, down)
+    assert y.shape == (0, 30) and ids.shape == weights.shape == (0, 2)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_two_streams_and_graphs(L, bits):
+    """Two captured calls and an eager one, each with scratch of its own, on streams of their own."""
+    from paper_1505_04956_amd import experts as X
+    x, logits, up, down, _, _ = make(L, 16, 20, 300, 128, 90, bits, torch.bfloat16, 4)
+    x, logits, rule = x.cuda(), logits.cuda(), X.Rule(4, score=X.SIGMOID)
+    a, b = (x[:9].clone(), logits[:9].clone()), (x[9:].clone(), logits[9:].clone())
+    want = [[t.clone() for t in L.layer(*c, rule, up, down)] for c in (a, b)]
+    graphs, held = [], []
+    for c in (a, b):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            held.append(L.layer(*c, rule, up, down))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for n in range(3):
+        for h in held:
+            for t in h:
+                t.zero_()
+        torch.cuda.synchronize()
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        eager = L.layer(*a, rule, up, down)
+        torch.cuda.synchronize()
+        for h, w in zip(held + [eager], want + want[:1]):
+            assert all(torch.equal(p, q) for p, q in zip(h, w))
+
+
+def test_trained_with_clipped_gradients_then_served(L):
+    """As the calls are used: experts are trained in 8 bits with clipped gradients, brought to 4 bits, and serve prompts and single rows; and
+    a layer of two matrices made of them serves a few rows."""
+    from paper_1505_04956_amd import experts as X, gradients as G, micro as M
+    g = torch.Generator().manual_seed(5)
+    T, E, D, N, k = 400, 6, 96, 80, 2
+    x, logits = torch.randn(T, D, generator=g).bfloat16().cuda(), torch.randn(T, E, generator=g).cuda()
+    w, target = (torch.randn(E, N, D, generator=g) / D ** 0.5).cuda(), torch.randn(T, N, generator=g).cuda()
+    rule = X.Rule(k)
+    ids, weights = X.route(logits, rule)
+    for _ in range(3):
+        y, kept = X.experts(x, ids, weights, X.quantize_weights(w), train=True)
+        d_y = ((y.float() - target) / T).bfloat16()
+        _, d_w, d_weights = X.experts_backward(d_y, kept, X.quantize_weights(w, turned=True))
+        d_logits = X.route_backward(logits, rule, ids, d_weights)
+        plain = torch.sqrt((d_w.double() ** 2).sum() + (d_logits.double() ** 2).sum())
+        was, limit = [d_w.clone(), d_logits.clone()], float(plain) / 3
+        norm = G.clip([d_w, d_logits], limit)
+        assert abs(norm.item() - plain.item()) <= 1e-6 * plain.item()
+        for a, b in zip((d_w, d_logits), was):
+            assert (a.double() - b.double() * (limit / plain)).abs().max() <= 3e-7 * b.abs().max()
+        w -= 0.1 * d_w
+    small = M.quantize(w)
+    many = M.experts(x, ids, weights, small)
+    few = M.experts(x[:10], ids[:10], weights[:10], small)
+    v = M.expand(small).cpu().double()
+    q = Q.four(x[:10].cpu().float())
+    c = weights[:10].cpu().double()
+    want = torch.stack([sum(c[t, j] * (v[ids[t, j]] @ q[t]) for j in range(k)) for t in range(10)])
+    for got in (many[:10], few):
+        assert (got.cpu().double() - want).abs().max() <= 2.0 ** -8 * want.abs().max() + 1e-5
+    up = M.quantize(torch.cat([w, w], 1).contiguous())                    # h = f(w x) * w x
+    down = M.quantize(w.transpose(1, 2).contiguous())
+    y, i, c = L.layer(x[:10], logits[:10], rule, up, down)
+    assert torch.equal(i, ids[:10]) and torch.equal(c, weights[:10])
+    want, bound = Q.layer(x[:10].cpu().float(), i.cpu(), c.cpu(), Q.matrix_of(up), Q.matrix_of(down), 4, False)
+    close(y, want, bound, torch.bfloat16)
