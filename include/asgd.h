@@ -466,7 +466,7 @@ int asgd_experts_sum_backward(const void *d_out, int type, int64_t stride, const
  * scratch, 16-byte aligned, of one call at a time.
  */
 enum { ASGD_ACTIVATION_SILU = 0, ASGD_ACTIVATION_GELU = 1 };
-size_t asgd_experts_layer_bytes(int64_t rows, int k, int64_t H);
+size_t asgd_experts_layer_bytes(int64_t rows, int k, int E, int64_t D, int64_t H);
 int asgd_experts_layer(const asgd_blocks *x, const void *logits, int logits_type, int64_t logits_stride, const float *bias,
                        const asgd_route_rule *rule, const asgd_blocks *up, const asgd_blocks *down, int activation, int32_t *ids,
                        float *weights, void *out, int type, int64_t stride, void *work, size_t work_bytes, void *hip_stream);

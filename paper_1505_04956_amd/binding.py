@@ -128,7 +128,7 @@ def lib():
             "asgd_experts_sum": (C.c_int, [vp, C.c_int, i64, i64, vp, vp, vp, C.c_int, i64, vp]),
             "asgd_experts_sum_backward": (C.c_int, [vp, C.c_int, i64, vp, C.c_int, i64, i64, vp, vp, vp]),
             "asgd_block_expand": (C.c_int, [vp, vp, C.c_int, i64, vp]),
-            "asgd_experts_layer_bytes": (C.c_size_t, [i64, C.c_int, i64]),
+            "asgd_experts_layer_bytes": (C.c_size_t, [i64, C.c_int, C.c_int, i64, i64]),
             "asgd_experts_layer": (C.c_int, [vp, vp, C.c_int, i64, vp, vp, vp, vp, C.c_int, vp, vp, vp, C.c_int, i64, vp, C.c_size_t, vp]),
             "asgd_gradient_bytes": (C.c_size_t, [vp, i64]),
             "asgd_gradient_norm": (C.c_int, [vp, i64, vp, vp, C.c_size_t, vp]),
@@ -316,8 +316,8 @@ def asgd_block_expand(x, out_ptr, type, stride, stream=0):
     _check(lib().asgd_block_expand(C.addressof(x), out_ptr, type, stride, stream), "asgd_block_expand")
 
 
-def asgd_experts_layer_bytes(rows, k, H) -> int:
-    return int(lib().asgd_experts_layer_bytes(rows, k, H))
+def asgd_experts_layer_bytes(rows, k, E, D, H) -> int:
+    return int(lib().asgd_experts_layer_bytes(rows, k, E, D, H))
 
 
 def asgd_experts_layer(x, logits_ptr, logits_type, logits_stride, bias_ptr, rule, up, down, activation, ids_ptr, weights_ptr, out_ptr, type,

@@ -222,9 +222,7 @@ int asgd_experts_direct(const asgd_blocks *x, const int32_t *ids, const float *w
     if (x->rows == 0) return ASGD_OK;
     if (!ids || !weights || !aligned(ids, 4) || !aligned(weights, 4) || !matrix_ok(out, type, x->rows, w->rows, stride)) return ASGD_EINVAL;
     if (w->form == ASGD_BLOCKS_FOURS) {
-        LayerArgs a = {};
-        a.x = x->values; a.x_stride = x->stride; a.T = (int)x->rows; a.k = k; a.E = w->count; a.ids = const_cast<int32_t *>(ids); a.weights = const_cast<float *>(weights);
-        a.down = *w; a.H = w->cols; a.N = w->rows; a.out = out; a.out_stride = stride; a.wide_out = four_wide(out, type, stride);
+        const DirectArgs a = {x->values, x->stride, x->cols, w->rows, (int)x->rows, k, w->count, ids, weights, *w, out, stride, four_wide(out, type, stride)};
         return done(launch_direct_four(a, x->type, type, (hipStream_t)hip_stream));
     }
     ProductArgs p = {};
@@ -255,10 +253,10 @@ int asgd_experts_sum_backward(const void *d_out, int type, int64_t stride, const
     return done(launch_experts_sum_backward(a, y_type, type, (hipStream_t)hip_stream));
 }
 
-size_t asgd_experts_layer_bytes(int64_t rows, int k, int64_t H)
+size_t asgd_experts_layer_bytes(int64_t rows, int k, int E, int64_t D, int64_t H)
 {
-    if (rows < 0 || rows > ASGD_PRODUCT_RAW_ROWS || k < 1 || k > ASGD_ROUTE_MAX_CHOSEN || H < 1 || H > MOST_COLS / 2) return 0;
-    return layer_bytes(rows, k, H);
+    if (rows < 0 || rows > ASGD_PRODUCT_RAW_ROWS || k < 1 || k > ASGD_ROUTE_MAX_CHOSEN || E < 1 || E > ASGD_ROUTE_MAX_EXPERTS || D < 1 || D > MOST_COLS || H < 1 || H > MOST_COLS / 2) return 0;
+    return layer_bytes(rows, k, E, D, H);
 }
 
 int asgd_experts_layer(const asgd_blocks *x, const void *logits, int logits_type, int64_t logits_stride, const float *bias,
@@ -272,16 +270,13 @@ int asgd_experts_layer(const asgd_blocks *x, const void *logits, int logits_type
     if (x->rows == 0) return ASGD_OK;
     if (!matrix_ok(logits, logits_type, x->rows, up->count, logits_stride) || !matrix_ok(out, type, x->rows, down->rows, stride)) return ASGD_EINVAL;
     if (!ids || !weights || !aligned(ids, 4) || !aligned(weights, 4) || !aligned(bias, 4)) return ASGD_EINVAL;
-    if (!work || !aligned(work, 16) || work_bytes < layer_bytes(x->rows, rule->k, down->cols)) return ASGD_EINVAL;
-    const hipStream_t s = (hipStream_t)hip_stream;
+    if (!work || !aligned(work, 16) || work_bytes < layer_bytes(x->rows, rule->k, up->count, x->cols, down->cols)) return ASGD_EINVAL;
     RouteArgs r = {};
-    r.logits = logits; r.bias = bias; r.ids = ids; r.weights = weights; r.T = x->rows; r.stride = logits_stride; r.E = up->count; r.rule = *rule;
-    const hipError_t e = launch_route(r, logits_type, s);
-    if (e != hipSuccess) return ASGD_EHIP;
+    r.logits = logits; r.bias = bias; r.T = x->rows; r.stride = logits_stride; r.E = up->count; r.rule = *rule;
     LayerArgs a = {};
-    a.x = x->values; a.x_stride = x->stride; a.T = (int)x->rows; a.k = rule->k; a.E = up->count; a.ids = ids; a.weights = weights; a.up = *up; a.down = *down;
-    a.D = x->cols; a.H = down->cols; a.N = down->rows; a.activation = activation; a.h = (float *)work; a.out = out; a.out_stride = stride; a.wide_out = four_wide(out, type, stride);
-    return done(launch_layer(a, x->type, type, s));
+    a.x = x->values; a.x_stride = x->stride; a.D = x->cols; a.H = down->cols; a.N = down->rows; a.x_type = x->type; a.T = (int)x->rows; a.k = rule->k; a.E = up->count;
+    a.activation = activation; a.up = *up; a.down = *down; a.ids = ids; a.weights = weights; a.out = out; a.out_stride = stride; a.wide_out = four_wide(out, type, stride);
+    return done(launch_layer(a, r, logits_type, type, work, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"

@@ -94,21 +94,29 @@ hipError_t launch_product_four_raw(const ProductArgs &p, int raw_type, int type,
 
 struct LayerArgs {
     const void *x;
-    int64_t x_stride;
-    int T, k, E;
+    int64_t x_stride, D, H, N;
+    int x_type, T, k, E, activation;
+    asgd_blocks up, down;
     int32_t *ids;
     float *weights;
-    asgd_blocks up, down;         // (direct: down alone, H columns of x)
-    int64_t D, H, N;
-    int activation;
-    float *h;                     // T * k rows of H
     void *out;
     int64_t out_stride;
     bool wide_out;
 };
-size_t layer_bytes(int64_t T, int k, int64_t H);
-hipError_t launch_layer(const LayerArgs &a, int x_type, int type, hipStream_t s);       // after the routing
-hipError_t launch_direct_four(const LayerArgs &a, int x_type, int type, hipStream_t s);
+size_t layer_bytes(int64_t T, int k, int64_t E, int64_t D, int64_t H);
+hipError_t launch_layer(const LayerArgs &a, const RouteArgs &r, int logits_type, int type, void *work, hipStream_t s);
+struct DirectArgs {               // x's rows of K columns times matrices of N rows in 4 bits
+    const void *x;
+    int64_t x_stride, K, N;
+    int T, k, E;
+    const int32_t *ids;
+    const float *weights;
+    asgd_blocks w;
+    void *out;
+    int64_t out_stride;
+    bool wide_out;
+};
+hipError_t launch_direct_four(const DirectArgs &a, int x_type, int type, hipStream_t s);
 
 struct SumArgs {
     const void *y, *d_out;

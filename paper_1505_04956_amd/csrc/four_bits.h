@@ -33,6 +33,21 @@ __device__ __forceinline__ uint32_t four_bits(const float *v, float scale)
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[6], v[7], scale, 3);
 }
 
+// eight elements at any address that an element may have
+template <class T> struct Eight { T v[8]; } __attribute__((packed));
+
+// elements c .. c + 7 of a row of cols
+template <class T> __device__ __forceinline__ void eight_of(const T *row, int64_t c, int64_t cols, float (&v)[8])
+{
+    if (c + 8 <= cols) {
+        const Eight<T> u = *(const Eight<T> *)(row + c);
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = (float)u.v[i];
+    } else
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = c + i < cols ? (float)row[c + i] : 0.0f;
+}
+
 // sixteen rows of b (a lane's 32 columns of row lane % 16, columns lane / 16 * 32 of 128) times sixteen of a, added to `sum`, in which a lane has
 // rows lane / 16 * 4 + i of b and row lane % 16 of a.  Scales: the bytes of the lane's own blocks.
 __device__ __forceinline__ v4f four_product(v4i b, uint32_t scale_b, v4i a, uint32_t scale_a, v4f sum)

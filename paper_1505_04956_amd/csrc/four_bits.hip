@@ -5,9 +5,6 @@ namespace asgd {
 
 namespace {
 
-// eight elements at any address that an element may have
-template <class T> struct Eight { T v[8]; } __attribute__((packed));
-
 // Four lanes take a block, eight elements each; 32 lanes a run of 256 columns, a wave two of them next to each other.
 template <class Ty> __global__ __launch_bounds__(256) void quantize_four_kernel(FourArgs q, int64_t groups)
 {
@@ -16,15 +13,8 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_four_kernel(
     const int part = threadIdx.x & 31;
     for (int64_t g = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); g < groups; g += (int64_t)gridDim.x * 8) {
         const int64_t r = g / runs, run = g - r * runs, c = run * RUN4 + part * 8;
-        const T *p = (const T *)q.x + r * q.stride + c;
         float v[8];
-        if (c + 8 <= q.cols) {
-            const Eight<T> u = *(const Eight<T> *)p;
-#pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = (float)u.v[i];
-        } else
-#pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = c + i < q.cols ? (float)p[i] : 0.0f;
+        eight_of((const T *)q.x + r * q.stride, c, q.cols, v);
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 8; i++) top = max(top, magnitude_bits(v[i]));

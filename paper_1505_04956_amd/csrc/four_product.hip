@@ -191,33 +191,37 @@ template <class In, int J, class Out> __global__ __launch_bounds__(64 * FEW4_WAV
         src[j] = p.mode == ASGD_PRODUCT_GATHER ? p.order.slots[r] / p.order.k : r;
     }
     const int64_t r = strip * 16 + tok, row_b = matrix * p.rows_b + (r < p.rows_b ? r : p.rows_b - 1);
-    const uint8_t *b = p.b + row_b * p.kb * RUN4_BYTES + quarter * 16, *sb = (const uint8_t *)p.sb + row_b * p.kb * RUN4_SCALES + quarter;
+    const uint8_t *b = p.b + row_b * p.kb * RUN4_BYTES + quarter * 16, *sb = (const uint8_t *)p.sb + row_b * p.kb * RUN4_SCALES;
+    const int byte = quarter * 8;                                 // of four scales, the lane's (a load of all eight of a run costs half of what two of a byte do)
     v4f sum[J];
 #pragma unroll
     for (int j = 0; j < J; j++) sum[j] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int64_t kb = wave; kb < p.kb; kb += FEW4_WAVES) {
-        v4i w[2];
-        uint32_t scale_b[2];
+        v4i w[2], a[J][2];
         RawFour<In> raw[2];
+        const uint2 of_b = *(const uint2 *)(sb + kb * RUN4_SCALES);
+        uint2 of_a[J];
 #pragma unroll
         for (int half = 0; half < 2; half++) {
             w[half] = *(const v4i *)(b + kb * RUN4_BYTES + half * 64);
-            scale_b[half] = sb[kb * RUN4_SCALES + half * 4];
             if constexpr (RAW) raw[half].load((const typename In::T *)p.a + src[0] * p.stride_raw, true, wide_in, kb * RUN4 + half * 128 + quarter * 32, p.cols);
         }
 #pragma unroll
-        for (int half = 0; half < 2; half++)
-#pragma unroll
-            for (int j = 0; j < J; j++) {
-                v4i a;
-                uint32_t scale_a;
-                if constexpr (RAW) raw[half].set(true, scale_a, a);
-                else {
-                    a = *(const v4i *)(p.a + src[j] * p.kb * RUN4_BYTES + kb * RUN4_BYTES + half * 64 + quarter * 16);
-                    scale_a = ((const uint8_t *)p.sa)[src[j] * p.kb * RUN4_SCALES + kb * RUN4_SCALES + half * 4 + quarter];
-                }
-                sum[j] = four_product(w[half], scale_b[half], a, scale_a, sum[j]);
+        for (int j = 0; j < J; j++) {
+            if constexpr (RAW) {
+                raw[0].set(true, of_a[j].x, a[j][0]);
+                raw[1].set(true, of_a[j].y, a[j][1]);
+            } else {
+                const uint8_t *at = p.a + (src[j] * p.kb + kb) * RUN4_BYTES + quarter * 16;
+                a[j][0] = *(const v4i *)at;
+                a[j][1] = *(const v4i *)(at + 64);
+                of_a[j] = *(const uint2 *)((const uint8_t *)p.sa + (src[j] * p.kb + kb) * RUN4_SCALES);
+                of_a[j].x = of_a[j].x >> byte & 255;
+                of_a[j].y = of_a[j].y >> byte & 255;
             }
+            sum[j] = four_product(w[0], of_b.x >> byte & 255, a[j][0], of_a[j].x, sum[j]);
+            sum[j] = four_product(w[1], of_b.y >> byte & 255, a[j][1], of_a[j].y, sum[j]);
+        }
     }
 #pragma unroll
     for (int j = 0; j < J; j++) parts[wave][j][lane] = sum[j];

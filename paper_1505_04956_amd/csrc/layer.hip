@@ -1,64 +1,169 @@
-// A whole layer of experts for few rows: what the routing chose, through both matrices of every expert that some row goes to.  An expert's weights are
-// read once for all rows: up to sixteen rows are the columns of one matrix instruction, and the columns of rows that do not go to an expert are not used.
+// A whole layer of experts for few rows in three launches.  An expert's weights are read once for all rows: up to sixteen rows are the columns of one
+// matrix instruction, and the columns of rows that do not go to an expert are not used.
 //
-// The first kernel forms h = f(gate) * up in 32 bits for every slot (a row and one of its choices), the second sums the rows' experts.
+//   choose  one workgroup routes the rows and lists the experts that have any; the others bring a row of x each to 8 or 4 bits
+//   up      a workgroup forms h = f(gate) * up, 32-bit, of 32 of an expert's hidden columns for all of its rows
+//   down    a workgroup sums sixteen columns of the result over all experts; its waves share the experts' blocks
 #include "four_bits.h"
+#include "route_row.h"
 
 namespace asgd {
 
 namespace {
 
-constexpr int UP_WAVES = 8, DOWN_WAVES = 16;
-constexpr int MOST_SLOTS = ASGD_PRODUCT_RAW_ROWS * ASGD_ROUTE_MAX_CHOSEN;
+constexpr int UP_WAVES = 8, DOWN_WAVES = 16, CHOOSE_THREADS = 1024, COLUMNS = 16;
+constexpr int MOST_SLOTS = ASGD_PRODUCT_RAW_ROWS * ASGD_ROUTE_MAX_CHOSEN, WORDS = ASGD_ROUTE_MAX_EXPERTS / 32;
+static_assert(ASGD_PRODUCT_RAW_ROWS == COLUMNS && CHOOSE_THREADS / 64 >= COLUMNS && MOST_SLOTS <= CHOOSE_THREADS, "");
 
-// ---- which experts have rows --------------------------------------------------------------------------------------
-// A bit for each expert that a slot goes to, in the LDS.
-__device__ __forceinline__ void mark_experts(const int32_t *ids, int slots, int E, uint32_t *bits)
+// A step of a contraction is what a row has in 128 bytes: a block of 128 columns in 8 bits, a run of 256 in 4.
+constexpr int STEP_BYTES = 128;
+__host__ __device__ inline int64_t steps_of(int bits, int64_t cols) { return bits == 8 ? blocks8(cols) : runs4(cols); }
+
+// Scratch of a call, each part at a multiple of sixteen bytes.
+struct Scratch {
+    int32_t *met, *experts;       // experts that have rows: how many, which, in ascending order
+    int16_t *slots;               // [met][sixteen rows]: the slot t * k + j with which row t goes to it, -1 if it does not
+    uint8_t *x, *x_scales;        // rows of x in 8 bits, a float for each step, or in 4, eight bytes for each
+    float *h;                     // [T * k] rows, h_pitch() apart
+};
+__host__ __device__ inline int64_t h_pitch(int64_t H) { return (H + 3) & ~(int64_t)3; }
+
+size_t scratch_of(int64_t T, int k, int64_t E, int64_t D, int64_t H, char *at, Scratch &s)
 {
-    for (int i = threadIdx.x; i < ASGD_ROUTE_MAX_EXPERTS / 32; i += blockDim.x) bits[i] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < slots; i += blockDim.x) {
-        const int e = ids[i];
-        if ((unsigned)e < (unsigned)E) atomicOr(&bits[e >> 5], 1u << (e & 31));
+    const int64_t most = T * k < E ? T * k : E, steps = blocks8(D);        // (enough for either)
+    size_t n = 0;
+    const auto take = [&](size_t bytes) { char *p = at + n; n += (bytes + 15) & ~(size_t)15; return p; };
+    s.met = (int32_t *)take(4);
+    s.experts = (int32_t *)take(4 * most);
+    s.slots = (int16_t *)take(2 * COLUMNS * most);
+    s.x = (uint8_t *)take(T * steps * STEP_BYTES);
+    s.x_scales = (uint8_t *)take(T * steps * 8);
+    s.h = (float *)take(sizeof(float) * T * k * h_pitch(H));
+    return n;
+}
+
+// ---- bringing rows to 8 or 4 bits -----------------------------------------------------------------------------------
+// Eight neighbours of a step for each lane: sixteen lanes a step of 8 bits, of which four bytes times two and (the first lane's) a scale come, 32 lanes
+// one of 4 bits.
+template <int BITS> struct Parts;
+template <> struct Parts<8> {
+    static constexpr int LANES = 16, BYTES = 8;
+    typedef uint2 Bytes;
+    typedef float Scale;
+    static __device__ __forceinline__ Bytes to(const float (&v)[8], Scale &scale)
+    {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) top = max(top, magnitude_bits(v[i]));
+        float inverse;
+        block_scale((uint32_t)row_max((int)top), scale, inverse);
+        return make_uint2(eight_bits(v[0], v[1], v[2], v[3], inverse), eight_bits(v[4], v[5], v[6], v[7], inverse));
+    }
+    static __device__ __forceinline__ void put_scale(uint8_t *scales, int part, Scale scale) { if (part == 0) *(float *)scales = scale; }
+    static constexpr int SCALES = 4;             // bytes of a step
+};
+template <> struct Parts<4> {
+    static constexpr int LANES = 32, BYTES = 4;
+    typedef uint32_t Bytes;
+    typedef uint32_t Scale;
+    static __device__ __forceinline__ Bytes to(const float (&v)[8], Scale &scale)
+    {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) top = max(top, magnitude_bits(v[i]));
+        top = max(top, (uint32_t)across<XOR1>((int)top));
+        top = max(top, (uint32_t)across<XOR2>((int)top));
+        scale = four_scale(top);
+        return four_bits(v, four_scale_value(scale));
+    }
+    static __device__ __forceinline__ void put_scale(uint8_t *scales, int part, Scale scale) { if ((part & 3) == 0) scales[part >> 2] = (uint8_t)scale; }
+    static constexpr int SCALES = 8;
+};
+
+template <int BITS, class T> __device__ __forceinline__ void bring_row(const T *row, int64_t cols, uint8_t *values, uint8_t *scales)
+{
+    typedef Parts<BITS> P;
+    const int part = threadIdx.x % P::LANES;
+    const int64_t steps = steps_of(BITS, cols);
+    for (int64_t step = threadIdx.x / P::LANES; step < steps; step += blockDim.x / P::LANES) {
+        float v[8];
+        eight_of(row, (step * P::LANES + part) * 8, cols, v);
+        typename P::Scale scale;
+        *(typename P::Bytes *)(values + step * STEP_BYTES + part * P::BYTES) = P::to(v, scale);
+        P::put_scale(scales + step * P::SCALES, part, scale);
+    }
+}
+
+// ---- choose -----------------------------------------------------------------------------------------------------------
+template <class Ty, int V> __global__ __launch_bounds__(CHOOSE_THREADS) void layer_choose_kernel(RouteArgs r, LayerArgs a, Scratch s, bool wide)
+{
+    __shared__ int32_t ids[MOST_SLOTS];
+    __shared__ float weights[MOST_SLOTS];
+    __shared__ uint32_t bits[WORDS];
+    __shared__ int before[WORDS + 1];                              // experts with rows in the words before
+    __shared__ int16_t slots[MOST_SLOTS * COLUMNS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (blockIdx.x > 0) {
+        const int64_t t = blockIdx.x - 1;
+        const auto go = [&](const auto *x) {
+            if (a.up.form == ASGD_BLOCKS_FOURS) bring_row<4>(x + t * a.x_stride, a.D, s.x + t * runs4(a.D) * STEP_BYTES, s.x_scales + t * runs4(a.D) * Parts<4>::SCALES);
+            else bring_row<8>(x + t * a.x_stride, a.D, s.x + t * blocks8(a.D) * STEP_BYTES, s.x_scales + t * blocks8(a.D) * Parts<8>::SCALES);
+        };
+        if (a.x_type == ASGD_TYPE_F32) go((const float *)a.x);
+        else if (a.x_type == ASGD_TYPE_BF16) go((const __bf16 *)a.x);
+        else go((const _Float16 *)a.x);
+        return;
+    }
+    if (threadIdx.x < WORDS) bits[threadIdx.x] = 0;
+    if (wave < a.T) {
+        const Lane<Ty, V> row = load_lane<Ty, V>((const typename Ty::T *)r.logits + wave * r.stride, lane * V, r.E, wide);
+        float bias[V];
+        load_bias<V>(r.bias, r.E, lane, bias);
+        r.ids = ids;
+        r.weights = weights;
+        route_row<Ty, V, true>(r, wave, lane, row, bias);
     }
     __syncthreads();
+    const int all = a.T * a.k, me = threadIdx.x, e = me < all ? ids[me] : -1;
+    if (me < all) {
+        a.ids[me] = e;
+        a.weights[me] = weights[me];
+    }
+    if (e >= 0) atomicOr(&bits[e >> 5], 1u << (e & 31));
+    __syncthreads();
+    if (wave == 0) {
+        const int c = lane < WORDS ? __popc(bits[lane]) : 0, sum = wave_scan(c);
+        if (lane <= WORDS) before[lane] = sum - c;
+    }
+    __syncthreads();
+    const int met = before[WORDS];
+    for (int i = me; i < met * COLUMNS; i += CHOOSE_THREADS) slots[i] = -1;
+    __syncthreads();
+    if (e >= 0) {
+        const int n = before[e >> 5] + __popc(bits[e >> 5] & ((1u << (e & 31)) - 1));
+        slots[n * COLUMNS + me / a.k] = (int16_t)me;
+        s.experts[n] = e;                                          // (every slot of an expert: the same number)
+    }
+    if (me == 0) *s.met = met;
+    __syncthreads();
+    for (int i = me; i < met * COLUMNS; i += CHOOSE_THREADS) s.slots[i] = slots[i];
 }
 
-// The n-th of them, -1 if there are not so many.  All lanes of a wave.
-__device__ __forceinline__ int nth_expert(const uint32_t *bits, int n)
-{
-    const int lane = threadIdx.x & 63;
-    const uint32_t word = lane < ASGD_ROUTE_MAX_EXPERTS / 32 ? bits[lane] : 0;
-    const int sum = wave_scan(__popc(word)), before = sum - __popc(word);
-    const unsigned long long past = __ballot(sum > n);
-    if (!past) return -1;
-    const int at = __ffsll((long long)past) - 1;
-    uint32_t rest = (uint32_t)__builtin_amdgcn_readlane((int)word, at);
-    for (int skip = n - __builtin_amdgcn_readlane(before, at); skip > 0; skip--) rest &= rest - 1;
-    return at * 32 + __ffs((int)rest) - 1;
-}
+// ---- sixteen rows of an expert's weights, and the columns that they are multiplied by ------------------------------------
+template <int BITS> struct Weights;                               // of a step.  row: a lane's own, tile: the first of the sixteen
+template <int BITS> struct Columns;                               // of a step, a lane's 32 or two times 32 of row lane % 16
 
-// ---- sixteen rows of an expert's weights ----------------------------------------------------------------------------
-// A step is a block of 128 columns (8 bits) or a run of 256 (4 bits).  Which rows: a lane's own (row), the first of the sixteen (tile).
-template <int BITS> struct Weights;
-
+template <> struct Columns<8> {
+    v4i lo, hi;
+    float scale;
+    __device__ __forceinline__ void load(const uint8_t *values, const uint8_t *scales, int quarter)
+    {
+        lo = *(const v4i *)(values + quarter * 32);
+        hi = *(const v4i *)(values + quarter * 32 + 16);
+        scale = *(const float *)scales;
+    }
+};
 template <> struct Weights<8> {
-    static constexpr int STEP = BLOCK8;
-    template <class In> struct Rows {                              // the columns' rows of a step
-        RawBlock<In> raw;
-        Operand<true> a;
-        float scale;
-        __device__ __forceinline__ void load(const typename In::T *row, bool there, bool wide, int64_t step, int quarter, int64_t cols)
-        {
-            raw.load(row, there, wide, step * BLOCK8 + quarter * 32, cols);
-        }
-        __device__ __forceinline__ void set(bool there)
-        {
-            v4i lo, hi;
-            raw.set(there, scale, lo, hi);
-            a.set(lo, hi);
-        }
-    };
     v4i lo, hi;
     float scale[2];                                                // of the square that the first of the sixteen rows lies in, and of that of the last
     __device__ __forceinline__ void load(const asgd_blocks &w, int64_t steps, int64_t matrix, int64_t row, int64_t tile, int64_t step, int quarter)
@@ -67,189 +172,252 @@ template <> struct Weights<8> {
         lo = *(const v4i *)p;
         hi = *(const v4i *)(p + 16);
         const float *s = w.scales + matrix * blocks8(w.rows) * steps + step;
-        scale[0] = s[tile / BLOCK8 * steps];
+        scale[0] = s[min(tile, w.rows - 1) / BLOCK8 * steps];
         scale[1] = s[min(tile + 15, w.rows - 1) / BLOCK8 * steps];
     }
-    // the products are added to `sum`, a row of the result for each lane and i
-    template <class In> __device__ __forceinline__ v4f times(const Rows<In> &r, int64_t tile, int quarter, v4f sum) const
+    // adds the products times `factor` to `sum`, a row of the result for each lane and i
+    __device__ __forceinline__ v4f times(const Columns<8> &c, int64_t tile, int quarter, float factor, v4f sum) const
     {
-        Operand<true> b;
+        Operand<true> a, b;
+        a.set(c.lo, c.hi);
         b.set(lo, hi);
-        const v4f part = block_product(b, r.a);
+        const v4f part = block_product(b, a);
         const int second = BLOCK8 - (int)(tile % BLOCK8) - quarter * 4;      // from this i on the lane's rows lie in the second square
 #pragma unroll
-        for (int i = 0; i < 4; i++) sum[i] = fmaf(part[i], r.scale * (i < second ? scale[0] : scale[1]), sum[i]);
+        for (int i = 0; i < 4; i++) sum[i] = fmaf(part[i], c.scale * factor * (i < second ? scale[0] : scale[1]), sum[i]);
         return sum;
     }
 };
 
-template <> struct Weights<4> {
-    static constexpr int STEP = RUN4;
-    template <class In> struct Rows {
-        RawFour<In> raw[2];
-        v4i a[2];
-        uint32_t scale[2];
-        __device__ __forceinline__ void load(const typename In::T *row, bool there, bool wide, int64_t step, int quarter, int64_t cols)
-        {
-#pragma unroll
-            for (int half = 0; half < 2; half++) raw[half].load(row, there, wide, step * RUN4 + half * 128 + quarter * 32, cols);
-        }
-        __device__ __forceinline__ void set(bool there)
-        {
-#pragma unroll
-            for (int half = 0; half < 2; half++) raw[half].set(there, scale[half], a[half]);
-        }
-    };
+template <> struct Columns<4> {
     v4i v[2];
-    uint32_t scale[2];
+    uint2 scales;
+    __device__ __forceinline__ void load(const uint8_t *values, const uint8_t *of, int quarter)
+    {
+#pragma unroll
+        for (int half = 0; half < 2; half++) v[half] = *(const v4i *)(values + half * 64 + quarter * 16);
+        scales = *(const uint2 *)of;
+    }
+};
+template <> struct Weights<4> {
+    v4i v[2];
+    uint2 scales;                                                  // all eight of a run: two loads of a byte each cost as much as the values' do
     __device__ __forceinline__ void load(const asgd_blocks &w, int64_t steps, int64_t matrix, int64_t row, int64_t, int64_t step, int quarter)
     {
         const int64_t at = (matrix * w.rows + row) * steps + step;
-        const uint8_t *p = (const uint8_t *)w.values + at * RUN4_BYTES + quarter * 16, *s = (const uint8_t *)w.scales + at * RUN4_SCALES + quarter;
+        const uint8_t *p = (const uint8_t *)w.values + at * RUN4_BYTES + quarter * 16;
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-            v[half] = *(const v4i *)(p + half * 64);
-            scale[half] = s[half * 4];
-        }
+        for (int half = 0; half < 2; half++) v[half] = *(const v4i *)(p + half * 64);
+        scales = *(const uint2 *)((const uint8_t *)w.scales + at * RUN4_SCALES);
     }
-    template <class In> __device__ __forceinline__ v4f times(const Rows<In> &r, int64_t, int, v4f sum) const
+    __device__ __forceinline__ v4f times(const Columns<4> &c, v4f sum) const
     {
+        const int at = (threadIdx.x >> 4 & 3) * 8;                 // the lane's quarter
+        sum = four_product(v[0], scales.x >> at & 255, c.v[0], c.scales.x >> at & 255, sum);
+        return four_product(v[1], scales.y >> at & 255, c.v[1], c.scales.y >> at & 255, sum);
+    }
+    __device__ __forceinline__ v4f times(const Columns<4> &c, int64_t, int, float factor, v4f sum) const
+    {
+        const v4f part = times(c, v4f{0.0f, 0.0f, 0.0f, 0.0f});
 #pragma unroll
-        for (int half = 0; half < 2; half++) sum = four_product(v[half], scale[half], r.a[half], r.scale[half], sum);
+        for (int i = 0; i < 4; i++) sum[i] = fmaf(part[i], factor, sum[i]);
         return sum;
     }
 };
 
-// ---- kernels --------------------------------------------------------------------------------------------------------
+// ---- up -----------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ float activated(float gate, float up, int activation)
 {
     const float f = activation == ASGD_ACTIVATION_SILU ? gate / (1.0f + expf(-gate)) : 0.5f * gate * (1.0f + erff(gate * 0.70710678f));
     return f * up;
 }
 
-__host__ __device__ inline int64_t h_pitch(int64_t H) { return (H + 3) & ~(int64_t)3; }
-
-// grid: strips of sixteen of H, experts
-template <class In, int BITS> __global__ __launch_bounds__(64 * UP_WAVES) void layer_up_kernel(LayerArgs a, bool wide)
+// grid: strips of 32 of H, experts.  Even waves take the first sixteen of the strip, odd ones the others, rows of the gate and rows that it multiplies; four
+// waves share the steps, and the loads of AHEAD of a wave's steps are on their way together.
+template <int BITS> __global__ __launch_bounds__(64 * UP_WAVES, 4) void layer_up_kernel(LayerArgs a, Scratch s)
 {
-    typedef Weights<BITS> W;
-    __shared__ uint32_t bits[ASGD_ROUTE_MAX_EXPERTS / 32];
+    constexpr int AHEAD = 2, SHARE = UP_WAVES / 2;
     __shared__ v4f parts[UP_WAVES][2][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tok = lane & 15, quarter = lane >> 4;
-    mark_experts(a.ids, a.T * a.k, a.E, bits);
-    const int e = nth_expert(bits, blockIdx.y);
-    if (e < 0) return;
-    int slot = -1;
-    if (tok < a.T)
-        for (int j = quarter; j < a.k; j += 4)
-            if (a.ids[tok * a.k + j] == e) slot = tok * a.k + j;
-    slot = max(slot, __shfl_xor(slot, 16));
-    slot = max(slot, __shfl_xor(slot, 32));
+    const int n = blockIdx.y, met = *s.met, e = s.experts[n], slot = s.slots[n * COLUMNS + tok];
+    if (n >= met) return;
     const bool there = slot >= 0;
-    const int64_t strip = (int64_t)blockIdx.x * 16, steps = (a.D + W::STEP - 1) / W::STEP, of_lane = min(strip + tok, a.H - 1);
-    const typename In::T *row = (const typename In::T *)a.x + (there ? tok : 0) * a.x_stride;
+    const int64_t strip = (int64_t)blockIdx.x * 32 + (wave & 1) * 16;
+    const int steps = (int)steps_of(BITS, a.D);
+    const uint8_t *const x = s.x + (there ? tok : 0) * (int64_t)steps * STEP_BYTES, *const x_scales = s.x_scales + (there ? tok : 0) * (int64_t)steps * Parts<BITS>::SCALES;
+    const int64_t tile[2] = {strip, a.H + strip}, of_lane = min(strip + tok, a.H - 1);
     v4f sum[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
-    for (int64_t step = wave; step < steps; step += UP_WAVES) {
-        W w[2];
-        typename W::template Rows<In> r;
+    for (int step0 = wave >> 1; step0 < steps; step0 += SHARE * AHEAD) {
+        Weights<BITS> w[AHEAD][2];
+        Columns<BITS> c[AHEAD];
 #pragma unroll
-        for (int n = 0; n < 2; n++) w[n].load(a.up, steps, e, n * a.H + of_lane, n * a.H + strip, step, quarter);
-        r.load(row, there, wide, step, quarter, a.D);
-        r.set(there);
+        for (int i = 0; i < AHEAD; i++) {
+            const int step = step0 + i * SHARE;
+            if (step >= steps) break;
 #pragma unroll
-        for (int n = 0; n < 2; n++) sum[n] = w[n].template times<In>(r, n * a.H + strip, quarter, sum[n]);
-    }
+            for (int m = 0; m < 2; m++) w[i][m].load(a.up, steps, e, m * a.H + of_lane, tile[m], step, quarter);
+            c[i].load(x + (int64_t)step * STEP_BYTES, x_scales + (int64_t)step * Parts<BITS>::SCALES, quarter);
+        }
 #pragma unroll
-    for (int n = 0; n < 2; n++) parts[wave][n][lane] = sum[n];
-    __syncthreads();
-    if (wave > 0 || !there) return;
-    v4f total[2] = {parts[0][0][lane], parts[0][1][lane]};
+        for (int i = 0; i < AHEAD; i++) {
+            if (step0 + i * SHARE >= steps) break;
 #pragma unroll
-    for (int w = 1; w < UP_WAVES; w++)
-#pragma unroll
-        for (int n = 0; n < 2; n++) total[n] += parts[w][n][lane];
-#pragma unroll
-    for (int i = 0; i < 4; i++)
-        if (strip + quarter * 4 + i < a.H) a.h[slot * h_pitch(a.H) + strip + quarter * 4 + i] = activated(total[0][i], total[1][i], a.activation);
-}
-
-// grid: strips of sixteen of N.  The waves share the steps of all experts.
-template <int BITS, class Out> __global__ __launch_bounds__(64 * DOWN_WAVES) void layer_down_kernel(LayerArgs a, bool wide)
-{
-    typedef Weights<BITS> W;
-    extern __shared__ int16_t slots[];                            // [experts that have rows][sixteen rows]: the slot, -1 without one
-    __shared__ uint32_t bits[ASGD_ROUTE_MAX_EXPERTS / 32];
-    __shared__ int before[ASGD_ROUTE_MAX_EXPERTS / 32 + 1];       // experts with rows in the words before
-    __shared__ int16_t experts[MOST_SLOTS];
-    __shared__ v4f parts[DOWN_WAVES][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tok = lane & 15, quarter = lane >> 4;
-    const int all = a.T * a.k;
-    mark_experts(a.ids, all, a.E, bits);
-    if (wave == 0) {
-        const int c = lane < ASGD_ROUTE_MAX_EXPERTS / 32 ? __popc(bits[lane]) : 0, sum = wave_scan(c);
-        if (lane <= ASGD_ROUTE_MAX_EXPERTS / 32) before[lane] = sum - c;
-    }
-    __syncthreads();
-    const int met = before[ASGD_ROUTE_MAX_EXPERTS / 32];
-    for (int i = threadIdx.x; i < met * 16; i += blockDim.x) slots[i] = -1;
-    __syncthreads();
-    for (int i = threadIdx.x; i < all; i += blockDim.x) {
-        const int e = a.ids[i];
-        if ((unsigned)e < (unsigned)a.E) {
-            const int n = before[e >> 5] + __popc(bits[e >> 5] & ((1u << (e & 31)) - 1));
-            slots[n * 16 + i / a.k] = (int16_t)i;
-            experts[n] = (int16_t)e;                               // (every slot of an expert: the same number)
+            for (int m = 0; m < 2; m++) {
+                if constexpr (BITS == 8) sum[m] = w[i][m].times(c[i], tile[m], quarter, 1.0f, sum[m]);
+                else sum[m] = w[i][m].times(c[i], sum[m]);
+            }
         }
     }
-    __syncthreads();
-    const int64_t strip = (int64_t)blockIdx.x * 16, of_lane = min(strip + tok, a.N - 1);
-    const int steps = (int)((a.H + W::STEP - 1) / W::STEP);
-    v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int item = wave; item < met * steps; item += DOWN_WAVES) {
-        const int n = item / steps, step = item - n * steps, slot = slots[n * 16 + tok];
-        const bool there = slot >= 0;
-        W w;
-        typename W::template Rows<F32> r;
-        w.load(a.down, steps, experts[n], of_lane, strip, step, quarter);
-        r.load(a.h + (there ? slot : 0) * h_pitch(a.H), there, wide, step, quarter, a.H);
-        const float weight = there ? a.weights[slot] : 0.0f;
-        r.set(there);
-        const v4f part = w.template times<F32>(r, strip, quarter, v4f{0.0f, 0.0f, 0.0f, 0.0f});
 #pragma unroll
-        for (int i = 0; i < 4; i++) sum[i] = there ? fmaf(part[i], weight, sum[i]) : sum[i];     // (a scale that is not a number spoils its own expert's rows alone)
+    for (int m = 0; m < 2; m++) parts[wave][m][lane] = sum[m];
+    __syncthreads();
+    if (wave > 1 || !there) return;
+    v4f gate = parts[wave][0][lane], up = parts[wave][1][lane];
+#pragma unroll
+    for (int w = 1; w < SHARE; w++) {
+        gate += parts[2 * w + wave][0][lane];
+        up += parts[2 * w + wave][1][lane];
     }
-    parts[wave][lane] = sum;
-    __syncthreads();
-    if (wave > 0 || tok >= a.T) return;
-#pragma unroll
-    for (int w = 1; w < DOWN_WAVES; w++) sum += parts[w][lane];
     const int64_t c = strip + quarter * 4;
-    store_four<Out>((typename Out::T *)a.out + tok * a.out_stride + c, a.N - c, a.wide_out, sum);
+    if (c >= a.H) return;
+    v4f h;
+#pragma unroll
+    for (int i = 0; i < 4; i++) h[i] = c + i < a.H ? activated(gate[i], up[i], a.activation) : 0.0f;
+    *(v4f *)(s.h + slot * h_pitch(a.H) + c) = h;                   // (a row has a multiple of four)
 }
 
+// ---- down ---------------------------------------------------------------------------------------------------------------
+// An item is G neighbouring steps of an expert; the waves of a workgroup take items in turn.  A wave brings the item's part of h to 8 or 4 bits itself, sixteen or 32
+// lanes a row and step, and hands it round through the LDS; the weights of its next items are on their way meanwhile.
+//
+// G = 2, for up to eight rows: the sixteen rows of the matrix instruction are eight of the weights with two steps each, and its columns eight rows of h with
+// the same two; what belongs together is half of what it gives.  So a workgroup takes eight columns of the result, and there are twice as many of them.
+template <int BITS, int G, class Out> __global__ __launch_bounds__(64 * DOWN_WAVES, 4) void layer_down_kernel(LayerArgs a, Scratch s, int most)
+{
+    typedef Parts<BITS> P;
+    constexpr int PITCH = STEP_BYTES + 16, GROUPS = 64 / P::LANES, AHEAD = 2, R = COLUMNS / G;
+    __shared__ int16_t slots[MOST_SLOTS * COLUMNS];
+    __shared__ int16_t experts[MOST_SLOTS];
+    __shared__ float weights[MOST_SLOTS];
+    __shared__ __align__(16) uint8_t columns[DOWN_WAVES][COLUMNS * PITCH];
+    __shared__ __align__(16) uint8_t scales[DOWN_WAVES][COLUMNS * 8];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tok = lane & 15, quarter = lane >> 4;
+    const int row = tok % R, g = tok / R;                          // of the weights and of x; which of the item's steps
+    // (all that there can be: how many there are is on its way as well)
+    for (int i = threadIdx.x; i < most * COLUMNS; i += blockDim.x) slots[i] = s.slots[i];
+    for (int i = threadIdx.x; i < most; i += blockDim.x) experts[i] = (int16_t)s.experts[i];
+    for (int i = threadIdx.x; i < a.T * a.k; i += blockDim.x) weights[i] = a.weights[i];
+    const int met = *s.met, steps = (int)steps_of(BITS, a.H), each = (steps + G - 1) / G, items = met * each;
+    __syncthreads();
+    const int64_t strip = (int64_t)blockIdx.x * R, of_lane = min(strip + row, a.N - 1);
+    const int part = lane % P::LANES, group = lane / P::LANES;
+
+    struct Item {
+        Weights<BITS> w;
+        float h[8];
+        int slot, step;           // of the lane's column (-1: not used); the first of the item
+        uint32_t rows;            // rows of x that go to the expert
+    };
+    const auto nth_row = [](uint32_t rows, int n) {
+        for (; n > 0; n--) rows &= rows - 1;
+        return __ffs((int)rows) - 1;
+    };
+    // the at-th used column (the last one if there are fewer), and its part of h
+    const auto column_of = [&](uint32_t rows, int at) {
+        const int last = min(at, __popc(rows) * G - 1);
+        return nth_row(rows, last / G) + last % G * R;
+    };
+    const auto take_h = [&](int n, int step, int column, float (&h)[8]) {
+        eight_of(s.h + slots[n * COLUMNS + column % R] * h_pitch(a.H), ((int64_t)(step + column / R) * P::LANES + part) * 8, a.H, h);
+    };
+    const auto fetch = [&](int item, Item &i) {
+        const int n = item / each;
+        i.step = (item - n * each) * G;
+        i.slot = slots[n * COLUMNS + row];
+        i.rows = (uint32_t)__ballot(i.slot >= 0) & ((1u << R) - 1);
+        i.w.load(a.down, steps, experts[n], of_lane, strip, min(i.step + g, steps - 1), quarter);
+        take_h(n, i.step, column_of(i.rows, group), i.h);
+    };
+    uint8_t *const mine = columns[wave], *const my_scales = scales[wave];
+    const auto put = [&](int column, const float (&h)[8]) {
+        typename P::Scale scale;
+        *(typename P::Bytes *)(mine + column * PITCH + part * P::BYTES) = P::to(h, scale);
+        P::put_scale(my_scales + column * P::SCALES, part, scale);
+    };
+    v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    const auto use = [&](int item, const Item &i) {
+        const int count = __popc(i.rows) * G;
+        put(column_of(i.rows, group), i.h);
+        for (int at = GROUPS; at < count; at += GROUPS) {
+            float h[8];
+            const int column = column_of(i.rows, at + group);
+            take_h(item / each, i.step, column, h);
+            put(column, h);
+        }
+        __builtin_amdgcn_wave_barrier();
+        __threadfence_block();
+        Columns<BITS> c;
+        c.load(mine + tok * PITCH, my_scales + tok * P::SCALES, quarter);
+        // (what a step past the last has of h is zeros)
+        const bool there = i.slot >= 0 && (G == 1 || quarter * 4 / R == g);
+        const v4f got = i.w.times(c, strip, quarter % (R / 4), there ? weights[i.slot] : 0.0f, sum);
+#pragma unroll
+        for (int k = 0; k < 4; k++) sum[k] = there ? got[k] : sum[k];       // (what is not a number in a column that is not used stays there)
+        __builtin_amdgcn_wave_barrier();
+        __threadfence_block();
+    };
+    Item held[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; i++)
+        if (wave + i * DOWN_WAVES < items) fetch(wave + i * DOWN_WAVES, held[i]);
+    for (int item = wave; item < items;)
+#pragma unroll
+        for (int i = 0; i < AHEAD; i++) {
+            if (item >= items) break;
+            use(item, held[i]);
+            if (item + AHEAD * DOWN_WAVES < items) fetch(item + AHEAD * DOWN_WAVES, held[i]);
+            item += DOWN_WAVES;
+        }
+    __syncthreads();
+    v4f(*const sums)[64] = (v4f(*)[64])columns;
+    static_assert(sizeof(columns) >= DOWN_WAVES * 64 * sizeof(v4f), "");
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave > 0 || quarter * 4 >= R || tok >= a.T) return;
+#pragma unroll
+    for (int w = 0; w < DOWN_WAVES; w++)
+#pragma unroll
+        for (int m = 0; m < G; m++)
+            if (w + m > 0) sum += sums[w][lane + m * (R / 4 * 16 + R)];
+    const int64_t c = strip + quarter * 4;
+    store_four<Out>((typename Out::T *)a.out + tok * a.out_stride + c, min(a.N - c, (int64_t)4), a.wide_out, sum);
+}
+
+// ---- experts of one matrix ------------------------------------------------------------------------------------------------
 // The experts of few rows in 4 bits in one launch, without an order: a workgroup takes sixteen rows of the weights of every expert of one row of x
 // (blockIdx.y), which it brings to 4 bits itself.
-template <class In, class Out> __global__ __launch_bounds__(64 * DOWN_WAVES) void direct_four_kernel(LayerArgs a, bool wide)
+template <class In, class Out> __global__ __launch_bounds__(64 * DOWN_WAVES) void direct_four_kernel(DirectArgs a, bool wide)
 {
-    typedef Weights<4> W;
     __shared__ v4f parts[DOWN_WAVES][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tok = lane & 15, quarter = lane >> 4;
     const int64_t t = blockIdx.y, strip = (int64_t)blockIdx.x * 16, of_lane = min(strip + tok, a.N - 1);
-    const int steps = (int)runs4(a.H);
+    const int steps = (int)runs4(a.K);
     v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int step = wave; step < steps; step += DOWN_WAVES) {
-        typename W::template Rows<In> r;
-        r.load((const typename In::T *)a.x + t * a.x_stride, tok == 0, wide, step, quarter, a.H);
-        r.set(tok == 0);
+        RawFour<In> raw[2];
+        Columns<4> c;
+        uint32_t scale[2];
+#pragma unroll
+        for (int half = 0; half < 2; half++) raw[half].load((const typename In::T *)a.x + t * a.x_stride, tok == 0, wide, (int64_t)step * RUN4 + half * 128 + quarter * 32, a.K);
+#pragma unroll
+        for (int half = 0; half < 2; half++) raw[half].set(tok == 0, scale[half], c.v[half]);
+        c.scales = make_uint2(scale[0] << quarter * 8, scale[1] << quarter * 8);
         for (int j = 0; j < a.k; j++) {
             const int e = a.ids[t * a.k + j];
             if ((unsigned)e >= (unsigned)a.E) continue;            // (all lanes or none)
-            W w;
-            w.load(a.down, steps, e, of_lane, strip, step, quarter);
-            const v4f part = w.template times<In>(r, strip, quarter, v4f{0.0f, 0.0f, 0.0f, 0.0f});
-            const float weight = a.weights[t * a.k + j];
-#pragma unroll
-            for (int i = 0; i < 4; i++) sum[i] = fmaf(part[i], weight, sum[i]);
+            Weights<4> w;
+            w.load(a.w, steps, e, of_lane, strip, step, quarter);
+            sum = w.times(c, strip, quarter, a.weights[t * a.k + j], sum);
         }
     }
     parts[wave][lane] = sum;
@@ -262,36 +430,53 @@ template <class In, class Out> __global__ __launch_bounds__(64 * DOWN_WAVES) voi
 }
 
 bool rows_wide(const void *p, int64_t stride, int type) { return (uintptr_t)p % 16 == 0 && stride * (int64_t)type_size(type) % 16 == 0; }
-unsigned strips_of(int64_t n) { return (unsigned)((n + 15) / 16); }
+unsigned strips_of(int64_t n, int rows) { return (unsigned)((n + rows - 1) / rows); }
 
 }  // namespace
 
-size_t layer_bytes(int64_t T, int k, int64_t H) { return sizeof(float) * (size_t)(T * k) * (size_t)h_pitch(H); }
-
-hipError_t launch_layer(const LayerArgs &a, int x_type, int type, hipStream_t s)
+size_t layer_bytes(int64_t T, int k, int64_t E, int64_t D, int64_t H)
 {
-    const int most = a.T * a.k < a.E ? a.T * a.k : a.E;
+    Scratch s;
+    return scratch_of(T, k, E, D, H, nullptr, s);
+}
+
+hipError_t launch_layer(const LayerArgs &a, const RouteArgs &r, int logits_type, int type, void *work, hipStream_t s)
+{
+    Scratch w;
+    scratch_of(a.T, a.k, a.E, a.D, a.H, (char *)work, w);
+    const unsigned most = (unsigned)(a.T * a.k < a.E ? a.T * a.k : a.E);
     const bool four = a.up.form == ASGD_BLOCKS_FOURS;
-    const dim3 grid(strips_of(a.H), (unsigned)most);
-    const hipError_t e = with_type(x_type, [&](auto in) {
-        typedef decltype(in) In;
-        if (four) layer_up_kernel<In, 4><<<grid, 64 * UP_WAVES, 0, s>>>(a, rows_wide(a.x, a.x_stride, x_type));
-        else layer_up_kernel<In, 8><<<grid, 64 * UP_WAVES, 0, s>>>(a, rows_wide(a.x, a.x_stride, x_type));
-        return hipGetLastError();
+    hipError_t e = with_type(logits_type, [&](auto ty) {
+        return with_width(a.E, [&](auto v) {
+            constexpr int V = decltype(v)::value;
+            layer_choose_kernel<decltype(ty), V><<<1 + a.T, CHOOSE_THREADS, 0, s>>>(r, a, w, rows_of_lanes<decltype(ty), V>(r.logits, r.stride, r.E));
+            return hipGetLastError();
+        });
     });
     if (e != hipSuccess) return e;
+    const dim3 grid(strips_of(a.H, 32), most);
+    if (four) layer_up_kernel<4><<<grid, 64 * UP_WAVES, 0, s>>>(a, w);
+    else layer_up_kernel<8><<<grid, 64 * UP_WAVES, 0, s>>>(a, w);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
     return with_type(type, [&](auto out) {
-        typedef decltype(out) Out;
-        const size_t lds = (size_t)most * 16 * sizeof(int16_t);
-        if (four) layer_down_kernel<4, Out><<<strips_of(a.N), 64 * DOWN_WAVES, lds, s>>>(a, true);
-        else layer_down_kernel<8, Out><<<strips_of(a.N), 64 * DOWN_WAVES, lds, s>>>(a, true);
+        const auto go = [&](auto bits, auto group) {
+            constexpr int G = decltype(group)::value;
+            layer_down_kernel<decltype(bits)::value, G, decltype(out)><<<strips_of(a.N, COLUMNS / G), 64 * DOWN_WAVES, 0, s>>>(a, w, (int)most);
+        };
+        const std::integral_constant<int, 1> one;
+        const std::integral_constant<int, 2> two;
+        const std::integral_constant<int, 4> bits4;
+        const std::integral_constant<int, 8> bits8;
+        if (a.T <= 8) four ? go(bits4, two) : go(bits8, two);
+        else four ? go(bits4, one) : go(bits8, one);
         return hipGetLastError();
     });
 }
 
-hipError_t launch_direct_four(const LayerArgs &a, int x_type, int type, hipStream_t s)
+hipError_t launch_direct_four(const DirectArgs &a, int x_type, int type, hipStream_t s)
 {
-    const dim3 grid(strips_of(a.N), (unsigned)a.T);
+    const dim3 grid(strips_of(a.N, 16), (unsigned)a.T);
     return with_type(x_type, [&](auto in) {
         return with_type(type, [&](auto out) {
             direct_four_kernel<decltype(in), decltype(out)><<<grid, 64 * DOWN_WAVES, 0, s>>>(a, rows_wide(a.x, a.x_stride, x_type));

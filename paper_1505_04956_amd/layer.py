@@ -45,7 +45,7 @@ def layer(x, logits, rule, up, down, bias=None, activation=SILU):
     weights = torch.empty((T, k), dtype=torch.float32, device=x.device)
     if not T:
         return y, ids, weights
-    size = B.asgd_experts_layer_bytes(T, k, down._cols)
+    size = B.asgd_experts_layer_bytes(T, k, E, up._cols, down._cols)
     work = torch.empty(size, dtype=torch.uint8, device=x.device)
     B.asgd_experts_layer(raw, logits.data_ptr(), type_of_logits, stride, None if bias is None else bias.data_ptr(), rule._c, up._c, down._c,
                          activation, ids.data_ptr(), weights.data_ptr(), y.data_ptr(), raw.type, down._rows, work.data_ptr(), size, s)

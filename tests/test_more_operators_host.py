@@ -90,10 +90,10 @@ def test_layers_that_are_refused(form):
 
     def go(x=None, up=up, down=down, rule=None, logits=P, ltype=0, lstride=E, bias=None, act=0, ids=P, weights=P, out=P, type=1, stride=N, work=P, size=None):
         x, rule = x or raw(T, D), rule or B.asgd_route_rule(k, 0, 1, 1, 0, 1, 1.0)
-        size = B.asgd_experts_layer_bytes(T, k, H) if size is None else size
+        size = B.asgd_experts_layer_bytes(T, k, E, D, H) if size is None else size
         return B.lib().asgd_experts_layer(C.addressof(x), logits, ltype, lstride, bias, C.addressof(rule), C.addressof(up), C.addressof(down), act, ids, weights, out, type, stride,
                                           work, size, None)
-    need = B.asgd_experts_layer_bytes(T, k, H)
+    need = B.asgd_experts_layer_bytes(T, k, E, D, H)
     assert need >= T * k * H * 4
     for over in (dict(x=raw(17, D)), dict(x=raw(T, D + 1)), dict(x=blocks(T, D)), dict(up=blocks(2 * H + 1, D, form, E)), dict(up=blocks(2 * H, D, form, E + 1)), dict(up=blocks(2 * H, D, other, E)),
                  dict(down=blocks(N, H + 1, form, E)), dict(down=blocks(0, H, form, E)), dict(up=blocks(2 * H, D, B.BLOCKS_ROWS), down=blocks(N, H, B.BLOCKS_ROWS)),
@@ -102,7 +102,8 @@ def test_layers_that_are_refused(form):
                  dict(weights=P + 1), dict(out=None), dict(out=P + 1), dict(type=3), dict(stride=N - 1), dict(work=None), dict(work=P + 8), dict(size=need - 1)):
         assert go(**over) == B.EINVAL, over
     assert go(x=raw(0, D)) == B.OK
-    assert B.asgd_experts_layer_bytes(17, 2, 5) == B.asgd_experts_layer_bytes(1, 0, 5) == B.asgd_experts_layer_bytes(1, 65, 5) == B.asgd_experts_layer_bytes(1, 1, 0) == B.asgd_experts_layer_bytes(-1, 1, 5) == 0
+    for sizes in ((17, 2, 5, 9, 9), (1, 0, 5, 9, 9), (1, 65, 5, 9, 9), (1, 1, 0, 9, 9), (1, 1, 1025, 9, 9), (1, 1, 5, 0, 9), (1, 1, 5, 9, 0), (-1, 1, 5, 9, 9)):
+        assert B.asgd_experts_layer_bytes(*sizes) == 0
 
 
 def spans(*runs):
