@@ -48,6 +48,42 @@ template <class T> __device__ __forceinline__ void eight_of(const T *row, int64_
         for (int i = 0; i < 8; i++) v[i] = c + i < cols ? (float)row[c + i] : 0.0f;
 }
 
+// To 8 or 4 bits, eight neighbours a lane: sixteen lanes take a block of 128 columns in 8 bits, 32 lanes a run of 256 in 4 bits; either is 128 bytes and its scales.
+template <int BITS> struct Parts;
+template <> struct Parts<8> {
+    static constexpr int LANES = 16, BYTES = 8;
+    typedef uint2 Bytes;
+    typedef float Scale;
+    static __device__ __forceinline__ Bytes to(const float (&v)[8], Scale &scale)
+    {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) top = max(top, magnitude_bits(v[i]));
+        float inverse;
+        block_scale((uint32_t)row_max((int)top), scale, inverse);
+        return make_uint2(eight_bits(v[0], v[1], v[2], v[3], inverse), eight_bits(v[4], v[5], v[6], v[7], inverse));
+    }
+    static __device__ __forceinline__ void put_scale(uint8_t *scales, int part, Scale scale) { if (part == 0) *(float *)scales = scale; }
+    static constexpr int SCALES = 4;             // bytes of a step
+};
+template <> struct Parts<4> {
+    static constexpr int LANES = 32, BYTES = 4;
+    typedef uint32_t Bytes;
+    typedef uint32_t Scale;
+    static __device__ __forceinline__ Bytes to(const float (&v)[8], Scale &scale)
+    {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) top = max(top, magnitude_bits(v[i]));
+        top = max(top, (uint32_t)across<XOR1>((int)top));
+        top = max(top, (uint32_t)across<XOR2>((int)top));
+        scale = four_scale(top);
+        return four_bits(v, four_scale_value(scale));
+    }
+    static __device__ __forceinline__ void put_scale(uint8_t *scales, int part, Scale scale) { if ((part & 3) == 0) scales[part >> 2] = (uint8_t)scale; }
+    static constexpr int SCALES = 8;
+};
+
 // sixteen rows of b (a lane's 32 columns of row lane % 16, columns lane / 16 * 32 of 128) times sixteen of a, added to `sum`, in which a lane has
 // rows lane / 16 * 4 + i of b and row lane % 16 of a.  Scales: the bytes of the lane's own blocks.
 __device__ __forceinline__ v4f four_product(v4i b, uint32_t scale_b, v4i a, uint32_t scale_a, v4f sum)
@@ -55,36 +91,6 @@ __device__ __forceinline__ v4f four_product(v4i b, uint32_t scale_b, v4i a, uint
     const v8i u = {b[0], b[1], b[2], b[3], 0, 0, 0, 0}, w = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, w, sum, 4, 4, 0, (int)scale_b, 0, (int)scale_a);
 }
-
-// a lane's 32 elements of a row from column c on, fetched early, brought to 4 bits when they are there
-template <class Ty> struct RawFour {
-    typename Ty::T u[BLOCK4];
-    __device__ __forceinline__ void load(const typename Ty::T *row, bool there, bool wide, int64_t c, int64_t cols)
-    {
-        if (wide && c + BLOCK4 <= cols) {
-            if (there)
-#pragma unroll
-                for (int n = 0; n < (int)(BLOCK4 * sizeof(typename Ty::T) / 16); n++) *((uint4 *)u + n) = *((const uint4 *)(row + c) + n);
-        } else
-#pragma unroll
-            for (int i = 0; i < BLOCK4; i++) u[i] = there && c + i < cols ? row[c + i] : (typename Ty::T)0.0f;
-    }
-    __device__ __forceinline__ void set(bool there, uint32_t &scale, v4i &values) const
-    {
-        float v[BLOCK4];
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < BLOCK4; i++) {
-            v[i] = there ? (float)u[i] : 0.0f;
-            top = max(top, magnitude_bits(v[i]));
-        }
-        scale = four_scale(top);
-        const float s = four_scale_value(scale);
-#pragma unroll
-        for (int i = 0; i < 4; i++) values[i] = (int)four_bits(v + 8 * i, s);
-    }
-};
-template <> struct RawFour<void> {};
 
 }  // namespace
 

@@ -15,14 +15,9 @@ template <class Ty> __global__ __launch_bounds__(256) void quantize_four_kernel(
         const int64_t r = g / runs, run = g - r * runs, c = run * RUN4 + part * 8;
         float v[8];
         eight_of((const T *)q.x + r * q.stride, c, q.cols, v);
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; i++) top = max(top, magnitude_bits(v[i]));
-        top = max(top, (uint32_t)across<XOR1>((int)top));
-        top = max(top, (uint32_t)across<XOR2>((int)top));
-        const uint32_t scale = four_scale(top);
-        *(uint32_t *)(q.values + g * RUN4_BYTES + part * 4) = four_bits(v, four_scale_value(scale));
-        if ((part & 3) == 0) q.scales[g * RUN4_SCALES + (part >> 2)] = (uint8_t)scale;
+        uint32_t scale;
+        *(uint32_t *)(q.values + g * RUN4_BYTES + part * 4) = Parts<4>::to(v, scale);
+        Parts<4>::put_scale(q.scales + g * RUN4_SCALES, part, scale);
     }
 }
 

@@ -166,17 +166,21 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, TOK_WAVES * WT_WAVES <= 
 }
 
 // ---- few rows -----------------------------------------------------------------------------------------------------
-// The weights go from memory to registers, sixteen rows of a run of 256 columns a wave, and the eight waves of a workgroup share the runs of the
-// contraction of sixteen rows of b.  Rows of a, J times sixteen, come from the caches; RAW ones are brought to 4 bits in the lanes that need them.
+// The weights go from memory to registers, sixteen rows of a run of 256 columns a wave.  A workgroup takes STRIPS times sixteen rows of b, and as many of
+// its eight waves share the runs of each.  Rows of a, J times sixteen, come from the caches.  RAW ones, up to sixteen, are brought to 4 bits by the
+// workgroup, CHUNK runs at a time, while the first weights are on their way, and handed round through the LDS.
 constexpr int FEW4_WAVES = 8;
 
-// grid: strips of sixteen rows of b, tiles of 16 * J rows of a
-template <class In, int J, class Out> __global__ __launch_bounds__(64 * FEW4_WAVES) void product_four_few_kernel(ProductArgs p, bool wide_in, bool wide)
+// grid: groups of strips of sixteen rows of b, tiles of 16 * J rows of a
+template <class In, int J, int STRIPS, class Out> __global__ __launch_bounds__(64 * FEW4_WAVES) void product_four_few_kernel(ProductArgs p, bool wide)
 {
     constexpr bool RAW = !std::is_same<In, void>::value;
+    constexpr int SHARE = FEW4_WAVES / STRIPS, AHEAD = STRIPS == 1 ? 2 : 4, CHUNK = 16, PITCH = RUN4_BYTES + 16;
+    typedef Parts<4> P;
     __shared__ v4f parts[FEW4_WAVES][J][64];
+    __shared__ __align__(16) uint8_t columns[RAW ? CHUNK * 16 * PITCH : 16], scales[RAW ? CHUNK * 16 * RUN4_SCALES : 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t strip = blockIdx.x;
+    const int64_t strip = (int64_t)blockIdx.x * STRIPS + wave % STRIPS;
     int64_t matrix = 0, first = (int64_t)blockIdx.y * (16 * J), end = p.rows_a;
     if (p.mode == ASGD_PRODUCT_GATHER || p.mode == ASGD_PRODUCT_PLACES) {
         int e;
@@ -192,45 +196,73 @@ template <class In, int J, class Out> __global__ __launch_bounds__(64 * FEW4_WAV
     }
     const int64_t r = strip * 16 + tok, row_b = matrix * p.rows_b + (r < p.rows_b ? r : p.rows_b - 1);
     const uint8_t *b = p.b + row_b * p.kb * RUN4_BYTES + quarter * 16, *sb = (const uint8_t *)p.sb + row_b * p.kb * RUN4_SCALES;
-    const int byte = quarter * 8;                                 // of four scales, the lane's (a load of all eight of a run costs half of what two of a byte do)
+    const int byte = quarter * 8, kb = (int)p.kb;                 // of four scales, the lane's (a load of all eight of a run costs half of what two of a byte do)
     v4f sum[J];
 #pragma unroll
     for (int j = 0; j < J; j++) sum[j] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t kb = wave; kb < p.kb; kb += FEW4_WAVES) {
-        v4i w[2], a[J][2];
-        RawFour<In> raw[2];
-        const uint2 of_b = *(const uint2 *)(sb + kb * RUN4_SCALES);
-        uint2 of_a[J];
+    v4i w[AHEAD][2];
+    uint2 of_b[AHEAD];
+    const auto fetch = [&](int run0, int end_run) {
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-            w[half] = *(const v4i *)(b + kb * RUN4_BYTES + half * 64);
-            if constexpr (RAW) raw[half].load((const typename In::T *)p.a + src[0] * p.stride_raw, true, wide_in, kb * RUN4 + half * 128 + quarter * 32, p.cols);
+        for (int n = 0; n < AHEAD; n++) {
+            const int run = run0 + n * SHARE;
+            if (run >= end_run) break;
+            of_b[n] = *(const uint2 *)(sb + (int64_t)run * RUN4_SCALES);
+#pragma unroll
+            for (int half = 0; half < 2; half++) w[n][half] = *(const v4i *)(b + (int64_t)run * RUN4_BYTES + half * 64);
         }
+    };
+    const auto use = [&](int run0, int end_run, int chunk) {
 #pragma unroll
-        for (int j = 0; j < J; j++) {
-            if constexpr (RAW) {
-                raw[0].set(true, of_a[j].x, a[j][0]);
-                raw[1].set(true, of_a[j].y, a[j][1]);
-            } else {
-                const uint8_t *at = p.a + (src[j] * p.kb + kb) * RUN4_BYTES + quarter * 16;
-                a[j][0] = *(const v4i *)at;
-                a[j][1] = *(const v4i *)(at + 64);
-                of_a[j] = *(const uint2 *)((const uint8_t *)p.sa + (src[j] * p.kb + kb) * RUN4_SCALES);
-                of_a[j].x = of_a[j].x >> byte & 255;
-                of_a[j].y = of_a[j].y >> byte & 255;
+        for (int n = 0; n < AHEAD; n++) {
+            const int run = run0 + n * SHARE;
+            if (run >= end_run) break;
+#pragma unroll
+            for (int j = 0; j < J; j++) {
+                const int64_t at = RAW ? (run - chunk) * 16 + tok : src[j] * kb + run;
+                const uint8_t *values = RAW ? columns + at * PITCH + quarter * 16 : p.a + at * RUN4_BYTES + quarter * 16;
+                const v4i a0 = *(const v4i *)values, a1 = *(const v4i *)(values + 64);
+                const uint2 of_a = *(const uint2 *)((RAW ? scales : (const uint8_t *)p.sa) + at * RUN4_SCALES);
+                sum[j] = four_product(w[n][0], of_b[n].x >> byte & 255, a0, of_a.x >> byte & 255, sum[j]);
+                sum[j] = four_product(w[n][1], of_b[n].y >> byte & 255, a1, of_a.y >> byte & 255, sum[j]);
             }
-            sum[j] = four_product(w[0], of_b.x >> byte & 255, a[j][0], of_a[j].x, sum[j]);
-            sum[j] = four_product(w[1], of_b.y >> byte & 255, a[j][1], of_a[j].y, sum[j]);
         }
-    }
+    };
+    const int mine = wave / STRIPS;
+    if constexpr (RAW) {
+        const int rows = (int)min(end - first, (int64_t)16), part = lane & 31;
+        for (int chunk = 0; chunk < kb; chunk += CHUNK) {
+            const int end_run = min(chunk + CHUNK, kb);
+            fetch(chunk + mine, end_run);
+            if (chunk > 0) __syncthreads();
+            for (int i = (int)threadIdx.x >> 5; i < (end_run - chunk) * rows; i += FEW4_WAVES * 2) {
+                const int run = i / rows, row = i - run * rows;
+                float v[8];
+                eight_of((const typename In::T *)p.a + __shfl(src[0], row) * p.stride_raw, (int64_t)(chunk + run) * RUN4 + part * 8, p.cols, v);
+                uint32_t scale;
+                *(uint32_t *)(columns + (run * 16 + row) * PITCH + part * 4) = P::to(v, scale);
+                P::put_scale(scales + (run * 16 + row) * RUN4_SCALES, part, scale);
+            }
+            __syncthreads();
+            for (int run0 = chunk + mine; run0 < end_run; run0 += SHARE * AHEAD) {
+                use(run0, end_run, chunk);
+                fetch(run0 + SHARE * AHEAD, end_run);
+            }
+        }
+    } else
+        for (int run0 = mine; run0 < kb; run0 += SHARE * AHEAD) {
+            fetch(run0, kb);
+            use(run0, kb, 0);
+        }
 #pragma unroll
     for (int j = 0; j < J; j++) parts[wave][j][lane] = sum[j];
     __syncthreads();
-    for (int n = wave; n < J; n += FEW4_WAVES) {
-        v4f total = parts[0][n][lane];
+    for (int n = wave; n < J * STRIPS; n += FEW4_WAVES) {
+        const int j = n / STRIPS, which = n % STRIPS;
+        v4f total = parts[which][j][lane];
 #pragma unroll
-        for (int w = 1; w < FEW4_WAVES; w++) total += parts[w][n][lane];
-        const int64_t row = first + n * 16 + tok, c = strip * 16 + quarter * 4;
+        for (int w = 1; w < SHARE; w++) total += parts[w * STRIPS + which][j][lane];
+        const int64_t row = first + j * 16 + tok, c = ((int64_t)blockIdx.x * STRIPS + which) * 16 + quarter * 4;
         if (row < end) store_four<Out>((typename Out::T *)p.out + row * p.stride + c, p.rows_b - c, wide, total);
     }
 }
@@ -242,6 +274,10 @@ bool grouped4(const ProductArgs &p) { return p.mode == ASGD_PRODUCT_GATHER || p.
 
 // rows of a (of an expert, on average)
 int64_t rows_each4(const ProductArgs &p) { return grouped4(p) ? p.order.T * p.order.k / p.order.E : p.rows_a; }
+
+// Four strips a workgroup (its rows of a, its place among the experts and its end are then there once for four) where that leaves more than a workgroup for
+// each of the 256 compute units.
+bool more_strips4(unsigned strips, unsigned tiles) { return (int64_t)strips * tiles >= 2048; }
 
 template <int N> using Int = std::integral_constant<int, N>;
 
@@ -266,7 +302,9 @@ hipError_t launch_product_four(const ProductArgs &p, int type, hipStream_t s)
         typedef decltype(out) Out;
         const auto few = [&](auto j) {
             constexpr int J = decltype(j)::value;
-            product_four_few_kernel<void, J, Out><<<dim3((unsigned)((p.rows_b + 15) / 16), (unsigned)tiles_of(16 * J)), 64 * FEW4_WAVES, 0, s>>>(p, false, wide4);
+            const unsigned strips = (unsigned)((p.rows_b + 15) / 16), tiles = (unsigned)tiles_of(16 * J);
+            if (more_strips4(strips, tiles)) product_four_few_kernel<void, J, 4, Out><<<dim3((strips + 3) / 4, tiles), 64 * FEW4_WAVES, 0, s>>>(p, wide4);
+            else product_four_few_kernel<void, J, 1, Out><<<dim3(strips, tiles), 64 * FEW4_WAVES, 0, s>>>(p, wide4);
             return hipGetLastError();
         };
         const auto tiles = [&](auto tok, auto wt, auto waves_tok, auto waves_wt, auto by_expert) {
@@ -286,11 +324,11 @@ hipError_t launch_product_four(const ProductArgs &p, int type, hipStream_t s)
 hipError_t launch_product_four_raw(const ProductArgs &p, int raw_type, int type, hipStream_t s)
 {
     const bool wide = p.stride % 4 == 0 && (uintptr_t)p.out % (4 * type_size(type)) == 0;
-    const bool wide_in = p.stride_raw * (int64_t)type_size(raw_type) % 16 == 0 && ((uintptr_t)p.a & 15) == 0;
     const unsigned strips = (unsigned)((p.rows_b + 15) / 16), tiles = grouped4(p) ? (unsigned)most_tiles4(p.order.T * p.order.k, p.order.E, 16) : 1u;
     return with_type(raw_type, [&](auto in) {
         return with_type(type, [&](auto out) {
-            product_four_few_kernel<decltype(in), 1, decltype(out)><<<dim3(strips, tiles), 64 * FEW4_WAVES, 0, s>>>(p, wide_in, wide);
+            if (more_strips4(strips, tiles)) product_four_few_kernel<decltype(in), 1, 4, decltype(out)><<<dim3((strips + 3) / 4, tiles), 64 * FEW4_WAVES, 0, s>>>(p, wide);
+            else product_four_few_kernel<decltype(in), 1, 1, decltype(out)><<<dim3(strips, tiles), 64 * FEW4_WAVES, 0, s>>>(p, wide);
             return hipGetLastError();
         });
     });

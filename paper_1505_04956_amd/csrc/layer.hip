@@ -43,43 +43,6 @@ size_t scratch_of(int64_t T, int k, int64_t E, int64_t D, int64_t H, char *at, S
 }
 
 // ---- bringing rows to 8 or 4 bits -----------------------------------------------------------------------------------
-// Eight neighbours of a step for each lane: sixteen lanes a step of 8 bits, of which four bytes times two and (the first lane's) a scale come, 32 lanes
-// one of 4 bits.
-template <int BITS> struct Parts;
-template <> struct Parts<8> {
-    static constexpr int LANES = 16, BYTES = 8;
-    typedef uint2 Bytes;
-    typedef float Scale;
-    static __device__ __forceinline__ Bytes to(const float (&v)[8], Scale &scale)
-    {
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; i++) top = max(top, magnitude_bits(v[i]));
-        float inverse;
-        block_scale((uint32_t)row_max((int)top), scale, inverse);
-        return make_uint2(eight_bits(v[0], v[1], v[2], v[3], inverse), eight_bits(v[4], v[5], v[6], v[7], inverse));
-    }
-    static __device__ __forceinline__ void put_scale(uint8_t *scales, int part, Scale scale) { if (part == 0) *(float *)scales = scale; }
-    static constexpr int SCALES = 4;             // bytes of a step
-};
-template <> struct Parts<4> {
-    static constexpr int LANES = 32, BYTES = 4;
-    typedef uint32_t Bytes;
-    typedef uint32_t Scale;
-    static __device__ __forceinline__ Bytes to(const float (&v)[8], Scale &scale)
-    {
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; i++) top = max(top, magnitude_bits(v[i]));
-        top = max(top, (uint32_t)across<XOR1>((int)top));
-        top = max(top, (uint32_t)across<XOR2>((int)top));
-        scale = four_scale(top);
-        return four_bits(v, four_scale_value(scale));
-    }
-    static __device__ __forceinline__ void put_scale(uint8_t *scales, int part, Scale scale) { if ((part & 3) == 0) scales[part >> 2] = (uint8_t)scale; }
-    static constexpr int SCALES = 8;
-};
-
 template <int BITS, class T> __device__ __forceinline__ void bring_row(const T *row, int64_t cols, uint8_t *values, uint8_t *scales)
 {
     typedef Parts<BITS> P;
@@ -395,30 +358,43 @@ template <int BITS, int G, class Out> __global__ __launch_bounds__(64 * DOWN_WAV
 
 // ---- experts of one matrix ------------------------------------------------------------------------------------------------
 // The experts of few rows in 4 bits in one launch, without an order: a workgroup takes sixteen rows of the weights of every expert of one row of x
-// (blockIdx.y), which it brings to 4 bits itself.
-template <class In, class Out> __global__ __launch_bounds__(64 * DOWN_WAVES) void direct_four_kernel(DirectArgs a, bool wide)
+// (blockIdx.y), which it brings to 4 bits, CHUNK runs at a time.  Its waves share the runs and, where there are fewer runs than waves, the choices; the weights of EXPERTS of them are on
+// their way at a time.
+template <class In, class Out> __global__ __launch_bounds__(64 * DOWN_WAVES) void direct_four_kernel(DirectArgs a)
 {
+    constexpr int EXPERTS = 4, CHUNK = 32;
     __shared__ v4f parts[DOWN_WAVES][64];
+    __shared__ __align__(16) uint8_t columns[CHUNK * STEP_BYTES], scales[CHUNK * RUN4_SCALES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tok = lane & 15, quarter = lane >> 4;
     const int64_t t = blockIdx.y, strip = (int64_t)blockIdx.x * 16, of_lane = min(strip + tok, a.N - 1);
-    const int steps = (int)runs4(a.K);
+    const int steps = (int)runs4(a.K), share = steps <= 4 ? 4 : steps <= 8 ? 2 : 1;       // waves that share a run's choices
+    const int32_t *ids = a.ids + t * a.k;
     v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int step = wave; step < steps; step += DOWN_WAVES) {
-        RawFour<In> raw[2];
-        Columns<4> c;
-        uint32_t scale[2];
+    Weights<4> w[EXPERTS];
+    const auto id_of = [&](int j) { return j < a.k && (unsigned)ids[j] < (unsigned)a.E ? ids[j] : -1; };       // (the same for all lanes)
+    const auto fetch = [&](int j0, int step) {
 #pragma unroll
-        for (int half = 0; half < 2; half++) raw[half].load((const typename In::T *)a.x + t * a.x_stride, tok == 0, wide, (int64_t)step * RUN4 + half * 128 + quarter * 32, a.K);
-#pragma unroll
-        for (int half = 0; half < 2; half++) raw[half].set(tok == 0, scale[half], c.v[half]);
-        c.scales = make_uint2(scale[0] << quarter * 8, scale[1] << quarter * 8);
-        for (int j = 0; j < a.k; j++) {
-            const int e = a.ids[t * a.k + j];
-            if ((unsigned)e >= (unsigned)a.E) continue;            // (all lanes or none)
-            Weights<4> w;
-            w.load(a.w, steps, e, of_lane, strip, step, quarter);
-            sum = w.times(c, strip, quarter, a.weights[t * a.k + j], sum);
+        for (int i = 0; i < EXPERTS; i++) {
+            const int e = id_of(j0 + i * share);
+            if (e >= 0) w[i].load(a.w, steps, e, of_lane, strip, step, quarter);
         }
+    };
+    const int of_choice = wave % share, first = wave / share, apart = DOWN_WAVES / share;
+    for (int chunk = 0; chunk < steps; chunk += CHUNK) {
+        const int end = min(chunk + CHUNK, steps);
+        if (chunk + first < end) fetch(of_choice, chunk + first);
+        if (chunk > 0) __syncthreads();
+        bring_row<4>((const typename In::T *)a.x + t * a.x_stride + (int64_t)chunk * RUN4, min(a.K - (int64_t)chunk * RUN4, (int64_t)CHUNK * RUN4), columns, scales);
+        __syncthreads();
+        for (int step = chunk + first; step < end; step += apart)
+            for (int j0 = of_choice; j0 < a.k; j0 += EXPERTS * share) {
+                if (step > chunk + first || j0 > of_choice) fetch(j0, step);
+                Columns<4> c;
+                c.load(columns + (step - chunk) * STEP_BYTES, scales + (step - chunk) * RUN4_SCALES, quarter);       // (all sixteen columns: the one row)
+#pragma unroll
+                for (int i = 0; i < EXPERTS; i++)
+                    if (id_of(j0 + i * share) >= 0) sum = w[i].times(c, strip, quarter, a.weights[t * a.k + j0 + i * share], sum);
+            }
     }
     parts[wave][lane] = sum;
     __syncthreads();
@@ -429,7 +405,6 @@ template <class In, class Out> __global__ __launch_bounds__(64 * DOWN_WAVES) voi
     store_four<Out>((typename Out::T *)a.out + t * a.out_stride + c, a.N - c, a.wide_out, sum);
 }
 
-bool rows_wide(const void *p, int64_t stride, int type) { return (uintptr_t)p % 16 == 0 && stride * (int64_t)type_size(type) % 16 == 0; }
 unsigned strips_of(int64_t n, int rows) { return (unsigned)((n + rows - 1) / rows); }
 
 }  // namespace
@@ -479,7 +454,7 @@ hipError_t launch_direct_four(const DirectArgs &a, int x_type, int type, hipStre
     const dim3 grid(strips_of(a.N, 16), (unsigned)a.T);
     return with_type(x_type, [&](auto in) {
         return with_type(type, [&](auto out) {
-            direct_four_kernel<decltype(in), decltype(out)><<<grid, 64 * DOWN_WAVES, 0, s>>>(a, rows_wide(a.x, a.x_stride, x_type));
+            direct_four_kernel<decltype(in), decltype(out)><<<grid, 64 * DOWN_WAVES, 0, s>>>(a);
             return hipGetLastError();
         });
     });
