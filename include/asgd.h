@@ -482,7 +482,7 @@ typedef struct asgd_span {
  * norm (one float, device memory) = the square root of the sum of the squares of all elements of `count` runs, whose squares and sums
  * are 64-bit.  The same runs give the same bits.  work: asgd_gradient_bytes() of scratch, 16-byte aligned, of one call at a time.
  */
-size_t asgd_gradient_bytes(const asgd_span *runs, int64_t count);
+size_t asgd_gradient_bytes(int64_t count);
 int asgd_gradient_norm(const asgd_span *runs, int64_t count, float *norm, void *work, size_t work_bytes, void *hip_stream);
 
 /*

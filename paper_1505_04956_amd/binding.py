@@ -130,7 +130,7 @@ def lib():
             "asgd_block_expand": (C.c_int, [vp, vp, C.c_int, i64, vp]),
             "asgd_experts_layer_bytes": (C.c_size_t, [i64, C.c_int, C.c_int, i64, i64]),
             "asgd_experts_layer": (C.c_int, [vp, vp, C.c_int, i64, vp, vp, vp, vp, C.c_int, vp, vp, vp, C.c_int, i64, vp, C.c_size_t, vp]),
-            "asgd_gradient_bytes": (C.c_size_t, [vp, i64]),
+            "asgd_gradient_bytes": (C.c_size_t, [i64]),
             "asgd_gradient_norm": (C.c_int, [vp, i64, vp, vp, C.c_size_t, vp]),
             "asgd_gradient_clip": (C.c_int, [vp, vp, i64, dbl, vp, vp, C.c_size_t, vp]),
         }
@@ -328,8 +328,8 @@ def asgd_experts_layer(x, logits_ptr, logits_type, logits_stride, bias_ptr, rule
 
 
 # gradients: runs are (address, elements, TYPE_*) as 64-bit integers one after the other, host memory; the tensor-level calls are in gradients.py
-def asgd_gradient_bytes(runs_ptr, count) -> int:
-    return int(lib().asgd_gradient_bytes(runs_ptr, count))
+def asgd_gradient_bytes(count) -> int:
+    return int(lib().asgd_gradient_bytes(count))
 
 
 def asgd_gradient_norm(runs_ptr, count, norm_ptr, work_ptr, work_bytes, stream=0):

@@ -4,7 +4,7 @@
 // adds up, and with it every bit, depends on the sizes alone.  Squares and sums are 64-bit: 10^9 squares added in 32 bits would lose digits, and those
 // of numbers beyond 1.8e19 would be infinite.
 #include <algorithm>
-#include <new>
+#include <type_traits>
 #include <vector>
 
 #include "experts_internal.h"
@@ -16,6 +16,9 @@ namespace {
 constexpr int THREADS = 256, CHUNK = 4096;      // elements
 constexpr int MOST_GROUPS = 2048;               // workgroups, and so sums, of one call: eight a compute unit
 constexpr int IN_ARGUMENTS = 64;                // runs that travel as a launch's arguments; more are written to the scratch first
+constexpr int FEW_THREADS = 1024, FEW_CHUNKS = 16;      // up to so many chunks are one workgroup's, in one launch
+
+#define GLOBAL __attribute__((address_space(1)))
 
 struct Entry {
     const void *in;
@@ -30,64 +33,159 @@ __global__ void table_kernel(Table t, Entry *to, int n)
     if ((int)threadIdx.x < n) to[threadIdx.x] = t.e[threadIdx.x];
 }
 
-// sixteen bytes at any address that an element may have
-template <class T> struct Wide { T v[16 / sizeof(T)]; } __attribute__((packed));
+// N elements, 8 or 16 bytes, at any address that an element may have, which the hardware takes as it does aligned ones
+template <int BYTES> struct Bytes;
+template <> struct Bytes<16> { typedef int T __attribute__((ext_vector_type(4), aligned(2))); };
+template <> struct Bytes<8> { typedef int T __attribute__((ext_vector_type(2), aligned(2))); };
+template <class T, int N> struct Wide {
+    typedef typename Bytes<N * sizeof(T)>::T B;
+    T v[N];
+    __device__ __forceinline__ void load(const GLOBAL T *p)
+    {
+        const B b = *(const GLOBAL B *)p;
+        __builtin_memcpy(v, &b, sizeof(b));
+    }
+    __device__ __forceinline__ void store(GLOBAL T *p) const
+    {
+        B b;
+        __builtin_memcpy(&b, v, sizeof(b));
+        *(GLOBAL B *)p = b;
+    }
+};
 
-template <class T> __device__ __forceinline__ double squares(const T *p, int64_t n, double sum)
+// f(element) for every wide load of a workgroup's part [0, n), four of them together, then what is left, an element each
+template <int N, int GROUP, class F, class G> __device__ __forceinline__ void parts_of(int64_t n, F wide, G one)
+{
+    constexpr int64_t STEP = (int64_t)GROUP * N;
+    const int64_t whole = n / N * N;
+    int64_t i = (int64_t)threadIdx.x * N;
+    for (; i + 3 * STEP < whole; i += 4 * STEP) wide(i, STEP, std::integral_constant<int, 4>());
+    for (; i < whole; i += STEP) wide(i, STEP, std::integral_constant<int, 1>());
+    if (whole + threadIdx.x < n) one(whole + threadIdx.x);
+}
+
+template <int GROUP, class T> __device__ __forceinline__ double squares(const T *in, int64_t n, double sum)
 {
     constexpr int N = 16 / sizeof(T);
-    for (int64_t i = (int64_t)threadIdx.x * N; i < n; i += THREADS * N) {
-        if (i + N <= n) {
-            const Wide<T> w = *(const Wide<T> *)(p + i);
+    typedef Wide<T, N> W;
+    const GLOBAL T *const p = (const GLOBAL T *)in;
+    parts_of<N, GROUP>(n, [&](int64_t i, int64_t step, auto times) {
+        W w[times.value];
 #pragma unroll
-            for (int k = 0; k < N; k++) sum = fma((double)(float)w.v[k], (double)(float)w.v[k], sum);
-        } else
-            for (int64_t k = i; k < n; k++) sum = fma((double)(float)p[k], (double)(float)p[k], sum);
-    }
+        for (int m = 0; m < times.value; m++) w[m].load(p + i + m * step);
+#pragma unroll
+        for (int m = 0; m < times.value; m++)
+#pragma unroll
+            for (int k = 0; k < N; k++) sum = fma((double)(float)w[m].v[k], (double)(float)w[m].v[k], sum);
+    }, [&](int64_t i) { sum = fma((double)(float)p[i], (double)(float)p[i], sum); });
     return sum;
 }
 
+template <int GROUP, class T, class O> __device__ __forceinline__ void scaled(const T *in, O *out, int64_t n, float factor)
+{
+    constexpr int N = 16 / (sizeof(T) > sizeof(O) ? sizeof(T) : sizeof(O));
+    typedef Wide<T, N> W;
+    typedef Wide<O, N> V;
+    const GLOBAL T *const p = (const GLOBAL T *)in;
+    GLOBAL O *const q = (GLOBAL O *)out;
+    parts_of<N, GROUP>(n, [&](int64_t i, int64_t step, auto times) {
+        W w[times.value];
+#pragma unroll
+        for (int m = 0; m < times.value; m++) w[m].load(p + i + m * step);
+#pragma unroll
+        for (int m = 0; m < times.value; m++) {
+            V o;
+#pragma unroll
+            for (int k = 0; k < N; k++) o.v[k] = (O)((float)w[m].v[k] * factor);
+            o.store(q + i + m * step);
+        }
+    }, [&](int64_t i) { q[i] = (O)((float)p[i] * factor); });
+}
+
 // the sum over a workgroup, in all of its threads
-__device__ __forceinline__ double group_sum(double v, double *parts)
+template <int GROUP> __device__ __forceinline__ double group_sum(double v, double *parts)
 {
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = v;
     __syncthreads();
     v = parts[0];
-    for (int w = 1; w < THREADS / 64; w++) v += parts[w];
+    for (int w = 1; w < GROUP / 64; w++) v += parts[w];
     return v;
 }
 
-// chunks [first, last) of a workgroup; calls f(entry, element, elements)
-template <class F> __device__ __forceinline__ void my_chunks(const Entry *e, int count, int64_t chunks, F f)
+// The chunks of workgroup `group` of `groups`, as pieces of runs of at most PIECE chunks, first to last or (LAST_FIRST) the other way: f(entry, element, elements).
+template <bool LAST_FIRST, class F> __device__ __forceinline__ void my_pieces(const Entry *e, int count, int64_t chunks, int64_t group, int64_t groups, F f)
 {
-    const int64_t first = chunks * blockIdx.x / gridDim.x, last = chunks * (blockIdx.x + 1) / gridDim.x;
-    if (first >= last) return;
-    int lo = 0, hi = count;                     // the last run that begins at or before the first chunk and has any
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (e[mid].first <= first) lo = mid; else hi = mid;
-    }
-    for (int64_t c = first; c < last;) {
-        while (lo + 1 < count && e[lo + 1].first <= c) lo++;
-        const int64_t end = lo + 1 < count && e[lo + 1].first < last ? e[lo + 1].first : last;
-        const int64_t from = (c - e[lo].first) * CHUNK, to = (end - e[lo].first) * CHUNK;
-        f(e[lo], from, (to < e[lo].n ? to : e[lo].n) - from);
-        c = end;
+    constexpr int64_t PIECE = 4;
+    const int64_t begin = chunks * group / groups, end = chunks * (group + 1) / groups;
+    if (begin >= end) return;
+    const auto run_of = [&](int64_t c) {        // the last run that begins at or before chunk c (and so has it)
+        int lo = 0, hi = count;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (e[mid].first <= c) lo = mid; else hi = mid;
+        }
+        return lo;
+    };
+    const auto piece = [&](int run, int64_t from, int64_t to) {
+        const Entry &x = e[run];
+        const int64_t element = (from - x.first) * CHUNK, past = (to - x.first) * CHUNK;
+        f(x, element, (past < x.n ? past : x.n) - element);
+    };
+    if (LAST_FIRST) {
+        int run = run_of(end - 1);
+        for (int64_t c = end; c > begin;) {
+            while (e[run].first >= c) run--;
+            int64_t from = c - PIECE > begin ? c - PIECE : begin;
+            if (from < e[run].first) from = e[run].first;
+            piece(run, from, c);
+            c = from;
+        }
+    } else {
+        int run = run_of(begin);
+        for (int64_t c = begin; c < end;) {
+            while (run + 1 < count && e[run + 1].first <= c) run++;
+            int64_t to = c + PIECE < end ? c + PIECE : end;
+            if (run + 1 < count && to > e[run + 1].first) to = e[run + 1].first;
+            piece(run, c, to);
+            c = to;
+        }
     }
 }
+
+template <int GROUP> __device__ __forceinline__ double my_squares(const Entry *e, int count, int64_t chunks, int64_t group, int64_t groups)
+{
+    double sum = 0.0;
+    my_pieces<false>(e, count, chunks, group, groups, [&](const Entry &x, int64_t from, int64_t n) {
+        if (x.type == ASGD_TYPE_F32) sum = squares<GROUP>((const float *)x.in + from, n, sum);
+        else if (x.type == ASGD_TYPE_BF16) sum = squares<GROUP>((const __bf16 *)x.in + from, n, sum);
+        else sum = squares<GROUP>((const _Float16 *)x.in + from, n, sum);
+    });
+    return sum;
+}
+
+// In the other direction than the squares were formed in: what was read last is still in the last cache.
+template <int GROUP> __device__ __forceinline__ void my_scaled(const Entry *e, int count, int64_t chunks, int64_t group, int64_t groups, float factor)
+{
+    my_pieces<true>(e, count, chunks, group, groups, [&](const Entry &x, int64_t from, int64_t n) {
+        const auto to = [&](const auto *p) {
+            if (x.out_type == ASGD_TYPE_F32) scaled<GROUP>(p, (float *)x.out + from, n, factor);
+            else if (x.out_type == ASGD_TYPE_BF16) scaled<GROUP>(p, (__bf16 *)x.out + from, n, factor);
+            else scaled<GROUP>(p, (_Float16 *)x.out + from, n, factor);
+        };
+        if (x.type == ASGD_TYPE_F32) to((const float *)x.in + from);
+        else if (x.type == ASGD_TYPE_BF16) to((const __bf16 *)x.in + from);
+        else to((const _Float16 *)x.in + from);
+    });
+}
+
+__device__ __forceinline__ float factor_of(double norm, double limit) { return norm <= limit ? 1.0f : (float)(limit / norm); }
 
 __global__ __launch_bounds__(THREADS) void squares_kernel(Table t, const Entry *more, int count, int64_t chunks, double *sums)
 {
     __shared__ double parts[THREADS / 64];
-    double sum = 0.0;
-    my_chunks(more ? more : t.e, count, chunks, [&](const Entry &e, int64_t from, int64_t n) {
-        if (e.type == ASGD_TYPE_F32) sum = squares((const float *)e.in + from, n, sum);
-        else if (e.type == ASGD_TYPE_BF16) sum = squares((const __bf16 *)e.in + from, n, sum);
-        else sum = squares((const _Float16 *)e.in + from, n, sum);
-    });
-    sum = group_sum(sum, parts);
+    const double sum = group_sum<THREADS>(my_squares<THREADS>(more ? more : t.e, count, chunks, blockIdx.x, gridDim.x), parts);
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;
 }
 
@@ -95,7 +193,7 @@ __device__ __forceinline__ double norm_of(const double *sums, int n, double *par
 {
     double sum = 0.0;
     for (int i = threadIdx.x; i < n; i += THREADS) sum += sums[i];
-    return sqrt(group_sum(sum, parts));
+    return sqrt(group_sum<THREADS>(sum, parts));
 }
 
 __global__ __launch_bounds__(THREADS) void norm_kernel(const double *sums, int n, float *norm)
@@ -105,40 +203,26 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const double *sums, int n
     if (threadIdx.x == 0) *norm = (float)v;
 }
 
-template <class T, class O> __device__ __forceinline__ void scaled(const T *p, O *q, int64_t n, float factor)
-{
-    constexpr int N = 16 / (sizeof(T) > sizeof(O) ? sizeof(T) : sizeof(O));
-    struct In { T v[N]; } __attribute__((packed));
-    struct Out { O v[N]; } __attribute__((packed));
-    for (int64_t i = (int64_t)threadIdx.x * N; i < n; i += THREADS * N) {
-        if (i + N <= n) {
-            const In w = *(const In *)(p + i);
-            Out o;
-#pragma unroll
-            for (int k = 0; k < N; k++) o.v[k] = (O)((float)w.v[k] * factor);
-            *(Out *)(q + i) = o;
-        } else
-            for (int64_t k = i; k < n; k++) q[k] = (O)((float)p[k] * factor);
-    }
-}
-
 __global__ __launch_bounds__(THREADS) void clip_kernel(Table t, const Entry *more, int count, int64_t chunks, const double *sums, int n, double limit, bool in_place, float *norm)
 {
     __shared__ double parts[THREADS / 64];
     const double v = norm_of(sums, n, parts);
     if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
-    const float factor = v <= limit ? 1.0f : (float)(limit / v);
+    const float factor = factor_of(v, limit);
     if (in_place && factor == 1.0f) return;
-    my_chunks(more ? more : t.e, count, chunks, [&](const Entry &e, int64_t from, int64_t m) {
-        const auto to = [&](const auto *p) {
-            if (e.out_type == ASGD_TYPE_F32) scaled(p, (float *)e.out + from, m, factor);
-            else if (e.out_type == ASGD_TYPE_BF16) scaled(p, (__bf16 *)e.out + from, m, factor);
-            else scaled(p, (_Float16 *)e.out + from, m, factor);
-        };
-        if (e.type == ASGD_TYPE_F32) to((const float *)e.in + from);
-        else if (e.type == ASGD_TYPE_BF16) to((const __bf16 *)e.in + from);
-        else to((const _Float16 *)e.in + from);
-    });
+    my_scaled<THREADS>(more ? more : t.e, count, chunks, blockIdx.x, gridDim.x, factor);
+}
+
+// Both at once for few chunks: the second launch would take longer than one workgroup does.
+template <bool CLIP> __global__ __launch_bounds__(FEW_THREADS) void few_kernel(Table t, int count, int64_t chunks, double limit, bool in_place, float *norm)
+{
+    __shared__ double parts[FEW_THREADS / 64];
+    const double v = sqrt(group_sum<FEW_THREADS>(my_squares<FEW_THREADS>(t.e, count, chunks, 0, 1), parts));
+    if (threadIdx.x == 0) *norm = (float)v;
+    if (!CLIP) return;
+    const float factor = factor_of(v, limit);
+    if (in_place && factor == 1.0f) return;
+    my_scaled<FEW_THREADS>(t.e, count, chunks, 0, 1, factor);
 }
 
 bool span_ok(const asgd_span &s)
@@ -184,35 +268,36 @@ bool apart(const asgd_span *runs, const asgd_span *out, int64_t count)
 int groups_of(int64_t chunks) { return (int)(chunks < MOST_GROUPS ? chunks : MOST_GROUPS); }
 
 // sums first, then the table of more runs than a launch takes as arguments
-size_t bytes_of(int64_t chunks, int64_t count) { return 16 + sizeof(double) * (size_t)((groups_of(chunks) + 1) & ~1) + (count > IN_ARGUMENTS ? sizeof(Entry) * (size_t)count : 0); }
+size_t bytes_of(int64_t count) { return sizeof(double) * MOST_GROUPS + (count > IN_ARGUMENTS ? sizeof(Entry) * (size_t)count : 0); }
 
-struct Work {
-    Table t;
-    Entry *more;
-    double *sums;
-    int64_t chunks;
-    int groups;
-};
-
-// brings the table to where the kernels read it
-hipError_t set_up(const asgd_span *runs, const asgd_span *out, int64_t count, int64_t chunks, void *work, Work &w, hipStream_t s)
+// The norm, and (limit >= 0) what follows from it.
+hipError_t launch(const asgd_span *runs, const asgd_span *out, int64_t count, int64_t chunks, double limit, bool in_place, float *norm, void *work, hipStream_t s)
 {
-    w.chunks = chunks;
-    w.groups = groups_of(chunks);
-    w.sums = (double *)work;
-    w.more = count > IN_ARGUMENTS ? (Entry *)((char *)work + sizeof(double) * (size_t)((w.groups + 1) & ~1)) : nullptr;
+    Table t;
+    double *const sums = (double *)work;
+    Entry *const more = count > IN_ARGUMENTS ? (Entry *)(sums + MOST_GROUPS) : nullptr;
+    const int groups = groups_of(chunks), n = (int)count;
     int64_t first = 0;
     for (int64_t i = 0; i < count; i++) {
         const asgd_span &o = out ? out[i] : runs[i];
-        w.t.e[i % IN_ARGUMENTS] = {runs[i].data, o.data, runs[i].n, first, (int32_t)runs[i].type, (int32_t)o.type};
+        t.e[i % IN_ARGUMENTS] = {runs[i].data, o.data, runs[i].n, first, (int32_t)runs[i].type, (int32_t)o.type};
         first += (runs[i].n + CHUNK - 1) / CHUNK;
-        if (w.more && (i % IN_ARGUMENTS == IN_ARGUMENTS - 1 || i == count - 1)) {
-            table_kernel<<<1, IN_ARGUMENTS, 0, s>>>(w.t, w.more + i / IN_ARGUMENTS * IN_ARGUMENTS, (int)(i % IN_ARGUMENTS) + 1);
+        if (more && (i % IN_ARGUMENTS == IN_ARGUMENTS - 1 || i == count - 1)) {
+            table_kernel<<<1, IN_ARGUMENTS, 0, s>>>(t, more + i / IN_ARGUMENTS * IN_ARGUMENTS, (int)(i % IN_ARGUMENTS) + 1);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
     }
-    if (w.groups) squares_kernel<<<w.groups, THREADS, 0, s>>>(w.t, w.more, (int)count, chunks, w.sums);
+    if (!more && chunks <= FEW_CHUNKS) {
+        if (limit >= 0.0) few_kernel<true><<<1, FEW_THREADS, 0, s>>>(t, n, chunks, limit, in_place, norm);
+        else few_kernel<false><<<1, FEW_THREADS, 0, s>>>(t, n, chunks, limit, in_place, norm);
+        return hipGetLastError();
+    }
+    if (groups) squares_kernel<<<groups, THREADS, 0, s>>>(t, more, n, chunks, sums);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (limit >= 0.0) clip_kernel<<<groups ? groups : 1, THREADS, 0, s>>>(t, more, n, chunks, sums, groups, limit, in_place, norm);
+    else norm_kernel<<<1, THREADS, 0, s>>>(sums, groups, norm);
     return hipGetLastError();
 }
 
@@ -224,29 +309,20 @@ using namespace asgd;
 
 extern "C" {
 
-size_t asgd_gradient_bytes(const asgd_span *runs, int64_t count)
-{
-    const int64_t chunks = chunks_of(runs, count);
-    return chunks < 0 ? 0 : bytes_of(chunks, count);
-}
+size_t asgd_gradient_bytes(int64_t count) { return count < 0 || count > MOST_SPANS ? 0 : bytes_of(count); }
 
 int asgd_gradient_norm(const asgd_span *runs, int64_t count, float *norm, void *work, size_t work_bytes, void *hip_stream)
 {
     const int64_t chunks = chunks_of(runs, count);
-    if (chunks < 0 || !norm || (uintptr_t)norm % 4 || !work || (uintptr_t)work % 16 || work_bytes < bytes_of(chunks, count)) return ASGD_EINVAL;
-    const hipStream_t s = (hipStream_t)hip_stream;
-    Work w;
-    const hipError_t e = set_up(runs, nullptr, count, chunks, work, w, s);
-    if (e != hipSuccess) return ASGD_EHIP;
-    norm_kernel<<<1, THREADS, 0, s>>>(w.sums, w.groups, norm);
-    return hipGetLastError() == hipSuccess ? ASGD_OK : ASGD_EHIP;
+    if (chunks < 0 || !norm || (uintptr_t)norm % 4 || !work || (uintptr_t)work % 16 || work_bytes < bytes_of(count)) return ASGD_EINVAL;
+    return launch(runs, nullptr, count, chunks, -1.0, false, norm, work, (hipStream_t)hip_stream) == hipSuccess ? ASGD_OK : ASGD_EHIP;
 }
 
 int asgd_gradient_clip(const asgd_span *runs, const asgd_span *out, int64_t count, double limit, float *norm, void *work, size_t work_bytes,
                        void *hip_stream)
 {
     const int64_t chunks = chunks_of(runs, count);
-    if (chunks < 0 || !norm || (uintptr_t)norm % 4 || !work || (uintptr_t)work % 16 || work_bytes < bytes_of(chunks, count) || !(limit >= 0.0)) return ASGD_EINVAL;
+    if (chunks < 0 || !norm || (uintptr_t)norm % 4 || !work || (uintptr_t)work % 16 || work_bytes < bytes_of(count) || !(limit >= 0.0)) return ASGD_EINVAL;
     if (out) {
         if (chunks_of(out, count) < 0) return ASGD_EINVAL;
         for (int64_t i = 0; i < count; i++)
@@ -259,12 +335,7 @@ int asgd_gradient_clip(const asgd_span *runs, const asgd_span *out, int64_t coun
     }
     bool in_place = true;
     for (int64_t i = 0; out && i < count; i++) in_place &= out[i].n == 0 || (out[i].data == runs[i].data && out[i].type == runs[i].type);
-    const hipStream_t s = (hipStream_t)hip_stream;
-    Work w;
-    const hipError_t e = set_up(runs, out, count, chunks, work, w, s);
-    if (e != hipSuccess) return ASGD_EHIP;
-    clip_kernel<<<w.groups ? w.groups : 1, THREADS, 0, s>>>(w.t, w.more, (int)count, chunks, w.sums, w.groups, limit, in_place, norm);
-    return hipGetLastError() == hipSuccess ? ASGD_OK : ASGD_EHIP;
+    return launch(runs, out, count, chunks, limit, in_place, norm, work, (hipStream_t)hip_stream) == hipSuccess ? ASGD_OK : ASGD_EHIP;
 }
 
 }  // extern "C"

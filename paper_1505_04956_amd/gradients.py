@@ -9,6 +9,7 @@ for: the norm is a tensor, and what it decides is decided on the GPU.
 from __future__ import annotations
 
 from array import array
+from functools import lru_cache
 
 import torch
 from torch.autograd import forward_ad
@@ -17,30 +18,36 @@ from . import binding as B
 from . import experts as X
 
 
-def _spans(tensors, like, name):
-    """(ptr, n, type) of each, one after the other."""
-    index, spans = like.get_device(), array("q")
+def _spans(tensors, index, name):
+    """(ptr, n, type) of each, one after the other, for the library."""
+    spans, types, dual = [], X._TYPES, forward_ad._current_level >= 0
     for t in tensors:
-        if t.requires_grad or forward_ad._current_level >= 0:
+        if t.requires_grad or dual:
             X._no_history(t, name)
         if t.get_device() != index:
-            raise ValueError("tensors on %s and %s" % (like.device, t.device))
+            raise ValueError("tensors on %s and %s" % (tensors[0].device, t.device))
         if not t.is_contiguous():
             raise ValueError("%s: contiguous tensors are wanted, not %s with strides %s" % (name, tuple(t.shape), t.stride()))
-        spans.extend((t.data_ptr(), t.numel(), X._type(t.dtype)))
-    return spans
+        code = types.get(t.dtype)
+        spans += (t.data_ptr(), t.numel(), X._type(t.dtype) if code is None else code)
+    return array("q", spans)
 
 
 def _prepare(tensors):
     tensors = list(tensors)
     if not tensors:
         raise ValueError("no tensors")
-    return tensors, _spans(tensors, tensors[0], "gradients")
+    return tensors, _spans(tensors, tensors[0].get_device(), "gradients")
 
 
-def _memory(spans, count, device):
-    size = B.asgd_gradient_bytes(spans.buffer_info()[0], count)
-    return torch.empty((), dtype=torch.float32, device=device), torch.empty(size, dtype=torch.uint8, device=device), size
+@lru_cache(maxsize=64)
+def _scratch_bytes(count):
+    return B.asgd_gradient_bytes(count)
+
+
+def _memory(count, like):
+    size = _scratch_bytes(count)
+    return like.new_empty((), dtype=torch.float32), like.new_empty(size, dtype=torch.uint8), size
 
 
 def norm(tensors):
@@ -48,7 +55,7 @@ def norm(tensors):
     in 64 bits: it is infinite only where an element is, or the norm is beyond float32.  The same tensors give the same bits."""
     tensors, spans = _prepare(tensors)
     s = X._stream(tensors[0])
-    out, work, size = _memory(spans, len(tensors), tensors[0].device)
+    out, work, size = _memory(len(tensors), tensors[0])
     B.asgd_gradient_norm(spans.buffer_info()[0], len(tensors), out.data_ptr(), work.data_ptr(), size, s)
     return out
 
@@ -64,11 +71,11 @@ def clip(tensors, limit, out=None):
     to = None
     if out is not None:
         out = list(out)
-        if len(out) != len(tensors) or any(a.shape != b.shape for a, b in zip(out, tensors)):
+        if len(out) != len(tensors) or [t.shape for t in out] != [t.shape for t in tensors]:
             raise ValueError("out: a tensor of the same size for each gradient is wanted")
-        to = _spans(out, tensors[0], "out")
+        to = _spans(out, tensors[0].get_device(), "out")
     s = X._stream(tensors[0])
-    result, work, size = _memory(spans, len(tensors), tensors[0].device)
+    result, work, size = _memory(len(tensors), tensors[0])
     B.asgd_gradient_clip(spans.buffer_info()[0], None if to is None else to.buffer_info()[0], len(tensors), limit, result.data_ptr(),
                          work.data_ptr(), size, s)
     return result

@@ -9,6 +9,8 @@ For prompts and for training there are the calls that it stands for: experts.rou
 """
 from __future__ import annotations
 
+from functools import lru_cache
+
 import torch
 
 from . import binding as B
@@ -17,6 +19,11 @@ from . import micro as M
 
 SILU, GELU = B.ACTIVATION_SILU, B.ACTIVATION_GELU
 ROWS = B.PRODUCT_RAW_ROWS        # that a call takes at most
+
+
+@lru_cache(maxsize=256)
+def _scratch_bytes(T, k, E, D, H):
+    return B.asgd_experts_layer_bytes(T, k, E, D, H)
 
 
 def layer(x, logits, rule, up, down, bias=None, activation=SILU):
@@ -31,7 +38,7 @@ def layer(x, logits, rule, up, down, bias=None, activation=SILU):
     if down._count != E or up._rows != 2 * down._cols:
         raise ValueError("up, %d experts [%d, %d], and down, %d [%d, %d], do not belong together" % (
             E, up._rows, up._cols, down._count, down._rows, down._cols))
-    X._same_device(x, logits, up._values, down._values, bias)
+    X._same_device(x, logits, *((up._memory, down._memory) if isinstance(up, M.Micro) else (up._values, down._values)), bias)
     raw = X._raw(x)
     T = raw.rows
     if x.shape[1] != up._cols or T > ROWS:
@@ -40,13 +47,13 @@ def layer(x, logits, rule, up, down, bias=None, activation=SILU):
     if bias is not None:
         X._flat(bias, (E,), torch.float32, "bias")
     s, k = X._stream(x), rule._k
-    y = torch.empty((T, down._rows), dtype=x.dtype, device=x.device)
-    ids = torch.empty((T, k), dtype=torch.int32, device=x.device)
-    weights = torch.empty((T, k), dtype=torch.float32, device=x.device)
+    y = x.new_empty((T, down._rows))
+    ids = x.new_empty((T, k), dtype=torch.int32)
+    weights = x.new_empty((T, k), dtype=torch.float32)
     if not T:
         return y, ids, weights
-    size = B.asgd_experts_layer_bytes(T, k, E, up._cols, down._cols)
-    work = torch.empty(size, dtype=torch.uint8, device=x.device)
+    size = _scratch_bytes(T, k, E, up._cols, down._cols)
+    work = x.new_empty(size, dtype=torch.uint8)
     B.asgd_experts_layer(raw, logits.data_ptr(), type_of_logits, stride, None if bias is None else bias.data_ptr(), rule._c, up._c, down._c,
                          activation, ids.data_ptr(), weights.data_ptr(), y.data_ptr(), raw.type, down._rows, work.data_ptr(), size, s)
     return y, ids, weights

@@ -11,6 +11,8 @@ bfloat16 or float16.
 """
 from __future__ import annotations
 
+import math
+
 import torch
 from torch.autograd import forward_ad
 
@@ -28,22 +30,47 @@ def _runs(cols):
 class Micro:
     """A matrix, or one for each expert, in 4 bits: values [..., rows, 128 * ceil(cols / 256)] uint8, two e2m1 numbers a byte, the first in the low four
     bits, zeros from `cols` on; scales [..., rows, 8 * ceil(cols / 256)] uint8, 2^(byte - 127) for 32 columns each, 255: not a number."""
-    __slots__ = ("_values", "_scales", "_rows", "_cols", "_count", "_c")
-    values, scales, rows, cols, count = X._fixed("values", "scales", "rows", "cols", "count")
+    __slots__ = ("_memory", "_values", "_scales", "_rows", "_cols", "_count", "_lead", "_c")
+    rows, cols, count = X._fixed("rows", "cols", "count")
 
     def __init__(self, values, scales, cols):
-        kf, shape, dims = _runs(cols), values.shape, values.dim()
-        if values.dtype is not torch.uint8 or dims not in (2, 3) or shape[-1] != kf * (RUN // 2) or not values.is_contiguous():
+        kf, shape = _runs(cols), values.shape
+        if values.dtype is not torch.uint8 or len(shape) not in (2, 3) or shape[-1] != kf * (RUN // 2) or not values.is_contiguous():
             raise ValueError("values: contiguous uint8 [..., rows, %d] are wanted, not %s %s" % (kf * (RUN // 2), values.dtype, tuple(shape)))
-        X._flat(scales, (*shape[:-1], kf * (RUN // SMALL)), torch.uint8, "scales")
+        lead = shape[:-1]
+        X._flat(scales, (*lead, kf * (RUN // SMALL)), torch.uint8, "scales")
         X._same_device(values, scales)
-        self._set(values, scales, cols)
+        self._memory, self._values, self._scales = values, values, scales
+        self._set(lead, cols, values.data_ptr(), scales.data_ptr())
 
-    def _set(self, values, scales, cols):
-        shape = values.shape
-        self._values, self._scales, self._cols = values, scales, cols
-        self._rows, self._count = shape[-2], shape[0] if len(shape) == 3 else 1
-        self._c = B.asgd_blocks(values.data_ptr(), scales.data_ptr(), self._rows, cols, B.BLOCKS_FOURS, self._count, 0, 0)
+    def _set(self, lead, cols, values, scales):
+        self._lead, self._rows, self._cols, self._count = lead, lead[-1], cols, lead[0] if len(lead) == 2 else 1
+        self._c = B.asgd_blocks(values, scales, self._rows, cols, B.BLOCKS_FOURS, self._count, 0, 0)
+
+    @classmethod
+    def _empty(cls, lead, cols, like):
+        """Room for one in one piece of memory (values and scales are made of it when they are asked for)."""
+        self = cls.__new__(cls)
+        n = math.prod(lead) * _runs(cols)
+        self._memory = torch.empty(n * (RUN // 2 + RUN // SMALL), dtype=torch.uint8, device=like.device)
+        self._values = self._scales = None
+        at = self._memory.data_ptr()
+        self._set(lead, cols, at, at + n * (RUN // 2))
+        return self
+
+    @property
+    def values(self):
+        if self._values is None:
+            n = self._memory.numel() // 17 * 16                        # (128 bytes of values, 8 of scales)
+            self._values = self._memory[:n].view(*self._lead, -1) if n else self._memory.view(*self._lead, _runs(self._cols) * (RUN // 2))
+        return self._values
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            n = self._memory.numel() // 17 * 16
+            self._scales = self._memory[n:].view(*self._lead, -1) if n else self._memory.view(*self._lead, _runs(self._cols) * (RUN // SMALL))
+        return self._scales
 
 
 def quantize(x):
@@ -54,15 +81,13 @@ def quantize(x):
             raise ValueError("x: a contiguous [experts, rows, cols] is wanted, not %s" % (tuple(x.shape),))
         if x.requires_grad or forward_ad._current_level >= 0:
             X._no_history(x, "x")
-        lead, rows, cols = x.shape[:1], *x.shape[1:]
+        lead, (rows, cols) = x.shape[:2], x.shape[1:]
         type, stride = X._type(x.dtype), cols
     else:
         type, rows, cols, stride = X._matrix(x)
-        lead = ()
+        lead = (rows,)
     s = X._stream(x)
-    out = Micro.__new__(Micro)
-    out._set(torch.empty((*lead, rows, _runs(cols) * (RUN // 2)), dtype=torch.uint8, device=x.device),
-             torch.empty((*lead, rows, _runs(cols) * (RUN // SMALL)), dtype=torch.uint8, device=x.device), cols)
+    out = Micro._empty(lead, cols, x)
     if rows:
         B.asgd_block_quantize(x.data_ptr(), type, rows, cols, stride, 0, None, None, out._c, s)
     return out
@@ -70,18 +95,10 @@ def quantize(x):
 
 def expand(m, dtype=torch.float32):
     """The values that m stands for, [..., rows, cols] in `dtype`."""
-    type, s = X._type(dtype), X._stream(m._values)
-    out = torch.empty((*m._values.shape[:-1], m._cols), dtype=dtype, device=m._values.device)
+    type, s = X._type(dtype), X._stream(m._memory)
+    out = torch.empty((*m._lead, m._cols), dtype=dtype, device=m._memory.device)
     if out.numel():
         B.asgd_block_expand(m._c, out.data_ptr(), type, m._cols, s)
-    return out
-
-
-def _product(a, rows, w, dtype, plan, mode, out_rows, device):
-    type, s = X._type(dtype), X._raw_stream(device.index)
-    out = torch.empty((out_rows, w._rows), dtype=dtype, device=device)
-    if out_rows:
-        B.asgd_block_product(a, w._c, mode, 1, None if plan is None else plan._c, out.data_ptr(), type, w._rows, s)
     return out
 
 
@@ -89,55 +106,59 @@ def product(a, b, dtype, plan=None, gather=False):
     """a b^T in `dtype` of two Micro of the same cols.  With a plan b has a matrix for each expert, and row p of the result is that of
     the place p with the matrix of its expert: a has a row for each place, or with `gather` one for each of the plan's T rows.  Rows at
     places that are not in use are left as they were allocated.  Products are summed in 32 bits."""
-    X._same_device(a._values, b._values, None if plan is None else plan._memory)
-    X._stream(a._values)
-    return _product(a._c, a._rows, b, dtype, plan, B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER if gather else B.PRODUCT_PLACES,
-                    a._rows if plan is None else plan._T * plan._k, a._values.device)
-
-
-def _product_of(x, w, dtype, plan=None):
-    """x, one row for each of the plan's T, times w."""
-    rows = x.shape[0] if plan is None else plan._T * plan._k
-    mode = B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER
-    # (few rows of an expert: bringing them to 4 bits again in each strip of its weights takes less than another launch)
-    if 0 < rows <= (B.PRODUCT_RAW_ROWS if plan is None else min(B.PRODUCT_RAW_SLOTS, 16 * plan._E)):
-        raw = X._raw(x)
-        X._stream(x)
-    else:
-        small = quantize(x)
-        raw = small._c
-    return _product(raw, x.shape[0], w, dtype, plan, mode, rows, x.device)
+    X._same_device(a._memory, b._memory, None if plan is None else plan._memory)
+    type, s = X._type(dtype), X._stream(a._memory)
+    rows = a._rows if plan is None else plan._T * plan._k
+    out = torch.empty((rows, b._rows), dtype=dtype, device=a._memory.device)
+    if rows:
+        B.asgd_block_product(a._c, b._c, B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER if gather else B.PRODUCT_PLACES, 1,
+                             None if plan is None else plan._c, out.data_ptr(), type, b._rows, s)
+    return out
 
 
 def _check(x, w, experts=False):
-    if not isinstance(w, Micro) or (w._count != 1 and not experts):
+    if type(w) is not Micro or (w._count != 1 and not experts):
         raise ValueError("weights in 4 bits are wanted%s" % ("" if experts else ", one matrix of them"))
-    if x.dim() != 2 or x.shape[1] != w._cols:
-        raise ValueError("x: [rows, %d] is wanted, not %s" % (w._cols, tuple(x.shape)))
+    shape = x.shape
+    if len(shape) != 2 or shape[1] != w._cols:
+        raise ValueError("x: [rows, %d] is wanted, not %s" % (w._cols, tuple(shape)))
+    return shape[0]
 
 
 def linear(x, w):
     """x [rows, K] times w^T, in x's type: x is brought to 4 bits on the way, w is quantize() of [N, K]."""
-    _check(x, w)
-    X._same_device(x, w._values)
-    return _product_of(x, w, x.dtype)
+    rows = _check(x, w)
+    X._same_device(x, w._memory)
+    # (few rows: bringing them to 4 bits again in each strip of the weights takes less than another launch)
+    if rows > B.PRODUCT_RAW_ROWS:
+        return product(quantize(x), w, x.dtype)
+    raw = X._raw(x)
+    s, out = X._stream(x), x.new_empty((rows, w._rows))
+    if rows:
+        B.asgd_block_product(raw, w._c, B.PRODUCT_ALL, 1, None, out.data_ptr(), raw.type, w._rows, s)
+    return out
 
 
 def experts(x, ids, weights, w):
     """[T, N] in x's type: for each row of x [T, K] the sum of its experts' products with it, weights [T, k] times w[ids] x, ids as
     experts.route() gives them (what is outside 0 .. E - 1 has no expert).  w is quantize() of [E, N, K]; x is brought to 4 bits on the way."""
-    _check(x, w, experts=True)
-    X._same_device(x, ids, weights, w._values)
-    T = x.shape[0]
+    T = _check(x, w, experts=True)
+    X._same_device(x, ids, weights, w._memory)
     if ids.dim() != 2 or ids.shape[0] != T:
         raise ValueError("ids: [%d, k] is wanted, not %s" % (T, tuple(ids.shape)))
     X._flat(ids, ids.shape, torch.int32, "ids")
     X._flat(weights, ids.shape, torch.float32, "weights")
-    if 0 < T <= B.PRODUCT_RAW_ROWS and ids.numel() * w._rows * w._cols <= 2 * X.DIRECT_BYTES:
-        raw, s = X._raw(x), X._stream(x)
-        out = torch.empty((T, w._rows), dtype=x.dtype, device=x.device)
-        B.asgd_experts_direct(raw, ids.data_ptr(), weights.data_ptr(), ids.shape[1], w._c, 1, out.data_ptr(), X._type(x.dtype), w._rows, s)
+    raw = X._raw(x)
+    s, slots = X._stream(x), ids.numel()
+    if 0 < T <= B.PRODUCT_RAW_ROWS and slots * w._rows * w._cols <= 2 * X.DIRECT_BYTES:
+        out = x.new_empty((T, w._rows))
+        B.asgd_experts_direct(raw, ids.data_ptr(), weights.data_ptr(), ids.shape[1], w._c, 1, out.data_ptr(), raw.type, w._rows, s)
         return out
-    X._matrix(x)
     order = X.plan(ids, w._count)
-    return X.experts_sum(_product_of(x, w, torch.float32, order), order, x.dtype, weights)
+    # 32-bit until the sum: one rounding to the result's type.  (Few rows of an expert are brought to 4 bits inside the product.)
+    if 0 < slots <= min(B.PRODUCT_RAW_SLOTS, 16 * w._count):
+        y = torch.empty((slots, w._rows), dtype=torch.float32, device=x.device)
+        B.asgd_block_product(raw, w._c, B.PRODUCT_GATHER, 1, order._c, y.data_ptr(), B.TYPE_F32, w._rows, s)
+    else:
+        y = product(quantize(x), w, torch.float32, order, gather=True)
+    return X.experts_sum(y, order, x.dtype, weights)
