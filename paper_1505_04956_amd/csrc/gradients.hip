@@ -16,6 +16,7 @@ namespace {
 constexpr int THREADS = 256, CHUNK = 4096;      // elements
 constexpr int MOST_GROUPS = 2048;               // workgroups, and so sums, of one call: eight a compute unit
 constexpr int IN_ARGUMENTS = 64;                // runs that travel as a launch's arguments; more are written to the scratch first
+constexpr int64_t LAST_CACHE = 256 << 20;       // bytes
 constexpr int FEW_THREADS = 1024, FEW_CHUNKS = 16;      // up to so many chunks are one workgroup's, in one launch
 
 #define GLOBAL __attribute__((address_space(1)))
@@ -40,9 +41,11 @@ template <> struct Bytes<8> { typedef int T __attribute__((ext_vector_type(2), a
 template <class T, int N> struct Wide {
     typedef typename Bytes<N * sizeof(T)>::T B;
     T v[N];
-    __device__ __forceinline__ void load(const GLOBAL T *p)
+    template <bool ONCE> __device__ __forceinline__ void load(const GLOBAL T *p)
     {
-        const B b = *(const GLOBAL B *)p;
+        B b;
+        if constexpr (ONCE) b = __builtin_nontemporal_load((const GLOBAL B *)p);
+        else b = *(const GLOBAL B *)p;
         __builtin_memcpy(v, &b, sizeof(b));
     }
     __device__ __forceinline__ void store(GLOBAL T *p) const
@@ -64,7 +67,7 @@ template <int N, int GROUP, class F, class G> __device__ __forceinline__ void pa
     if (whole + threadIdx.x < n) one(whole + threadIdx.x);
 }
 
-template <int GROUP, class T> __device__ __forceinline__ double squares(const T *in, int64_t n, double sum)
+template <int GROUP, bool ONCE, class T> __device__ __forceinline__ double squares(const T *in, int64_t n, double sum)
 {
     constexpr int N = 16 / sizeof(T);
     typedef Wide<T, N> W;
@@ -72,7 +75,7 @@ template <int GROUP, class T> __device__ __forceinline__ double squares(const T 
     parts_of<N, GROUP>(n, [&](int64_t i, int64_t step, auto times) {
         W w[times.value];
 #pragma unroll
-        for (int m = 0; m < times.value; m++) w[m].load(p + i + m * step);
+        for (int m = 0; m < times.value; m++) w[m].template load<ONCE>(p + i + m * step);
 #pragma unroll
         for (int m = 0; m < times.value; m++)
 #pragma unroll
@@ -91,7 +94,7 @@ template <int GROUP, class T, class O> __device__ __forceinline__ void scaled(co
     parts_of<N, GROUP>(n, [&](int64_t i, int64_t step, auto times) {
         W w[times.value];
 #pragma unroll
-        for (int m = 0; m < times.value; m++) w[m].load(p + i + m * step);
+        for (int m = 0; m < times.value; m++) w[m].template load<false>(p + i + m * step);
 #pragma unroll
         for (int m = 0; m < times.value; m++) {
             V o;
@@ -114,61 +117,43 @@ template <int GROUP> __device__ __forceinline__ double group_sum(double v, doubl
     return v;
 }
 
-// The chunks of workgroup `group` of `groups`, as pieces of runs of at most PIECE chunks, first to last or (LAST_FIRST) the other way: f(entry, element, elements).
-template <bool LAST_FIRST, class F> __device__ __forceinline__ void my_pieces(const Entry *e, int count, int64_t chunks, int64_t group, int64_t groups, F f)
+// The chunks of workgroup `group` of `groups`, as parts of runs: f(entry, element, elements)
+template <class F> __device__ __forceinline__ void my_parts(const Entry *e, int count, int64_t chunks, int64_t group, int64_t groups, F f)
 {
-    constexpr int64_t PIECE = 4;
     const int64_t begin = chunks * group / groups, end = chunks * (group + 1) / groups;
     if (begin >= end) return;
-    const auto run_of = [&](int64_t c) {        // the last run that begins at or before chunk c (and so has it)
-        int lo = 0, hi = count;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (e[mid].first <= c) lo = mid; else hi = mid;
-        }
-        return lo;
-    };
-    const auto piece = [&](int run, int64_t from, int64_t to) {
+    int run = 0, past = count;                  // the last run that begins at or before the first chunk (and so has it)
+    while (past - run > 1) {
+        const int mid = (run + past) / 2;
+        if (e[mid].first <= begin) run = mid; else past = mid;
+    }
+    for (int64_t c = begin; c < end;) {
+        while (run + 1 < count && e[run + 1].first <= c) run++;
         const Entry &x = e[run];
-        const int64_t element = (from - x.first) * CHUNK, past = (to - x.first) * CHUNK;
-        f(x, element, (past < x.n ? past : x.n) - element);
-    };
-    if (LAST_FIRST) {
-        int run = run_of(end - 1);
-        for (int64_t c = end; c > begin;) {
-            while (e[run].first >= c) run--;
-            int64_t from = c - PIECE > begin ? c - PIECE : begin;
-            if (from < e[run].first) from = e[run].first;
-            piece(run, from, c);
-            c = from;
-        }
-    } else {
-        int run = run_of(begin);
-        for (int64_t c = begin; c < end;) {
-            while (run + 1 < count && e[run + 1].first <= c) run++;
-            int64_t to = c + PIECE < end ? c + PIECE : end;
-            if (run + 1 < count && to > e[run + 1].first) to = e[run + 1].first;
-            piece(run, c, to);
-            c = to;
-        }
+        const int64_t to = run + 1 < count && e[run + 1].first < end ? e[run + 1].first : end;
+        const int64_t element = (c - x.first) * CHUNK, last = (to - x.first) * CHUNK;
+        f(x, element, (last < x.n ? last : x.n) - element);
+        c = to;
     }
 }
 
-template <int GROUP> __device__ __forceinline__ double my_squares(const Entry *e, int count, int64_t chunks, int64_t group, int64_t groups)
+// once: more than the last cache holds, which it passes by (it holds what was written before, and what is read again would not be there any more: the squares
+// of 1.6 GB take 253 us so and 303 through it, clipping them to 0.8 GB next 534 and 518)
+template <int GROUP> __device__ __forceinline__ double my_squares(const Entry *e, int count, int64_t chunks, int64_t group, int64_t groups, bool once)
 {
     double sum = 0.0;
-    my_pieces<false>(e, count, chunks, group, groups, [&](const Entry &x, int64_t from, int64_t n) {
-        if (x.type == ASGD_TYPE_F32) sum = squares<GROUP>((const float *)x.in + from, n, sum);
-        else if (x.type == ASGD_TYPE_BF16) sum = squares<GROUP>((const __bf16 *)x.in + from, n, sum);
-        else sum = squares<GROUP>((const _Float16 *)x.in + from, n, sum);
+    my_parts(e, count, chunks, group, groups, [&](const Entry &x, int64_t from, int64_t n) {
+        const auto add = [&](const auto *p) { sum = once ? squares<GROUP, true>(p, n, sum) : squares<GROUP, false>(p, n, sum); };
+        if (x.type == ASGD_TYPE_F32) add((const float *)x.in + from);
+        else if (x.type == ASGD_TYPE_BF16) add((const __bf16 *)x.in + from);
+        else add((const _Float16 *)x.in + from);
     });
     return sum;
 }
 
-// In the other direction than the squares were formed in: what was read last is still in the last cache.
 template <int GROUP> __device__ __forceinline__ void my_scaled(const Entry *e, int count, int64_t chunks, int64_t group, int64_t groups, float factor)
 {
-    my_pieces<true>(e, count, chunks, group, groups, [&](const Entry &x, int64_t from, int64_t n) {
+    my_parts(e, count, chunks, group, groups, [&](const Entry &x, int64_t from, int64_t n) {
         const auto to = [&](const auto *p) {
             if (x.out_type == ASGD_TYPE_F32) scaled<GROUP>(p, (float *)x.out + from, n, factor);
             else if (x.out_type == ASGD_TYPE_BF16) scaled<GROUP>(p, (__bf16 *)x.out + from, n, factor);
@@ -182,10 +167,10 @@ template <int GROUP> __device__ __forceinline__ void my_scaled(const Entry *e, i
 
 __device__ __forceinline__ float factor_of(double norm, double limit) { return norm <= limit ? 1.0f : (float)(limit / norm); }
 
-__global__ __launch_bounds__(THREADS) void squares_kernel(Table t, const Entry *more, int count, int64_t chunks, double *sums)
+__global__ __launch_bounds__(THREADS) void squares_kernel(Table t, const Entry *more, int count, int64_t chunks, bool once, double *sums)
 {
     __shared__ double parts[THREADS / 64];
-    const double sum = group_sum<THREADS>(my_squares<THREADS>(more ? more : t.e, count, chunks, blockIdx.x, gridDim.x), parts);
+    const double sum = group_sum<THREADS>(my_squares<THREADS>(more ? more : t.e, count, chunks, blockIdx.x, gridDim.x, once), parts);
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;
 }
 
@@ -217,7 +202,7 @@ __global__ __launch_bounds__(THREADS) void clip_kernel(Table t, const Entry *mor
 template <bool CLIP> __global__ __launch_bounds__(FEW_THREADS) void few_kernel(Table t, int count, int64_t chunks, double limit, bool in_place, float *norm)
 {
     __shared__ double parts[FEW_THREADS / 64];
-    const double v = sqrt(group_sum<FEW_THREADS>(my_squares<FEW_THREADS>(t.e, count, chunks, 0, 1), parts));
+    const double v = sqrt(group_sum<FEW_THREADS>(my_squares<FEW_THREADS>(t.e, count, chunks, 0, 1, false), parts));
     if (threadIdx.x == 0) *norm = (float)v;
     if (!CLIP) return;
     const float factor = factor_of(v, limit);
@@ -277,11 +262,12 @@ hipError_t launch(const asgd_span *runs, const asgd_span *out, int64_t count, in
     double *const sums = (double *)work;
     Entry *const more = count > IN_ARGUMENTS ? (Entry *)(sums + MOST_GROUPS) : nullptr;
     const int groups = groups_of(chunks), n = (int)count;
-    int64_t first = 0;
+    int64_t first = 0, bytes = 0;
     for (int64_t i = 0; i < count; i++) {
         const asgd_span &o = out ? out[i] : runs[i];
         t.e[i % IN_ARGUMENTS] = {runs[i].data, o.data, runs[i].n, first, (int32_t)runs[i].type, (int32_t)o.type};
         first += (runs[i].n + CHUNK - 1) / CHUNK;
+        bytes += runs[i].n * (int64_t)type_size((int)runs[i].type);
         if (more && (i % IN_ARGUMENTS == IN_ARGUMENTS - 1 || i == count - 1)) {
             table_kernel<<<1, IN_ARGUMENTS, 0, s>>>(t, more + i / IN_ARGUMENTS * IN_ARGUMENTS, (int)(i % IN_ARGUMENTS) + 1);
             const hipError_t e = hipGetLastError();
@@ -293,7 +279,7 @@ hipError_t launch(const asgd_span *runs, const asgd_span *out, int64_t count, in
         else few_kernel<false><<<1, FEW_THREADS, 0, s>>>(t, n, chunks, limit, in_place, norm);
         return hipGetLastError();
     }
-    if (groups) squares_kernel<<<groups, THREADS, 0, s>>>(t, more, n, chunks, sums);
+    if (groups) squares_kernel<<<groups, THREADS, 0, s>>>(t, more, n, chunks, bytes > LAST_CACHE, sums);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (limit >= 0.0) clip_kernel<<<groups ? groups : 1, THREADS, 0, s>>>(t, more, n, chunks, sums, groups, limit, in_place, norm);
