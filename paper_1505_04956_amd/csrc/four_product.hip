@@ -11,22 +11,22 @@ namespace {
 
 // ---- many rows ----------------------------------------------------------------------------------------------------
 // A tile of TOK rows of a and WT rows of b; the waves are TOK_WAVES x WT_WAVES, each with I x J pieces of 16 x 16.  A stage in the LDS is a run of 256
-// columns of all rows, 128 bytes of values and 8 of scales each, filled straight from memory while the other is multiplied; sixteen-byte pieces of a row lie at their
-// number xor the row's low bits, so that the lanes of a read spread over the banks.
-template <int TOK, int WT> struct Stage4 {
-    static constexpr int VALUES = (TOK + WT) * RUN4_BYTES, BYTES = VALUES + (TOK + WT) * RUN4_SCALES;
-};
-
-template <int TOK, int WT, int TOK_WAVES, int WT_WAVES, bool GROUPED, class Out>
-__global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, TOK_WAVES * WT_WAVES <= 4 ? 1 : 2) void product_four_kernel(ProductArgs p, uint32_t tiles_tok, uint32_t tiles_wt, bool wide)
+// columns of all rows, 128 bytes of values each, filled straight from memory while others are multiplied; sixteen-byte pieces of a row lie at their number xor the
+// row's low bits, so that the lanes of a read spread over the banks.  A row's scales are eight bytes of a run: they come for four runs at a time, 32 bytes of a
+// row, since what counts for memory is how many lines are asked for (a run at a time they were as many as the values'), to one of two places of
+// their own, eight bytes of a row at their number xor two of the row's bits.
+template <int TOK, int WT, int TOK_WAVES, int WT_WAVES, int STAGES, bool GROUPED, class Out>
+__global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_four_kernel(ProductArgs p, uint32_t tiles_tok, uint32_t tiles_wt, bool wide)
 {
-    typedef Stage4<TOK, WT> S;
-    constexpr int WAVES = TOK_WAVES * WT_WAVES, J = TOK / TOK_WAVES / 16, I = WT / WT_WAVES / 16;
-    constexpr int SEGMENTS = (TOK + WT) / 8 / WAVES;             // of eight rows, that a wave brings
-    constexpr int PIECES = (TOK + WT) / 32 / WAVES;              // of 32 rows' scales
-    static_assert((TOK + WT) % (32 * WAVES) == 0 && TOK % (16 * TOK_WAVES) == 0 && WT % (16 * WT_WAVES) == 0 && TOK % 32 == 0, "");
-    __shared__ __align__(16) uint8_t stage0[S::BYTES];
-    __shared__ __align__(16) uint8_t stage1[S::BYTES];
+    constexpr int WAVES = TOK_WAVES * WT_WAVES, J = TOK / TOK_WAVES / 16, I = WT / WT_WAVES / 16, ROWS_ALL = TOK + WT, ROUND = 4;
+    constexpr int SEGMENTS = ROWS_ALL / 8 / WAVES;               // of eight rows, that a wave brings: values of a run, and scales of four
+    constexpr int BYTES = ROWS_ALL * RUN4_BYTES, SCALES = ROWS_ALL * RUN4_SCALES * ROUND;
+    static_assert(ROWS_ALL / 8 % WAVES == 0 && SEGMENTS % 2 == 0 && TOK % (16 * TOK_WAVES) == 0 && WT % (16 * WT_WAVES) == 0 && (STAGES == 2 || STAGES == 4), "");
+    __shared__ __align__(16) uint8_t stage0[BYTES];
+    __shared__ __align__(16) uint8_t stage1[BYTES];
+    __shared__ __align__(16) uint8_t stage2[STAGES > 2 ? BYTES : 16];
+    __shared__ __align__(16) uint8_t stage3[STAGES > 3 ? BYTES : 16];
+    __shared__ __align__(16) uint8_t scales[2][SCALES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wave_tok = wave % TOK_WAVES * (J * 16), wave_wt = wave / TOK_WAVES * (I * 16);
 
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, TOK_WAVES * WT_WAVES <= 
 
     // Where a lane's pieces come from, in bytes from the tile's first row (gathered rows of a may be further apart than 2^32)
     typedef typename std::conditional<GROUPED, uint64_t, uint32_t>::type Offset;
-    Offset from[SEGMENTS], scale_from[PIECES];
+    Offset from[SEGMENTS], scale_from[SEGMENTS];
     const int64_t base_a = GROUPED ? 0 : first, base_b = matrix * p.rows_b + first_wt;
     const uint8_t *const a_base = p.a + base_a * row_bytes, *const b_base = p.b + base_b * row_bytes;
     const uint8_t *const sa_base = (const uint8_t *)p.sa + base_a * scale_bytes, *const sb_base = (const uint8_t *)p.sb + base_b * scale_bytes;
@@ -64,23 +64,25 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, TOK_WAVES * WT_WAVES <= 
         const int row = (wave * SEGMENTS + s) * 8 + (lane >> 3), piece = (lane & 7) ^ (lane >> 3);
         const int64_t r = row < TOK ? row_of_a(first + row) - base_a : row_of_b(first_wt + row - TOK) - first_wt;
         from[s] = (Offset)(r * row_bytes + piece * 16);
+        scale_from[s] = (Offset)(r * scale_bytes);
     }
-#pragma unroll
-    for (int s = 0; s < PIECES; s++) {
-        const int row = (wave * PIECES + s) * 32 + (lane >> 1);
-        const int64_t r = row < TOK ? row_of_a(first + row) - base_a : row_of_b(first_wt + row - TOK) - first_wt;
-        scale_from[s] = (Offset)(r * scale_bytes + (lane & 1) * 4);
-    }
+    const int n = (int)p.kb;
     const auto bring = [&](int kb, uint8_t *stage) {
 #pragma unroll
         for (int l = 0; l < SEGMENTS; l++) {
             const int segment = wave * SEGMENTS + l;
+            asm volatile("" : "+v"(from[l]));                     // (else its sum with the base is kept, in twice the registers)
             to_lds((segment * 8 < TOK ? a_base : b_base) + (int64_t)kb * RUN4_BYTES, from[l], stage + segment * 1024);
         }
+    };
+    // half of a wave's scales of four runs (a lane has four bytes; past the last run: the last four again)
+    const auto bring_scales = [&](int group, int half) {
+        const int row = wave * SEGMENTS * 8 + (lane >> 3);        // (its bits 2 and 3 are those of all its segments but for the segment's own)
 #pragma unroll
-        for (int l = 0; l < PIECES; l++) {
-            const int piece = wave * PIECES + l;
-            to_lds4((piece * 32 < TOK ? sa_base : sb_base) + (int64_t)kb * RUN4_SCALES, scale_from[l], stage + S::VALUES + piece * 256);
+        for (int l = half * SEGMENTS / 2; l < (half + 1) * SEGMENTS / 2; l++) {
+            const int segment = wave * SEGMENTS + l, which = (lane & 7) ^ ((row + l * 8) >> 2 & 3) * 2;
+            asm volatile("" : "+v"(scale_from[l]));
+            to_lds4((segment * 8 < TOK ? sa_base : sb_base), scale_from[l] + 4 * (uint32_t)min(group * ROUND * 2 + which, 2 * n - 1), scales[group & 1] + segment * 256);
         }
     };
 
@@ -90,57 +92,72 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, TOK_WAVES * WT_WAVES <= 
 #pragma unroll
         for (int j = 0; j < J; j++) sum[i][j] = {0.0f, 0.0f, 0.0f, 0.0f};
 
-    const int low = ((lane >> 4) ^ (lane & 7)) * 16;
+    const int low = ((lane >> 4) ^ (lane & 7)) * 16, byte = (lane >> 4) * 8;
     const int at_a = (wave_tok + (lane & 15)) * RUN4_BYTES + low, at_w = (TOK + wave_wt + (lane & 15)) * RUN4_BYTES + low;
-    const int at_sa = S::VALUES + (wave_tok + (lane & 15)) * RUN4_SCALES + (lane >> 4), at_sb = S::VALUES + (TOK + wave_wt + (lane & 15)) * RUN4_SCALES + (lane >> 4);
-    struct Raw { v4i v; uint32_t scale; };
-    const auto operand = [&](const uint8_t *stage, int at, int at_scale, int half, int piece) {
-        return Raw{*(const v4i *)(stage + (at ^ half * 64) + piece * 16 * RUN4_BYTES), stage[at_scale + half * 4 + piece * 16 * RUN4_SCALES]};
-    };
-    // Multiplies the run in `stage` and brings run `next` to `other`.  Sixteen rows of b are read from the LDS while those before are multiplied, and the
-    // second half's rows of a during the first half.
-    const auto multiply = [&](const uint8_t *stage, int next, uint8_t *other) {
-        Raw a[2][J], after = operand(stage, at_w, at_sb, 0, 0);
+    const auto operand = [&](const uint8_t *stage, int at, int half, int piece) { return *(const v4i *)(stage + (at ^ half * 64) + piece * 16 * RUN4_BYTES); };
+    // Step N of a round of four multiplies a run and fills the stage that was multiplied before it with the run STAGES - 1 further on (the last run once more where
+    // there is none left); the first two bring the next round's scales.  Before that a wave's loads of this run and of its round's scales have arrived, those of
+    // later runs need not have, and all waves are done with the stage that is filled.  Sixteen rows of b are read from the LDS while those before are
+    // multiplied, and the second half's rows of a during the first half.
+    uint8_t *const stages[4] = {stage0, stage1, stage2, stage3};
+    const auto step = [&](int kb, auto at) {
+        constexpr int N = decltype(at)::value, FREE = (N + STAGES - 1) % STAGES;
+        constexpr int FLYING = STAGES == 2 ? 0 : 2 * SEGMENTS + (N == 1 || N == 3 ? SEGMENTS / 2 : N == 2 ? SEGMENTS : 0);       // loads of the two steps before
+        const uint8_t *const stage = stages[N % STAGES];
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt((FLYING & 15) | 7 << 4 | FLYING >> 4 << 14);       // (vmcnt, and lgkmcnt to zero)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        // (all of the run's scales before the next are asked for: the compiler does not tell their places apart and would wait for those)
+        const uint8_t *const of = scales[kb / ROUND & 1] + ((N ^ ((lane & 15) >> 2)) * 8) + (lane & 15) * 32;
+        uint2 sa[J], sb[I];
 #pragma unroll
-        for (int j = 0; j < J; j++) a[0][j] = operand(stage, at_a, at_sa, 0, j);
-        bring(next, other);
+        for (int j = 0; j < J; j++) sa[j] = *(const uint2 *)(of + (wave_tok + j * 16) * 32);
+#pragma unroll
+        for (int i = 0; i < I; i++) sb[i] = *(const uint2 *)(of + (TOK + wave_wt + i * 16) * 32);
+        v4i a[2][J], after = operand(stage, at_w, 0, 0);
+#pragma unroll
+        for (int j = 0; j < J; j++) a[0][j] = operand(stage, at_a, 0, j);
+        bring(min(kb + STAGES - 1, n - 1), stages[FREE]);
+        if constexpr (N < 2) bring_scales(kb / ROUND + 1, N);
 #pragma unroll
         for (int q = 0; q < 2 * I; q++) {
             const int half = q / I, i = q % I;
-            const Raw w = after;
-            if (q + 1 < 2 * I) after = operand(stage, at_w, at_sb, (q + 1) / I, (q + 1) % I);
+            const v4i w = after;
+            if (q + 1 < 2 * I) after = operand(stage, at_w, (q + 1) / I, (q + 1) % I);
             if (half == 0)
 #pragma unroll
-                for (int j = i * J / I; j < (i + 1) * J / I; j++) a[1][j] = operand(stage, at_a, at_sa, 1, j);
+                for (int j = i * J / I; j < (i + 1) * J / I; j++) a[1][j] = operand(stage, at_a, 1, j);
+            const uint32_t of_w = (half ? sb[i].y : sb[i].x) >> byte;
 #pragma unroll
-            for (int j = 0; j < J; j++) sum[i][j] = four_product(w.v, w.scale, a[half][j].v, a[half][j].scale, sum[i][j]);
+            for (int j = 0; j < J; j++) sum[i][j] = four_product(w, of_w, a[half][j], (half ? sa[j].y : sa[j].x) >> byte, sum[i][j]);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // This stage's loads have arrived, and all waves are done with the other, whose place the next run takes.
-    const auto arrive = [&] {
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(7 << 4);                       // (vmcnt and lgkmcnt, to zero)
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-    };
-
-    const int n = (int)p.kb;
-    bring(0, stage0);
-    for (int kb = 0; kb < n; kb += 2) {
-        arrive();
-        multiply(stage0, min(kb + 1, n - 1), stage1);
-        arrive();
-        if (kb + 1 < n) multiply(stage1, min(kb + 2, n - 1), stage0);
+    bring_scales(0, 0);
+    bring_scales(0, 1);
+#pragma unroll
+    for (int m = 0; m < STAGES - 1; m++) bring(min(m, n - 1), stages[m]);
+    int kb = 0;
+    for (; kb + ROUND - 1 < n; kb += ROUND) {
+        step(kb, One<0>());
+        step(kb + 1, One<1>());
+        step(kb + 2, One<2>());
+        step(kb + 3, One<3>());
     }
-    arrive();
+    if (kb < n) step(kb, One<0>());
+    if (kb + 1 < n) step(kb + 1, One<1>());
+    if (kb + 2 < n) step(kb + 2, One<2>());
+    // (the last steps brought the last run once more: to stages that results go to now, so it has to be there before any wave's barrier)
+    __builtin_amdgcn_s_waitcnt(7 << 4);
+    __syncthreads();
 
     // Out through the LDS, sixteen rows of a at a time, in whole lines
     typedef typename Out::T T;
     constexpr int ROW = I * 16 * sizeof(T), PITCH = ROW + 16, PER_ROW = ROW / 16, ROWS = 64 / PER_ROW;       // bytes; lanes of a row, rows of an instruction
     T *out = (T *)p.out;
     constexpr int HALF = (WAVES + 1) / 2;
-    static_assert(HALF * 16 * PITCH <= S::BYTES, "");
+    static_assert(HALF * 16 * PITCH <= BYTES, "");
     uint8_t *mine = (wave < HALF ? stage0 : stage1) + (wave < HALF ? wave : wave - HALF) * 16 * PITCH;
 #pragma unroll
     for (int j = 0; j < J; j++) {
@@ -279,16 +296,25 @@ int64_t rows_each4(const ProductArgs &p) { return grouped4(p) ? p.order.T * p.or
 // each of the 256 compute units.
 bool more_strips4(unsigned strips, unsigned tiles) { return (int64_t)strips * tiles >= 2048; }
 
-template <int N> using Int = std::integral_constant<int, N>;
-
 }  // namespace
+
+// Which tile: us of n tiles on 256 compute units, from what a tile's run takes with a unit to itself, what it takes among many, and what a tile takes
+// besides, its results above all; all measured: 64 x 64 0.4, 0.21 and 0.8, 128 x 128 0.8, 0.55 and 1.8, 256 x 256 1.75, 1.75 and 8.9.  What each takes, and so what the rule
+// decides between, in that order: 777 x 1001 x 1100 6.8, 10.0, 26.0; 256 x 4096 x 4096 10.2, 15.3, 30.6; 2048^3 13.6, 10.8, 19.2; 8192 x 8192 x 512 78, 46, 50;
+// 4096^3 72.9, 44.3, 40.6; 8192^3 486, 310, 259 us.
+static double tiles_time4(int64_t rows, int64_t outs, int64_t runs, int tile, double alone, double among, double once)
+{
+    const double rounds = (double)((((rows + tile - 1) / tile) * ((outs + tile - 1) / tile) + 255) / 256);
+    return (double)runs * (alone > rounds * among ? alone : rounds * among) + rounds * once;
+}
 
 int product_four_form(const ProductArgs &p)
 {
     if (rows_each4(p) <= 32) return ASGD_PRODUCT_FORM_FEW;
     if (grouped4(p)) return ASGD_PRODUCT_FORM_TILES_128;
-    const int64_t tiles = ((p.rows_a + 255) / 256) * ((p.rows_b + 255) / 256);
-    return tiles >= 256 ? ASGD_PRODUCT_FORM_TILES_256 : ASGD_PRODUCT_FORM_TILES_128;
+    const double t64 = tiles_time4(p.rows_a, p.rows_b, p.kb, 64, 0.4, 0.21, 0.8), t128 = tiles_time4(p.rows_a, p.rows_b, p.kb, 128, 0.8, 0.55, 1.8);
+    if (t64 < t128) return ASGD_PRODUCT_FORM_TILES_64;
+    return tiles_time4(p.rows_a, p.rows_b, p.kb, 256, 1.75, 1.75, 8.9) < t128 ? ASGD_PRODUCT_FORM_TILES_256 : ASGD_PRODUCT_FORM_TILES_128;
 }
 
 hipError_t launch_product_four(const ProductArgs &p, int type, hipStream_t s)
@@ -307,17 +333,18 @@ hipError_t launch_product_four(const ProductArgs &p, int type, hipStream_t s)
             else product_four_few_kernel<void, J, 1, Out><<<dim3(strips, tiles), 64 * FEW4_WAVES, 0, s>>>(p, wide4);
             return hipGetLastError();
         };
-        const auto tiles = [&](auto tok, auto wt, auto waves_tok, auto waves_wt, auto by_expert) {
+        const auto tiles = [&](auto tok, auto wt, auto waves_tok, auto waves_wt, auto stages, auto by_expert) {
             constexpr int TOK = decltype(tok)::value, WT = decltype(wt)::value, WAVES = decltype(waves_tok)::value * decltype(waves_wt)::value;
             const int64_t tiles_tok = tiles_of(TOK), tiles_wt = (p.rows_b + WT - 1) / WT;
-            product_four_kernel<TOK, WT, decltype(waves_tok)::value, decltype(waves_wt)::value, decltype(by_expert)::value, Out>
+            product_four_kernel<TOK, WT, decltype(waves_tok)::value, decltype(waves_wt)::value, decltype(stages)::value, decltype(by_expert)::value, Out>
                 <<<(unsigned)(tiles_tok * tiles_wt), 64 * WAVES, 0, s>>>(p, (uint32_t)tiles_tok, (uint32_t)tiles_wt, wide16);
             return hipGetLastError();
         };
-        if (form == ASGD_PRODUCT_FORM_FEW) return rows_each4(p) <= 16 ? few(Int<1>()) : few(Int<2>());
-        if (grouped) return tiles(Int<128>(), Int<128>(), Int<2>(), Int<2>(), std::true_type());
-        if (form == ASGD_PRODUCT_FORM_TILES_256) return tiles(Int<256>(), Int<256>(), Int<4>(), Int<2>(), std::false_type());
-        return tiles(Int<128>(), Int<128>(), Int<2>(), Int<2>(), std::false_type());
+        if (form == ASGD_PRODUCT_FORM_FEW) return rows_each4(p) <= 16 ? few(One<1>()) : few(One<2>());
+        if (grouped) return tiles(One<128>(), One<128>(), One<2>(), One<4>(), One<2>(), std::true_type());
+        if (form == ASGD_PRODUCT_FORM_TILES_64) return tiles(One<64>(), One<64>(), One<2>(), One<2>(), One<4>(), std::false_type());
+        if (form == ASGD_PRODUCT_FORM_TILES_256) return tiles(One<256>(), One<256>(), One<4>(), One<2>(), One<2>(), std::false_type());
+        return tiles(One<128>(), One<128>(), One<2>(), One<4>(), One<2>(), std::false_type());
     });
 }
 

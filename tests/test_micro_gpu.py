@@ -120,12 +120,13 @@ def test_products(M, rows, outs, cols, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("rows,outs,cols", [(4096, 4096, 300), (4100, 4090, 70), (8200, 2050, 513)])
-def test_large_tiles(M, rows, outs, cols, dtype):
+@pytest.mark.parametrize("tile,rows,outs,cols", [(64, 300, 500, 2100), (64, 1000, 700, 900), (128, 2048, 2048, 300), (128, 1100, 4000, 70), (128, 2000, 2000, 1500), (64, 4100, 1030, 2049), (128, 4000, 1020, 2049),
+                                                 (256, 4096, 4096, 1100), (256, 3900, 4090, 2049), (256, 8100, 2040, 1300)])
+def test_large_tiles(M, tile, rows, outs, cols, dtype):
     from paper_1505_04956_amd import binding as B
     x, w = data(rows, cols, 5, dtype), data(outs, cols, 6)
     ma, mw = M.quantize(x.cuda()), M.quantize(w.cuda())
-    assert B.asgd_block_product_form(ma._c, mw._c, B.PRODUCT_ALL, 0, None) == B.PRODUCT_FORM_TILES_256
+    assert B.asgd_block_product_form(ma._c, mw._c, B.PRODUCT_ALL, 0, None) == {64: B.PRODUCT_FORM_TILES_64, 128: B.PRODUCT_FORM_TILES_128, 256: B.PRODUCT_FORM_TILES_256}[tile]
     y = M.product(ma, mw, dtype)
     pick = torch.cat([torch.arange(0, rows, 97), torch.arange(rows - 300, rows)])
     a, b = Q.four(x[pick].float()), Q.four(w)
