@@ -2,7 +2,7 @@
 // matrix instruction, and the columns of rows that do not go to an expert are not used.
 //
 //   choose  one workgroup routes the rows and lists the experts that have any; the others bring a row of x each to 8 or 4 bits
-//   up      a workgroup forms h = f(gate) * up, 32-bit, of 32 of an expert's hidden columns for all of its rows
+//   up      a workgroup forms h = f(gate) * up, 32-bit, of sixteen of an expert's hidden columns for all of its rows
 //   down    a workgroup sums sixteen columns of the result over all experts; its waves share the experts' blocks
 #include "four_bits.h"
 #include "route_row.h"
@@ -11,7 +11,7 @@ namespace asgd {
 
 namespace {
 
-constexpr int UP_WAVES = 8, DOWN_WAVES = 16, CHOOSE_THREADS = 1024, COLUMNS = 16;
+constexpr int UP_WAVES = 4, DOWN_WAVES = 16, CHOOSE_THREADS = 1024, COLUMNS = 16;
 constexpr int MOST_SLOTS = ASGD_PRODUCT_RAW_ROWS * ASGD_ROUTE_MAX_CHOSEN, WORDS = ASGD_ROUTE_MAX_EXPERTS / 32;
 static_assert(ASGD_PRODUCT_RAW_ROWS == COLUMNS && CHOOSE_THREADS / 64 >= COLUMNS && MOST_SLOTS <= CHOOSE_THREADS, "");
 
@@ -113,7 +113,7 @@ template <class Ty, int V> __global__ __launch_bounds__(CHOOSE_THREADS) void lay
 }
 
 // ---- sixteen rows of an expert's weights, and the columns that they are multiplied by ------------------------------------
-template <int BITS> struct Weights;                               // of a step.  row: a lane's own, tile: the first of the sixteen
+template <int BITS> struct Weights;                               // of a step.  row: the lane's operand's, first: the first of the four rows of the result that it gets
 template <int BITS> struct Columns;                               // of a step, a lane's 32 or two times 32 of row lane % 16
 
 template <> struct Columns<8> {
@@ -128,24 +128,25 @@ template <> struct Columns<8> {
 };
 template <> struct Weights<8> {
     v4i lo, hi;
-    float scale[2];                                                // of the square that the first of the sixteen rows lies in, and of that of the last
-    __device__ __forceinline__ void load(const asgd_blocks &w, int64_t steps, int64_t matrix, int64_t row, int64_t tile, int64_t step, int quarter)
+    float scale[2];                                                // of the square that the first of the lane's four rows lies in, and of that of the last (a load of the lane's
+                                                                   // own: the same for all, it would be a scalar one, which the compiler puts after the wait for the values)
+    __device__ __forceinline__ void load(const asgd_blocks &w, int64_t steps, int64_t matrix, int64_t row, int64_t first, int64_t step, int quarter)
     {
         const uint8_t *p = (const uint8_t *)w.values + ((matrix * w.rows + row) * steps + step) * BLOCK8 + quarter * 32;
         lo = *(const v4i *)p;
         hi = *(const v4i *)(p + 16);
         const float *s = w.scales + matrix * blocks8(w.rows) * steps + step;
-        scale[0] = s[min(tile, w.rows - 1) / BLOCK8 * steps];
-        scale[1] = s[min(tile + 15, w.rows - 1) / BLOCK8 * steps];
+        scale[0] = s[min(first, w.rows - 1) / BLOCK8 * steps];
+        scale[1] = s[min(first + 3, w.rows - 1) / BLOCK8 * steps];
     }
     // adds the products times `factor` to `sum`, a row of the result for each lane and i
-    __device__ __forceinline__ v4f times(const Columns<8> &c, int64_t tile, int quarter, float factor, v4f sum) const
+    __device__ __forceinline__ v4f times(const Columns<8> &c, int64_t first, float factor, v4f sum) const
     {
         Operand<true> a, b;
         a.set(c.lo, c.hi);
         b.set(lo, hi);
         const v4f part = block_product(b, a);
-        const int second = BLOCK8 - (int)(tile % BLOCK8) - quarter * 4;      // from this i on the lane's rows lie in the second square
+        const int second = BLOCK8 - (int)(first % BLOCK8);         // from this i on they lie in the second
 #pragma unroll
         for (int i = 0; i < 4; i++) sum[i] = fmaf(part[i], c.scale * factor * (i < second ? scale[0] : scale[1]), sum[i]);
         return sum;
@@ -179,7 +180,7 @@ template <> struct Weights<4> {
         sum = four_product(v[0], scales.x >> at & 255, c.v[0], c.scales.x >> at & 255, sum);
         return four_product(v[1], scales.y >> at & 255, c.v[1], c.scales.y >> at & 255, sum);
     }
-    __device__ __forceinline__ v4f times(const Columns<4> &c, int64_t, int, float factor, v4f sum) const
+    __device__ __forceinline__ v4f times(const Columns<4> &c, int64_t, float factor, v4f sum) const
     {
         const v4f part = times(c, v4f{0.0f, 0.0f, 0.0f, 0.0f});
 #pragma unroll
@@ -195,38 +196,38 @@ __device__ __forceinline__ float activated(float gate, float up, int activation)
     return f * up;
 }
 
-// grid: strips of 32 of H, experts.  Even waves take the first sixteen of the strip, odd ones the others, rows of the gate and rows that it multiplies; four
-// waves share the steps, and the loads of AHEAD of a wave's steps are on their way together.
+// grid: strips of sixteen of H, experts.  A workgroup takes sixteen rows of the gate and the sixteen that they multiply; its waves share the steps, and the loads of
+// AHEAD of a wave's steps are on their way together.  (Small workgroups spread evenly: with 32 of H and eight waves one token's took 14.1 us for 12.)
 template <int BITS> __global__ __launch_bounds__(64 * UP_WAVES, 4) void layer_up_kernel(LayerArgs a, Scratch s)
 {
-    constexpr int AHEAD = 2, SHARE = UP_WAVES / 2;
+    constexpr int AHEAD = 2;
     __shared__ v4f parts[UP_WAVES][2][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tok = lane & 15, quarter = lane >> 4;
     const int n = blockIdx.y, met = *s.met, e = s.experts[n], slot = s.slots[n * COLUMNS + tok];
     if (n >= met) return;
     const bool there = slot >= 0;
-    const int64_t strip = (int64_t)blockIdx.x * 32 + (wave & 1) * 16;
+    const int64_t strip = (int64_t)blockIdx.x * 16;
     const int steps = (int)steps_of(BITS, a.D);
     const uint8_t *const x = s.x + (there ? tok : 0) * (int64_t)steps * STEP_BYTES, *const x_scales = s.x_scales + (there ? tok : 0) * (int64_t)steps * Parts<BITS>::SCALES;
-    const int64_t tile[2] = {strip, a.H + strip}, of_lane = min(strip + tok, a.H - 1);
+    const int64_t first[2] = {strip + quarter * 4, a.H + strip + quarter * 4}, of_lane = min(strip + tok, a.H - 1);
     v4f sum[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
-    for (int step0 = wave >> 1; step0 < steps; step0 += SHARE * AHEAD) {
+    for (int step0 = wave; step0 < steps; step0 += UP_WAVES * AHEAD) {
         Weights<BITS> w[AHEAD][2];
         Columns<BITS> c[AHEAD];
 #pragma unroll
         for (int i = 0; i < AHEAD; i++) {
-            const int step = step0 + i * SHARE;
+            const int step = step0 + i * UP_WAVES;
             if (step >= steps) break;
 #pragma unroll
-            for (int m = 0; m < 2; m++) w[i][m].load(a.up, steps, e, m * a.H + of_lane, tile[m], step, quarter);
+            for (int m = 0; m < 2; m++) w[i][m].load(a.up, steps, e, m * a.H + of_lane, first[m], step, quarter);
             c[i].load(x + (int64_t)step * STEP_BYTES, x_scales + (int64_t)step * Parts<BITS>::SCALES, quarter);
         }
 #pragma unroll
         for (int i = 0; i < AHEAD; i++) {
-            if (step0 + i * SHARE >= steps) break;
+            if (step0 + i * UP_WAVES >= steps) break;
 #pragma unroll
             for (int m = 0; m < 2; m++) {
-                if constexpr (BITS == 8) sum[m] = w[i][m].times(c[i], tile[m], quarter, 1.0f, sum[m]);
+                if constexpr (BITS == 8) sum[m] = w[i][m].times(c[i], first[m], 1.0f, sum[m]);
                 else sum[m] = w[i][m].times(c[i], sum[m]);
             }
         }
@@ -234,12 +235,12 @@ template <int BITS> __global__ __launch_bounds__(64 * UP_WAVES, 4) void layer_up
 #pragma unroll
     for (int m = 0; m < 2; m++) parts[wave][m][lane] = sum[m];
     __syncthreads();
-    if (wave > 1 || !there) return;
-    v4f gate = parts[wave][0][lane], up = parts[wave][1][lane];
+    if (wave > 0 || !there) return;
+    v4f gate = parts[0][0][lane], up = parts[0][1][lane];
 #pragma unroll
-    for (int w = 1; w < SHARE; w++) {
-        gate += parts[2 * w + wave][0][lane];
-        up += parts[2 * w + wave][1][lane];
+    for (int w = 1; w < UP_WAVES; w++) {
+        gate += parts[w][0][lane];
+        up += parts[w][1][lane];
     }
     const int64_t c = strip + quarter * 4;
     if (c >= a.H) return;
@@ -272,7 +273,7 @@ template <int BITS, int G, class Out> __global__ __launch_bounds__(64 * DOWN_WAV
     for (int i = threadIdx.x; i < a.T * a.k; i += blockDim.x) weights[i] = a.weights[i];
     const int met = *s.met, steps = (int)steps_of(BITS, a.H), each = (steps + G - 1) / G, items = met * each;
     __syncthreads();
-    const int64_t strip = (int64_t)blockIdx.x * R, of_lane = min(strip + row, a.N - 1);
+    const int64_t strip = (int64_t)blockIdx.x * R, of_lane = min(strip + row, a.N - 1), first = strip + quarter % (R / 4) * 4;
     const int part = lane % P::LANES, group = lane / P::LANES;
 
     struct Item {
@@ -298,7 +299,7 @@ template <int BITS, int G, class Out> __global__ __launch_bounds__(64 * DOWN_WAV
         i.step = (item - n * each) * G;
         i.slot = slots[n * COLUMNS + row];
         i.rows = (uint32_t)__ballot(i.slot >= 0) & ((1u << R) - 1);
-        i.w.load(a.down, steps, experts[n], of_lane, strip, min(i.step + g, steps - 1), quarter);
+        i.w.load(a.down, steps, experts[n], of_lane, first, min(i.step + g, steps - 1), quarter);
         take_h(n, i.step, column_of(i.rows, group), i.h);
     };
     uint8_t *const mine = columns[wave], *const my_scales = scales[wave];
@@ -323,7 +324,7 @@ template <int BITS, int G, class Out> __global__ __launch_bounds__(64 * DOWN_WAV
         c.load(mine + tok * PITCH, my_scales + tok * P::SCALES, quarter);
         // (what a step past the last has of h is zeros)
         const bool there = i.slot >= 0 && (G == 1 || quarter * 4 / R == g);
-        const v4f got = i.w.times(c, strip, quarter % (R / 4), there ? weights[i.slot] : 0.0f, sum);
+        const v4f got = i.w.times(c, first, there ? weights[i.slot] : 0.0f, sum);
 #pragma unroll
         for (int k = 0; k < 4; k++) sum[k] = there ? got[k] : sum[k];       // (what is not a number in a column that is not used stays there)
         __builtin_amdgcn_wave_barrier();
@@ -393,7 +394,7 @@ template <class In, class Out> __global__ __launch_bounds__(64 * DOWN_WAVES) voi
                 c.load(columns + (step - chunk) * STEP_BYTES, scales + (step - chunk) * RUN4_SCALES, quarter);       // (all sixteen columns: the one row)
 #pragma unroll
                 for (int i = 0; i < EXPERTS; i++)
-                    if (id_of(j0 + i * share) >= 0) sum = w[i].times(c, strip, quarter, a.weights[t * a.k + j0 + i * share], sum);
+                    if (id_of(j0 + i * share) >= 0) sum = w[i].times(c, strip, a.weights[t * a.k + j0 + i * share], sum);
             }
     }
     parts[wave][lane] = sum;
@@ -429,7 +430,7 @@ hipError_t launch_layer(const LayerArgs &a, const RouteArgs &r, int logits_type,
         });
     });
     if (e != hipSuccess) return e;
-    const dim3 grid(strips_of(a.H, 32), most);
+    const dim3 grid(strips_of(a.H, 16), most);
     if (four) layer_up_kernel<4><<<grid, 64 * UP_WAVES, 0, s>>>(a, w);
     else layer_up_kernel<8><<<grid, 64 * UP_WAVES, 0, s>>>(a, w);
     e = hipGetLastError();
