@@ -437,8 +437,8 @@ int asgd_block_product_form(const asgd_blocks *a, const asgd_blocks *b, int mode
 
 /*
  * The experts of few rows in one launch, without an order: out[t] = sum over j of weights[t][j] * (x's row t times the
- * matrix ids[t][j] of w), ids outside 0 .. w->count - 1 left out.  x: RAW, at most ASGD_PRODUCT_RAW_ROWS rows; w: SQUARES or FOURS;
- * ids and weights: rows x k.  Every row reads its experts' matrices for itself.
+ * matrix ids[t][j] of w), ids outside 0 .. w->count - 1 left out.  x: RAW, at most ASGD_PRODUCT_RAW_ROWS rows (w SQUARES) or
+ * ASGD_PRODUCT_RAW_SLOTS (w FOURS); ids and weights: rows x k.  Every row reads its experts' matrices for itself.
  */
 int asgd_experts_direct(const asgd_blocks *x, const int32_t *ids, const float *weights, int k, const asgd_blocks *w, int exact,
                         void *out, int type, int64_t stride, void *hip_stream);

@@ -216,8 +216,9 @@ int asgd_block_product_form(const asgd_blocks *a, const asgd_blocks *b, int mode
 int asgd_experts_direct(const asgd_blocks *x, const int32_t *ids, const float *weights, int k, const asgd_blocks *w, int exact,
                         void *out, int type, int64_t stride, void *hip_stream)
 {
-    if (!blocks_ok(x) || x->form != ASGD_BLOCKS_RAW || x->rows > ASGD_PRODUCT_RAW_ROWS || !blocks_ok(w) || (w->form != ASGD_BLOCKS_SQUARES && w->form != ASGD_BLOCKS_FOURS) || w->cols != x->cols || w->rows < 1 || w->rows > MOST_COLS)
+    if (!blocks_ok(x) || x->form != ASGD_BLOCKS_RAW || !blocks_ok(w) || (w->form != ASGD_BLOCKS_SQUARES && w->form != ASGD_BLOCKS_FOURS) || w->cols != x->cols || w->rows < 1 || w->rows > MOST_COLS)
         return ASGD_EINVAL;
+    if (x->rows > (w->form == ASGD_BLOCKS_FOURS ? ASGD_PRODUCT_RAW_SLOTS : ASGD_PRODUCT_RAW_ROWS)) return ASGD_EINVAL;
     if (k < 1 || k > ASGD_ROUTE_MAX_CHOSEN || !type_ok(type) || (exact != 0 && exact != 1)) return ASGD_EINVAL;
     if (x->rows == 0) return ASGD_OK;
     if (!ids || !weights || !aligned(ids, 4) || !aligned(weights, 4) || !matrix_ok(out, type, x->rows, w->rows, stride)) return ASGD_EINVAL;

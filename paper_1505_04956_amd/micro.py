@@ -21,6 +21,10 @@ from . import experts as X
 
 RUN = 256                        # columns that a row is laid out in whole runs of
 SMALL = 32                       # columns that share a scale
+# Up to so many weights, an expert's counted for each row that goes to it, and results, one launch without an order is faster than an order, products and sums,
+# 27 us: 16 rows of four of 64 experts of 2048 x 2048, at both limits, 30 us for 31; 64 rows of two of 512 x 512, at the second, 15; 16 of eight of 2048 x 2048 51 for 38.
+DIRECT_NUMBERS = 1 << 28
+DIRECT_RESULTS = 1 << 15
 
 
 def _runs(cols):
@@ -34,12 +38,14 @@ class Micro:
     rows, cols, count = X._fixed("rows", "cols", "count")
 
     def __init__(self, values, scales, cols):
-        kf, shape = _runs(cols), values.shape
-        if values.dtype is not torch.uint8 or len(shape) not in (2, 3) or shape[-1] != kf * (RUN // 2) or not values.is_contiguous():
-            raise ValueError("values: contiguous uint8 [..., rows, %d] are wanted, not %s %s" % (kf * (RUN // 2), values.dtype, tuple(shape)))
+        kf, shape = -(-cols // RUN), values.shape
         lead = shape[:-1]
-        X._flat(scales, (*lead, kf * (RUN // SMALL)), torch.uint8, "scales")
-        X._same_device(values, scales)
+        if values.dtype is not torch.uint8 or len(lead) not in (1, 2) or shape[-1] != kf * (RUN // 2) or not values.is_contiguous():
+            raise ValueError("values: contiguous uint8 [..., rows, %d] are wanted, not %s %s" % (kf * (RUN // 2), values.dtype, tuple(shape)))
+        if scales.dtype is not torch.uint8 or scales.shape != lead + (kf * (RUN // SMALL),) or not scales.is_contiguous():
+            raise ValueError("scales: contiguous uint8 %s are wanted, not %s %s" % ((*lead, kf * (RUN // SMALL)), scales.dtype, tuple(scales.shape)))
+        if values.get_device() != scales.get_device():
+            raise ValueError("tensors on %s and %s" % (values.device, scales.device))
         self._memory, self._values, self._scales = values, values, scales
         self._set(lead, cols, values.data_ptr(), scales.data_ptr())
 
@@ -52,7 +58,7 @@ class Micro:
         """Room for one in one piece of memory (values and scales are made of it when they are asked for)."""
         self = cls.__new__(cls)
         n = math.prod(lead) * _runs(cols)
-        self._memory = torch.empty(n * (RUN // 2 + RUN // SMALL), dtype=torch.uint8, device=like.device)
+        self._memory = like.new_empty(n * (RUN // 2 + RUN // SMALL), dtype=torch.uint8)
         self._values = self._scales = None
         at = self._memory.data_ptr()
         self._set(lead, cols, at, at + n * (RUN // 2))
@@ -96,7 +102,7 @@ def quantize(x):
 def expand(m, dtype=torch.float32):
     """The values that m stands for, [..., rows, cols] in `dtype`."""
     type, s = X._type(dtype), X._stream(m._memory)
-    out = torch.empty((*m._lead, m._cols), dtype=dtype, device=m._memory.device)
+    out = m._memory.new_empty((*m._lead, m._cols), dtype=dtype)
     if out.numel():
         B.asgd_block_expand(m._c, out.data_ptr(), type, m._cols, s)
     return out
@@ -109,7 +115,7 @@ def product(a, b, dtype, plan=None, gather=False):
     X._same_device(a._memory, b._memory, None if plan is None else plan._memory)
     type, s = X._type(dtype), X._stream(a._memory)
     rows = a._rows if plan is None else plan._T * plan._k
-    out = torch.empty((rows, b._rows), dtype=dtype, device=a._memory.device)
+    out = a._memory.new_empty((rows, b._rows), dtype=dtype)
     if rows:
         B.asgd_block_product(a._c, b._c, B.PRODUCT_ALL if plan is None else B.PRODUCT_GATHER if gather else B.PRODUCT_PLACES, 1,
                              None if plan is None else plan._c, out.data_ptr(), type, b._rows, s)
@@ -128,7 +134,8 @@ def _check(x, w, experts=False):
 def linear(x, w):
     """x [rows, K] times w^T, in x's type: x is brought to 4 bits on the way, w is quantize() of [N, K]."""
     rows = _check(x, w)
-    X._same_device(x, w._memory)
+    if x.get_device() != w._memory.get_device():
+        X._same_device(x, w._memory)
     # (few rows: bringing them to 4 bits again in each strip of the weights takes less than another launch)
     if rows > B.PRODUCT_RAW_ROWS:
         return product(quantize(x), w, x.dtype)
@@ -150,7 +157,7 @@ def experts(x, ids, weights, w):
     X._flat(weights, ids.shape, torch.float32, "weights")
     raw = X._raw(x)
     s, slots = X._stream(x), ids.numel()
-    if 0 < T <= B.PRODUCT_RAW_ROWS and slots * w._rows * w._cols <= 2 * X.DIRECT_BYTES:
+    if 0 < T <= B.PRODUCT_RAW_SLOTS and slots * w._rows * w._cols <= DIRECT_NUMBERS and T * w._rows <= DIRECT_RESULTS:
         out = x.new_empty((T, w._rows))
         B.asgd_experts_direct(raw, ids.data_ptr(), weights.data_ptr(), ids.shape[1], w._c, 1, out.data_ptr(), raw.type, w._rows, s)
         return out

@@ -186,7 +186,8 @@ def experts_64(x, ids, weights, w):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T,E,k,N,K", [(1, 8, 2, 40, 300), (1, 64, 6, 130, 513), (16, 5, 3, 17, 64), (17, 9, 2, 100, 257), (24, 100, 5, 100, 500), (300, 7, 2, 129, 260),
-                                       (700, 3, 1, 256, 1000), (200, 300, 4, 20, 70)])
+                                       (700, 3, 1, 256, 1000), (200, 300, 4, 20, 70),
+                                       (200, 300, 4, 200, 70), (150, 12, 2, 300, 260), (400, 30, 1, 100, 600), (40, 6, 2, 17, 8300)])
 def test_experts(M, T, E, k, N, K, dtype):
     x, w = data(T, K, T, dtype), (data(E * N, K, E) * 0.1).view(E, N, K)
     ids, weights = routed(T, E, k, T + E)

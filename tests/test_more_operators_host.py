@@ -75,7 +75,7 @@ def test_experts_of_few_rows_that_are_refused():
     def go(x, w, ids=P, weights=P, k=2, out=P, stride=8):
         return B.lib().asgd_experts_direct(C.addressof(x), ids, weights, k, C.addressof(w), 1, out, 0, stride, None)
     w = blocks(count=3)
-    for x, m in ((raw(rows=17), w), (raw(cols=299), w), (blocks(), w), (raw(), blocks(form=B.BLOCKS_ROWS))):
+    for x, m in ((raw(rows=4097), w), (raw(rows=17), blocks(form=B.BLOCKS_SQUARES, count=3)), (raw(cols=299), w), (blocks(), w), (raw(), blocks(form=B.BLOCKS_ROWS))):
         assert go(x, m) == B.EINVAL
     for over in (dict(ids=None), dict(weights=None), dict(ids=P + 2), dict(k=0), dict(k=65), dict(out=None), dict(stride=7)):
         assert go(raw(), w, **over) == B.EINVAL
