@@ -1,7 +1,8 @@
-// A whole layer of experts for few rows in three launches.  An expert's weights are read once for all rows: up to sixteen rows are the columns of one
+// A whole layer of experts for few rows in three launches, or two.  An expert's weights are read once for all rows: up to sixteen rows are the columns of one
 // matrix instruction, and the columns of rows that do not go to an expert are not used.
 //
-//   choose  one workgroup routes the rows and lists the experts that have any; the others bring a row of x each to 8 or 4 bits
+//   choose  one workgroup routes the rows and lists the experts that have any; the others bring a row of x each to 8 or 4 bits (or, for very few rows, every
+//           workgroup of the next part does both)
 //   up      a workgroup forms h = f(gate) * up, 32-bit, of sixteen of an expert's hidden columns for all of its rows
 //   down    a workgroup sums sixteen columns of the result over all experts; its waves share the experts' blocks
 #include "four_bits.h"
@@ -11,9 +12,12 @@ namespace asgd {
 
 namespace {
 
-constexpr int UP_WAVES = 4, DOWN_WAVES = 16, CHOOSE_THREADS = 1024, COLUMNS = 16;
+constexpr int UP_WAVES = 4, DOWN_WAVES = 16, COLUMNS = 16;
+// Up to so many rows, experts, steps of all rows, and workgroups times rows (which all route and bring to 8 or 4 bits the same) one launch does the first two
+// parts.  One row of 64 experts of 2048 x 1408 so 22.0 us, else 24.5; two rows 29.3 and 30.3; four (4224) 55 and 48; five of 100 experts of 1000 x 700 (5500) 23.5 and 21.5.
+constexpr int FEW_ROWS = 8, FEW_EXPERTS = 256, FEW_STEPS = 128, FEW_GROUPS = 2560;
 constexpr int MOST_SLOTS = ASGD_PRODUCT_RAW_ROWS * ASGD_ROUTE_MAX_CHOSEN, WORDS = ASGD_ROUTE_MAX_EXPERTS / 32;
-static_assert(ASGD_PRODUCT_RAW_ROWS == COLUMNS && CHOOSE_THREADS / 64 >= COLUMNS && MOST_SLOTS <= CHOOSE_THREADS, "");
+static_assert(ASGD_PRODUCT_RAW_ROWS == COLUMNS, "");
 
 // A step of a contraction is what a row has in 128 bytes: a block of 128 columns in 8 bits, a run of 256 in 4.
 constexpr int STEP_BYTES = 128;
@@ -43,73 +47,19 @@ size_t scratch_of(int64_t T, int k, int64_t E, int64_t D, int64_t H, char *at, S
 }
 
 // ---- bringing rows to 8 or 4 bits -----------------------------------------------------------------------------------
-template <int BITS, class T> __device__ __forceinline__ void bring_row(const T *row, int64_t cols, uint8_t *values, uint8_t *scales)
+// (by `threads` threads, of which this is number `me`)
+template <int BITS, class T> __device__ __forceinline__ void bring_row(const T *row, int64_t cols, uint8_t *values, uint8_t *scales, int me, int threads)
 {
     typedef Parts<BITS> P;
-    const int part = threadIdx.x % P::LANES;
+    const int part = me % P::LANES;
     const int64_t steps = steps_of(BITS, cols);
-    for (int64_t step = threadIdx.x / P::LANES; step < steps; step += blockDim.x / P::LANES) {
+    for (int64_t step = me / P::LANES; step < steps; step += threads / P::LANES) {
         float v[8];
         eight_of(row, (step * P::LANES + part) * 8, cols, v);
         typename P::Scale scale;
         *(typename P::Bytes *)(values + step * STEP_BYTES + part * P::BYTES) = P::to(v, scale);
         P::put_scale(scales + step * P::SCALES, part, scale);
     }
-}
-
-// ---- choose -----------------------------------------------------------------------------------------------------------
-template <class Ty, int V> __global__ __launch_bounds__(CHOOSE_THREADS) void layer_choose_kernel(RouteArgs r, LayerArgs a, Scratch s, bool wide)
-{
-    __shared__ int32_t ids[MOST_SLOTS];
-    __shared__ float weights[MOST_SLOTS];
-    __shared__ uint32_t bits[WORDS];
-    __shared__ int before[WORDS + 1];                              // experts with rows in the words before
-    __shared__ int16_t slots[MOST_SLOTS * COLUMNS];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (blockIdx.x > 0) {
-        const int64_t t = blockIdx.x - 1;
-        const auto go = [&](const auto *x) {
-            if (a.up.form == ASGD_BLOCKS_FOURS) bring_row<4>(x + t * a.x_stride, a.D, s.x + t * runs4(a.D) * STEP_BYTES, s.x_scales + t * runs4(a.D) * Parts<4>::SCALES);
-            else bring_row<8>(x + t * a.x_stride, a.D, s.x + t * blocks8(a.D) * STEP_BYTES, s.x_scales + t * blocks8(a.D) * Parts<8>::SCALES);
-        };
-        if (a.x_type == ASGD_TYPE_F32) go((const float *)a.x);
-        else if (a.x_type == ASGD_TYPE_BF16) go((const __bf16 *)a.x);
-        else go((const _Float16 *)a.x);
-        return;
-    }
-    if (threadIdx.x < WORDS) bits[threadIdx.x] = 0;
-    if (wave < a.T) {
-        const Lane<Ty, V> row = load_lane<Ty, V>((const typename Ty::T *)r.logits + wave * r.stride, lane * V, r.E, wide);
-        float bias[V];
-        load_bias<V>(r.bias, r.E, lane, bias);
-        r.ids = ids;
-        r.weights = weights;
-        route_row<Ty, V, true>(r, wave, lane, row, bias);
-    }
-    __syncthreads();
-    const int all = a.T * a.k, me = threadIdx.x, e = me < all ? ids[me] : -1;
-    if (me < all) {
-        a.ids[me] = e;
-        a.weights[me] = weights[me];
-    }
-    if (e >= 0) atomicOr(&bits[e >> 5], 1u << (e & 31));
-    __syncthreads();
-    if (wave == 0) {
-        const int c = lane < WORDS ? __popc(bits[lane]) : 0, sum = wave_scan(c);
-        if (lane <= WORDS) before[lane] = sum - c;
-    }
-    __syncthreads();
-    const int met = before[WORDS];
-    for (int i = me; i < met * COLUMNS; i += CHOOSE_THREADS) slots[i] = -1;
-    __syncthreads();
-    if (e >= 0) {
-        const int n = before[e >> 5] + __popc(bits[e >> 5] & ((1u << (e & 31)) - 1));
-        slots[n * COLUMNS + me / a.k] = (int16_t)me;
-        s.experts[n] = e;                                          // (every slot of an expert: the same number)
-    }
-    if (me == 0) *s.met = met;
-    __syncthreads();
-    for (int i = me; i < met * COLUMNS; i += CHOOSE_THREADS) s.slots[i] = slots[i];
 }
 
 // ---- sixteen rows of an expert's weights, and the columns that they are multiplied by ------------------------------------
@@ -196,19 +146,14 @@ __device__ __forceinline__ float activated(float gate, float up, int activation)
     return f * up;
 }
 
-// grid: strips of sixteen of H, experts.  A workgroup takes sixteen rows of the gate and the sixteen that they multiply; its waves share the steps, and the loads of
-// AHEAD of a wave's steps are on their way together.  (Small workgroups spread evenly: with 32 of H and eight waves one token's took 14.1 us for 12.)
-template <int BITS> __global__ __launch_bounds__(64 * UP_WAVES, 4) void layer_up_kernel(LayerArgs a, Scratch s)
+// Sixteen rows of the gate and the sixteen that they multiply; a workgroup's waves share the steps, and the loads of AHEAD of a wave's steps are on their way together.
+// slot: of the lane's column; x, x_scales: of that column's row.
+template <int BITS> __device__ __forceinline__ void form_h(const LayerArgs &a, const Scratch &s, v4f (*parts)[2][64], int e, int slot, const uint8_t *x, const uint8_t *x_scales)
 {
     constexpr int AHEAD = 2;
-    __shared__ v4f parts[UP_WAVES][2][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tok = lane & 15, quarter = lane >> 4;
-    const int n = blockIdx.y, met = *s.met, e = s.experts[n], slot = s.slots[n * COLUMNS + tok];
-    if (n >= met) return;
-    const bool there = slot >= 0;
     const int64_t strip = (int64_t)blockIdx.x * 16;
     const int steps = (int)steps_of(BITS, a.D);
-    const uint8_t *const x = s.x + (there ? tok : 0) * (int64_t)steps * STEP_BYTES, *const x_scales = s.x_scales + (there ? tok : 0) * (int64_t)steps * Parts<BITS>::SCALES;
     const int64_t first[2] = {strip + quarter * 4, a.H + strip + quarter * 4}, of_lane = min(strip + tok, a.H - 1);
     v4f sum[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
     for (int step0 = wave; step0 < steps; step0 += UP_WAVES * AHEAD) {
@@ -235,7 +180,7 @@ template <int BITS> __global__ __launch_bounds__(64 * UP_WAVES, 4) void layer_up
 #pragma unroll
     for (int m = 0; m < 2; m++) parts[wave][m][lane] = sum[m];
     __syncthreads();
-    if (wave > 0 || !there) return;
+    if (wave > 0 || slot < 0) return;
     v4f gate = parts[0][0][lane], up = parts[0][1][lane];
 #pragma unroll
     for (int w = 1; w < UP_WAVES; w++) {
@@ -248,6 +193,132 @@ template <int BITS> __global__ __launch_bounds__(64 * UP_WAVES, 4) void layer_up
 #pragma unroll
     for (int i = 0; i < 4; i++) h[i] = c + i < a.H ? activated(gate[i], up[i], a.activation) : 0.0f;
     *(v4f *)(s.h + slot * h_pitch(a.H) + c) = h;                   // (a row has a multiple of four)
+}
+
+// ---- which experts have rows ------------------------------------------------------------------------------------------------
+// In the LDS: what a workgroup knows of the routing.
+template <int SLOTS> struct Chosen {
+    int32_t ids[SLOTS];
+    float weights[SLOTS];
+    uint32_t bits[WORDS];                                          // of each expert whether it has rows
+    int before[WORDS + 1];                                         // experts with rows in the words before
+    int16_t experts[SLOTS];
+};
+
+// Routes the rows, a wave each, and marks their experts.  The whole workgroup.
+template <class Ty, int V, int SLOTS> __device__ __forceinline__ void choose(RouteArgs r, const LayerArgs &a, Chosen<SLOTS> &c, bool wide)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    for (int i = threadIdx.x; i < WORDS; i += blockDim.x) c.bits[i] = 0;
+    r.ids = c.ids;
+    r.weights = c.weights;
+#pragma unroll 1
+    for (int t = wave; t < a.T; t += waves) {
+        float bias[V];
+        load_bias<V>(r.bias, r.E, lane, bias);
+        const Lane<Ty, V> row = load_lane<Ty, V>((const typename Ty::T *)r.logits + t * r.stride, lane * V, r.E, wide);
+        route_row<Ty, V, true>(r, t, lane, row, bias);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.T * a.k; i += blockDim.x) {
+        const int e = c.ids[i];
+        if (e >= 0) atomicOr(&c.bits[e >> 5], 1u << (e & 31));
+    }
+    __syncthreads();
+}
+
+// Writes ids, weights and the scratch's lists.  The whole workgroup.
+template <int SLOTS> __device__ __forceinline__ void list_chosen(const LayerArgs &a, const Scratch &s, Chosen<SLOTS> &c)
+{
+    const int lane = threadIdx.x & 63, all = a.T * a.k;
+    if (threadIdx.x < 64) {
+        const int n = lane < WORDS ? __popc(c.bits[lane]) : 0, sum = wave_scan(n);
+        if (lane <= WORDS) c.before[lane] = sum - n;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < all; i += blockDim.x) {
+        const int e = c.ids[i];
+        a.ids[i] = e;
+        a.weights[i] = c.weights[i];
+        if (e >= 0) c.experts[c.before[e >> 5] + __popc(c.bits[e >> 5] & ((1u << (e & 31)) - 1))] = (int16_t)e;      // (every slot of an expert: the same number)
+    }
+    __syncthreads();
+    const int met = c.before[WORDS];
+    if (threadIdx.x == 0) *s.met = met;
+    for (int i = threadIdx.x; i < met; i += blockDim.x) s.experts[i] = c.experts[i];
+    for (int i = threadIdx.x; i < met * COLUMNS; i += blockDim.x) {
+        const int e = c.experts[i / COLUMNS], t = i % COLUMNS;
+        int slot = -1;
+        for (int j = 0; t < a.T && j < a.k; j++)
+            if (c.ids[t * a.k + j] == e) slot = t * a.k + j;
+        s.slots[i] = (int16_t)slot;
+    }
+}
+
+template <int BITS> __device__ __forceinline__ void bring_x(const LayerArgs &a, int t, uint8_t *values, uint8_t *scales, int me, int threads)
+{
+    const int64_t at = t * a.x_stride;
+    if (a.x_type == ASGD_TYPE_F32) bring_row<BITS>((const float *)a.x + at, a.D, values, scales, me, threads);
+    else if (a.x_type == ASGD_TYPE_BF16) bring_row<BITS>((const __bf16 *)a.x + at, a.D, values, scales, me, threads);
+    else bring_row<BITS>((const _Float16 *)a.x + at, a.D, values, scales, me, threads);
+}
+
+// ---- many workgroups: choose, then up -------------------------------------------------------------------------------------------
+// a wave for each row, but for the most experts, which take the registers of two
+template <int V> constexpr int CHOOSE_THREADS = V < 16 ? 1024 : 512;
+template <class Ty, int V> __global__ __launch_bounds__(CHOOSE_THREADS<V>) void layer_choose_kernel(RouteArgs r, LayerArgs a, Scratch s, bool wide)
+{
+    __shared__ Chosen<MOST_SLOTS> chosen;
+    if (blockIdx.x > 0) {
+        const int t = blockIdx.x - 1;
+        if (a.up.form == ASGD_BLOCKS_FOURS) bring_x<4>(a, t, s.x + t * runs4(a.D) * STEP_BYTES, s.x_scales + t * runs4(a.D) * Parts<4>::SCALES, threadIdx.x, blockDim.x);
+        else bring_x<8>(a, t, s.x + t * blocks8(a.D) * STEP_BYTES, s.x_scales + t * blocks8(a.D) * Parts<8>::SCALES, threadIdx.x, blockDim.x);
+        return;
+    }
+    choose<Ty, V>(r, a, chosen, wide);
+    list_chosen(a, s, chosen);
+}
+
+// grid: strips of sixteen of H, experts.  (Small workgroups spread evenly: with 32 of H and eight waves one token's took 14.1 us for 12.)
+template <int BITS> __global__ __launch_bounds__(64 * UP_WAVES, 4) void layer_up_kernel(LayerArgs a, Scratch s)
+{
+    __shared__ v4f parts[UP_WAVES][2][64];
+    const int n = blockIdx.y, met = *s.met, e = s.experts[n], slot = s.slots[n * COLUMNS + (threadIdx.x & 15)];
+    if (n >= met) return;
+    const int64_t row = slot < 0 ? 0 : threadIdx.x & 15, steps = steps_of(BITS, a.D);
+    form_h<BITS>(a, s, parts, e, slot, s.x + row * steps * STEP_BYTES, s.x_scales + row * steps * Parts<BITS>::SCALES);
+}
+
+// ---- few workgroups: both in one launch -------------------------------------------------------------------------------------------
+// Every workgroup routes the rows and brings them to 8 or 4 bits for itself; the first writes the lists that the next launch reads.
+template <class Ty, int V, int BITS> __global__ __launch_bounds__(64 * UP_WAVES, 4) void layer_choose_up_kernel(RouteArgs r, LayerArgs a, Scratch s, bool wide)
+{
+    __shared__ Chosen<FEW_ROWS * ASGD_ROUTE_MAX_CHOSEN> chosen;
+    __shared__ v4f parts[UP_WAVES][2][64];
+    __shared__ __align__(16) uint8_t x[FEW_STEPS * STEP_BYTES], x_scales[FEW_STEPS * 8];
+    const int lane = threadIdx.x & 63, tok = lane & 15, steps = (int)steps_of(BITS, a.D);
+    // (where there are fewer rows than waves, by those that have none to route)
+    const int routing = a.T < UP_WAVES ? 64 * a.T : 0;
+    if ((int)threadIdx.x >= routing)
+        for (int t = 0; t < a.T; t++) bring_x<BITS>(a, t, x + t * steps * STEP_BYTES, x_scales + t * steps * Parts<BITS>::SCALES, threadIdx.x - routing, blockDim.x - routing);
+    choose<Ty, V>(r, a, chosen, wide);
+    if (blockIdx.x == 0 && blockIdx.y == 0) list_chosen(a, s, chosen);
+    // the expert of this workgroup: the blockIdx.y-th that has rows
+    const uint32_t word = lane < WORDS ? chosen.bits[lane] : 0;
+    const int sum = wave_scan(__popc(word)), n = blockIdx.y;
+    const unsigned long long past = __ballot(sum > n);
+    if (!past) return;                                             // (all waves alike)
+    const int at = __ffsll((long long)past) - 1;
+    uint32_t rest = (uint32_t)__builtin_amdgcn_readlane((int)word, at);
+    for (int skip = n - __builtin_amdgcn_readlane(sum - __popc(word), at); skip > 0; skip--) rest &= rest - 1;
+    const int e = at * 32 + __ffs((int)rest) - 1;
+    int slot = -1;
+    for (int j = lane >> 4; tok < a.T && j < a.k; j += 4)
+        if (chosen.ids[tok * a.k + j] == e) slot = tok * a.k + j;
+    slot = max(slot, __shfl_xor(slot, 16));
+    slot = max(slot, __shfl_xor(slot, 32));
+    const int row = slot < 0 ? 0 : tok;
+    form_h<BITS>(a, s, parts, e, slot, x + row * steps * STEP_BYTES, x_scales + row * steps * Parts<BITS>::SCALES);
 }
 
 // ---- down ---------------------------------------------------------------------------------------------------------------
@@ -385,7 +456,7 @@ template <class In, class Out> __global__ __launch_bounds__(64 * DOWN_WAVES) voi
         const int end = min(chunk + CHUNK, steps);
         if (chunk + first < end) fetch(of_choice, chunk + first);
         if (chunk > 0) __syncthreads();
-        bring_row<4>((const typename In::T *)a.x + t * a.x_stride + (int64_t)chunk * RUN4, min(a.K - (int64_t)chunk * RUN4, (int64_t)CHUNK * RUN4), columns, scales);
+        bring_row<4>((const typename In::T *)a.x + t * a.x_stride + (int64_t)chunk * RUN4, min(a.K - (int64_t)chunk * RUN4, (int64_t)CHUNK * RUN4), columns, scales, threadIdx.x, blockDim.x);
         __syncthreads();
         for (int step = chunk + first; step < end; step += apart)
             for (int j0 = of_choice; j0 < a.k; j0 += EXPERTS * share) {
@@ -422,17 +493,28 @@ hipError_t launch_layer(const LayerArgs &a, const RouteArgs &r, int logits_type,
     scratch_of(a.T, a.k, a.E, a.D, a.H, (char *)work, w);
     const unsigned most = (unsigned)(a.T * a.k < a.E ? a.T * a.k : a.E);
     const bool four = a.up.form == ASGD_BLOCKS_FOURS;
+    const dim3 grid(strips_of(a.H, 16), most);
+    const bool together = a.T <= FEW_ROWS && a.E <= FEW_EXPERTS && a.T * steps_of(four ? 4 : 8, a.D) <= FEW_STEPS && (int64_t)grid.x * grid.y * a.T <= FEW_GROUPS;
     hipError_t e = with_type(logits_type, [&](auto ty) {
         return with_width(a.E, [&](auto v) {
+            typedef decltype(ty) Ty;
             constexpr int V = decltype(v)::value;
-            layer_choose_kernel<decltype(ty), V><<<1 + a.T, CHOOSE_THREADS, 0, s>>>(r, a, w, rows_of_lanes<decltype(ty), V>(r.logits, r.stride, r.E));
+            const bool wide = rows_of_lanes<Ty, V>(r.logits, r.stride, r.E);
+            if constexpr (V * 64 <= FEW_EXPERTS)
+                if (together) {
+                    if (four) layer_choose_up_kernel<Ty, V, 4><<<grid, 64 * UP_WAVES, 0, s>>>(r, a, w, wide);
+                    else layer_choose_up_kernel<Ty, V, 8><<<grid, 64 * UP_WAVES, 0, s>>>(r, a, w, wide);
+                    return hipGetLastError();
+                }
+            layer_choose_kernel<Ty, V><<<1 + a.T, CHOOSE_THREADS<V>, 0, s>>>(r, a, w, wide);
             return hipGetLastError();
         });
     });
     if (e != hipSuccess) return e;
-    const dim3 grid(strips_of(a.H, 16), most);
-    if (four) layer_up_kernel<4><<<grid, 64 * UP_WAVES, 0, s>>>(a, w);
-    else layer_up_kernel<8><<<grid, 64 * UP_WAVES, 0, s>>>(a, w);
+    if (!together) {
+        if (four) layer_up_kernel<4><<<grid, 64 * UP_WAVES, 0, s>>>(a, w);
+        else layer_up_kernel<8><<<grid, 64 * UP_WAVES, 0, s>>>(a, w);
+    }
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     return with_type(type, [&](auto out) {

@@ -41,7 +41,7 @@ def close(got, want, bound, dtype):
 
 
 SHAPES = [(1, 8, 2, 64, 32, 48), (1, 64, 6, 300, 200, 130), (2, 5, 5, 257, 129, 100), (5, 100, 5, 100, 70, 33), (15, 9, 2, 513, 260, 17), (16, 40, 3, 128, 128, 256),
-          (16, 7, 7, 1000, 40, 1), (3, 300, 8, 33, 1, 20), (1, 1, 1, 1, 1, 1), (4, 1024, 20, 40, 24, 16), (2, 64, 64, 40, 24, 16)]
+          (16, 7, 7, 1000, 40, 1), (3, 300, 8, 33, 1, 20), (1, 1, 1, 1, 1, 1), (4, 1024, 20, 40, 24, 16), (2, 64, 64, 40, 24, 16), (16, 1000, 3, 50, 24, 16), (8, 256, 8, 100, 300, 40), (7, 33, 2, 5000, 20, 30), (1, 200, 3, 9000, 33, 40), (8, 12, 2, 600, 100, 70)]
 
 
 @pytest.mark.parametrize("bits", [8, 4])
