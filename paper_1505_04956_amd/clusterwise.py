@@ -1,11 +1,12 @@
 """A model of routed linear experts whose router is a clustering: ASGD learns the centroids, their scores route the samples, and
 the experts and the router are then trained by gradient steps through the 8-bit products.
 
-    python -m paper_1505_04956_amd.clusterwise [--samples N] [--steps S] [--shared]
+    python -m paper_1505_04956_amd.clusterwise [--samples N] [--steps S] [--shared] [--limit L] [--small]
 
 The samples are a mixture around k centres (the generator of the clustering workloads); the target of a sample is a linear map of it
 that differs from centre to centre, so a model that sends every sample to the map of its cluster can learn what one map cannot.  With
---shared every sample also passes through one map that all clusters have in common, so that the experts learn what differs.
+--shared every sample also passes through one map that all clusters have in common, so that the experts learn what differs.  With --limit
+a step's gradients are clipped to that norm, with --small the trained maps are also evaluated in 4 bits.
 """
 from __future__ import annotations
 
@@ -16,6 +17,8 @@ import torch
 
 from . import binding as B
 from . import experts as X
+from . import gradients as G
+from . import micro as M
 from . import workloads
 
 
@@ -49,8 +52,20 @@ class ClusterwiseLinear:
             y = y.float() + s.float()
         return (y, (logits, ids, kept, of_all)) if train else y
 
-    def step(self, x, target, rate):
-        """One step against half the mean squared error; returns that error before the step."""
+    def small(self):
+        """The maps in 4 bits, kept for evaluation: a function of samples x that gives what forward(x) does, at a quarter of 16-bit weights' bytes."""
+        w = M.quantize(self.w)
+        shared = None if self.shared is None else M.quantize(self.shared)
+
+        def forward(x):
+            ids, weights = X.route(self.logits(x), self.rule)
+            x = x.bfloat16()
+            y = M.experts(x, ids, weights, w)
+            return y if shared is None else y.float() + M.linear(x, shared).float()
+        return forward
+
+    def step(self, x, target, rate, limit=None):
+        """One step against half the mean squared error, its gradients clipped to the norm `limit`; returns that error before the step."""
         y, (logits, ids, kept, of_all) = self.forward(x, train=True)
         off = y.float() - target
         loss = 0.5 * (off * off).sum(1).mean()
@@ -60,6 +75,9 @@ class ClusterwiseLinear:
         d_c = self.sharpness * (d_logits.t() @ x - d_logits.sum(0)[:, None] * self.centroids)
         if of_all is not None:
             _, d_shared = X.linear_backward(d_y, of_all, X.quantize_weights(self.shared, turned=True))
+        if limit is not None:
+            G.clip([d_w, d_c] if of_all is None else [d_w, d_c, d_shared], limit)
+        if of_all is not None:
             self.shared -= rate * self.rule.k / len(self.w) * d_shared         # (all rows pass through it, so many times more than through an expert)
         self.w -= rate * d_w
         self.centroids = self.centroids - rate * d_c
@@ -79,8 +97,9 @@ def learn_centroids(x, k, workers=64, minibatch=500, epochs=3):
     return w
 
 
-def run(samples=200_000, steps=60, k=16, d=32, outputs=24, batch=8192, rate=0.05, seed=1234, shared=False, report=None):
-    """(losses of the steps, loss of the best single linear map) on one synthetic data set."""
+def run(samples=200_000, steps=60, k=16, d=32, outputs=24, batch=8192, rate=0.05, seed=1234, shared=False, report=None, limit=None, small=None):
+    """(losses of the steps, loss of the best single linear map) on one synthetic data set.  limit: of the norm of a step's gradients; small: is given the
+    loss of the trained model over all samples in 8 and in 4 bits."""
     wl = workloads.Workload("clusterwise", samples, d, k, 64, 500, 0.05, 4, 3, 1.0, "uniform10", "equal", data_seed=seed)
     x = torch.from_numpy(workloads.generate_host(wl)).cuda()
     gen = torch.Generator(device="cuda")
@@ -99,9 +118,11 @@ def run(samples=200_000, steps=60, k=16, d=32, outputs=24, batch=8192, rate=0.05
     losses = []
     for s in range(steps):
         at = torch.randint(0, samples, (batch,), generator=gen, device="cuda")
-        losses.append(model.step(x[at], target[at], rate).item())
+        losses.append(model.step(x[at], target[at], rate, limit).item())
         if report:
             report("step %d: loss %.4f" % (s, losses[-1]))
+    if small:
+        small(*(0.5 * (f(x).float() - target).square().sum(1).mean().item() for f in (model.forward, model.small())))
     return losses, single
 
 
@@ -110,6 +131,9 @@ if __name__ == "__main__":
     p.add_argument("--samples", type=int, default=200_000)
     p.add_argument("--steps", type=int, default=60)
     p.add_argument("--shared", action="store_true")
+    p.add_argument("--limit", type=float)
+    p.add_argument("--small", action="store_true")
     a = p.parse_args()
-    got, alone = run(a.samples, a.steps, shared=a.shared, report=print)
+    got, alone = run(a.samples, a.steps, shared=a.shared, report=print, limit=a.limit,
+                     small=(lambda eight, four: print("loss over all samples in 8 bits %.4f, in 4 bits %.4f" % (eight, four))) if a.small else None)
     print("loss %.4f after %d steps; the best single linear map: %.4f" % (got[-1], len(got), alone))

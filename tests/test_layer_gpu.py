@@ -200,3 +200,39 @@ def test_trained_with_clipped_gradients_then_served(L):
     assert torch.equal(i, ids[:10]) and torch.equal(c, weights[:10])
     want, bound = Q.layer(x[:10].cpu().float(), i.cpu(), c.cpu(), Q.matrix_of(up), Q.matrix_of(down), 4, False)
     close(y, want, bound, torch.bfloat16)
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_the_example_clips_its_gradients_and_serves_in_four_bits(L, shared):
+    """A step with a limit moves by the gradients of one without, all scaled alike; the maps in 4 bits are applied as experts() and linear() do."""
+    from paper_1505_04956_amd import clusterwise as C, experts as X, micro as M
+    g = torch.Generator().manual_seed(1)
+    k, d, n, rows, rate = 5, 40, 24, 600, 0.05
+    x, target = torch.randn(rows, d, generator=g).cuda(), torch.randn(rows, n, generator=g).cuda()
+    centroids = torch.randn(k, d, generator=g).cuda()
+    make = lambda: C.ClusterwiseLinear(centroids.clone(), n, shared=shared)  # noqa: E731
+    parts = lambda m: [t for t in (m.w, m.centroids, m.shared) if t is not None]  # noqa: E731
+    free, bound, far = make(), make(), make()
+    start = [t.clone() for t in parts(free)]
+    losses = [m.step(x, target, rate, limit).item() for m, limit in ((free, None), (bound, 0.01), (far, 1e6))]
+    assert losses[0] == losses[1] == losses[2]
+    assert all(torch.equal(a, b) for a, b in zip(parts(free), parts(far)))
+    rates = [rate, rate, rate * 2 / k]
+    moved = [[(a.double() - b.double()) / r for a, b, r in zip(start, parts(m), rates)] for m in (free, bound)]
+    norm = [sum(float((t ** 2).sum()) for t in m) ** 0.5 for m in moved]
+    # (what a step moves by is rounded to the weights' last bit: 2^-24 of weights up to 8, over the rate)
+    count = sum(t.numel() for t in start)
+    slack = 2.0 ** -24 * 8 / (rate * 2 / k) * count ** 0.5
+    assert norm[0] > 0.1 and abs(norm[1] - 0.01) <= slack
+    for a, b in zip(*moved):
+        assert (b - a * (0.01 / norm[0])).abs().max() <= 2 * slack
+    served = free.small()
+    y = served(x)
+    ids, weights = X.route(free.logits(x), free.rule)
+    want = M.experts(x.bfloat16(), ids, weights, M.quantize(free.w))
+    if shared:
+        want = want.float() + M.linear(x.bfloat16(), M.quantize(free.shared)).float()
+    assert torch.equal(y, want) and torch.equal(served(x[:3]).float(), served(x[:3]).float()) and y.shape == (rows, n)
+    said = []
+    got, _ = C.run(samples=60_000, steps=2, k=4, batch=1000, shared=shared, limit=0.5, small=lambda *l: said.extend(l))
+    assert len(got) == 2 and len(said) == 2 and all(0 < v < 1e9 for v in got + said)
