@@ -432,14 +432,14 @@ template <int BITS, int G, class Out> __global__ __launch_bounds__(64 * DOWN_WAV
 // The experts of few rows in 4 bits in one launch, without an order: a workgroup takes sixteen rows of the weights of every expert of one row of x
 // (blockIdx.y), which it brings to 4 bits, CHUNK runs at a time.  Its waves share the runs and, where there are fewer runs than waves, the choices; the weights of EXPERTS of them are on
 // their way at a time.
-template <class In, class Out> __global__ __launch_bounds__(64 * DOWN_WAVES) void direct_four_kernel(DirectArgs a)
+template <class In, class Out, int WAVES> __global__ __launch_bounds__(64 * WAVES) void direct_four_kernel(DirectArgs a)
 {
     constexpr int EXPERTS = 4, CHUNK = 32;
-    __shared__ v4f parts[DOWN_WAVES][64];
+    __shared__ v4f parts[WAVES][64];
     __shared__ __align__(16) uint8_t columns[CHUNK * STEP_BYTES], scales[CHUNK * RUN4_SCALES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tok = lane & 15, quarter = lane >> 4;
     const int64_t t = blockIdx.y, strip = (int64_t)blockIdx.x * 16, of_lane = min(strip + tok, a.N - 1);
-    const int steps = (int)runs4(a.K), share = steps <= 4 ? 4 : steps <= 8 ? 2 : 1;       // waves that share a run's choices
+    const int steps = (int)runs4(a.K), share = steps * 4 <= WAVES ? 4 : steps * 2 <= WAVES ? 2 : 1;       // waves that share a run's choices
     const int32_t *ids = a.ids + t * a.k;
     v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
     Weights<4> w[EXPERTS];
@@ -451,7 +451,7 @@ template <class In, class Out> __global__ __launch_bounds__(64 * DOWN_WAVES) voi
             if (e >= 0) w[i].load(a.w, steps, e, of_lane, strip, step, quarter);
         }
     };
-    const int of_choice = wave % share, first = wave / share, apart = DOWN_WAVES / share;
+    const int of_choice = wave % share, first = wave / share, apart = WAVES / share;
     for (int chunk = 0; chunk < steps; chunk += CHUNK) {
         const int end = min(chunk + CHUNK, steps);
         if (chunk + first < end) fetch(of_choice, chunk + first);
@@ -472,7 +472,7 @@ template <class In, class Out> __global__ __launch_bounds__(64 * DOWN_WAVES) voi
     __syncthreads();
     if (wave > 0 || tok > 0) return;
 #pragma unroll
-    for (int w = 1; w < DOWN_WAVES; w++) sum += parts[w][lane];
+    for (int w = 1; w < WAVES; w++) sum += parts[w][lane];
     const int64_t c = strip + quarter * 4;
     store_four<Out>((typename Out::T *)a.out + t * a.out_stride + c, a.N - c, a.wide_out, sum);
 }
@@ -537,7 +537,10 @@ hipError_t launch_direct_four(const DirectArgs &a, int x_type, int type, hipStre
     const dim3 grid(strips_of(a.N, 16), (unsigned)a.T);
     return with_type(x_type, [&](auto in) {
         return with_type(type, [&](auto out) {
-            direct_four_kernel<decltype(in), decltype(out)><<<grid, 64 * DOWN_WAVES, 0, s>>>(a);
+            // Sixteen waves where there is a workgroup for each compute unit at most, four where more than one shares it: six experts of 2048 x 2048, 128 workgroups,
+            // 7.3 us and 10.0; four rows of four, 512, 10.8 and 10.6; 24 of five of 1000 x 1100, 1656, 23.0 and 15.1; 64 of two of 512 x 512, 2048, 15.7 and 6.4
+            if ((int64_t)grid.x * grid.y <= 256) direct_four_kernel<decltype(in), decltype(out), 16><<<grid, 64 * 16, 0, s>>>(a);
+            else direct_four_kernel<decltype(in), decltype(out), 4><<<grid, 64 * 4, 0, s>>>(a);
             return hipGetLastError();
         });
     });

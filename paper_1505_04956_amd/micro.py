@@ -22,9 +22,10 @@ from . import experts as X
 RUN = 256                        # columns that a row is laid out in whole runs of
 SMALL = 32                       # columns that share a scale
 # Up to so many weights, an expert's counted for each row that goes to it, and results, one launch without an order is faster than an order, products and sums,
-# 27 us: 16 rows of four of 64 experts of 2048 x 2048, at both limits, 30 us for 31; 64 rows of two of 512 x 512, at the second, 15; 16 of eight of 2048 x 2048 51 for 38.
+# 27 us and more: 16 rows of six of 64 experts of 2048 x 2048 34 us for 34, 32 rows of two, at the first limit, 24 for 30; 512 rows of one of 512 x 512, at the second, 26
+# for 35; 2048 of one of 256 x 64, beyond it, 52.
 DIRECT_NUMBERS = 1 << 28
-DIRECT_RESULTS = 1 << 15
+DIRECT_RESULTS = 1 << 18
 
 
 def _runs(cols):

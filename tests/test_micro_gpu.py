@@ -187,7 +187,8 @@ def experts_64(x, ids, weights, w):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T,E,k,N,K", [(1, 8, 2, 40, 300), (1, 64, 6, 130, 513), (16, 5, 3, 17, 64), (17, 9, 2, 100, 257), (24, 100, 5, 100, 500), (300, 7, 2, 129, 260),
                                        (700, 3, 1, 256, 1000), (200, 300, 4, 20, 70),
-                                       (200, 300, 4, 200, 70), (150, 12, 2, 300, 260), (400, 30, 1, 100, 600), (40, 6, 2, 17, 8300)])
+                                       (200, 300, 4, 200, 70), (1500, 120, 2, 300, 60), (1200, 40, 1, 300, 260), (900, 50, 1, 300, 600), (3000, 500, 4, 100, 70), (1000, 100, 1, 300, 200),
+                                       (1100, 3, 2, 300, 1300), (2100, 5, 1, 129, 2600), (40, 6, 2, 17, 8300)])
 def test_experts(M, T, E, k, N, K, dtype):
     x, w = data(T, K, T, dtype), (data(E * N, K, E) * 0.1).view(E, N, K)
     ids, weights = routed(T, E, k, T + E)
@@ -206,11 +207,11 @@ def test_the_same_expert_twice(M):
     close(M.experts(x.repeat(8, 1).cuda(), ids.repeat(8, 1).cuda(), weights.repeat(8, 1).cuda(), mw), want.repeat(8, 1), bound.repeat(8, 1), torch.float32)
 
 
-@pytest.mark.parametrize("T,k,E", [(9, 2, 5), (300, 2, 3)])
-def test_products_by_place(M, X, T, k, E):
+@pytest.mark.parametrize("T,k,E,N", [(9, 2, 5, 40), (300, 2, 3, 40), (300, 2, 3, 200), (600, 2, 100, 400), (600, 2, 50, 400)])
+def test_products_by_place(M, X, T, k, E, N):
     """gather and places, and places that are not in use left as they were."""
     ids, _ = routed(T, E, k, 3)
-    x, w = data(T, 300, 1), data(E * 40, 300, 2).view(E, 40, 300)
+    x, w = data(T, 300, 1), data(E * N, 300, 2).view(E, N, 300)
     order, mw = X.plan(ids.cuda(), E), M.quantize(w.cuda())
     offsets, _, slots, _ = R.order_of(ids, E)
     used = offsets[-1]
@@ -225,8 +226,8 @@ def test_products_by_place(M, X, T, k, E):
     rows[:used] = x[token]
     close(M.product(M.quantize(rows.cuda()), mw, torch.float32, order)[:used], want, bound, torch.float32)
     from paper_1505_04956_amd import binding as B
-    out = torch.full((T * k, 40), 7.0, device="cuda")
-    B.asgd_block_product(a._c, mw._c, B.PRODUCT_GATHER, 0, order._c, out.data_ptr(), B.TYPE_F32, 40, torch.cuda.current_stream().cuda_stream)
+    out = torch.full((T * k, N), 7.0, device="cuda")
+    B.asgd_block_product(a._c, mw._c, B.PRODUCT_GATHER, 0, order._c, out.data_ptr(), B.TYPE_F32, N, torch.cuda.current_stream().cuda_stream)
     assert (out[used:] == 7.0).all() and used < T * k
     close(out[:used], want, bound, torch.float32)
 
