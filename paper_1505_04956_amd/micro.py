@@ -137,13 +137,18 @@ def linear(x, w):
     rows = _check(x, w)
     if x.get_device() != w._memory.get_device():
         X._same_device(x, w._memory)
+    raw = X._raw(x)
+    s, out, type = X._stream(x), x.new_empty((rows, w._rows)), raw.type
     # (few rows: bringing them to 4 bits again in each strip of the weights takes less than another launch)
     if rows > B.PRODUCT_RAW_ROWS:
-        return product(quantize(x), w, x.dtype)
-    raw = X._raw(x)
-    s, out = X._stream(x), x.new_empty((rows, w._rows))
+        n = rows * _runs(w._cols)
+        memory = x.new_empty(n * (RUN // 2 + RUN // SMALL), dtype=torch.uint8)
+        at = memory.data_ptr()
+        small = B.asgd_blocks(at, at + n * (RUN // 2), rows, w._cols, B.BLOCKS_FOURS, 1, 0, 0)
+        B.asgd_block_quantize(raw.values, type, rows, w._cols, raw.stride, 0, None, None, small, s)
+        raw = small
     if rows:
-        B.asgd_block_product(raw, w._c, B.PRODUCT_ALL, 1, None, out.data_ptr(), raw.type, w._rows, s)
+        B.asgd_block_product(raw, w._c, B.PRODUCT_ALL, 1, None, out.data_ptr(), type, w._rows, s)
     return out
 
 
