@@ -361,8 +361,8 @@ int64_t asgd_route_max_blocks(int64_t T, int k, int E);
  * or in 4-bit floating point:
  *   ASGD_BLOCKS_FOURS    blocks of 1 x 32.  values: e2m1, two a byte, the first in the low four bits, `count` matrices of rows x
  *                        (128 * kf) bytes, kf = ceil(cols / 256), zeros from column cols on; scales: bytes, count x rows x (8 * kf),
- *                        2^(byte - 127) is the scale of 32 columns, 255: it is not a number; both 16-byte aligned.  Rows of
- *                        activations and of weights (any count) are alike
+ *                        2^(byte - 127) is the scale of 32 columns, 255: it is not a number (not beyond cols); 16 and 8 bytes
+ *                        aligned.  Rows of activations and of weights (any count) are alike
  */
 enum { ASGD_BLOCKS_ROWS = 0, ASGD_BLOCKS_SQUARES = 1, ASGD_BLOCKS_RAW = 2, ASGD_BLOCKS_FOURS = 4 };
 typedef struct asgd_blocks {

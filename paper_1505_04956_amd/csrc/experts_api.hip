@@ -39,7 +39,7 @@ bool blocks_ok(const asgd_blocks *m)
 {
     if (!m || !m->values || m->rows < 0 || m->rows > MOST_ROWS || m->cols < 1 || m->cols > MOST_COLS || m->count < 1) return false;
     if (m->form == ASGD_BLOCKS_RAW) return m->count == 1 && matrix_ok(m->values, m->type, m->rows, m->cols, m->stride);
-    if (m->form == ASGD_BLOCKS_FOURS) return m->scales && aligned(m->values, 16) && aligned(m->scales, 16) && m->count <= ASGD_ROUTE_MAX_EXPERTS;
+    if (m->form == ASGD_BLOCKS_FOURS) return m->scales && aligned(m->values, 16) && aligned(m->scales, 8) && m->count <= ASGD_ROUTE_MAX_EXPERTS;
     if (m->form != ASGD_BLOCKS_ROWS && m->form != ASGD_BLOCKS_SQUARES) return false;
     return m->scales && aligned(m->values, 16) && aligned(m->scales, 4) && (m->form == ASGD_BLOCKS_SQUARES || m->count == 1) && m->count <= ASGD_ROUTE_MAX_EXPERTS;
 }
@@ -147,7 +147,7 @@ int asgd_block_quantize(const void *x, int type, int64_t rows, int64_t cols, int
     if (out->rows != want_rows || out->cols != want_cols) return ASGD_EINVAL;
     if (out->form == ASGD_BLOCKS_FOURS) {
         if (rows * out->count > MOST_ROWS) return ASGD_EINVAL;
-        const FourArgs f = {x, rows * out->count, cols, rows > 1 || out->count == 1 ? stride : cols, (uint8_t *)out->values, (uint8_t *)out->scales};
+        const FourArgs f = {x, rows * out->count, cols, stride, (uint8_t *)out->values, (uint8_t *)out->scales};
         return done(launch_quantize_four(f, type, (hipStream_t)hip_stream));
     }
     QuantArgs q = {};

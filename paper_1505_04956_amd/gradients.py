@@ -62,7 +62,7 @@ def norm(tensors):
 
 def clip(tensors, limit, out=None):
     """Multiplies all elements by limit / norm(tensors) where the norm is larger than limit, and returns the norm, a float32 tensor without dimensions.  In
-    place, or into `out`, tensors of the same sizes and of any of the three types, in the same order: each is its gradient itself or shares no
+    place, or into `out`, tensors of as many elements and of any of the three types, in the same order: each is its gradient itself or shares no
     memory with any other.  A norm that is not a number makes all elements not a number; an infinite one makes the finite elements zeros."""
     limit = float(limit)
     if not limit >= 0.0:
@@ -71,9 +71,9 @@ def clip(tensors, limit, out=None):
     to = None
     if out is not None:
         out = list(out)
-        if len(out) != len(tensors) or [t.shape for t in out] != [t.shape for t in tensors]:
-            raise ValueError("out: a tensor of the same size for each gradient is wanted")
         to = _spans(out, tensors[0].get_device(), "out")
+        if to[1::3] != spans[1::3]:
+            raise ValueError("out: a tensor of as many elements for each gradient is wanted")
     s = X._stream(tensors[0])
     result, work, size = _memory(len(tensors), tensors[0])
     B.asgd_gradient_clip(spans.buffer_info()[0], None if to is None else to.buffer_info()[0], len(tensors), limit, result.data_ptr(),

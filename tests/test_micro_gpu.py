@@ -65,6 +65,22 @@ def test_strided_rows_and_experts(M, dtype):
     assert torch.equal(M.expand(m)[3].cpu().double(), Q.matrix_of(m)[3])
 
 
+def test_one_expert_of_many(M):
+    """Its scales begin at a multiple of eight bytes."""
+    m = M.quantize(data(5 * 33, 700, 1).view(5, 33, 700).cuda())
+    x = data(40, 700, 2).cuda()
+    for e in range(5):
+        one = M.Micro(m.values[e], m.scales[e], 700)
+        assert torch.equal(M.expand(one), M.expand(m)[e])
+        for rows in (1, 20, 40):
+            want = M.linear(x[:rows], M.Micro(m.values[e].clone(), m.scales[e].clone(), 700))
+            assert torch.equal(M.linear(x[:rows], one), want)
+        ids = torch.zeros(2, 1, dtype=torch.int32, device="cuda")
+        a = M.Micro(m.values[e:e + 1], m.scales[e:e + 1], 700)
+        q, v = Q.four(x[:2].cpu()), Q.matrix_of(one)
+        close(M.experts(x[:2], ids, torch.ones(2, 1, device="cuda"), a), q @ v.t(), Q.product_bound(q.abs() @ v.abs().t(), 700), torch.float32)
+
+
 def test_extremes_of_a_block(M):
     x = torch.zeros(14, 300)
     x[0, 3], x[0, 200] = 3.4028234e38, 1.5e-45                      # the largest number, and nearly the smallest

@@ -183,7 +183,7 @@ def test_layers_of_tensors_that_are_refused():
 def test_gradients_of_tensors_that_are_refused():
     x = torch.zeros(4, 6)
     for call in (lambda: G.norm([]), lambda: G.norm([x.t()]), lambda: G.norm([x.double()]), lambda: G.norm([x[:, :3]]), lambda: G.clip([x], -1.0), lambda: G.clip([x], float("nan")),
-                 lambda: G.clip([x], 1.0, out=[]), lambda: G.clip([x], 1.0, out=[x[:3]]), lambda: G.clip([x], 1.0, out=[x.t()]), lambda: G.clip([x], 1.0, out=[x.view(6, 4)])):
+                 lambda: G.clip([x], 1.0, out=[]), lambda: G.clip([x], 1.0, out=[x[:3]]), lambda: G.clip([x], 1.0, out=[x.t()]), lambda: G.clip([x], 1.0, out=[x, x])):
         with pytest.raises(ValueError):
             call()
     with pytest.raises(ValueError, match="no CPU fallback"):
