@@ -289,3 +289,69 @@ def test_the_same_bits_again_on_a_stream_and_in_a_graph(M):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held, want))
+
+
+def test_beyond_four_gigabytes(M, X):
+    """Weights, rows and results whose places pass 32 bits: what lies at their ends is found."""
+    from paper_1505_04956_amd import layer as L
+    E, N, K = 520, 2048, 8192                                       # 4.4 GB of values
+    w = data(N, K, 1) * 0.1
+    one = M.quantize(w.cuda())
+    values = torch.zeros(E, N, K // 2, dtype=torch.uint8, device="cuda")
+    scales = torch.full((E, N, K // 32), 127, dtype=torch.uint8, device="cuda")
+    values[-1], scales[-1] = one.values, one.scales
+    many = M.Micro(values, scales, K)
+    b = Q.four(w)
+    for T in (1, 40):
+        x = data(T, K, T, torch.bfloat16)
+        a = Q.four(x.float())
+        want, bound = a @ b.t(), Q.product_bound(a.abs() @ b.abs().t(), K)
+        ids = torch.full((T, 1), E - 1, dtype=torch.int32, device="cuda")
+        close(M.experts(x.cuda(), ids, torch.ones(T, 1, device="cuda"), many), want, bound + 8 * Q.U * want.abs(), torch.bfloat16)
+        order = X.plan(ids, E)
+        close(M.product(M.quantize(x.cuda()), many, torch.float32, order, gather=True), want, bound, torch.float32)
+    # a layer whose second matrix this is: h is 8192 columns
+    H, D = K, 64
+    up = data(2 * H, D, 5) * 0.1
+    u = M.quantize(up.cuda())
+    uv, us = torch.zeros(E, 2 * H, 128, dtype=torch.uint8, device="cuda"), torch.full((E, 2 * H, 8), 127, dtype=torch.uint8, device="cuda")
+    uv[-1], us[-1] = u.values, u.scales
+    x = data(3, D, 9)
+    logits = torch.full((3, E), -float("inf"))
+    logits[:, -1] = 1.0
+    y, ids, weights = L.layer(x.cuda(), logits.cuda(), X.Rule(1), M.Micro(uv, us, D), many)
+    assert (ids == E - 1).all() and (weights == 1).all()
+    want, bound = Q.layer(x, torch.zeros(3, 1, dtype=torch.int32), torch.ones(3, 1), Q.matrix_of(u)[None], Q.matrix_of(one)[None], 4, False)
+    close(y, want, bound, torch.float32)
+    del values, scales, many, uv, us
+    # rows of activations, and the results of bringing them to 4 bits and back
+    rows = (1 << 19) + 130
+    v, s = torch.zeros(rows, K // 2, dtype=torch.uint8, device="cuda"), torch.full((rows, K // 32), 127, dtype=torch.uint8, device="cuda")
+    assert v.numel() > 1 << 31
+    tail = data(70, K, 3)
+    t = M.quantize(tail.cuda())
+    v[-70:], s[-70:] = t.values, t.scales
+    small = M.quantize((data(40, K, 4) * 0.1).cuda())
+    q, z = Q.four(tail), Q.matrix_of(small)
+    y = M.product(M.Micro(v, s, K), small, torch.float32)
+    close(y[-70:], q @ z.t(), Q.product_bound(q.abs() @ z.abs().t(), K), torch.float32)
+    assert (y[:-70] == 0).all()
+    back = M.expand(M.Micro(v, s, K), torch.bfloat16)               # 8.6 GB
+    assert torch.equal(back[-70:].cpu().double(), Q.matrix_of(t).bfloat16().double()) and (back[:1000] == 0).all()
+    again = M.quantize(back)
+    assert torch.equal(again.values[-70:], t.values)
+
+
+@pytest.mark.parametrize("rows", [1, 3, 16, 17, 32])
+def test_few_rows_of_wide_results(M, rows):
+    """Four strips of the weights a workgroup, and more runs than are brought to 4 bits at a time."""
+    N, K = 33_000, 17 * 256
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    values = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.randint(118, 128, (N, K // 32), generator=g, device="cuda", dtype=torch.uint8)
+    w, x = M.Micro(values, scales, K), data(rows, K, rows, torch.float16)
+    pick = torch.cat([torch.arange(0, N, 331), torch.arange(N - 40, N)])
+    a, b = Q.four(x.float()), Q.from_four(Q.codes(values[pick.cuda()]), scales[pick.cuda()].cpu())
+    want, bound = a @ b.t(), Q.product_bound(a.abs() @ b.abs().t(), K)
+    close(M.product(M.quantize(x.cuda()), w, torch.float32)[:, pick.cuda()], want, bound, torch.float32)
+    close(M.linear(x.float().cuda(), w)[:, pick.cuda()], want, bound, torch.float32)
