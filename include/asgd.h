@@ -357,7 +357,7 @@ int64_t asgd_route_max_blocks(int64_t T, int k, int E);
  *   ASGD_BLOCKS_SQUARES  blocks of 128 x 128: scales[count][ceil(rows / 128)][kb]
  *   ASGD_BLOCKS_RAW      not in 8 bits yet: values are rows x cols of `type`, rows `stride` elements apart, scales is
  *                        not used (count = 1); the product brings them to 8 bits as ASGD_BLOCKS_ROWS would on the way (to 4, if
-                        the other operand is ASGD_BLOCKS_FOURS)
+ *                        the other operand is ASGD_BLOCKS_FOURS)
  * or in 4-bit floating point:
  *   ASGD_BLOCKS_FOURS    blocks of 1 x 32.  values: e2m1, two a byte, the first in the low four bits, `count` matrices of rows x
  *                        (128 * kf) bytes, kf = ceil(cols / 256), zeros from column cols on; scales: bytes, count x rows x (8 * kf),

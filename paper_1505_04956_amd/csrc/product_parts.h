@@ -60,7 +60,7 @@ template <class Offset> __device__ __forceinline__ void to_lds(const uint8_t *ba
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + offset),
                                      (__attribute__((address_space(3))) void *)to, 16, 0, 0);
 }
-__device__ __forceinline__ void to_lds4(const uint8_t *base, uint32_t offset, uint8_t *to)
+template <class Offset> __device__ __forceinline__ void to_lds4(const uint8_t *base, Offset offset, uint8_t *to)
 {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + offset),
                                      (__attribute__((address_space(3))) void *)to, 4, 0, 0);
