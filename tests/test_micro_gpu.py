@@ -342,6 +342,25 @@ def test_beyond_four_gigabytes(M, X):
     assert torch.equal(again.values[-70:], t.values)
 
 
+def test_gathered_scales_beyond_four_gigabytes(M, X):
+    """Gathered rows of activations whose scales lie beyond 2^32 bytes of the first: they are their own, not those 2^32 bytes before."""
+    K, used = 1 << 20, 6
+    T = (1 << 32) // (K // 32) + used
+    tail = data(used, K, 1).abs() * 64                              # of one sign: no sum hides a scale that is not its own
+    w = data(20, K, 2).abs()
+    q, small = M.quantize(tail.cuda()), M.quantize(w.cuda())
+    values = torch.empty(T, K // 2, dtype=torch.uint8, device="cuda")   # 69 GB, of which the rows at its ends are written and read
+    scales = torch.full((T, K // 32), 127, dtype=torch.uint8, device="cuda")
+    assert (T - used) * scales.stride(0) == 1 << 32
+    values[-used:], scales[-used:] = q.values, q.scales
+    ids = torch.full((T, 1), -1, dtype=torch.int32, device="cuda")
+    ids[-used:] = 0
+    a, b = Q.four(tail), Q.four(w)
+    want = a @ b.t()
+    y = M.product(M.Micro(values, scales, K), M.Micro(small.values[None], small.scales[None], K), torch.float32, X.plan(ids, 1), gather=True)
+    close(y[:used], want, Q.product_bound(want, K), torch.float32)  # (the places in use are the first)
+
+
 @pytest.mark.parametrize("rows", [1, 3, 16, 17, 32])
 def test_few_rows_of_wide_results(M, rows):
     """Four strips of the weights a workgroup, and more runs than are brought to 4 bits at a time."""
