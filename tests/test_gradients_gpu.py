@@ -162,3 +162,24 @@ def test_more_than_two_to_the_32_bytes(G):
     g[5] = 12.0
     assert G.clip([g], 6.5).item() == 13.0
     assert g[5] == 6.0 and g[-3] == 1.5 and g[-1] == 2.0 and g[-2] == 0.0 and (g != 0).sum() == 3
+
+
+def test_what_is_clipped_counts_as_modified(G):
+    """A backward pass through what was clipped after it was saved is refused, as after an operation of torch in place: autograd's, and experts_backward()'s."""
+    from paper_1505_04956_amd import experts as X
+    a, b = torch.ones(5000, device="cuda", requires_grad=True), torch.ones(5000, device="cuda")
+    y, z = (a * b).sum(), (a * b).sum()
+    out, was = torch.empty_like(b), b._version
+    G.norm([b]), G.clip([b], 1.0, out=[out])
+    z.backward()                                                    # (it was only read)
+    assert out._version > 0 and b._version == was and (a.grad == 1).all()
+    G.clip([b], 1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    w = torch.randn(3, 20, 40, device="cuda")
+    x = torch.randn(7, 40, device="cuda")
+    ids, weights = X.route(torch.randn(7, 3, device="cuda"), X.Rule(2))
+    got, kept = X.experts(x, ids, weights, X.quantize_weights(w), train=True)
+    G.clip([weights], 0.5)
+    with pytest.raises(ValueError, match="have changed"):
+        X.experts_backward(got, kept, X.quantize_weights(w, turned=True))

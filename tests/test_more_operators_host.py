@@ -201,3 +201,48 @@ def test_the_definition_of_four_bits():
     assert s[:, 0].tolist() == [127, 127, 128, 125, 1] and s[0, 1] == 1
     assert code[0, :4].tolist() == [7, 0, 2, 12] and code[1, :2].tolist() == [7, 6] and code[2, :3].tolist() == [6, 1, 0] and code[3, 0] == 6
     assert Q.four(x)[2, :3].tolist() == [8.0, 1.0, 0.0]
+
+
+def test_what_clipping_writes_counts_as_written(monkeypatch):
+    """The library writes through addresses, so clip() moves the versions of the tensors that it writes, of no others, and of none where it refuses.  (The
+    library and the stream stand aside here: nothing is computed.)"""
+    calls = []
+    monkeypatch.setattr(X, "_stream", lambda t: 0)
+    monkeypatch.setattr(B, "asgd_gradient_clip", lambda *a: calls.append(a))
+    monkeypatch.setattr(B, "asgd_gradient_norm", lambda *a: calls.append(a))
+    versions = lambda tensors: [t._version for t in tensors]  # noqa: E731
+    grads, out = [torch.zeros(4), torch.zeros(3, 2, dtype=torch.bfloat16), torch.zeros(0)], [torch.zeros(4), torch.zeros(6), torch.zeros(0)]
+    G.norm(grads)
+    assert versions(grads) == [0, 0, 0]
+    G.clip(iter(grads), 1.0)
+    assert all(v > 0 for v in versions(grads)) and versions(out) == [0, 0, 0]
+    was = versions(grads)
+    G.clip(grads, 1.0, out=iter(out))
+    assert versions(grads) == was and all(v > 0 for v in versions(out))
+    G.clip(grads, 1.0, out=[grads[0], out[1], out[2]])
+    assert grads[0]._version > was[0] and versions(grads[1:]) == was[1:]
+    # a view's is its base's, and a leaf's moves where no gradients are recorded
+    base, leaf = torch.zeros(10), torch.zeros(4, requires_grad=True)
+    with torch.no_grad():
+        G.clip([base[2:5], leaf], 1.0)
+    assert base._version > 0 and leaf._version > 0
+    # tensors of inference mode have none
+    with torch.inference_mode():
+        free = torch.zeros(4)
+        G.clip([free, base], 1.0)
+    G.clip([free], 1.0)
+    # what was saved and is clipped before its backward
+    a, b = torch.ones(4, requires_grad=True), torch.ones(4)
+    y = (a * b).sum()
+    G.clip([b], 1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    assert len(calls) == 8
+
+    def refused(*a):
+        raise B.AsgdError(B.EINVAL, "asgd_gradient_clip")
+    monkeypatch.setattr(B, "asgd_gradient_clip", refused)
+    was = versions(grads + out)
+    with pytest.raises(B.AsgdError):
+        G.clip(grads, 1.0, out=out)
+    assert versions(grads + out) == was
