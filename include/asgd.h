@@ -488,8 +488,8 @@ int asgd_gradient_norm(const asgd_span *runs, int64_t count, float *norm, void *
 /*
  * That norm, and out[i] = runs[i] * factor, factor = limit / norm (64-bit, rounded to 32) where norm > limit, 1 where it is not, not a number where the norm is
  * none; a product is rounded to 32 bits, then to the type of out[i].  limit >= 0.  An infinite norm, then, gives zeros and, of
- * infinities, what is not a number.  out may be NULL (runs are clipped in place); out[i] has as many elements as runs[i], is runs[i] itself
- * or shares no byte with any run or other out.  In place nothing is written where the factor is 1.
+ * infinities, what is not a number.  out may be NULL (every out[i] is runs[i]); out[i] has as many elements as runs[i], is runs[i] itself
+ * or shares no byte with it, and none with any other run or out.  Runs that are only read may share theirs.  In place nothing is written where the factor is 1.
  */
 int asgd_gradient_clip(const asgd_span *runs, const asgd_span *out, int64_t count, double limit, float *norm, void *work, size_t work_bytes,
                        void *hip_stream);

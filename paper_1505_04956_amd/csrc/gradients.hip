@@ -232,22 +232,30 @@ int64_t chunks_of(const asgd_span *s, int64_t count)
     return chunks;
 }
 
-struct Interval { uintptr_t from, to; };
+struct Interval {
+    uintptr_t from, to;
+    bool written;
+};
 
-// whether what is written shares a byte with anything but what it is made of
+// whether what is written shares no byte with anything but what it is made of (runs that are only read may share theirs)
 bool apart(const asgd_span *runs, const asgd_span *out, int64_t count)
 {
     std::vector<Interval> all;
     all.reserve(2 * count);
-    const auto add = [&](const asgd_span &s) { if (s.n) all.push_back({(uintptr_t)s.data, (uintptr_t)s.data + s.n * type_size((int)s.type)}); };
+    const auto add = [&](const asgd_span &s, bool written) { if (s.n) all.push_back({(uintptr_t)s.data, (uintptr_t)s.data + s.n * type_size((int)s.type), written}); };
     for (int64_t i = 0; i < count; i++) {
-        add(runs[i]);
-        if (out && !(out[i].data == runs[i].data && out[i].type == runs[i].type)) add(out[i]);
+        const bool in_place = !out || (out[i].data == runs[i].data && out[i].type == runs[i].type);
+        add(runs[i], in_place);
+        if (!in_place) add(out[i], true);
     }
     const auto before = [](const Interval &a, const Interval &b) { return a.from < b.from; };
     if (!std::is_sorted(all.begin(), all.end(), before)) std::sort(all.begin(), all.end(), before);
-    for (size_t i = 1; i < all.size(); i++)
-        if (all[i].from < all[i - 1].to) return false;
+    uintptr_t end = 0, end_written = 0;         // of those before, and of the written ones among them
+    for (const Interval &i : all) {
+        if (i.from < (i.written ? end : end_written)) return false;
+        end = std::max(end, i.to);
+        if (i.written) end_written = std::max(end_written, i.to);
+    }
     return true;
 }
 

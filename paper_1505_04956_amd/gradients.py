@@ -64,7 +64,7 @@ def norm(tensors):
 def clip(tensors, limit, out=None):
     """Multiplies all elements by limit / norm(tensors) where the norm is larger than limit, and returns the norm, a float32 tensor without dimensions.  In
     place, or into `out`, tensors of as many elements and of any of the three types, in the same order: each is its gradient itself or shares no
-    memory with any other.  What is written counts as modified for autograd, as by an operation of torch in place, whether or not the norm is larger.  A norm that is not a number makes all elements not a number; an infinite one makes the finite elements zeros."""
+    memory with any other (gradients that are only read may).  What is written counts as modified for autograd, as by an operation of torch in place, whether or not the norm is larger.  A norm that is not a number makes all elements not a number; an infinite one makes the finite elements zeros."""
     limit = float(limit)
     if not limit >= 0.0:
         raise ValueError("limit: a number from 0 on is wanted, not %r" % limit)

@@ -183,3 +183,16 @@ def test_what_is_clipped_counts_as_modified(G):
     G.clip([weights], 0.5)
     with pytest.raises(ValueError, match="have changed"):
         X.experts_backward(got, kept, X.quantize_weights(w, turned=True))
+
+
+@pytest.mark.parametrize("n", [1000, 100_000])
+def test_runs_that_are_only_read_may_share_memory(G, n):
+    """The same gradient twice, and views that overlap, into memory of their own: each counts as often as it is listed."""
+    flat = make([n], torch.float32, n)[0]
+    was = flat.clone()
+    for grads in ([flat, flat], [flat[:n // 2], flat[n // 3:], flat], [flat[n // 2:], flat[:n // 2 + 3]]):
+        want, out = exact_norm(grads), [torch.empty_like(t, dtype=d) for t, d in zip(grads, TYPES)]
+        assert near(G.clip(grads, want * 0.3, out=out).item(), want)
+        for a, b in zip(out, grads):
+            check(a, b, 0.3)
+    assert torch.equal(flat, was)

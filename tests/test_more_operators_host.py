@@ -246,3 +246,16 @@ def test_what_clipping_writes_counts_as_written(monkeypatch):
     with pytest.raises(B.AsgdError):
         G.clip(grads, 1.0, out=out)
     assert versions(grads + out) == was
+
+
+def test_what_is_written_shares_memory_with_nothing():
+    """Wherever it lies among runs that are only read, inside long ones and behind short ones that lie in them too."""
+    A, F = 1 << 24, 1 << 25
+    go = lambda runs, out: B.lib().asgd_gradient_clip(runs.buffer_info()[0], out.buffer_info()[0], len(runs) // 3, 1.0, P, P, 1 << 30, None)  # noqa: E731
+    for runs, out in ((spans((A, 1000, 0), (A + 40, 10, 0)), spans((F, 1000, 0), (A + 2000, 10, 0))), (spans((A + 40, 10, 0), (A, 1000, 0)), spans((A + 3996, 10, 0), (F, 1000, 0))),
+                      (spans((A, 100, 0), (A, 100, 0)), spans((A, 100, 0), (F, 100, 0))), (spans((A, 100, 0), (A, 100, 0)), spans((F, 100, 0), (F, 100, 0))),
+                      (spans((A, 100, 0), (A, 100, 0)), spans((A, 100, 0), (A, 100, 0))), (spans((A + 100, 50, 0), (A, 1000, 0)), spans((A + 100, 50, 0), (F, 1000, 0))),
+                      (spans((A + 4, 10, 0), (A + 8, 10, 0), (F, 2, 0)), spans((F + 8, 10, 0), (F + 400, 10, 0), (A, 2, 0))),
+                      (spans((F, 1000, 0), (A, 2, 0)), spans((A, 1000, 0), (A + 500, 2, 0)))):
+        assert out[1::3] == runs[1::3]
+        assert go(runs, out) == B.EINVAL
