@@ -144,9 +144,10 @@ template <> struct Weights<4> {
 };
 
 // ---- up -----------------------------------------------------------------------------------------------------------------
+// (1 + erf(v) is formed as erfc(-v): far below zero the sum would cancel, and from a gate of -5.6 on be zero, so that blocks of such h would be lost.  0.1 us of 112: sixteen rows of eight of 128 experts)
 __device__ __forceinline__ float activated(float gate, float up, int activation)
 {
-    const float f = activation == ASGD_ACTIVATION_SILU ? gate / (1.0f + expf(-gate)) : 0.5f * gate * (1.0f + erff(gate * 0.70710678f));
+    const float f = activation == ASGD_ACTIVATION_SILU ? gate / (1.0f + expf(-gate)) : 0.5f * gate * erfcf(gate * -0.70710678f);
     return f * up;
 }
 

@@ -236,3 +236,38 @@ def test_the_example_clips_its_gradients_and_serves_in_four_bits(L, shared):
     said = []
     got, _ = C.run(samples=60_000, steps=2, k=4, batch=1000, shared=shared, limit=0.5, small=lambda *l: said.extend(l))
     assert len(got) == 2 and len(said) == 2 and all(0 < v < 1e9 for v in got + said)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("T", [3, 12])
+@pytest.mark.parametrize("low", [-3.0, -5.0, -6.5, -9.0, -11.0])
+def test_gates_far_below_zero(L, monkeypatch, low, T, bits):
+    """g / 2 * (1 + erf(g / sqrt(2))) where the two all but cancel: h keeps its digits, and blocks of such h are not lost.  For g < 0, |f'(g)| is at most
+    (|g| + 1) |f(g)| (Mills' ratio); the argument of the error function is within 2 units of 2^-24, the function within 16 of its last place, and there are
+    two products more."""
+    from paper_1505_04956_amd import experts as X, micro as M
+
+    def activated(g, u, gelu):
+        assert gelu and (g < 0).all()
+        return 0.5 * g * torch.special.erfc(-g / 2 ** 0.5) * u
+
+    def bound(g, u, dg, du, gelu):
+        f = activated(g, torch.ones_like(u), gelu).abs()
+        assert ((g.abs() + 1) * dg < 0.1).all()                     # (e^0.1 < 1.11: what the second order adds)
+        return f * ((g.abs() + 1) * (dg + 2 * Q.U * g.abs()) * 1.11 + 40 * Q.U) * (u.abs() + du) + f * du + 2 * Q.U * f * u.abs() + 1e-37
+    monkeypatch.setattr(Q, "activated", activated)
+    monkeypatch.setattr(Q, "activated_bound", bound)
+    E, D, H, N = 3, 64, 97, 40
+    g = torch.Generator().manual_seed(int(-10 * low) + T)
+    rand = lambda *shape: torch.rand(*shape, generator=g)  # noqa: E731
+    x, logits = 0.9 + 0.2 * rand(T, D), torch.randn(T, E, generator=g)
+    up = torch.cat([(low - 0.5 * rand(E, H, 1)) / D * (0.9 + 0.2 * rand(E, H, D)), (0.5 + rand(E, H, D)) / D], 1)
+    down = torch.randn(E, N, H, generator=g) / H ** 0.5
+    of = M.quantize if bits == 4 else X.quantize_weights
+    up, down = of(up.cuda()), of(down.cuda())
+    full = lambda m: Q.matrix_of(m) if bits == 4 else torch.stack([R.from_squares(v, s)[:, :m.cols] for v, s in zip(m.values.cpu(), m.scales.cpu())])  # noqa: E731
+    y, ids, weights = L.layer(x.cuda(), logits.cuda(), X.Rule(2), up, down, activation=L.GELU)
+    want, off = Q.layer(x, ids.cpu(), weights.cpu(), full(up), full(down), bits, True)
+    # (what may be off is a small part of what is there, so the test says something)
+    assert off.norm() < 0.1 * want.norm()
+    close(y, want, off, torch.float32)
