@@ -271,3 +271,84 @@ def test_gates_far_below_zero(L, monkeypatch, low, T, bits):
     # (what may be off is a small part of what is there, so the test says something)
     assert off.norm() < 0.1 * want.norm()
     close(y, want, off, torch.float32)
+
+
+# (rows, experts, groups): routed in the first product's launch, and by one of its own; groups of whole lanes and others, all widths of a lane
+GROUPS = [(5, 60, 6), (8, 64, 8), (3, 128, 4), (2, 256, 8), (8, 250, 5), (16, 60, 6), (16, 64, 8), (9, 128, 4), (16, 250, 5), (16, 256, 8), (16, 512, 16), (3, 300, 10), (7, 512, 64), (16, 1000, 10), (16, 1024, 64),
+          (2, 1001, 7), (1, 1024, 16)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,E,groups", GROUPS)
+def test_groups_scores_and_logits_of_every_type(L, T, E, groups, dtype):
+    """In both launches that route: the choice and the weights are route()'s bit for bit, whatever the rule, the logits' type and how they lie."""
+    from paper_1505_04956_amd import experts as X
+    D, H, N = 40, 24, 16
+    for n, (score, by, with_bias, renormalize) in enumerate([(X.SOFTMAX, X.BEST, False, True), (X.SIGMOID, X.BEST_TWO, True, True), (X.SOFTMAX, X.BEST_TWO, True, False),
+                                                             (X.SOFTMAX, X.BEST_TWO, False, True), (X.SIGMOID, X.BEST, False, False), (X.SOFTMAX, X.BEST, True, True)]):
+        bits = 4 if (n + E) % 2 else 8
+        x, logits, up, down, u64, d64 = make(L, T, E, D, H, N, bits, torch.float32, E + n)
+        apart = torch.zeros(T, E + 9, dtype=dtype, device="cuda")
+        l = apart[:, n % 3:n % 3 + E]                               # rows that begin anywhere, and aligned ones
+        l.copy_(logits)
+        if T > 2:
+            l[1] = -float("inf")
+            l[2, E // groups:] = -float("inf")                      # one group left, and fewer experts than are chosen of it
+            l[2, 3:] = -float("inf")
+        bias = (torch.randn(E, generator=torch.Generator().manual_seed(n)) * 0.2).cuda() if with_bias else None
+        rule = X.Rule(4, score=score, groups=groups, kept=max(1, groups // 3), group_by=by, renormalize=renormalize, scale=2.0)
+        for lay in (l, l.contiguous()):
+            y, ids, weights = L.layer(x.cuda(), lay, rule, up, down, bias=bias)
+            i2, w2 = X.route(lay, rule, bias=bias)
+            assert torch.equal(ids, i2) and torch.equal(weights, w2)
+        if T > 2:
+            assert (ids[1] == -1).all() and (y[1] == 0).all() and (ids[2] >= 0).sum() == 3
+        want, bound = Q.layer(x, ids.cpu(), weights.cpu(), u64, d64, bits, False)
+        close(y, want, bound, torch.float32)
+
+
+@pytest.mark.parametrize("T,E", [(6, 60), (6, 61), (16, 300), (16, 301), (16, 1000), (16, 1001)])
+def test_sixteen_bit_logits_in_both_launches(L, T, E):
+    from paper_1505_04956_amd import experts as X
+    x, logits, up, down, _, _ = make(L, T, E, 64, 24, 20, 4, torch.bfloat16, T + E)
+    for dtype in (torch.bfloat16, torch.float16):
+        l = logits.to(dtype).cuda()
+        got, want = L.layer(x.cuda(), l, X.Rule(5), up, down), L.layer(x.cuda(), l.float(), X.Rule(5), up, down)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_what_the_example_says_of_its_maps_in_four_bits(L, shared, monkeypatch):
+    """The evaluation in 4 bits is that of the trained maps' 4-bit values, and the two losses that are said differ by no more than the two results do:
+    |l4 - l8| <= sqrt(2 l8 m) + m / 2 with m the mean square of the difference (Cauchy and Schwarz), and what 32-bit means lose."""
+    from paper_1505_04956_amd import clusterwise as C, experts as X
+    held, said = {}, []
+    small = C.ClusterwiseLinear.small
+
+    def watched(self):
+        served = small(self)
+
+        def forward(x):
+            held["x"], held["y8"], held["y4"], held["model"] = x, self.forward(x), served(x), self
+            return held["y4"]
+        return forward
+    monkeypatch.setattr(C.ClusterwiseLinear, "small", watched)
+    C.run(samples=60_000, steps=2, k=4, batch=1000, shared=shared, limit=0.5, small=lambda *l: said.extend(l))
+    l8, l4 = said
+    m = float((held["y4"].double() - held["y8"].double()).square().sum(1).mean())
+    assert m > 0 and abs(l4 - l8) <= ((2 * l8 * m) ** 0.5 + m / 2) * (1 + 1e-3) + 1e-4 * l8
+    model, x = held["model"], held["x"][:50]
+    ids, weights = X.route(model.logits(held["x"]), model.rule)
+    q, maps = Q.four(x.bfloat16().float().cpu()), [Q.four(w.cpu()) for w in model.w]
+    y, mags = torch.zeros(50, maps[0].shape[0], dtype=torch.float64), torch.zeros(50, maps[0].shape[0], dtype=torch.float64)
+    for t in range(50):
+        for e, c in zip(ids[t].tolist(), weights[t].tolist()):
+            y[t] += c * (maps[e] @ q[t])
+            mags[t] += abs(c) * (maps[e].abs() @ q[t].abs())
+    allowed = Q.product_bound(mags, x.shape[1]) + 2.0 ** -8 * y.abs() + 8 * Q.U * mags
+    if shared:
+        b = Q.four(model.shared.cpu())
+        allowed += Q.product_bound(q.abs() @ b.abs().t(), x.shape[1]) + 2.0 ** -8 * (q @ b.t()).abs()
+        y = y + q @ b.t()
+        allowed += 2 * Q.U * y.abs()
+    assert ((held["y4"][:50].cpu().double() - y).abs() <= 1.01 * allowed).all()
