@@ -383,7 +383,7 @@ typedef struct asgd_blocks {
  * out in 4 bits (ASGD_BLOCKS_FOURS; turned = 0, order = NULL): a block whose largest magnitude is m gets the scale 2^e, e =
  * floor(log2 m) - 2, one more where m is at least 1.75 * 2^floor(log2 m), at least -126 and at most 125, and the values v / 2^e to the
  * nearest e2m1 number (0, 0.5, 1, 1.5, 2, 3, 4, 6), ties to even, cut at 6.  (m then rounds to at most 6, but where m / 2^e lies
- * between 6 and 7 and is cut.)  The scales of columns beyond cols are 2^-126.
+ * between 6 and 7, or, m from 1.75 * 2^127 on, between 7 and 8, and is cut.)  The scales of columns beyond cols are 2^-126.
  *   turned = 1   the transpose of x is brought to 8 bits: out has cols rows; blocks lie along x's rows
  *   order        (ASGD_BLOCKS_ROWS only, count = 1, or NULL) x has one row for each of the order's T rows; row p of what is
  *                brought to 8 bits is x's row of the slot at place p, times weights[slot] (float T x k, or NULL).  Not

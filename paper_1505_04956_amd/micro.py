@@ -82,7 +82,8 @@ class Micro:
 
 def quantize(x):
     """x [rows, cols], or contiguous [experts, rows, cols], in 4 bits (Micro).  The scale of 32 columns is the power of two that takes their
-    largest magnitude to at most 6, the largest number of the format, or to where it is cut to it (below 7); a block with something that is not a finite number is not a number."""
+    largest magnitude to at most 6, the largest number of the format, or to where it is cut to it (below 7; below 8 from 1.75 * 2^127 on, where the
+    next scale's numbers would pass float32); a block with something that is not a finite number is not a number."""
     if x.dim() == 3:
         if not x.is_contiguous() or x.numel() == 0:
             raise ValueError("x: a contiguous [experts, rows, cols] is wanted, not %s" % (tuple(x.shape),))

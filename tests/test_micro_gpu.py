@@ -374,3 +374,17 @@ def test_few_rows_of_wide_results(M, rows):
     want, bound = a @ b.t(), Q.product_bound(a.abs() @ b.abs().t(), K)
     close(M.product(M.quantize(x.cuda()), w, torch.float32)[:, pick.cuda()], want, bound, torch.float32)
     close(M.linear(x.float().cuda(), w)[:, pick.cuda()], want, bound, torch.float32)
+
+
+def test_the_largest_numbers(M):
+    """From 1.75 * 2^127 on there is no larger scale whose numbers are finite: up to eight times the scale are cut to six, by a quarter at most."""
+    top = [1.75 * 2.0 ** 127, 3.4028234663852886e38, 1.7499999 * 2.0 ** 127, 1.5 * 2.0 ** 127, 2.0 ** 127, 1.75 * 2.0 ** 126, 1.7499999 * 2.0 ** 126]
+    x = torch.zeros(len(top), 32)
+    x[:, 0], x[:, 1] = torch.tensor(top, dtype=torch.float64).float(), -2.0 ** 125
+    m = M.quantize(x.cuda())
+    assert same(m, x)
+    got = M.expand(m).cpu().double()
+    assert torch.isfinite(got).all()
+    share = (got[:, 0] / x[:, 0].double()).tolist()
+    assert share[1] == pytest.approx(0.75, abs=1e-6) and all(0.75 <= v < 6 / 7 + 1e-6 for v in share[:2]) and all(6 / 7 - 1e-6 <= v <= 8 / 7 + 1e-6 for v in share[2:])
+    assert (m.scales.cpu()[:5, 0] == 252).all() and got[0, 0] == 6 * 2.0 ** 125
