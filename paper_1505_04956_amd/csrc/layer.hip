@@ -7,8 +7,8 @@
 //   down    a workgroup sums sixteen columns of the result over all experts; its waves share the experts' blocks
 //
 // The weights' way from memory bounds the second and third: sixteen rows of eight of 128 experts of 4096 x 1024 in 4 bits 67 us (5.4 TB/s) and 38 (4.7), one row of six of 64
-// of 2048 x 1408 in 8 bits, 34.6 and 17.3 MB, 11.9 us and 8.0, where a chain of loads (lists, rows, weights) is as long as what they bring; choose 3.5 to 6 us, a
-// launch and a row's routing.
+// of 2048 x 1408 in 8 bits, 34.6 and 17.3 MB, 11.9 us and 8.0, where a chain of loads (lists, rows, weights) is as long as what they bring (those weights lay in the last cache; from memory both
+// take 1.5 us more); choose 3.5 to 6 us, a launch and a row's routing.
 #include "four_bits.h"
 #include "route_row.h"
 
@@ -18,7 +18,9 @@ namespace {
 
 constexpr int UP_WAVES = 4, DOWN_WAVES = 16, COLUMNS = 16;
 // Up to so many rows, experts, steps of all rows, and workgroups times rows (which all route and bring to 8 or 4 bits the same) one launch does the first two
-// parts.  One row of 64 experts of 2048 x 1408 so 22.0 us, else 24.5; two rows 29.3 and 30.3; four (4224) 55 and 48; five of 100 experts of 1000 x 700 (5500) 23.5 and 21.5.
+// parts.  Layers in 8 bits so and else, us of a run of them in a graph: one row of six of 64 experts of 2048 x 1408 (528 workgroups times rows) 20.6 and 22.8, two rows (2112) 26.2 and
+// 28.5, two of eight (2816) 34.4 and 34.9, three of four (3168) 31.9 and 28.3, four of six (8448) 45.9 and 40.8; three of eight of 64 of 1024 x 704 (3168) 21.6 and 23.0; five of four
+// of 40 of 512 x 512 (3200) 15.7 and 14.8; six of three of 64 (3456) 16.0 and 14.7; in 4 bits five of five of 100 of 1000 x 700 (5500) 22.5 and 20.4.
 constexpr int FEW_ROWS = 8, FEW_EXPERTS = 256, FEW_STEPS = 128, FEW_GROUPS = 2560;
 constexpr int MOST_SLOTS = ASGD_PRODUCT_RAW_ROWS * ASGD_ROUTE_MAX_CHOSEN, WORDS = ASGD_ROUTE_MAX_EXPERTS / 32;
 static_assert(ASGD_PRODUCT_RAW_ROWS == COLUMNS, "");
