@@ -194,7 +194,7 @@ __global__ __launch_bounds__(64 * TOK_WAVES * WT_WAVES, 2) void product_four_ker
 // workgroup, CHUNK runs at a time, while the first weights are on their way, and handed round through the LDS (by every wave for itself: 27.7 us where 10.7 do for 120 rows of
 // 100 experts of 1000 x 1100).  Where the weights are few a workgroup's own chain bounds it (x, its 4 bits,
 // a barrier, the waves' sums): of a run of launches one row times 4096 x 4096 takes 4.9 us, 3.8 where the last cache has the weights, and 3.5 with one strip of them alone, of which
-// an empty launch is 1.6.  Memory does where they are many: 8192 x 8192 10.7 us, 3.3 TB/s.
+// a launch that writes one number is 1.6.  Memory does where they are many: 8192 x 8192 10.7 us, 3.3 TB/s.
 constexpr int FEW4_WAVES = 8;
 
 // grid: groups of strips of sixteen rows of b, tiles of 16 * J rows of a
