@@ -35,8 +35,8 @@ class ClusterwiseLinear:
         self.shared = torch.zeros((outputs, d), device=centroids.device) if shared else None
         self.rule = X.Rule(choices, score=X.SOFTMAX)
 
-    def logits(self, x):
-        c = self.centroids
+    def logits(self, x, centroids=None):
+        c = self.centroids if centroids is None else centroids
         return self.sharpness * (x @ c.t() - 0.5 * (c * c).sum(1))
 
     def forward(self, x, train=False):
@@ -53,12 +53,14 @@ class ClusterwiseLinear:
         return (y, (logits, ids, kept, of_all)) if train else y
 
     def small(self):
-        """The maps in 4 bits, kept for evaluation: a function of samples x that gives what forward(x) does, at a quarter of 16-bit weights' bytes."""
+        """The maps in 4 bits, kept for evaluation with the router that belongs to them: a function of samples x that gives what forward(x) does now, also
+        when the model is trained on, at a quarter of 16-bit weights' bytes."""
+        centroids = self.centroids.clone()
         w = M.quantize(self.w)
         shared = None if self.shared is None else M.quantize(self.shared)
 
         def forward(x):
-            ids, weights = X.route(self.logits(x), self.rule)
+            ids, weights = X.route(self.logits(x, centroids), self.rule)
             x = x.bfloat16()
             y = M.experts(x, ids, weights, w)
             return y if shared is None else y.float() + M.linear(x, shared).float()

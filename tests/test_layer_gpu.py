@@ -352,3 +352,17 @@ def test_what_the_example_says_of_its_maps_in_four_bits(L, shared, monkeypatch):
         y = y + q @ b.t()
         allowed += 2 * Q.U * y.abs()
     assert ((held["y4"][:50].cpu().double() - y).abs() <= 1.01 * allowed).all()
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_the_examples_maps_in_four_bits_stay_what_they_were(L, shared):
+    """What small() gave goes on giving the model of that moment, router and maps, while the model is trained on."""
+    from paper_1505_04956_amd import clusterwise as C
+    g = torch.Generator().manual_seed(2)
+    x, target = torch.randn(300, 40, generator=g).cuda(), torch.randn(300, 24, generator=g).cuda()
+    model = C.ClusterwiseLinear(torch.randn(5, 40, generator=g).cuda(), 24, shared=shared)
+    served = model.small()
+    was = served(x)
+    for _ in range(3):
+        model.step(x, target, 0.5)
+    assert torch.equal(served(x), was) and not torch.equal(model.small()(x), was)
